@@ -351,6 +351,147 @@ const char* dpa4c_stage_name(int stage);
 int dpa4c_debug_gemm(const float* A, const float* B, float* C, int M, int N, int K,
                      void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * Fitting the energy MLP with weights of each element type
+ * ---------------------------------------------------------------------------
+ * Rows of atoms, grouped by element type, through layers whose weights belong
+ * to the group; the gradients of such a layer; and the Newton-Schulz update of
+ * the weights.  Nothing here touches a model handle.  All calls are
+ * asynchronous on ``stream``, allocate nothing, read nothing back and may be
+ * captured in a HIP graph.  Scratch is the caller's: each call has a
+ * dpa4c_*_work function that gives the bytes its arguments need (host only);
+ * ``work`` is 256-byte aligned device memory of at least that size, free for
+ * reuse once the stream has passed the call.  Outputs do not overlap inputs
+ * or each other.
+ * Every sum runs in a fixed order: repeated calls give the same bits.
+ */
+#define DPA4C_F32 0
+#define DPA4C_F16 1
+#define DPA4C_BF16 2
+
+#define DPA4C_ACT_NONE 0
+#define DPA4C_ACT_SILU 1
+
+/*
+ * Rows by group.  group: device int32 [n]; ids outside [0, n_groups) belong to
+ * no group (padding atoms).
+ *   group_ptr  device int64 [n_groups + 1] out: group g holds the places
+ *              group_ptr[g] .. group_ptr[g + 1] of ``order``
+ *   order      device int32 [n] out: the rows in group order, ascending
+ *              within a group; then the rows of no group, ascending
+ * 0 <= n < 2^31, 1 <= n_groups <= 512 (UNSUPPORTED above).
+ */
+int dpa4c_group_rows_work(int64_t n, int n_groups, int64_t* bytes);
+int dpa4c_group_rows(const int32_t* group, int64_t n, int n_groups, int64_t* group_ptr,
+                     int32_t* order, void* work, int64_t work_bytes, void* stream);
+
+/*
+ * The rows and weights that a grouped layer works on.  Row order[p] (or row p
+ * when order is NULL), p in [group_ptr[g], group_ptr[g + 1]), belongs to group
+ * g; group_ptr[0] = 0 and group_ptr does not decrease.  Rows at places from
+ * group_ptr[n_groups] on belong to no group: their outputs are zero and they
+ * enter no gradient.  ``order`` holds each row once; entries outside [0, n)
+ * are passed over.
+ *   x       [n][k] of ``dtype``, rows ldx entries apart (0: one row for all)
+ *   weight  [n_groups][k][n_out], contiguous
+ * 0 <= n < 2^31; 1 <= k, n_out <= 65536; 1 <= n_groups <= 65536.
+ * ``dtype`` is the type of every array of a call.  Products are accumulated in
+ * float32 and each output is rounded once.  float32 operands are carried as
+ * pairs of float16 under power-of-two scales, which hold them to about 2^-23
+ * of themselves or 2^-32 of the largest entry of their row, whichever is more;
+ * a row (for gradients of weights, a column) with an infinity or NaN gives NaN.
+ */
+typedef struct dpa4c_grouped {
+  int dtype;
+  int n_groups;
+  int k;
+  int n_out;
+  int64_t n;
+  const int64_t* group_ptr; /* device int64 [n_groups + 1] */
+  const int32_t* order;     /* device int32 [n] or NULL */
+  const void* x;            /* device */
+  int64_t ldx;
+  const void* weight;       /* device */
+} dpa4c_grouped;
+
+/*
+ * A layer of the energy MLP (Eqs. (atomic-energy), (fitting)) with weights of
+ * each group:
+ *     z_r = x_r W_g + b_g,   y_r = act(z_r) (+ x_r with ``residual``, k = n_out).
+ * bias [n_groups][n_out] or NULL; y [n][n_out]; z [n][n_out] (the
+ * pre-activation, which the backward pass needs) or NULL; contiguous.
+ */
+int dpa4c_grouped_linear_work(const dpa4c_grouped* layer, int64_t* bytes);
+int dpa4c_grouped_linear(const dpa4c_grouped* layer, const void* bias, int activation,
+                         int residual, void* y, void* z, void* work, int64_t work_bytes,
+                         void* stream);
+
+/*
+ * The gradients of that layer from dy = dL/dy [n][n_out], rows ldy entries
+ * apart, and z (rows ldz apart) as the forward pass gave it; z = NULL is the
+ * layer without activation:
+ *     dz_r = dy_r act'(z_r),   dx_r = dz_r W_g^T (+ dy_r with ``residual``),
+ *     dW_g = sum_r x_r^T dz_r,   db_g = sum_r dz_r.
+ * dx [n][k], dw [n_groups][k][n_out], db [n_groups][n_out], contiguous; each
+ * may be NULL (not formed).  Groups without rows get zeros.
+ */
+int dpa4c_grouped_linear_backward_work(const dpa4c_grouped* layer, int64_t* bytes);
+int dpa4c_grouped_linear_backward(const dpa4c_grouped* layer, const void* dy, int64_t ldy,
+                                  const void* z, int64_t ldz, int residual, void* dx, void* dw,
+                                  void* db, void* work, int64_t work_bytes, void* stream);
+
+/*
+ * Newton-Schulz orthogonalisation, as the Muon optimiser (K. Jordan et al.,
+ * 2024) uses it.  For every matrix G:
+ *     X = G / (|G|_F + eps),  then ``steps`` times
+ *     A = X X^T,  X <- a X + (b A + c A A) X,
+ * on the transpose where G has more rows than columns.  A stack is ``batch``
+ * contiguous row-major matrices of one shape; a call takes up to 32 stacks of
+ * any shapes.  Iterates are held as pairs of float16 at a fixed scale, 2^-23 of
+ * an entry or 2^-33 absolute, sums in float32, the norm's in float64; the
+ * coefficients have to keep |X| below 128 and |b A + c A A| below 512 entry by
+ * entry (the usual ones stay below 2 and 8).  A matrix with an infinity or NaN
+ * gives NaN; a zero matrix gives zero.
+ */
+typedef struct dpa4c_stack {
+  const void* in;
+  void* out;
+  int64_t batch;
+  int rows;
+  int cols;
+} dpa4c_stack;
+
+typedef struct dpa4c_newton {
+  int steps;      /* 0 .. 100 */
+  float a, b, c;
+  float eps;      /* > 0 */
+} dpa4c_newton;
+
+int dpa4c_orthogonalize_work(int count, const dpa4c_stack* stacks, int64_t* bytes);
+int dpa4c_orthogonalize(int dtype, int count, const dpa4c_stack* stacks, const dpa4c_newton* how,
+                        void* work, int64_t work_bytes, void* stream);
+
+/*
+ * One Muon update, in place:
+ *     M <- momentum M + G;   U = G + momentum M with ``nesterov``, else M;
+ *     W <- (1 - lr weight_decay) W - lr sqrt(max(1, cols / rows)) NS(U).
+ * param and grad are of ``dtype``, momentum_buf float32.
+ */
+typedef struct dpa4c_update {
+  void* param;
+  const void* grad;
+  float* momentum_buf;
+  int64_t batch;
+  int rows;
+  int cols;
+} dpa4c_update;
+
+int dpa4c_muon_step_work(int count, const dpa4c_update* updates, int64_t* bytes);
+int dpa4c_muon_step(int dtype, int count, const dpa4c_update* updates, const dpa4c_newton* how,
+                    float lr, float momentum, int nesterov, float weight_decay, void* work,
+                    int64_t work_bytes, void* stream);
+
 /* Thread-local description of the last error (library-owned string). */
 const char* dpa4c_last_error(void);
 

@@ -43,6 +43,7 @@ def library():
                                               "python -m paper_2608_19041_amd.build")
         lib = ctypes.CDLL(LIB_PATH)
         vp, i64, i32, dbl = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_double
+        flt = ctypes.c_float
         sig = {
             "dpa4c_model_create": (i32, [vp, ctypes.c_size_t, i32, ctypes.POINTER(vp)]),
             "dpa4c_model_destroy": (None, [vp]),
@@ -65,6 +66,17 @@ def library():
             "dpa4c_get_timings": (i32, [vp, vp, vp, i32]),
             "dpa4c_stage_name": (ctypes.c_char_p, [i32]),
             "dpa4c_debug_gemm": (i32, [vp, vp, vp, i32, i32, i32, vp]),
+            "dpa4c_group_rows_work": (i32, [i64, i32, vp]),
+            "dpa4c_group_rows": (i32, [vp, i64, i32, vp, vp, vp, i64, vp]),
+            "dpa4c_grouped_linear_work": (i32, [vp, vp]),
+            "dpa4c_grouped_linear": (i32, [vp, vp, i32, i32, vp, vp, vp, i64, vp]),
+            "dpa4c_grouped_linear_backward_work": (i32, [vp, vp]),
+            "dpa4c_grouped_linear_backward": (i32, [vp, vp, i64, vp, i64, i32, vp, vp, vp, vp, i64,
+                                                    vp]),
+            "dpa4c_orthogonalize_work": (i32, [i32, vp, vp]),
+            "dpa4c_orthogonalize": (i32, [i32, i32, vp, vp, vp, i64, vp]),
+            "dpa4c_muon_step_work": (i32, [i32, vp, vp]),
+            "dpa4c_muon_step": (i32, [i32, i32, vp, vp, flt, flt, i32, flt, vp, i64, vp]),
             "dpa4c_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -80,7 +92,11 @@ def exported_symbols() -> list[str]:
             "compute_energy_forces", "compute_energy_forces_virial",
             "compute_energy_forces_noalloc", "verlet_step", "nvt_step",
             "dpa4c_debug_stages", "dpa4c_debug_gradient", "dpa4c_set_timing",
-            "dpa4c_get_timings", "dpa4c_stage_name", "dpa4c_debug_gemm", "dpa4c_last_error"]
+            "dpa4c_get_timings", "dpa4c_stage_name", "dpa4c_debug_gemm",
+            "dpa4c_group_rows_work", "dpa4c_group_rows", "dpa4c_grouped_linear_work",
+            "dpa4c_grouped_linear", "dpa4c_grouped_linear_backward_work",
+            "dpa4c_grouped_linear_backward", "dpa4c_orthogonalize_work", "dpa4c_orthogonalize",
+            "dpa4c_muon_step_work", "dpa4c_muon_step", "dpa4c_last_error"]
 
 
 def stage_names() -> list[str]:
@@ -382,3 +398,7 @@ class Model:
         if k < 0:
             _check(k)
         return {lib.dpa4c_stage_name(s).decode(): (ms[s], cnt[s]) for s in range(k)}
+
+
+from .fitting import (group_rows, grouped_linear, grouped_linear_backward,  # noqa: E402
+                      muon_step, orthogonalize)

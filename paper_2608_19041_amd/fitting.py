@@ -1,0 +1,286 @@
+"""Operators that fit the energy MLP with weights of each element type.
+
+Rows of atoms go through layers whose weights belong to the row's group (its
+element type), the gradients of such a layer, and the Newton-Schulz update of
+the weights (the Muon optimiser).  Argument marshalling only, as in the rest
+of the binding: every step runs in the HIP kernels of the library, on the
+caller's stream, and scratch comes from torch's allocator on that stream.
+
+    ptr, order = group_rows(species, 118)
+    y, z = grouped_linear(x, w, ptr, order, bias=b, activation="silu", preact=True)
+    dx, dw, db = grouped_linear_backward(dy, x, w, ptr, order, preact=z)
+    muon_step([w], [dw], [momentum], lr=0.02)
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+import math
+
+from . import _check, _ptr, _require, library
+
+F32, F16, BF16 = 0, 1, 2
+ACTIVATIONS = {None: 0, "silu": 1}
+#: the quintic iteration of the Muon optimiser
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+MAX_STACKS = 32
+
+
+class _Grouped(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_groups", ctypes.c_int), ("k", ctypes.c_int),
+                ("n_out", ctypes.c_int), ("n", ctypes.c_int64), ("group_ptr", ctypes.c_void_p),
+                ("order", ctypes.c_void_p), ("x", ctypes.c_void_p), ("ldx", ctypes.c_int64),
+                ("weight", ctypes.c_void_p)]
+
+
+class _Stack(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("batch", ctypes.c_int64),
+                ("rows", ctypes.c_int), ("cols", ctypes.c_int)]
+
+
+class _Update(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("momentum_buf", ctypes.c_void_p), ("batch", ctypes.c_int64),
+                ("rows", ctypes.c_int), ("cols", ctypes.c_int)]
+
+
+class _Newton(ctypes.Structure):
+    _fields_ = [("steps", ctypes.c_int), ("a", ctypes.c_float), ("b", ctypes.c_float),
+                ("c", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+def _dtype_code(t, name):
+    import torch
+    codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in codes:
+        raise ValueError(f"{name} must be a CUDA tensor of float32, float16 or bfloat16")
+    return codes[t.dtype]
+
+
+def _rows(t, dtype, shape, device, name):
+    """A matrix of rows any distance apart; returns the distance in entries."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a tensor of {dtype} on {device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit stride within a row")
+    ld = t.stride(0) if shape[0] > 1 else shape[1]
+    if ld != 0 and ld < shape[1]:
+        raise ValueError(f"the rows of {name} overlap")
+    return ld
+
+
+def _same(t, dtype, shape, device, name):
+    _require(t, dtype, shape, name)
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+
+
+@contextlib.contextmanager
+def _launch(device, stream):
+    """The stream's handle, with ``device`` current and torch's allocator on that stream."""
+    import torch
+    if stream is None and device.index == torch.cuda.current_device():
+        yield ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return
+    with torch.cuda.device(device):
+        stream = stream if stream is not None else torch.cuda.current_stream()
+        with torch.cuda.stream(stream):
+            yield ctypes.c_void_p(stream.cuda_stream)
+
+
+def _scratch(size_of, device):
+    """(tensor or None, bytes) for a call whose scratch ``size_of`` writes to its argument."""
+    import torch
+    need = ctypes.c_int64(0)
+    _check(size_of(ctypes.byref(need)))
+    work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+    return work, need.value
+
+
+def group_rows(group, n_groups: int, stream=None):
+    """(group_ptr int64 [n_groups + 1], order int32 [n]): the rows in group order.
+
+    ``group``: int32 [n].  Rows keep their order within a group; rows whose id
+    is outside [0, n_groups) belong to no group and come last.
+    """
+    import torch
+    _require(group, torch.int32, None, "group")
+    if group.dim() != 1:
+        raise ValueError("group must have one dimension")
+    n, lib = group.shape[0], library()
+    with _launch(group.device, stream) as st:
+        work, size = _scratch(lambda need: lib.dpa4c_group_rows_work(n, int(n_groups), need),
+                              group.device)
+        ptr = torch.empty(int(n_groups) + 1, dtype=torch.int64, device=group.device)
+        order = torch.empty(n, dtype=torch.int32, device=group.device)
+        _check(lib.dpa4c_group_rows(_ptr(group), n, int(n_groups), _ptr(ptr), _ptr(order),
+                                    _ptr(work), size, st))
+    return ptr, order
+
+
+def _layer(x, weight, group_ptr, order):
+    import torch
+    code = _dtype_code(weight, "weight")
+    if weight.dim() != 3 or not weight.is_contiguous():
+        raise ValueError("weight must be contiguous with shape [groups, k, n]")
+    groups, k, n_out = weight.shape
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a matrix of rows")
+    n = x.shape[0]
+    ldx = _rows(x, weight.dtype, (n, k), weight.device, "x")
+    _same(group_ptr, torch.int64, (groups + 1,), weight.device, "group_ptr")
+    if order is not None:
+        _same(order, torch.int32, (n,), weight.device, "order")
+    return _Grouped(code, groups, k, n_out, n, group_ptr.data_ptr(),
+                    None if order is None else order.data_ptr(), x.data_ptr(), ldx,
+                    weight.data_ptr())
+
+
+def grouped_linear(x, weight, group_ptr, order=None, bias=None, activation=None, residual=False,
+                   preact=False, stream=None):
+    """y = act(x W_g + b_g) (+ x), with the weights of each row's group.
+
+    x [n, k] (rows may be any distance apart), weight [groups, k, m], bias
+    [groups, m] or None, all of one type (float32, float16, bfloat16);
+    group_ptr and order as ``group_rows`` gives them (order None: the rows are
+    in group order already).  ``activation``: None or "silu"; ``residual``
+    adds x (k = m).  With ``preact`` returns (y, z), z the value before the
+    activation.  Rows of no group give zeros.
+    """
+    import torch
+    layer = _layer(x, weight, group_ptr, order)
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {list(ACTIVATIONS)}")
+    if residual and layer.k != layer.n_out:
+        raise ValueError("a residual needs as many outputs as inputs")
+    if bias is not None:
+        _same(bias, weight.dtype, (layer.n_groups, layer.n_out), weight.device, "bias")
+    lib = library()
+    with _launch(weight.device, stream) as st:
+        work, size = _scratch(lambda need: lib.dpa4c_grouped_linear_work(ctypes.byref(layer), need),
+                              weight.device)
+        y = torch.empty(layer.n, layer.n_out, dtype=weight.dtype, device=weight.device)
+        z = torch.empty_like(y) if preact else None
+        _check(lib.dpa4c_grouped_linear(ctypes.byref(layer), _ptr(bias), ACTIVATIONS[activation],
+                                        int(bool(residual)), _ptr(y), _ptr(z), _ptr(work), size,
+                                        st))
+    return (y, z) if preact else y
+
+
+def grouped_linear_backward(dy, x, weight, group_ptr, order=None, preact=None, residual=False,
+                            need=(True, True, True), stream=None):
+    """(dx, dw, db) of ``grouped_linear`` from dy = dL/dy.
+
+    ``preact``: z of the forward pass of a layer with SiLU; None: the layer had
+    no activation.  ``need`` says which gradients to form; the others are None.
+    """
+    import torch
+    layer = _layer(x, weight, group_ptr, order)
+    n, m, dev = layer.n, layer.n_out, weight.device
+    if residual and layer.k != m:
+        raise ValueError("a residual needs as many outputs as inputs")
+    ldy = _rows(dy, weight.dtype, (n, m), dev, "dy")
+    ldz = 0 if preact is None else _rows(preact, weight.dtype, (n, m), dev, "preact")
+    lib = library()
+    with _launch(dev, stream) as st:
+        work, size = _scratch(
+            lambda want: lib.dpa4c_grouped_linear_backward_work(ctypes.byref(layer), want), dev)
+        dx = torch.empty(n, layer.k, dtype=weight.dtype, device=dev) if need[0] else None
+        dw = torch.empty_like(weight) if need[1] else None
+        db = torch.empty(layer.n_groups, m, dtype=weight.dtype, device=dev) if need[2] else None
+        _check(lib.dpa4c_grouped_linear_backward(
+            ctypes.byref(layer), _ptr(dy), ldy, _ptr(preact), ldz, int(bool(residual)), _ptr(dx),
+            _ptr(dw), _ptr(db), _ptr(work), size, st))
+    return dx, dw, db
+
+
+def _stack_list(name, tensors):
+    import torch
+    if isinstance(tensors, torch.Tensor):
+        raise ValueError(f"{name} must be a list of tensors")
+    tensors = list(tensors)
+    for t in tensors:
+        _dtype_code(t, name)
+        if t.dim() < 2 or not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous matrices or stacks of matrices")
+        if t.dtype != tensors[0].dtype or t.device != tensors[0].device:
+            raise ValueError(f"{name} must share one type and one device")
+        if t.shape[-1] < 1 or t.shape[-2] < 1:
+            raise ValueError(f"{name} must not have empty matrices")
+    return tensors
+
+
+def _newton(steps, coefficients, eps):
+    a, b, c = (float(v) for v in coefficients)
+    return _Newton(int(steps), a, b, c, float(eps))
+
+
+def _batch(t):
+    return math.prod(t.shape[:-2])
+
+
+def orthogonalize(matrices, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps: float = 1e-7,
+                  stream=None):
+    """Newton-Schulz orthogonalisation of every matrix; a list of results.
+
+    ``matrices``: a list of contiguous matrices or stacks [..., rows, cols] of
+    one type.  X = G / (|G| + eps), then ``steps`` times A = X X^T,
+    X <- a X + (b A + c A A) X, on the shorter side.
+    """
+    import torch
+    matrices = _stack_list("matrices", matrices)
+    if not matrices:
+        return []
+    how, lib, dev = _newton(steps, coefficients, eps), library(), matrices[0].device
+    with _launch(dev, stream) as st:
+        out = [torch.empty_like(t) for t in matrices]
+        for at in range(0, len(matrices), MAX_STACKS):
+            part = matrices[at:at + MAX_STACKS]
+            stacks = (_Stack * len(part))(*[
+                _Stack(t.data_ptr(), o.data_ptr(), _batch(t), t.shape[-2], t.shape[-1])
+                for t, o in zip(part, out[at:at + MAX_STACKS])])
+            work, size = _scratch(
+                lambda need: lib.dpa4c_orthogonalize_work(len(part), stacks, need), dev)
+            _check(lib.dpa4c_orthogonalize(_dtype_code(part[0], "matrices"), len(part), stacks,
+                                           ctypes.byref(how), _ptr(work), size, st))
+    return out
+
+
+def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nesterov: bool = True,
+              weight_decay: float = 0.0, steps: int = 5, coefficients=MUON_COEFFICIENTS,
+              eps: float = 1e-7, stream=None):
+    """One Muon update of every weight matrix, in place.
+
+    M <- momentum M + G; U = G + momentum M (``nesterov``) or M;
+    W <- (1 - lr weight_decay) W - lr sqrt(max(1, cols / rows)) NS(U).
+    ``params``, ``grads``: lists of contiguous matrices or stacks of one type;
+    ``momenta``: float32 tensors of the same shapes.
+    """
+    import torch
+    params, grads = _stack_list("params", params), _stack_list("grads", grads)
+    momenta = _stack_list("momenta", momenta)
+    if not len(params) == len(grads) == len(momenta):
+        raise ValueError("params, grads and momenta must have the same length")
+    if not params:
+        return
+    dev = params[0].device
+    for w, g, m in zip(params, grads, momenta):
+        _same(g, w.dtype, w.shape, dev, "grads")
+        _same(m, torch.float32, w.shape, dev, "momenta")
+    how, lib = _newton(steps, coefficients, eps), library()
+    with _launch(dev, stream) as st:
+        for at in range(0, len(params), MAX_STACKS):
+            cut = slice(at, at + MAX_STACKS)
+            part = params[cut]
+            ups = (_Update * len(part))(*[
+                _Update(w.data_ptr(), g.data_ptr(), m.data_ptr(), _batch(w), w.shape[-2],
+                        w.shape[-1])
+                for w, g, m in zip(part, grads[cut], momenta[cut])])
+            work, size = _scratch(lambda need: lib.dpa4c_muon_step_work(len(part), ups, need), dev)
+            _check(lib.dpa4c_muon_step(_dtype_code(part[0], "params"), len(part), ups,
+                                       ctypes.byref(how), float(lr), float(momentum),
+                                       int(bool(nesterov)), float(weight_decay), _ptr(work), size,
+                                       st))
