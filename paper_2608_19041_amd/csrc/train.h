@@ -8,7 +8,7 @@
 namespace dpa4c {
 
 constexpr int kMaxSortGroups = 512;       // of dpa4c_group_rows: its counters live in LDS
-constexpr int kMaxGroups = 65536;
+constexpr int kMaxGroups = 4096;          // of a layer: the starts of their tiles live in LDS
 constexpr int kMaxWidth = 65536;
 constexpr int kMaxStacks = 32;            // of one call; their descriptors are kernel arguments
 

@@ -56,7 +56,7 @@ def test_layer_call_refused():
     assert back(ref, None, 7, None, 0, 0, 256, None, None, 256, big, None) == INVALID
     assert back(ref, 256, 6, None, 0, 0, 256, None, None, 256, big, None) == INVALID
     assert back(ref, 256, 7, 256, 6, 0, 256, None, None, 256, big, None) == INVALID
-    l65 = layer(n_groups=65537)
+    l65 = layer(n_groups=4097)
     assert lib.dpa4c_grouped_linear(ctypes.byref(l65), None, 0, 0, 256, None, 256, big, None) == UNSUPPORTED
 
 
