@@ -448,10 +448,11 @@ int dpa4c_grouped_linear_backward(const dpa4c_grouped* layer, const void* dy, in
  *     A = X X^T,  X <- a X + (b A + c A A) X,
  * on the transpose where G has more rows than columns.  A stack is ``batch``
  * contiguous row-major matrices of one shape; a call takes up to 32 stacks of
- * any shapes.  Iterates are held as pairs of float16 at a fixed scale, 2^-23 of
- * an entry or 2^-33 absolute, sums in float32, the norm's in float64; the
- * coefficients have to keep |X| below 128 and |b A + c A A| below 512 entry by
- * entry (the usual ones stay below 2 and 8).  A matrix with an infinity or NaN
+ * any shapes.  Iterates are held as pairs of float16 at fixed scales, 2^-24 of
+ * an entry or 2^-38 absolute (A: 2^-36, b A + c A A: 2^-34), sums in float32,
+ * the norm's in float64; the coefficients have to keep |X|, |A| and
+ * |b A + c A A| below 4, 16 and 64 entry by entry (the usual ones stay below
+ * 1.3, 1.6 and 8; beyond, entries become NaN).  A matrix with an infinity or NaN
  * gives NaN; a zero matrix gives zero.
  */
 typedef struct dpa4c_stack {
