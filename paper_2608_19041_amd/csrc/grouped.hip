@@ -137,96 +137,88 @@ struct PrepArgs {
   int list_blocks;          // workgroups that list tiles, after those of the weights
 };
 
-// 64 columns of one group's weights by a workgroup: lane -> column, wave ->
-// reduction entries
+// 32 columns of one group's weights by a workgroup of 512 threads.  The entries
+// of the columns are read along the rows of W: 32 columns of one entry, or (Back,
+// a column is a row of W) 64 entries of one column a wave.  float32 columns
+// are read twice, for the largest entry and for the planes (from L2).
+constexpr int kPrepThreads = 512, kPrepCols = 32;
+
 template <class T, bool Back>
 __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
   const Span s = span_of(a.ptr, g, a.n_groups, a.n);
   if (s.begin == s.end) return;
   const T* w = static_cast<const T*>(a.w) + int64_t(g) * a.depth * a.cols;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  // Back: a row of W is a column here, so eight lanes take eight entries each
-  // of a row; lanes still cover 64 entries x 8 rows
   constexpr bool kSplit = sizeof(T) == 4;
-  __shared__ float most[4][64];
-  __shared__ int32_t exps[64];
+  __shared__ float most[kPrepThreads / kPrepCols][kPrepCols];
+  __shared__ int32_t exps[kPrepCols];
   auto at = [&](int c, int k) {
     return to_f32(Back ? w[int64_t(c) * a.depth + k] : w[int64_t(k) * a.cols + c]);
   };
   if (kSplit) {
-    if (!Back) {
-      float m = 0.0f;
-      const int c = c0 + lane;
-      if (c < a.cols)
-        for (int k = wave; k < a.depth; k += 4) m = fmaxf(m, fabsf(at(c, k)));
-      most[wave][lane] = m;
-      __syncthreads();
-    } else {
-      for (int r = wave; r < 64; r += 4) {
-        float m = 0.0f;
-        if (c0 + r < a.cols)
-          for (int k = lane; k < a.depth; k += 64) m = fmaxf(m, fabsf(at(c0 + r, k)));
-        for (int d = 32; d > 0; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
-        if (lane == 0) most[0][r] = m;
-      }
-      __syncthreads();
+    // column c0 + r, entries q, q + 16, ..; Back: eight neighbours q a lane
+    const int r = Back ? threadIdx.x / 16 : threadIdx.x % kPrepCols;
+    const int q = Back ? threadIdx.x % 16 : threadIdx.x / kPrepCols;
+    float m = 0.0f;
+    if (c0 + r < a.cols) {
+#pragma unroll 8
+      for (int k = q; k < a.depth; k += 16) m = fmaxf(m, fabsf(at(c0 + r, k)));
     }
-    if (threadIdx.x < 64) {
-      float m = most[0][threadIdx.x];
-      if (!Back)
-        for (int i = 1; i < 4; ++i) m = fmaxf(m, most[i][threadIdx.x]);
+    most[q][r] = m;
+    __syncthreads();
+    if (threadIdx.x < kPrepCols) {
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, most[i][threadIdx.x]);
       const int e = m > 0.0f ? exp_for(m) : 0;
       exps[threadIdx.x] = e;
-      if (c0 + threadIdx.x < a.out.cols_pad) a.out.exps[int64_t(g) * a.out.cols_pad + c0 + threadIdx.x] = e;
+      a.out.exps[int64_t(g) * a.out.cols_pad + c0 + threadIdx.x] = e;
     }
     __syncthreads();
   }
-  // slots (column, 8 entries): lane -> column (Back: eight lanes a column)
-  for (int step = 0; step < a.out.steps; ++step) {
-    char* out = a.out.planes + (int64_t(g) * a.out.steps + step) * a.out.step_bytes();
-    for (int i = threadIdx.x; i < 64 * 8; i += kThreads) {
-      const int r = Back ? i / 8 : i % 64, slot = Back ? i % 8 : i / 64;
-      const int c = c0 + r, k0 = step * kDepth + slot * 8;
-      float f[8];
+  // slots (column, 8 entries)
+  const int r = Back ? threadIdx.x / 8 % kPrepCols : threadIdx.x % kPrepCols;
+  const int first = Back ? threadIdx.x % 8 + threadIdx.x / 256 * 8 : threadIdx.x / kPrepCols;
+  const int c = c0 + r;
+  const float scale = kSplit ? exp2_of(exps[r]) : 1.0f;
+#pragma unroll 2
+  for (int sl = first; sl < a.out.steps * 8; sl += 16) {
+    float f[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) f[j] = c < a.cols && k0 + j < a.depth ? at(c, k0 + j) : 0.0f;
-      u4 hi, lo;
-      if constexpr (kSplit) {
-        const float scale = exp2_of(exps[r]);
+    for (int j = 0; j < 8; ++j) f[j] = c < a.cols && sl * 8 + j < a.depth ? at(c, sl * 8 + j) : 0.0f;
+    u4 hi, lo;
+    if constexpr (kSplit) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          unsigned h, l;
-          split2(f[2 * j] * scale, f[2 * j + 1] * scale, &h, &l);
-          hi[j] = h;
-          lo[j] = l;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const T x = from_f32<T>(f[2 * j]), y = from_f32<T>(f[2 * j + 1]);
-          hi[j] = unsigned(__builtin_bit_cast(unsigned short, x)) |
-                  unsigned(__builtin_bit_cast(unsigned short, y)) << 16;
-        }
+      for (int j = 0; j < 4; ++j) {
+        unsigned h, l;
+        split2(f[2 * j] * scale, f[2 * j + 1] * scale, &h, &l);
+        hi[j] = h;
+        lo[j] = l;
       }
-      *reinterpret_cast<u4*>(out + slot_at(c, slot)) = hi;
-      if (kSplit) *reinterpret_cast<u4*>(out + int64_t(a.out.cols_pad) * 128 + slot_at(c, slot)) = lo;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const T x = from_f32<T>(f[2 * j]), y = from_f32<T>(f[2 * j + 1]);
+        hi[j] = unsigned(__builtin_bit_cast(unsigned short, x)) |
+                unsigned(__builtin_bit_cast(unsigned short, y)) << 16;
+      }
     }
+    char* to = a.out.planes + (int64_t(g) * a.out.steps + sl / 8) * a.out.step_bytes() + slot_at(c, sl % 8);
+    *reinterpret_cast<u4*>(to) = hi;
+    if (kSplit) *reinterpret_cast<u4*>(to + int64_t(a.out.cols_pad) * 128) = lo;
   }
 }
 
 template <class T, bool Back>
-__global__ void __launch_bounds__(kThreads) grouped_prepare_kernel(PrepArgs a) {
+__global__ void __launch_bounds__(kPrepThreads) grouped_prepare_kernel(PrepArgs a) {
   extern __shared__ int32_t starts[];
-  const int col_blocks = a.out.cols_pad / 64;
-  const int64_t weights = a.w ? int64_t(a.n_groups) * col_blocks : 0;
-  if (blockIdx.x < weights) {
-    lay_weights<T, Back>(a, blockIdx.x / col_blocks, blockIdx.x % col_blocks * 64);
+  // the lists first: the other workgroups' work hides theirs
+  if (blockIdx.x < unsigned(a.list_blocks)) {
+    if (a.tiles.list) list_tiles(a.tiles, a.ptr, a.n_groups, a.n, blockIdx.x, a.list_blocks, starts);
+    __syncthreads();
+    if (a.blocks.list) list_tiles(a.blocks, a.ptr, a.n_groups, a.n, blockIdx.x, a.list_blocks, starts);
     return;
   }
-  const int b = static_cast<int>(blockIdx.x - weights);
-  if (a.tiles.list) list_tiles(a.tiles, a.ptr, a.n_groups, a.n, b, a.list_blocks, starts);
-  __syncthreads();
-  if (a.blocks.list) list_tiles(a.blocks, a.ptr, a.n_groups, a.n, b, a.list_blocks, starts);
+  const int col_blocks = a.out.cols_pad / kPrepCols;
+  const int64_t b = int64_t(blockIdx.x) - a.list_blocks;
+  lay_weights<T, Back>(a, static_cast<int>(b / col_blocks), static_cast<int>(b % col_blocks) * kPrepCols);
 }
 
 // dz = dy act'(z) by place: float32 as it is, half types as a pair of their own
@@ -336,10 +328,9 @@ template <class T, Source S>
 __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
   constexpr int PA = planes_of<S>(), PB = S == kFloat ? 2 : 1;
   constexpr bool kBf = std::is_same<T, __bf16>::value;
-  constexpr int kPitch = kTileCols + 4;   // floats of a row of the output stage
-  constexpr int kStage = 64 * kPitch * 4;
   constexpr int kOperands = (PA + PB) * kPlane;
-  __shared__ __attribute__((aligned(16))) char lds[kOperands > kStage ? kOperands : kStage];
+  __shared__ __attribute__((aligned(16))) char lds[kOperands > kStageBytes ? kOperands : kStageBytes];
+  __shared__ int32_t row_of[kTileRows];   // -1: nothing is stored
   __shared__ int32_t change[kTileRows];   // exponent that a row's sums are to move by
   __shared__ int32_t row_exp[kTileRows];
   __shared__ int32_t flag[2];
@@ -379,6 +370,10 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     int r = 32 * i + tid / 8;
     r = r < t.count ? r : t.count - 1;
     int64_t row = a.by_place ? t.first + r : row_at(a.order, t.first + r, a.n);
+    if (sub == 0) {
+      const int64_t to = a.by_place ? row_at(a.order, t.first + r, a.n) : row;
+      row_of[32 * i + tid / 8] = 32 * i + tid / 8 < t.count ? static_cast<int32_t>(to) : -1;
+    }
     row = row < 0 ? 0 : row;
     rows[i] = static_cast<const char*>(a.in) + row * a.ldin * kSize;
   }
@@ -513,10 +508,11 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
           }
       }
     }
-    tile_step<kBf, PA, PB>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
+    if (c0 + 64 * wn < a.kout)
+      tile_step<kBf, PA, PB>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
   }
 
-  // outputs through LDS, 64 rows at a time, so that rows are written in one piece
+  // outputs through LDS, so that rows are written in one piece: 32 lanes a row
   if (S == kFloat && sub == 0)
 #pragma unroll
     for (int i = 0; i < 4; ++i) row_exp[32 * i + tid / 8] = e[i];
@@ -530,45 +526,44 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     bq[j] = bias && c + j < a.kout ? to_f32(bias[c + j]) : 0.0f;
     if (S == kFloat) eq[j] = a.w.exps[int64_t(t.group) * a.w.cols_pad + c + j];
   }
+  __syncthreads();
+  stage_sums(stage, acc, wm, wn, lane, 1.0f);
+  __syncthreads();
+  if (c >= a.kout) return;
+  const bool whole = c + 4 <= a.kout;
+  constexpr int kBatch = 4;   // rows in flight
 #pragma unroll 1
-  for (int h = 0; h < 2; ++h) {
-    __syncthreads();
-    if (wm == h) {
+  for (int r0 = tid / 32; r0 < t.count; r0 += 8 * kBatch) {
+    int64_t row[kBatch];
+    Pack<T, 4> res[kBatch];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            stage[(32 * i + sum_row(lane, r)) * kPitch + 64 * wn + 32 * j + (lane & 31)] = acc.v[i][j][r];
-    }
-    __syncthreads();
-    for (int r = tid / 32; r < 64; r += kThreads / 32) {
-      const int rt = 64 * h + r;
-      if (rt >= t.count) break;
-      const int64_t row = row_at(a.order, t.first + rt, a.n);
-      if (row < 0 || c >= a.kout) continue;
-      const v4f s = *reinterpret_cast<const v4f*>(stage + r * kPitch + quad * 4);
-      const int er = S == kFloat ? row_exp[rt] : 0;
-      const bool whole = c + 4 <= a.kout;
-      Pack<T, 4> res, py, pz;
-      if (a.residual) {
-        const T* src = static_cast<const T*>(a.residual) + row * a.ldres + c;
+    for (int k = 0; k < kBatch; ++k) {
+      row[k] = row_of[r0 + 8 * k];
+      if (a.residual && row[k] >= 0) {
+        const T* src = static_cast<const T*>(a.residual) + row[k] * a.ldres + c;
         if (whole)
-          res = *reinterpret_cast<const Pack<T, 4>*>(src);
+          res[k] = *reinterpret_cast<const Pack<T, 4>*>(src);
         else
-          for (int j = 0; j < 4; ++j) res.v[j] = c + j < a.kout ? src[j] : from_f32<T>(0.0f);
+          for (int j = 0; j < 4; ++j) res[k].v[j] = c + j < a.kout ? src[j] : from_f32<T>(0.0f);
       }
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int r = r0 + 8 * k;
+      const v4f s = *reinterpret_cast<const v4f*>(stage + stage_at(r, quad * 4));
+      const int er = S == kFloat ? row_exp[r] : 0;
+      Pack<T, 4> py, pz;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         float z = S == kFloat ? ldexpf(s[j], -er - eq[j]) : s[j];
         z += bq[j];
         float y = a.silu ? z * logistic(z) : z;
-        if (a.residual) y += to_f32(res.v[j]);
+        if (a.residual) y += to_f32(res[k].v[j]);
         py.v[j] = from_f32<T>(y);
         pz.v[j] = from_f32<T>(z);
       }
-      const int64_t to = row * a.kout + c;
+      if (row[k] < 0) continue;
+      const int64_t to = row[k] * a.kout + c;
       if (whole) {
         *reinterpret_cast<Pack<T, 4>*>(out + to) = py;
         if (zout) *reinterpret_cast<Pack<T, 4>*>(zout + to) = pz;
@@ -773,7 +768,8 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
     }
     __syncthreads();
     if (p + kDepth < end) fetch(p + kDepth);
-    if (a.dw) tile_step<kBf, PA, PB>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
+    if (a.dw && r0 + 64 * wm < a.k && c0 + 64 * wn < a.m)
+      tile_step<kBf, PA, PB>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
   }
 
   const bool whole = t.parts == 1;   // no other block adds to this group
@@ -836,12 +832,15 @@ int64_t tiles_at_most(int64_t n, int n_groups, int64_t rows) {
   return n / rows + (n < n_groups + 1 ? n : n_groups + 1);
 }
 
-// Rows of a block of dW: enough blocks for some rounds of the chip's 512
-// resident workgroups, and no fewer rows than pay for writing a block's sums.
+// Rows of a block of dW: 4,096 workgroups in all, some rounds of the chip's 512
+// resident ones, but no fewer than 512 rows, so that a block's sums are small
+// beside its rows, and groups of a few hundred rows are one block, whose sums go
+// straight to dW.  Where even that gives fewer than 512 workgroups, 256.
 int outer_rows(const dpa4c_grouped& l) {
   const int64_t tiles = ((l.k + kTileRows - 1) / kTileRows) * int64_t((l.n_out + kTileCols - 1) / kTileCols);
+  if (l.n * tiles < 512 * 512) return 256;
   const int64_t rows = align_up((l.n * tiles + 4095) / 4096, kDepth);
-  return static_cast<int>(rows < 256 ? 256 : rows > 16384 ? 16384 : rows);
+  return static_cast<int>(rows < 512 ? 512 : rows > 16384 ? 16384 : rows);
 }
 
 Weights weights_of(Arena& ar, const dpa4c_grouped& l, bool back) {
@@ -914,9 +913,7 @@ int prepare(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, con
   if (w) {
     a.w = l.weight;
     a.out = *w;
-    grid = int64_t(l.n_groups) * (w->cols_pad / 64);
-  } else {
-    a.out.cols_pad = 64;
+    grid = int64_t(l.n_groups) * (w->cols_pad / kPrepCols);
   }
   if (tiles) {
     a.tiles = *tiles;
@@ -926,9 +923,9 @@ int prepare(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, con
     a.blocks = *blocks;
     list = std::max(list, tiles_at_most(l.n, l.n_groups, blocks->rows));
   }
-  a.list_blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(64, list / kThreads)));
+  a.list_blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(64, list / kPrepThreads)));
   grouped_prepare_kernel<T, Back>
-      <<<grid + a.list_blocks, kThreads, (l.n_groups + 2) * sizeof(int32_t), st>>>(a);
+      <<<grid + a.list_blocks, kPrepThreads, (l.n_groups + 2) * sizeof(int32_t), st>>>(a);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }

@@ -1,11 +1,12 @@
 // Newton-Schulz orthogonalisation of stacks of matrices, and the Muon update.
 //
 // Per step and matrix (lo x hi, the shorter side first):
-//   A = X X^T             lo lo hi     (half of it: A is symmetric)
-//   B = b A + c A A       lo lo lo     (half of it)
-//   X <- a X + B X        2 lo lo hi
-// each a product of float16 pairs on the matrix cores (tile.h), 3 x 2 x the
-// above in flops.  The iterates keep to fixed scales, since the norms are known:
+//   A = X X^T                  lo lo hi flops (half of a product: A is symmetric)
+//   B = a I + A (b I + c A)    lo lo lo       (half of one)
+//   X <- B X                   2 lo lo hi
+// each a product of float16 pairs on the matrix cores (tile.h), three times
+// the above.  The identities go into the factors as they are written, C = b I +
+// c A beside A, so no product has to read another operand at its end.  The iterates keep to fixed scales, since the norms are known:
 // |X| <= 1 at the start and the iteration bounds it afterwards.  So the planes
 // are written as the next product reads them: rows of 64 reduction entries.  X
 // is the operand of A along its rows and of B X along its columns and is
@@ -25,7 +26,7 @@ namespace {
 constexpr int kThreads = kTileThreads;
 constexpr int64_t kChunk = 8192;   // entries of a partial sum of squares
 
-// fixed scales of the planes: entries of X, A and B below 4, 16 and 64
+// fixed scales of the planes: entries of X, A and B (and C) below 4, 16 and 64
 constexpr float kScaleX = 8192.0f, kScaleA = 2048.0f, kScaleB = 512.0f;
 
 // One stack.  A plane set is [matrix][step of 64][hi, lo][rows padded to
@@ -36,7 +37,7 @@ struct Stack {
   float* momentum;
   char* xr[2];    // rows lo, entries along hi; read and written in turn
   char* xt[2];    // rows hi, entries along lo
-  char *a, *b;    // rows lo, entries along lo
+  char *a, *b, *c;   // rows lo, entries along lo
   double* squares;   // [matrix][chunks]
   int64_t batch;
   int rows, cols;
@@ -102,19 +103,16 @@ __global__ void __launch_bounds__(kThreads) newton_norm_kernel(Stacks all, Share
 }
 
 // ---------------------------------------------------------------------------
-// 64 x 128 results in LDS, and where they go
+// Results in LDS (stage_at), and where they go
 // ---------------------------------------------------------------------------
-constexpr int kPitch = kTileCols + 4;
-constexpr int kStageRows = 64;
 
-// eight results, ``step`` floats apart, as one slot of each plane
-__device__ inline void write_slot(char* set, int rows_pad, int row, int entry, const float* from,
-                                  int step, float scale) {
+// eight values as one slot of each plane of a set
+__device__ inline void write_slot(char* set, int rows_pad, int row, int entry, const float* f, float scale) {
   u4 hi, lo;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     unsigned h, l;
-    split2(from[2 * j * step] * scale, from[(2 * j + 1) * step] * scale, &h, &l);
+    split2(f[2 * j] * scale, f[2 * j + 1] * scale, &h, &l);
     hi[j] = h;
     lo[j] = l;
   }
@@ -123,44 +121,35 @@ __device__ inline void write_slot(char* set, int rows_pad, int row, int entry, c
   *reinterpret_cast<u4*>(to + int64_t(rows_pad) * 128) = lo;
 }
 
-// the stage's rows as rows r0 .. of a plane set, entries from c0
+// mul x the stage (+ diag on the matrix's diagonal) as rows r0 .. of a plane
+// set, entries from c0; Rows: the stage's rows
+template <int Rows>
 __device__ inline void write_rows(char* set, int rows_pad, int steps, int r0, int c0,
-                                  const float* stage, float scale) {
-  for (int i = threadIdx.x; i < kStageRows * (kTileCols / 8); i += kThreads) {
-    const int slot = i % 8, r = i / 8 % kStageRows, part = i / (8 * kStageRows);
-    const int c = part * kDepth + slot * 8;
-    if ((c0 + c) / kDepth < steps)
-      write_slot(set, rows_pad, r0 + r, c0 + c, stage + r * kPitch + c, 1, scale);
+                                  const float* stage, float scale, float mul = 1.0f, float diag = 0.0f) {
+#pragma unroll 4
+  for (int i = 0; i < Rows * 16 / kThreads; ++i) {
+    const int slot = threadIdx.x % 16, r = threadIdx.x / 16 + i * (kThreads / 16), c = slot * 8;
+    if ((c0 + c) / kDepth >= steps) continue;
+    float f[8];
+    *reinterpret_cast<v4f*>(f) = *reinterpret_cast<const v4f*>(stage + stage_at(r, c));
+    *reinterpret_cast<v4f*>(f + 4) = *reinterpret_cast<const v4f*>(stage + stage_at(r, c + 4));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = f[j] * mul + (r0 + r == c0 + c + j ? diag : 0.0f);
+    write_slot(set, rows_pad, r0 + r, c0 + c, f, scale);
   }
 }
 // the stage's columns as rows c0 .., entries from r0
+template <int Rows>
 __device__ inline void write_columns(char* set, int rows_pad, int steps, int r0, int c0,
-                                     const float* stage, float scale) {
-  if (r0 / kDepth >= steps) return;
-  for (int i = threadIdx.x; i < kTileCols * (kStageRows / 8); i += kThreads) {
-    const int c = i % kTileCols, slot = i / kTileCols;
-    write_slot(set, rows_pad, c0 + c, r0 + slot * 8, stage + slot * 8 * kPitch + c, kPitch, scale);
-  }
-}
-
-// entries (row, entry .. entry + 7) of a plane set, added to sums
-__device__ inline void add_slot(const char* set, int rows_pad, int row, int entry, float scale,
-                                float* sums) {
-  const char* from = set + int64_t(entry / kDepth) * 2 * rows_pad * 128 + slot_at(row, entry % kDepth / 8);
-  const v8h hi = *reinterpret_cast<const v8h*>(from);
-  const v8h lo = *reinterpret_cast<const v8h*>(from + int64_t(rows_pad) * 128);
+                                     const float* stage, float scale, float mul = 1.0f) {
+#pragma unroll 4
+  for (int i = 0; i < Rows * 16 / kThreads; ++i) {
+    const int c = threadIdx.x % kTileCols, slot = threadIdx.x / kTileCols + 2 * i;
+    if ((r0 + slot * 8) / kDepth >= steps) continue;
+    float f[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    sums[j] += scale * (static_cast<float>(hi[j]) + static_cast<float>(lo[j]));
-}
-// stage += scale x the set's rows r0 .., entries from c0
-__device__ inline void add_rows(const char* set, int rows_pad, int steps, int r0, int c0,
-                                float* stage, float scale) {
-  for (int i = threadIdx.x; i < kStageRows * (kTileCols / 8); i += kThreads) {
-    const int slot = i % 8, r = i / 8 % kStageRows, part = i / (8 * kStageRows);
-    const int c = part * kDepth + slot * 8;
-    if ((c0 + c) / kDepth < steps)
-      add_slot(set, rows_pad, r0 + r, c0 + c, scale, stage + r * kPitch + c);
+    for (int j = 0; j < 8; ++j) f[j] = stage[stage_at(slot * 8 + j, c)] * mul;
+    write_slot(set, rows_pad, c0 + c, r0 + slot * 8, f, scale);
   }
 }
 
@@ -169,33 +158,36 @@ struct Finish {
 };
 
 // the stage as the result: out = O, or the weights' update
-template <class T, bool Muon>
+template <class T, bool Muon, int Rows>
 __device__ inline void write_result(const Stack& s, int64_t m, int r0, int c0, const float* stage,
                                     const Finish& f) {
   T* out = static_cast<T*>(s.out) + m * s.rows * s.cols;
   const float step = Muon ? f.step * sqrtf(fmaxf(1.0f, float(s.cols) / float(s.rows))) : 0.0f;
-  for (int i = threadIdx.x; i < kStageRows * kTileCols; i += kThreads) {
-    const int r = s.turned ? i % kStageRows : i / kTileCols;
-    const int c = s.turned ? i / kStageRows : i % kTileCols;
+#pragma unroll 8
+  for (int i = threadIdx.x; i < Rows * kTileCols; i += kThreads) {
+    const int r = s.turned ? i % Rows : i / kTileCols;
+    const int c = s.turned ? i / Rows : i % kTileCols;
     if (r0 + r >= s.lo || c0 + c >= s.hi) continue;
     const int64_t at = s.turned ? int64_t(c0 + c) * s.cols + r0 + r : int64_t(r0 + r) * s.cols + c0 + c;
-    const float o = stage[r * kPitch + c];
+    const float o = stage[stage_at(r, c)];
     out[at] = from_f32<T>(Muon ? f.keep * to_f32(out[at]) - step * o : o);
   }
 }
+
+constexpr int kStartRows = 64;
 
 // X = U / (|U| + eps), 64 x 128 a workgroup
 template <class T, bool Muon, bool Last>
 __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shares sh, float beta,
                                                                 int nesterov, float eps, Finish f) {
-  __shared__ float stage[kStageRows * kPitch];
+  __shared__ __attribute__((aligned(16))) float stage[kStartRows * kTileCols];
   __shared__ double norm;
   const int i = stack_of(sh, all.count, blockIdx.x);
   const Stack& s = all.s[i];
   const int64_t item = blockIdx.x - sh.first[i];
-  const int tr = s.lo_pad / kStageRows, tc = s.hi_pad / kTileCols;
+  const int tr = s.lo_pad / kStartRows, tc = s.hi_pad / kTileCols;
   const int64_t m = item / (tr * tc);
-  const int r0 = static_cast<int>(item / tc % tr) * kStageRows, c0 = static_cast<int>(item % tc) * kTileCols;
+  const int r0 = static_cast<int>(item / tc % tr) * kStartRows, c0 = static_cast<int>(item % tc) * kTileCols;
   if (threadIdx.x < kWave) {
     double sum = 0.0;
     for (int j = threadIdx.x; j < s.chunks; j += kWave) sum += s.squares[m * s.chunks + j];
@@ -205,22 +197,23 @@ __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shar
   __syncthreads();
   const double inv = norm;
   const int64_t base = m * s.rows * s.cols;
-  for (int j = threadIdx.x; j < kStageRows * kTileCols; j += kThreads) {
-    const int r = s.turned ? j % kStageRows : j / kTileCols;
-    const int c = s.turned ? j / kStageRows : j % kTileCols;
+#pragma unroll 8
+  for (int j = threadIdx.x; j < kStartRows * kTileCols; j += kThreads) {
+    const int r = s.turned ? j % kStartRows : j / kTileCols;
+    const int c = s.turned ? j / kStartRows : j % kTileCols;
     float v = 0.0f;
     if (r0 + r < s.lo && c0 + c < s.hi) {
       const int64_t at = s.turned ? int64_t(c0 + c) * s.cols + r0 + r : int64_t(r0 + r) * s.cols + c0 + c;
       v = static_cast<float>(update_of<T, Muon>(s, base + at, beta, nesterov) * inv);
     }
-    stage[r * kPitch + c] = v;
+    stage[stage_at(r, c)] = v;
   }
   __syncthreads();
   if constexpr (Last) {
-    write_result<T, Muon>(s, m, r0, c0, stage, f);
+    write_result<T, Muon, kStartRows>(s, m, r0, c0, stage, f);
   } else {
-    write_rows(s.xr[0] + m * set_bytes(s.hi_steps, s.lo_pad), s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
-    write_columns(s.xt[0] + m * set_bytes(s.lo_steps, s.hi_pad), s.hi_pad, s.lo_steps, r0, c0, stage, kScaleX);
+    write_rows<kStartRows>(s.xr[0] + m * set_bytes(s.hi_steps, s.lo_pad), s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
+    write_columns<kStartRows>(s.xt[0] + m * set_bytes(s.lo_steps, s.hi_pad), s.hi_pad, s.lo_steps, r0, c0, stage, kScaleX);
   }
 }
 
@@ -261,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
   const char* xr = s.xr[from] + m * xr_bytes;
   const char* A = s.a + m * sq_bytes;
   const char* left = P == kGram ? xr : P == kPoly ? A : s.b + m * sq_bytes;
-  const char* right = P == kGram ? xr : P == kPoly ? A : s.xt[from] + m * xt_bytes;
+  const char* right = P == kGram ? xr : P == kPoly ? s.c + m * sq_bytes : s.xt[from] + m * xt_bytes;
   const int steps = P == kGram ? s.hi_steps : s.lo_steps;
   const int64_t lplane = int64_t(s.lo_pad) * 128, rplane = kWide ? int64_t(s.hi_pad) * 128 : lplane;
   left += int64_t(ti) * kPlane;
@@ -294,47 +287,36 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
       }
     __syncthreads();
     if (step + 1 < steps) fetch(step + 1);
-    tile_step<false, 2, 2>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
+    if (ti * kTileRows + 64 * wm < s.lo && tj * kTileCols + 64 * wn < (kWide ? s.hi : s.lo))
+      tile_step<false, 2, 2>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
   }
 
   float* stage = reinterpret_cast<float*>(lds);
-  const float undo = P == kGram   ? 1.0f / (kScaleX * kScaleX)
-                     : P == kPoly ? cc / (kScaleA * kScaleA)
-                                  : 1.0f / (kScaleB * kScaleX);
-#pragma unroll 1
-  for (int h = 0; h < 2; ++h) {
-    __syncthreads();
-    if (wm == h)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            stage[(32 * i + sum_row(lane, r)) * kPitch + 64 * wn + 32 * j + (lane & 31)] =
-                acc.v[i][j][r] * undo;
-    __syncthreads();
-    const int r0 = ti * kTileRows + h * kStageRows, c0 = tj * kTileCols;
-    if constexpr (P == kGram) {
-      char* out = s.a + m * sq_bytes;
-      write_rows(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
-      if (ti != tj) write_columns(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
-    } else if constexpr (P == kPoly) {
-      char* out = s.b + m * sq_bytes;
-      add_rows(A, s.lo_pad, s.lo_steps, r0, c0, stage, cb / kScaleA);
-      __syncthreads();
-      write_rows(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB);
-      if (ti != tj) write_columns(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB);
-    } else {
-      add_rows(xr, s.lo_pad, s.hi_steps, r0, c0, stage, ca / kScaleX);
-      __syncthreads();
-      if constexpr (P == kLast) {
-        write_result<T, Muon>(s, m, r0, c0, stage, f);
-      } else {
-        write_rows(s.xr[from ^ 1] + m * xr_bytes, s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
-        write_columns(s.xt[from ^ 1] + m * xt_bytes, s.hi_pad, s.lo_steps, r0, c0, stage, kScaleX);
-      }
+  __syncthreads();
+  stage_sums(stage, acc, wm, wn, lane,
+             P == kGram   ? 1.0f / (kScaleX * kScaleX)
+             : P == kPoly ? 1.0f / (kScaleA * kScaleB)
+                          : 1.0f / (kScaleB * kScaleX));
+  __syncthreads();
+  const int r0 = ti * kTileRows, c0 = tj * kTileCols;
+  if constexpr (P == kGram) {
+    char* out = s.a + m * sq_bytes;
+    char* mix = s.c + m * sq_bytes;
+    write_rows<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
+    write_rows<kTileRows>(mix, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, cc, cb);
+    if (ti != tj) {
+      write_columns<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
+      write_columns<kTileRows>(mix, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, cc);
     }
+  } else if constexpr (P == kPoly) {
+    char* out = s.b + m * sq_bytes;
+    write_rows<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, 1.0f, ca);
+    if (ti != tj) write_columns<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB);
+  } else if constexpr (P == kApply) {
+    write_rows<kTileRows>(s.xr[from ^ 1] + m * xr_bytes, s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
+    write_columns<kTileRows>(s.xt[from ^ 1] + m * xt_bytes, s.hi_pad, s.lo_steps, r0, c0, stage, kScaleX);
+  } else {
+    write_result<T, Muon, kTileRows>(s, m, r0, c0, stage, f);
   }
 }
 
@@ -364,6 +346,7 @@ Stacks lay_out(int count, const NewtonStack* in, void* work, int64_t* bytes) {
     }
     s.a = ar.take<char>(s.batch * set_bytes(s.lo_steps, s.lo_pad));
     s.b = ar.take<char>(s.batch * set_bytes(s.lo_steps, s.lo_pad));
+    s.c = ar.take<char>(s.batch * set_bytes(s.lo_steps, s.lo_pad));
     s.squares = ar.take<double>(s.batch * s.chunks);
   }
   *bytes = ar.used;
@@ -382,7 +365,7 @@ template <class T, bool Muon>
 int run(const Stacks& all, const dpa4c_newton& how, const MuonStep& mu, hipStream_t st) {
   const Shares norms = share(all, [](const Stack& s) { return int64_t(s.chunks); });
   const Shares starts = share(all, [](const Stack& s) {
-    return int64_t(s.lo_pad / kStageRows) * (s.hi_pad / kTileCols);
+    return int64_t(s.lo_pad / kStartRows) * (s.hi_pad / kTileCols);
   });
   const Shares squares = share(all, [](const Stack& s) {
     const int64_t t = s.lo_pad / kTileRows;

@@ -111,6 +111,24 @@ __device__ inline void tile_step(Sums& acc, const char* a, const char* b, int la
   }
 }
 
+// The tile's outputs pass through LDS once, 128 x 128 float32 in the operands'
+// place; the 16-byte chunks of a row are exchanged by the row's low three bits,
+// so that reads along rows and along columns both meet all banks.
+constexpr int kStageBytes = kTileRows * kTileCols * 4;
+__device__ inline int stage_at(int row, int col) { return row * kTileCols + (col ^ ((row & 7) << 2)); }
+
+// this wave's sums, scaled, into the stage; a barrier has to come before and after
+__device__ inline void stage_sums(float* stage, const Sums& acc, int wm, int wn, int lane, float scale) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        stage[stage_at(64 * wm + 32 * i + sum_row(lane, r), 64 * wn + 32 * j + (lane & 31))] =
+            acc.v[i][j][r] * scale;
+}
+
 // vector loads and stores at the alignment of the elements (rows of odd width)
 template <class T, int N>
 struct __attribute__((packed, aligned(sizeof(T)))) Pack {
