@@ -5,12 +5,12 @@
 //   dx        dz W_g^T (+ dy), dz = dy act'(z)    one product of depth n_out
 //   dW, db    x^T dz, sum of dz over a group      products of depth rows
 //
-// Rows are addressed by place in the group order; a tile of 128 places belongs
-// to one group.  A first launch lists the tiles (group_ptr lives on the
+// Rows are addressed by place in the group order; a tile of 64 or 128 places
+// belongs to one group.  A first launch lists the tiles (group_ptr lives on the
 // device, so the launch's grid is an upper bound, and the workgroups past the
 // last tile leave at once) and lays the weights of the groups that have rows
 // out as the product tile reads them: the reduction entries of a column
-// together, in steps of 64, padded with zeros, float32 as scaled float16 pairs.
+// together, in steps of 32, padded with zeros, float32 as scaled float16 pairs.
 // Per float32 weight that is 8 bytes written and read again once per row tile.
 #include <hip/hip_runtime.h>
 
@@ -117,13 +117,13 @@ __device__ inline void list_tiles(const TileList& tl, const int64_t* ptr, int n_
 // Weights as the product tile reads them
 // ---------------------------------------------------------------------------
 
-// [group][step of 64][plane][columns padded to 128][64 entries], and for
+// [group][step of 32][plane][columns padded to 128][32 entries], and for
 // float32 the exponent of each column
 struct Weights {
   char* planes;
   int32_t* exps;
   int steps, cols_pad, planes_n;
-  __host__ __device__ int64_t step_bytes() const { return int64_t(planes_n) * cols_pad * 128; }
+  __host__ __device__ int64_t step_bytes() const { return int64_t(planes_n) * cols_pad * kRowBytes; }
 };
 
 struct PrepArgs {
@@ -166,7 +166,7 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
     most[q][r] = m;
     __syncthreads();
     if (threadIdx.x < kPrepCols) {
-      for (int i = 0; i < 16; ++i) m = fmaxf(m, most[i][threadIdx.x]);
+      for (int i = 0; i < 16; ++i) m = i ? fmaxf(m, most[i][threadIdx.x]) : most[0][threadIdx.x];
       const int e = m > 0.0f ? exp_for(m) : 0;
       exps[threadIdx.x] = e;
       a.out.exps[int64_t(g) * a.out.cols_pad + c0 + threadIdx.x] = e;
@@ -174,12 +174,13 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
     __syncthreads();
   }
   // slots (column, 8 entries)
-  const int r = Back ? threadIdx.x / 8 % kPrepCols : threadIdx.x % kPrepCols;
-  const int first = Back ? threadIdx.x % 8 + threadIdx.x / 256 * 8 : threadIdx.x / kPrepCols;
+  constexpr int kSlots = kDepth / 8;
+  const int r = Back ? threadIdx.x / 16 : threadIdx.x % kPrepCols;
+  const int first = Back ? threadIdx.x % 16 : threadIdx.x / kPrepCols;
   const int c = c0 + r;
   const float scale = kSplit ? exp2_of(exps[r]) : 1.0f;
 #pragma unroll 2
-  for (int sl = first; sl < a.out.steps * 8; sl += 16) {
+  for (int sl = first; sl < a.out.steps * kSlots; sl += 16) {
     float f[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) f[j] = c < a.cols && sl * 8 + j < a.depth ? at(c, sl * 8 + j) : 0.0f;
@@ -200,9 +201,10 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
                 unsigned(__builtin_bit_cast(unsigned short, y)) << 16;
       }
     }
-    char* to = a.out.planes + (int64_t(g) * a.out.steps + sl / 8) * a.out.step_bytes() + slot_at(c, sl % 8);
+    char* to = a.out.planes + (int64_t(g) * a.out.steps + sl / kSlots) * a.out.step_bytes() +
+               slot_at(c, sl % kSlots);
     *reinterpret_cast<u4*>(to) = hi;
-    if (kSplit) *reinterpret_cast<u4*>(to + int64_t(a.out.cols_pad) * 128) = lo;
+    if (kSplit) *reinterpret_cast<u4*>(to + int64_t(a.out.cols_pad) * kRowBytes) = lo;
   }
 }
 
@@ -221,50 +223,48 @@ __global__ void __launch_bounds__(kPrepThreads) grouped_prepare_kernel(PrepArgs 
   lay_weights<T, Back>(a, static_cast<int>(b / col_blocks), static_cast<int>(b % col_blocks) * kPrepCols);
 }
 
-// dz = dy act'(z) by place: float32 as it is, half types as a pair of their own
-// type, hi + lo (16 or 22 bits: dz is an intermediate, rounded to its 8 or 11 bits
-// it would add as much error to dx and dW as their own rounding does)
-template <class T>
-__device__ inline unsigned pair_of(float x) {
-  const T hi = from_f32<T>(x), lo = from_f32<T>(x - to_f32(hi));
-  return unsigned(__builtin_bit_cast(unsigned short, hi)) |
-         unsigned(__builtin_bit_cast(unsigned short, lo)) << 16;
-}
-
+// dz = dy act'(z) by place: float32 as it is, half types as a plane of their own
+// type and one of what that leaves, hi + lo (16 or 22 bits: dz is an intermediate;
+// rounded to its 8 or 11 bits it would add as much error to dx and dW as their own
+// rounding does)
 template <class T>
 __global__ void __launch_bounds__(kThreads) grouped_dz_kernel(
     const int64_t* __restrict__ ptr, const int32_t* __restrict__ order, int n_groups, int64_t n,
     int cols, int pitch, const T* __restrict__ dy, int64_t ldy, const T* __restrict__ z, int64_t ldz,
-    unsigned* __restrict__ dz) {
+    T* __restrict__ dz) {
+  constexpr int kEach = 16 / sizeof(T);
   const int64_t live = clamp_place(ptr[n_groups], n);
-  const int quads = pitch / 4;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < live * quads;
+  const int each = pitch / kEach;
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < live * each;
        i += int64_t(gridDim.x) * kThreads) {
-    const int64_t place = i / quads;
-    const int c = static_cast<int>(i - place * quads) * 4;
+    const int64_t place = i / each;
+    const int c = static_cast<int>(i - place * each) * kEach;
     const int64_t row = row_at(order, place, n);
-    u4 out = {0, 0, 0, 0};
+    Pack<T, kEach> a = {}, b = {}, hi, lo;
     if (row >= 0) {
-      T a[4], b[4];
-      if (c + 4 <= cols) {
-        const Pack<T, 4> pa = *reinterpret_cast<const Pack<T, 4>*>(dy + row * ldy + c);
-        const Pack<T, 4> pb = *reinterpret_cast<const Pack<T, 4>*>(z + row * ldz + c);
-        for (int j = 0; j < 4; ++j) a[j] = pa.v[j], b[j] = pb.v[j];
+      if (c + kEach <= cols) {
+        a = *reinterpret_cast<const Pack<T, kEach>*>(dy + row * ldy + c);
+        b = *reinterpret_cast<const Pack<T, kEach>*>(z + row * ldz + c);
       } else {
-        for (int j = 0; j < 4; ++j) {
-          a[j] = c + j < cols ? dy[row * ldy + c + j] : from_f32<T>(0.0f);
-          b[j] = c + j < cols ? z[row * ldz + c + j] : from_f32<T>(0.0f);
-        }
-      }
-      for (int j = 0; j < 4; ++j) {
-        const float v = to_f32(a[j]) * silu_slope(to_f32(b[j]));
-        if constexpr (sizeof(T) == 4)
-          out[j] = __builtin_bit_cast(unsigned, v);
-        else
-          out[j] = pair_of<T>(v);
+        for (int j = 0; j < kEach; ++j)
+          if (c + j < cols) {
+            a.v[j] = dy[row * ldy + c + j];
+            b.v[j] = z[row * ldz + c + j];
+          }
       }
     }
-    *reinterpret_cast<u4*>(dz + place * pitch + c) = out;
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      float v = to_f32(a.v[j]) * silu_slope(to_f32(b.v[j]));
+      // v as one value: fused with the product, the two conversions below could
+      // round it to neighbouring hi at a tie
+      asm("" : "+v"(v));
+      hi.v[j] = from_f32<T>(v);
+      if (sizeof(T) == 2) lo.v[j] = from_f32<T>(v - to_f32(hi.v[j]));
+    }
+    typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
+    *reinterpret_cast<V*>(dz + place * pitch + c) = __builtin_bit_cast(V, hi);
+    if (sizeof(T) == 2) *reinterpret_cast<V*>(dz + (n + place) * pitch + c) = __builtin_bit_cast(V, lo);
   }
 }
 
@@ -272,10 +272,13 @@ __global__ void __launch_bounds__(kThreads) grouped_dz_kernel(
 // Rows times weights
 // ---------------------------------------------------------------------------
 
-// How an operand's entries come: float32, a half type, or pairs of one
+// How an operand's entries come: float32, a half type, or a plane of one and a
+// plane of what that leaves
 enum Source { kFloat, kHalf, kPair };
 template <Source S>
-constexpr int planes_of() { return S == kHalf ? 1 : 2; }
+constexpr int planes_of = S == kHalf ? 1 : 2;
+template <Source S>
+constexpr int bytes_of = S == kFloat ? 4 : 2;
 
 struct RowsArgs {
   const int32_t* order;
@@ -286,7 +289,7 @@ struct RowsArgs {
   int kin, kout;
   const void* in;   // rows of kin entries, ldin apart
   int64_t ldin;
-  int by_place;     // ``in`` is in group order
+  int by_place;     // ``in`` is in group order; its second plane n ldin entries on
   Weights w;
   const void* bias;
   int silu;
@@ -299,58 +302,72 @@ struct RowsArgs {
 // eight entries of a row as they come
 template <Source S>
 struct Raw {
-  u4 v[S == kHalf ? 1 : 2];
+  u4 v[planes_of<S>];
 };
 
+// entries k .. k + 7 of a row, zeros from kin on; ``row`` starts at any multiple
+// of an entry's size
 template <Source S>
-__device__ inline void load_raw(Raw<S>& r, const char* row, int k, int kin) {
-  constexpr int kSize = S == kHalf ? 2 : 4;
+__device__ inline void load_raw(Raw<S>& r, const char* row, int64_t plane, int k, int kin) {
   if (k + 8 <= kin) {
-    // rows start at multiples of the entry's size only
-    typedef typename std::conditional<S == kHalf, unsigned short, unsigned>::type W;
-    const Pack<W, 8> p = *reinterpret_cast<const Pack<W, 8>*>(row + int64_t(k) * kSize);
-    __builtin_memcpy(&r, &p, sizeof(r));
+    if constexpr (S == kFloat) {
+      const Pack<unsigned, 8> p = *reinterpret_cast<const Pack<unsigned, 8>*>(row + int64_t(k) * 4);
+      __builtin_memcpy(&r, &p, sizeof(r));
+    } else {
+#pragma unroll
+      for (int i = 0; i < planes_of<S>; ++i) {
+        const Pack<unsigned short, 8> p =
+            *reinterpret_cast<const Pack<unsigned short, 8>*>(row + i * plane + int64_t(k) * 2);
+        __builtin_memcpy(&r.v[i], &p, 16);
+      }
+    }
   } else {
     const u4 none = {0, 0, 0, 0};
-    for (unsigned i = 0; i < sizeof(r) / 16; ++i) r.v[i] = none;
+#pragma unroll
+    for (int i = 0; i < planes_of<S>; ++i) r.v[i] = none;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       if (k + j < kin) {
-        if constexpr (S == kHalf)
-          r.v[0][j / 2] |= unsigned(reinterpret_cast<const unsigned short*>(row)[k + j]) << (16 * (j & 1));
-        else
+        if constexpr (S == kFloat) {
           r.v[j / 4][j % 4] = reinterpret_cast<const unsigned*>(row)[k + j];
+        } else {
+#pragma unroll
+          for (int i = 0; i < planes_of<S>; ++i)
+            r.v[i][j / 2] |= unsigned(reinterpret_cast<const unsigned short*>(row + i * plane)[k + j])
+                             << (16 * (j & 1));
+        }
       }
   }
 }
 
-template <class T, Source S>
+template <class T, Source S, int NB>
 __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
-  constexpr int PA = planes_of<S>(), PB = S == kFloat ? 2 : 1;
+  constexpr int PA = planes_of<S>, PB = S == kFloat ? 2 : 1;
   constexpr bool kBf = std::is_same<T, __bf16>::value;
-  constexpr int kOperands = (PA + PB) * kPlane;
-  __shared__ __attribute__((aligned(16))) char lds[kOperands > kStageBytes ? kOperands : kStageBytes];
-  __shared__ int32_t row_of[kTileRows];   // -1: nothing is stored
-  __shared__ int32_t change[kTileRows];   // exponent that a row's sums are to move by
-  __shared__ int32_t row_exp[kTileRows];
-  __shared__ int32_t flag[2];
-  char* la = lds;
-  char* lb = lds + PA * kPlane;
+  constexpr int kTile = kSide<NB>, kOne = kPlane<NB>;
+  constexpr int kHalfLds = (PA + PB) * kOne;   // one step's operands
+  constexpr int kStageRows = kHalfLds * 2 >= kTile * kTile * 4 ? kTile : kTile / 2;
+  constexpr int kStage = kStageRows * kTile * 4;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds > kStage ? 2 * kHalfLds : kStage];
+  __shared__ int32_t row_of[kTile];      // -1: nothing is stored
+  __shared__ int32_t change[2][kTile];   // exponent that a row's sums are to move by
+  __shared__ int32_t row_exp[kTile];
+  __shared__ int32_t flag[3];
 
-  const int col_tiles = a.w.cols_pad / kTileCols;
+  const int col_tiles = (a.kout + kTile - 1) / kTile;
   const int64_t total = int64_t(*a.n_tiles) * col_tiles;
   if (blockIdx.x >= total) return;
   // the column tiles of a row tile follow each other on one XCD
   const int64_t work = xcd_block(blockIdx.x, total);
   const RowTile t = a.tiles[work / col_tiles];
-  const int c0 = static_cast<int>(work % col_tiles) * kTileCols;
+  const int c0 = static_cast<int>(work % col_tiles) * kTile;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1;
   T* out = static_cast<T*>(a.out);
   T* zout = static_cast<T*>(a.zout);
 
   if (t.group == a.n_groups) {   // rows of no group
-    const int width = a.kout - c0 < kTileCols ? a.kout - c0 : kTileCols;
+    const int width = a.kout - c0 < kTile ? a.kout - c0 : kTile;
     for (int i = tid; i < t.count * width; i += kThreads) {
       const int64_t row = row_at(a.order, t.first + i / width, a.n);
       if (row < 0) continue;
@@ -360,76 +377,82 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     return;
   }
 
-  // this thread's four rows (32 i + tid / 8) and its eight entries of a step;
-  // rows past the tile repeat its last one, and nothing of them is stored
-  const int sub = tid & 7;
-  constexpr int kSize = S == kHalf ? 2 : 4;
-  const char* rows[4];
+  // this thread's NB rows (64 i + tid / 4) and its eight entries of a step; rows
+  // past the tile repeat its last one, and nothing of them is stored
+  const int sub = tid & 3, own = tid / 4;
+  const char* rows[NB];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    int r = 32 * i + tid / 8;
+  for (int i = 0; i < NB; ++i) {
+    int r = 64 * i + own;
     r = r < t.count ? r : t.count - 1;
-    int64_t row = a.by_place ? t.first + r : row_at(a.order, t.first + r, a.n);
-    if (sub == 0) {
-      const int64_t to = a.by_place ? row_at(a.order, t.first + r, a.n) : row;
-      row_of[32 * i + tid / 8] = 32 * i + tid / 8 < t.count ? static_cast<int32_t>(to) : -1;
-    }
-    row = row < 0 ? 0 : row;
-    rows[i] = static_cast<const char*>(a.in) + row * a.ldin * kSize;
+    const int64_t to = row_at(a.order, t.first + r, a.n);
+    if (sub == 0) row_of[64 * i + own] = 64 * i + own < t.count ? static_cast<int32_t>(to) : -1;
+    const int64_t row = a.by_place ? t.first + r : to < 0 ? 0 : to;
+    rows[i] = static_cast<const char*>(a.in) + row * a.ldin * bytes_of<S>;
   }
-  const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * 128;
-  const int64_t wplane = int64_t(a.w.cols_pad) * 128;
+  const int64_t in_plane = a.n * a.ldin * bytes_of<S>;
+  const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
+  const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
 
-  Raw<S> ra[4];
-  u4 rb[PB][4];
-  auto fetch = [&](int step) {
-    const int k = step * kDepth + sub * 8;
-    if ((step + 1) * kDepth <= a.kin) {
+  Raw<S> ra[2][NB];
+  u4 rb[2][PB][NB];
+  auto fetch = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const bool in = step < a.w.steps;   // past the end: one line of the weights
+    const int k = in ? step * kDepth + sub * 8 : 0;
+    if (!in || (step + 1) * kDepth <= a.kin) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load_raw<S>(ra[i], rows[i], k, 1 << 30);
+      for (int i = 0; i < NB; ++i)
+        load_raw<S>(ra[q][i], in ? rows[i] : wsrc, in ? in_plane : 0, k, 1 << 30);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) load_raw<S>(ra[i], rows[i], k, a.kin);
+      for (int i = 0; i < NB; ++i) load_raw<S>(ra[q][i], rows[i], in_plane, k, a.kin);
     }
-    const char* src = wsrc + step * a.w.step_bytes();
+    const char* src = in ? wsrc + step * a.w.step_bytes() + tid * 16 : wsrc;
 #pragma unroll
     for (int p = 0; p < PB; ++p)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        rb[p][i] = *reinterpret_cast<const u4*>(src + p * wplane + i * 4096 + tid * 16);
+      for (int i = 0; i < NB; ++i)
+        rb[q][p][i] = *reinterpret_cast<const u4*>(src + (in ? p * wplane + i * 4096 : 0));
   };
 
-  Sums acc;
+  Sums<NB> acc;
+  acc.clear();
+  int e[NB];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) acc.v[i][j] = v16f{};
-  int e[4] = {kFirstExp, kFirstExp, kFirstExp, kFirstExp};
-  unsigned changed = 0;
+  for (int i = 0; i < NB; ++i) e[i] = kFirstExp;
+  unsigned changed[2] = {0, 0};
   if (S == kFloat) {
-    if (tid < kTileRows) change[tid] = 0;
-    if (tid < 2) flag[tid] = 0;
+    if (tid < 2 * kTile) change[tid / kTile][tid % kTile] = 0;
+    if (tid < 3) flag[tid] = 0;
+    __syncthreads();
   }
 
-  fetch(0);
-  for (int step = 0; step < a.w.steps; ++step) {
-    __syncthreads();   // the step before has been read
-    if constexpr (S == kFloat) {
-      if (tid == 0) flag[(step + 1) & 1] = 0;
-      if (changed) {
+  auto put = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    char* la = lds + q * kHalfLds;
+    char* lb = la + PA * kOne;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (changed >> i & 1) change[32 * i + tid / 8] = 0;
-        changed = 0;
+    for (int p = 0; p < PB; ++p)
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+        *reinterpret_cast<u4*>(lb + p * kOne + i * 4096 + tid * 16) = rb[q][p][i];
+    if constexpr (S == kFloat) {
+      if (tid == 0) flag[(step + 1) % 3] = 0;
+      if (changed[q]) {   // two steps ago; its readers are past it
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+          if (changed[q] >> i & 1) change[q][64 * i + own] = 0;
+        changed[q] = 0;
       }
-      float f[4][8];
+      float f[NB][8];
       bool over = false;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < NB; ++i) {
         float m = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const unsigned bits = ra[i].v[j / 4][j % 4];
+          const unsigned bits = ra[q][i].v[j / 4][j % 4];
           f[i][j] = __builtin_bit_cast(float, bits);
           m = fmaxf(m, fabsf(f[i][j]));
         }
@@ -437,26 +460,25 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
       }
       if (__ballot(over) != 0) {   // a row has outgrown its scale: rare past the first step
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NB; ++i) {
           float m = 0.0f;
 #pragma unroll
           for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[i][j]));
           m = fmaxf(m, __shfl_xor(m, 1));
           m = fmaxf(m, __shfl_xor(m, 2));
-          m = fmaxf(m, __shfl_xor(m, 4));
           if (m * exp2_of(e[i]) > kLimit) {
             const int now = exp_for(m);
             if (sub == 0) {
-              change[32 * i + tid / 8] = now - e[i];
-              changed |= 1u << i;
-              flag[step & 1] = 1;
+              change[q][64 * i + own] = now - e[i];
+              changed[q] |= 1u << i;
+              flag[step % 3] = 1;
             }
             e[i] = now;
           }
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < NB; ++i) {
         const float scale = exp2_of(e[i]);
         u4 hi, lo;
 #pragma unroll
@@ -466,58 +488,58 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
           hi[j] = h;
           lo[j] = l;
         }
-        const int at = slot_at(32 * i + tid / 8, sub);
+        const int at = slot_at(64 * i + own, sub);
         *reinterpret_cast<u4*>(la + at) = hi;
-        *reinterpret_cast<u4*>(la + kPlane + at) = lo;
+        *reinterpret_cast<u4*>(la + kOne + at) = lo;
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int at = slot_at(32 * i + tid / 8, sub);
-        if constexpr (S == kHalf) {
-          *reinterpret_cast<u4*>(la + at) = ra[i].v[0];
-        } else {
-          u4 hi, lo;
+      for (int i = 0; i < NB; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const unsigned x = ra[i].v[j / 2][2 * j % 4], y = ra[i].v[j / 2][2 * j % 4 + 1];
-            hi[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-            lo[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-          }
-          *reinterpret_cast<u4*>(la + at) = hi;
-          *reinterpret_cast<u4*>(la + kPlane + at) = lo;
-        }
-      }
+        for (int p = 0; p < PA; ++p)
+          *reinterpret_cast<u4*>(la + p * kOne + slot_at(64 * i + own, sub)) = ra[q][i].v[p];
     }
-#pragma unroll
-    for (int p = 0; p < PB; ++p)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<u4*>(lb + p * kPlane + i * 4096 + tid * 16) = rb[p][i];
-    __syncthreads();
-    if (step + 1 < a.w.steps) fetch(step + 1);
+  };
+  auto before = [&](int step) {
     if constexpr (S == kFloat) {
-      if (flag[step & 1]) {
+      if (flag[step % 3]) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            const int d = change[64 * wm + 32 * i + sum_row(lane, r)];
+            const int d = change[step & 1][kTile / 2 * wm + 32 * i + sum_row(lane, r)];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) acc.v[i][j][r] = ldexpf(acc.v[i][j][r], d);
+            for (int j = 0; j < NB; ++j) acc.v[i][j][r] = ldexpf(acc.v[i][j][r], d);
           }
       }
     }
-    if (c0 + 64 * wn < a.kout)
-      tile_step<kBf, PA, PB>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
-  }
+  };
+  const bool live = c0 + kTile / 2 * wn < a.kout && kTile / 2 * wm < t.count;
+  auto multiply = [&](int step, auto&& between) {
+    const char* la = lds + (step & 1) * kHalfLds + wm * (kTile / 2) * kRowBytes;
+    const char* lb = lds + (step & 1) * kHalfLds + PA * kOne + wn * (kTile / 2) * kRowBytes;
+    Part<NB, PA> fa[2];
+    Part<NB, PB> fb[2];
+    if (live) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        load_part(fa[ks], la, kOne, lane, ks);
+        load_part(fb[ks], lb, kOne, lane, ks);
+      }
+      multiply_parts<kBf>(acc, fa[0], fb[0]);
+    }
+    between();
+    if (live) multiply_parts<kBf>(acc, fa[1], fb[1]);
+  };
+  run_steps(a.w.steps, fetch, put, before, multiply);
 
-  // outputs through LDS, so that rows are written in one piece: 32 lanes a row
+  // outputs through LDS, so that rows are written in one piece
   if (S == kFloat && sub == 0)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) row_exp[32 * i + tid / 8] = e[i];
+    for (int i = 0; i < NB; ++i) row_exp[64 * i + own] = e[i];
   float* stage = reinterpret_cast<float*>(lds);
-  const int quad = tid & 31, c = c0 + quad * 4;
+  constexpr int kLanes = kTile / 4, kRowsOnce = kThreads / kLanes;   // lanes a row, rows at a time
+  const int quad = tid % kLanes, c = c0 + quad * 4;
   const T* bias = a.bias ? static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
   float bq[4];
   int eq[4] = {};
@@ -526,53 +548,59 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     bq[j] = bias && c + j < a.kout ? to_f32(bias[c + j]) : 0.0f;
     if (S == kFloat) eq[j] = a.w.exps[int64_t(t.group) * a.w.cols_pad + c + j];
   }
-  __syncthreads();
-  stage_sums(stage, acc, wm, wn, lane, 1.0f);
-  __syncthreads();
-  if (c >= a.kout) return;
   const bool whole = c + 4 <= a.kout;
-  constexpr int kBatch = 4;   // rows in flight
 #pragma unroll 1
-  for (int r0 = tid / 32; r0 < t.count; r0 += 8 * kBatch) {
-    int64_t row[kBatch];
-    Pack<T, 4> res[kBatch];
+  for (int h = 0; h < kTile; h += kStageRows) {
+    if (h > 0) __syncthreads();
+    if (kStageRows == kTile || kTile / 2 * wm == h)
+      stage_sums(stage, acc, kStageRows == kTile ? kTile / 2 * wm : 0, kTile / 2 * wn, lane, 1.0f);
+    __syncthreads();
+    if (c >= a.kout) continue;
+    constexpr int kBatch = 4;   // rows in flight
+    const int last = t.count - h < kStageRows ? t.count - h : kStageRows;
+#pragma unroll 1
+    for (int r0 = tid / kLanes; r0 < last; r0 += kRowsOnce * kBatch) {
+      int64_t row[kBatch];
+      Pack<T, 4> res[kBatch];
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      row[k] = row_of[r0 + 8 * k];
-      if (a.residual && row[k] >= 0) {
-        const T* src = static_cast<const T*>(a.residual) + row[k] * a.ldres + c;
-        if (whole)
-          res[k] = *reinterpret_cast<const Pack<T, 4>*>(src);
-        else
-          for (int j = 0; j < 4; ++j) res[k].v[j] = c + j < a.kout ? src[j] : from_f32<T>(0.0f);
+      for (int k = 0; k < kBatch; ++k) {
+        const int r = r0 + kRowsOnce * k;
+        row[k] = r < last ? row_of[h + r] : -1;
+        if (a.residual && row[k] >= 0) {
+          const T* src = static_cast<const T*>(a.residual) + row[k] * a.ldres + c;
+          if (whole)
+            res[k] = *reinterpret_cast<const Pack<T, 4>*>(src);
+          else
+            for (int j = 0; j < 4; ++j) res[k].v[j] = c + j < a.kout ? src[j] : from_f32<T>(0.0f);
+        }
       }
-    }
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
-      const int r = r0 + 8 * k;
-      const v4f s = *reinterpret_cast<const v4f*>(stage + stage_at(r, quad * 4));
-      const int er = S == kFloat ? row_exp[r] : 0;
-      Pack<T, 4> py, pz;
+      for (int k = 0; k < kBatch; ++k) {
+        if (row[k] < 0) continue;
+        const int r = r0 + kRowsOnce * k;
+        const v4f s = *reinterpret_cast<const v4f*>(stage + stage_at<NB>(r, quad * 4));
+        const int er = S == kFloat ? row_exp[h + r] : 0;
+        Pack<T, 4> py, pz;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float z = S == kFloat ? ldexpf(s[j], -er - eq[j]) : s[j];
-        z += bq[j];
-        float y = a.silu ? z * logistic(z) : z;
-        if (a.residual) y += to_f32(res[k].v[j]);
-        py.v[j] = from_f32<T>(y);
-        pz.v[j] = from_f32<T>(z);
-      }
-      if (row[k] < 0) continue;
-      const int64_t to = row[k] * a.kout + c;
-      if (whole) {
-        *reinterpret_cast<Pack<T, 4>*>(out + to) = py;
-        if (zout) *reinterpret_cast<Pack<T, 4>*>(zout + to) = pz;
-      } else {
-        for (int j = 0; j < 4; ++j)
-          if (c + j < a.kout) {
-            out[to + j] = py.v[j];
-            if (zout) zout[to + j] = pz.v[j];
-          }
+        for (int j = 0; j < 4; ++j) {
+          float z = S == kFloat ? ldexpf(s[j], -er - eq[j]) : s[j];
+          z += bq[j];
+          float y = a.silu ? z * logistic(z) : z;
+          if (a.residual) y += to_f32(res[k].v[j]);
+          py.v[j] = from_f32<T>(y);
+          pz.v[j] = from_f32<T>(z);
+        }
+        const int64_t to = row[k] * a.kout + c;
+        if (whole) {
+          *reinterpret_cast<Pack<T, 4>*>(out + to) = py;
+          if (zout) *reinterpret_cast<Pack<T, 4>*>(zout + to) = pz;
+        } else {
+          for (int j = 0; j < 4; ++j)
+            if (c + j < a.kout) {
+              out[to + j] = py.v[j];
+              if (zout) zout[to + j] = pz.v[j];
+            }
+        }
       }
     }
   }
@@ -590,7 +618,7 @@ struct OuterArgs {
   int k, m;
   const void* x;      // by row
   int64_t ldx;
-  const void* dz;     // by row, or by place
+  const void* dz;     // by row, or by place (its second plane n lddz entries on)
   int64_t lddz;
   int by_place;
   void* dw;           // null: not formed
@@ -599,211 +627,308 @@ struct OuterArgs {
   float* db_parts;    // [block][m]
 };
 
-// 32 places x 64 columns of an operand, a column a lane, as they come
+constexpr int kOuterTile = kSide<2>;
+
+// this workgroup's tile: columns r0 .. of x and c0 .. of dz over a block of rows;
+// false past the last
+struct OuterTile {
+  RowTile t;
+  int64_t block;
+  int r0, c0;
+};
+__device__ inline bool outer_tile(const OuterArgs& a, OuterTile& o) {
+  const int row_tiles = a.dw ? (a.k + kOuterTile - 1) / kOuterTile : 1;
+  const int col_tiles = (a.m + kOuterTile - 1) / kOuterTile;
+  const int64_t total = int64_t(*a.n_blocks) * row_tiles * col_tiles;
+  if (blockIdx.x >= total) return false;
+  // the tiles of a block of rows follow each other on one XCD
+  const int64_t work = xcd_block(blockIdx.x, total);
+  o.block = work / (row_tiles * col_tiles);
+  o.t = a.blocks[o.block];
+  o.r0 = static_cast<int>(work / col_tiles % row_tiles) * kOuterTile;
+  o.c0 = static_cast<int>(work % col_tiles) * kOuterTile;
+  return true;
+}
+
+// sums of a tile, scaled by 2^-(row exponent + column exponent), to dW where no
+// other block adds to the group, else to the block's own sums
+template <class T>
+__device__ inline void store_outer(const OuterArgs& a, const OuterTile& o, const Sums<2>& acc,
+                                   const int32_t* exps) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
+  const bool whole = o.t.parts == 1;
+  T* dw = static_cast<T*>(a.dw) + int64_t(o.t.group) * a.k * a.m;
+  float* part = a.parts + o.block * a.k * a.m;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int cl = 64 * wn + 32 * j + (lane & 31), c = o.c0 + cl;
+      const int ec = exps ? exps[kOuterTile + cl] : 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int rl = 64 * wm + 32 * i + sum_row(lane, r), row = o.r0 + rl;
+        if (row >= a.k || c >= a.m) continue;
+        float v = acc.v[i][j][r];
+        if (exps) v = ldexpf(v, -exps[rl] - ec);
+        if (whole)
+          dw[int64_t(row) * a.m + c] = from_f32<T>(v);
+        else
+          part[int64_t(row) * a.m + c] = v;
+      }
+    }
+}
+template <class T>
+__device__ inline void store_bias(const OuterArgs& a, const OuterTile& o, int col, float v) {
+  if (o.c0 + col >= a.m) return;
+  if (o.t.parts == 1)
+    static_cast<T*>(a.db)[int64_t(o.t.group) * a.m + o.c0 + col] = from_f32<T>(v);
+  else
+    a.db_parts[o.block * a.m + o.c0 + col] = v;
+}
+
+// float32.  A wave fetches 64 columns of one operand, so a lane has a column of a
+// step, and its scale, to itself.
 struct Column {
-  unsigned v[32];
+  float v[kDepth];
 };
 
 // Column ``col`` of the places first .. first + 31 (zeros from ``end`` on).  The
 // row is the same for all lanes, so its address is scalar work: a lane holds the
 // row of one place, and each load takes its own from there.
-template <Source S>
-__device__ inline void load_columns(Column& r, const void* base, int64_t ld, const int32_t* order,
-                                    int64_t n, int64_t first, int64_t end, int col) {
-  constexpr int kSize = S == kHalf ? 2 : 4;
+__device__ inline void load_column(Column& r, const float* base, int64_t ld, const int32_t* order,
+                                   int64_t n, int64_t first, int64_t end, int col) {
   const int64_t place = first + (threadIdx.x & 31);
   int64_t mine = -1;
   if (place < end) mine = row_at(order, place, n);
   const bool whole = __ballot(mine < 0) == 0;
   const int row = static_cast<int>(mine < 0 ? 0 : mine);
-  const int64_t pitch = ld * kSize;
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    const char* p = static_cast<const char*>(base) + __builtin_amdgcn_readlane(row, i) * pitch;
-    r.v[i] = S == kHalf ? reinterpret_cast<const unsigned short*>(p)[col]
-                        : reinterpret_cast<const unsigned*>(p)[col];
-  }
+  for (int i = 0; i < kDepth; ++i) r.v[i] = (base + __builtin_amdgcn_readlane(row, i) * ld)[col];
   if (!whole)
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-      r.v[i] = __builtin_amdgcn_readlane(static_cast<int>(mine < 0), i) ? 0 : r.v[i];
+    for (int i = 0; i < kDepth; ++i)
+      r.v[i] = __builtin_amdgcn_readlane(static_cast<int>(mine < 0), i) ? 0.0f : r.v[i];
 }
 
-template <class T, Source S>
-__device__ inline float value_of(unsigned v) {
-  if constexpr (S == kFloat) {
-    return __builtin_bit_cast(float, v);
-  } else {
-    const T hi = __builtin_bit_cast(T, static_cast<unsigned short>(v & 0xffff));
-    if constexpr (S == kHalf) return to_f32(hi);
-    return to_f32(hi) + to_f32(__builtin_bit_cast(T, static_cast<unsigned short>(v >> 16)));
-  }
-}
-
-// the column's 32 entries into slots 4 half .. 4 half + 3 of its row in LDS
-template <Source S>
-__device__ inline void store_columns(const Column& r, char* lds, int row, int half, float scale) {
-#pragma unroll
-  for (int s = 0; s < 4; ++s) {
-    u4 hi, lo;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned x = r.v[8 * s + 2 * j], y = r.v[8 * s + 2 * j + 1];
-      if constexpr (S == kFloat) {
-        unsigned h, l;
-        split2(__builtin_bit_cast(float, x) * scale, __builtin_bit_cast(float, y) * scale, &h, &l);
-        hi[j] = h;
-        lo[j] = l;
-      } else {
-        hi[j] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-        if (S == kPair) lo[j] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-      }
-    }
-    const int at = slot_at(row, 4 * half + s);
-    *reinterpret_cast<u4*>(lds + at) = hi;
-    if (S != kHalf) *reinterpret_cast<u4*>(lds + kPlane + at) = lo;
-  }
-}
-
-template <class T, Source SX, Source SZ>
 __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a) {
-  constexpr int PA = planes_of<SX>(), PB = planes_of<SZ>();
-  constexpr bool kBf = std::is_same<T, __bf16>::value;
-  __shared__ __attribute__((aligned(16))) char lds[(PA + PB) * kPlane];
-  __shared__ unsigned most[kTileRows + kTileCols];   // largest magnitude of a column, as bits
-  __shared__ int32_t exps[kTileRows + kTileCols], change[kTileRows + kTileCols];
-  __shared__ int32_t flag[2];
-  __shared__ float bias_part[2][kTileCols];
-  char* la = lds;
-  char* lb = lds + PA * kPlane;
-
-  const int row_tiles = a.dw ? (a.k + kTileRows - 1) / kTileRows : 1;
-  const int col_tiles = (a.m + kTileCols - 1) / kTileCols;
-  const int64_t total = int64_t(*a.n_blocks) * row_tiles * col_tiles;
-  if (blockIdx.x >= total) return;
-  // the tiles of a block of rows follow each other on one XCD
-  const int64_t work = xcd_block(blockIdx.x, total);
-  const int64_t block = work / (row_tiles * col_tiles);
-  const RowTile t = a.blocks[block];
-  const int r0 = static_cast<int>(work / col_tiles % row_tiles) * kTileRows;
-  const int c0 = static_cast<int>(work % col_tiles) * kTileCols;
+  constexpr int kOne = kPlane<2>, kHalfLds = 4 * kOne;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
+  // by column, x's then dz's: the exponent, and what it is to move by
+  __shared__ int32_t exps[2 * kOuterTile], change[2][2 * kOuterTile];
+  __shared__ int32_t flag[3];
+  OuterTile o;
+  if (!outer_tile(a, o)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const int side = wave & 1, half = wave >> 1;   // the columns and places that this wave fetches
-  const int mine = 64 * side + lane;
-  // columns past the last repeat it, and nothing of them is stored
-  const int xcol = r0 + mine < a.k ? r0 + mine : a.k - 1;
-  const int zcol = c0 + mine < a.m ? c0 + mine : a.m - 1;
-  const int64_t end = t.first + t.count;
-  const bool sums_bias = a.db && r0 == 0;
+  // waves 0 and 1 fetch x, 2 and 3 dz; columns past the last repeat it, and
+  // nothing of them is stored
+  const bool of_x = wave < 2;
+  const int mine = 64 * (wave & 1) + lane;
+  const int width = of_x ? a.k : a.m, at0 = of_x ? o.r0 : o.c0;
+  const int col = at0 + mine < width ? at0 + mine : width - 1;
+  const float* base = static_cast<const float*>(of_x ? a.x : a.dz);
+  const int64_t ld = of_x ? a.ldx : a.lddz;
+  const int32_t* order = !of_x && a.by_place ? nullptr : a.order;
+  const int64_t end = o.t.first + o.t.count;
+  const int steps = (o.t.count + kDepth - 1) / kDepth;
+  const bool sums_bias = a.db && o.r0 == 0 && !of_x;
 
-  Column cx, cz;
-  auto fetch = [&](int64_t first) {
-    load_columns<SX>(cx, a.x, a.ldx, a.order, a.n, first + 32 * half, end, xcol);
-    load_columns<SZ>(cz, a.dz, a.lddz, a.by_place ? nullptr : a.order, a.n, first + 32 * half, end,
-                     zcol);
+  Column c[2];
+  auto fetch = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    // past the end: the first row's first entry
+    const bool in = step < steps;
+    load_column(c[q], base, in ? ld : 0, in ? order : nullptr, a.n,
+                in ? o.t.first + int64_t(step) * kDepth : 0, in ? end : kDepth, in ? col : 0);
   };
-  Sums acc;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) acc.v[i][j] = v16f{};
-  float ex = exp2_of(kFirstExp), ez = ex, bias = 0.0f;
-  if (SX == kFloat) {
-    most[tid] = 0;
-    exps[tid] = kFirstExp;
-    if (tid < 2) flag[tid] = 0;
-    __syncthreads();
-  }
-
-  fetch(t.first);
-  int turn = 0;
-  for (int64_t p = t.first; p < end; p += kDepth, turn ^= 1) {
-    float mx = 0.0f, mz = 0.0f;
-    if constexpr (SX == kFloat) {
-#pragma unroll
-      for (int i = 0; i < 32; ++i) {
-        mx = fmaxf(mx, fabsf(__builtin_bit_cast(float, cx.v[i])));
-        mz = fmaxf(mz, fabsf(__builtin_bit_cast(float, cz.v[i])));
-      }
-      if (mx * ex > kLimit || mz * ez > kLimit) flag[turn] = 1;
-    }
+  Sums<2> acc;
+  acc.clear();
+  int e = kFirstExp;
+  bool changed[2] = {false, false};
+  float bias = 0.0f;
+  change[0][tid] = change[1][tid] = 0;
+  if (tid < 3) flag[tid] = 0;
+  __syncthreads();
+  auto put = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
     if (sums_bias)
 #pragma unroll
-      for (int i = 0; i < 32; ++i) bias += value_of<T, SZ>(cz.v[i]);
-    __syncthreads();   // the step before has been read; the flag is set
-    if constexpr (SX == kFloat) {
-      if (flag[turn]) {   // a column has outgrown its scale: rare past the first step
-        atomicMax(&most[mine], __builtin_bit_cast(unsigned, mx));
-        atomicMax(&most[kTileRows + mine], __builtin_bit_cast(unsigned, mz));
-        __syncthreads();
-        {
-          const float m = __builtin_bit_cast(float, most[tid]);
-          const int e = exps[tid];
-          const int now = m * exp2_of(e) > kLimit ? exp_for(m) : e;
-          change[tid] = now - e;
-          exps[tid] = now;
-        }
-        __syncthreads();
-        most[tid] = 0;
-        ex = exp2_of(exps[mine]);
-        ez = exp2_of(exps[kTileRows + mine]);
+      for (int i = 0; i < kDepth; ++i) bias += c[q].v[i];
+    if (!a.dw) return;
+    if (tid == 0) flag[(step + 1) % 3] = 0;
+    if (changed[q]) {   // two steps ago; its readers are past it
+      change[q][tid] = 0;
+      changed[q] = false;
+    }
+    float m = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kDepth; ++i) m = fmaxf(m, fabsf(c[q].v[i]));
+    if (m * exp2_of(e) > kLimit) {   // the column has outgrown its scale
+      const int now = exp_for(m);
+      change[q][tid] = now - e;
+      changed[q] = true;
+      flag[step % 3] = 1;
+      e = now;
+    }
+    const float scale = exp2_of(e);
+    char* to = lds + q * kHalfLds + (of_x ? 0 : 2 * kOne);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int d = change[64 * wm + 32 * i + sum_row(lane, r)];
+    for (int s = 0; s < kDepth / 8; ++s) {
+      u4 hi, lo;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-              acc.v[i][j][r] = ldexpf(acc.v[i][j][r],
-                                      d + change[kTileRows + 64 * wn + 32 * j + (lane & 31)]);
-          }
+      for (int j = 0; j < 4; ++j) {
+        unsigned h, l;
+        split2(c[q].v[8 * s + 2 * j] * scale, c[q].v[8 * s + 2 * j + 1] * scale, &h, &l);
+        hi[j] = h;
+        lo[j] = l;
       }
-      if (tid == 0) flag[turn ^ 1] = 0;
+      *reinterpret_cast<u4*>(to + slot_at(mine, s)) = hi;
+      *reinterpret_cast<u4*>(to + kOne + slot_at(mine, s)) = lo;
     }
-    if (a.dw) {
-      store_columns<SX>(cx, la, mine, half, ex);
-      store_columns<SZ>(cz, lb, mine, half, ez);
-    }
-    __syncthreads();
-    if (p + kDepth < end) fetch(p + kDepth);
-    if (a.dw && r0 + 64 * wm < a.k && c0 + 64 * wn < a.m)
-      tile_step<kBf, PA, PB>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
-  }
-
-  const bool whole = t.parts == 1;   // no other block adds to this group
-  if (a.dw) {
-    T* dw = static_cast<T*>(a.dw) + int64_t(t.group) * a.k * a.m;
-    float* part = a.parts + block * a.k * a.m;
+  };
+  auto before = [&](int step) {
+    if (!flag[step % 3]) return;
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int cl = 64 * wn + 32 * j + (lane & 31), c = c0 + cl;
-        const int ec = SX == kFloat ? exps[kTileRows + cl] : 0;
+      for (int r = 0; r < 16; ++r) {
+        const int d = change[step & 1][64 * wm + 32 * i + sum_row(lane, r)];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int rl = 64 * wm + 32 * i + sum_row(lane, r), row = r0 + rl;
-          if (row >= a.k || c >= a.m) continue;
-          float v = acc.v[i][j][r];
-          if (SX == kFloat) v = ldexpf(v, -exps[rl] - ec);
-          if (whole)
-            dw[int64_t(row) * a.m + c] = from_f32<T>(v);
-          else
-            part[int64_t(row) * a.m + c] = v;
-        }
+        for (int j = 0; j < 2; ++j)
+          acc.v[i][j][r] =
+              ldexpf(acc.v[i][j][r], d + change[step & 1][kOuterTile + 64 * wn + 32 * j + (lane & 31)]);
       }
-  }
-  if (sums_bias) {
-    bias_part[half][mine] = bias;
+  };
+  const bool live = a.dw && o.r0 + 64 * wm < a.k && o.c0 + 64 * wn < a.m;
+  auto multiply = [&](int step, auto&& between) {
+    const char* la = lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes;
+    const char* lb = lds + (step & 1) * kHalfLds + 2 * kOne + wn * 64 * kRowBytes;
+    Part<2, 2> fa[2], fb[2];
+    if (live) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        load_part(fa[ks], la, kOne, lane, ks);
+        load_part(fb[ks], lb, kOne, lane, ks);
+      }
+      multiply_parts<false>(acc, fa[0], fb[0]);
+    }
+    between();
+    if (live) multiply_parts<false>(acc, fa[1], fb[1]);
+  };
+  run_steps(steps, fetch, put, before, multiply);
+
+  if (a.dw) {
+    exps[tid] = e;
     __syncthreads();
-    if (tid < kTileCols && c0 + tid < a.m) {
-      const float v = bias_part[0][tid] + bias_part[1][tid];
-      if (whole)
-        static_cast<T*>(a.db)[int64_t(t.group) * a.m + c0 + tid] = from_f32<T>(v);
-      else
-        a.db_parts[block * a.m + c0 + tid] = v;
+    store_outer<float>(a, o, acc, exps);
+  }
+  if (sums_bias) store_bias<float>(a, o, mine, bias);
+}
+
+// Half types need no scale, so the rows go to LDS as they come, eight columns a
+// lane, and transposing reads turn them: 6 loads a lane and step for dz in two
+// planes, where a column a lane would take 64 loads of 2 or 4 bytes.
+template <class T, Source SZ>
+__global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterArgs a) {
+  constexpr int PB = planes_of<SZ>, kOne = kPlane<2>, kHalfLds = (1 + PB) * kOne;
+  constexpr bool kBf = std::is_same<T, __bf16>::value;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
+  __shared__ float bias_part[16][kOuterTile];
+  OuterTile o;
+  if (!outer_tile(a, o)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave >> 1, wn = wave & 1;
+  const int64_t end = o.t.first + o.t.count;
+  const int steps = (o.t.count + kDepth - 1) / kDepth;
+  const bool sums_bias = a.db && o.r0 == 0;
+  // places tid / 16 and tid / 16 + 16 of a step, columns 8 (tid % 16) .. of both operands
+  const int own = tid / 16, cg = tid % 16;
+  const int xc = o.r0 + 8 * cg, zc = o.c0 + 8 * cg;
+  const int64_t z_plane = a.n * a.lddz * 2;
+
+  // the row of each place, one step ahead of its use
+  int64_t row[2];
+  auto look_up = [&](int step) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t place = o.t.first + int64_t(step) * kDepth + 16 * i + own;
+      row[i] = place < end ? row_at(a.order, place, a.n) : -1;
+    }
+  };
+  Raw<kHalf> rx[2][2];
+  Raw<SZ> rz[2][2];
+  bool there[2][2];
+  look_up(0);
+  auto fetch = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      // places past the end: row 0, put as zeros
+      there[q][i] = row[i] >= 0;
+      const int64_t rx_row = there[q][i] ? row[i] : 0;
+      const int64_t rz_row =
+          !there[q][i] ? 0 : a.by_place ? o.t.first + int64_t(step) * kDepth + 16 * i + own : row[i];
+      const char* px = static_cast<const char*>(a.x) + rx_row * a.ldx * 2;
+      const char* pz = static_cast<const char*>(a.dz) + rz_row * a.lddz * 2;
+      load_raw<kHalf>(rx[q][i], px, 0, xc, a.k);
+      load_raw<SZ>(rz[q][i], pz, z_plane, zc, a.m);
+    }
+    look_up(step + 1);
+  };
+  float bias[8] = {};
+  auto put = [&](auto turn, int) {
+    constexpr int q = decltype(turn)::value;
+    const u4 none = {0, 0, 0, 0};
+    char* to = lds + q * kHalfLds + cg / 4 * 32 * kRowBytes;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int at = slot_at(16 * i + own, cg % 4);
+      *reinterpret_cast<u4*>(to + at) = there[q][i] ? rx[q][i].v[0] : none;
+#pragma unroll
+      for (int p = 0; p < PB; ++p) {
+        const u4 v = there[q][i] ? rz[q][i].v[p] : none;
+        *reinterpret_cast<u4*>(to + (1 + p) * kOne + at) = v;
+        if (sums_bias)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const unsigned w = v[j / 2];
+            bias[j] += to_f32(__builtin_bit_cast(T, static_cast<unsigned short>(j & 1 ? w >> 16 : w & 0xffff)));
+          }
+      }
+    }
+  };
+  Sums<2> acc;
+  acc.clear();
+  const bool live = a.dw && o.r0 + 64 * wm < a.k && o.c0 + 64 * wn < a.m;
+  auto multiply = [&](int step, auto&& between) {
+    const char* la = lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes;
+    const char* lb = lds + (step & 1) * kHalfLds + kOne + wn * 64 * kRowBytes;
+    Part<2, 1> fa[2];
+    Part<2, PB> fb[2];
+    if (live) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        load_part_turned(fa[ks], la, kOne, lane, ks);
+        load_part_turned(fb[ks], lb, kOne, lane, ks);
+      }
+      multiply_parts<kBf>(acc, fa[0], fb[0]);
+    }
+    between();
+    if (live) multiply_parts<kBf>(acc, fa[1], fb[1]);
+  };
+  run_steps(steps, fetch, put, [](int) {}, multiply);
+
+  if (a.dw) store_outer<T>(a, o, acc, nullptr);
+  if (sums_bias) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bias_part[own][8 * cg + j] = bias[j];
+    __syncthreads();
+    if (tid < kOuterTile) {
+      float v = 0.0f;
+      for (int i = 0; i < 16; ++i) v += bias_part[i][tid];
+      store_bias<T>(a, o, tid, v);
     }
   }
 }
@@ -832,12 +957,18 @@ int64_t tiles_at_most(int64_t n, int n_groups, int64_t rows) {
   return n / rows + (n < n_groups + 1 ? n : n_groups + 1);
 }
 
+// Rows (and columns) of a tile: 128 once such tiles fill the chip's 256 compute
+// units, 64 below.
+int tile_side(int64_t n, int cols) {
+  return (n / 128) * ((cols + 127) / 128) >= 256 ? 128 : 64;
+}
+
 // Rows of a block of dW: 4,096 workgroups in all, some rounds of the chip's 512
 // resident ones, but no fewer than 512 rows, so that a block's sums are small
 // beside its rows, and groups of a few hundred rows are one block, whose sums go
 // straight to dW.  Where even that gives fewer than 512 workgroups, 256.
 int outer_rows(const dpa4c_grouped& l) {
-  const int64_t tiles = ((l.k + kTileRows - 1) / kTileRows) * int64_t((l.n_out + kTileCols - 1) / kTileCols);
+  const int64_t tiles = ((l.k + kOuterTile - 1) / kOuterTile) * int64_t((l.n_out + kOuterTile - 1) / kOuterTile);
   if (l.n * tiles < 512 * 512) return 256;
   const int64_t rows = align_up((l.n * tiles + 4095) / 4096, kDepth);
   return static_cast<int>(rows < 512 ? 512 : rows > 16384 ? 16384 : rows);
@@ -847,7 +978,7 @@ Weights weights_of(Arena& ar, const dpa4c_grouped& l, bool back) {
   Weights w;
   const int depth = back ? l.n_out : l.k, cols = back ? l.k : l.n_out;
   w.steps = (depth + kDepth - 1) / kDepth;
-  w.cols_pad = static_cast<int>(align_up(cols, kTileCols));
+  w.cols_pad = static_cast<int>(align_up(cols, kPad));
   w.planes_n = l.dtype == DPA4C_F32 ? 2 : 1;
   w.planes = ar.take<char>(int64_t(l.n_groups) * w.steps * w.step_bytes());
   w.exps = ar.take<int32_t>(l.dtype == DPA4C_F32 ? int64_t(l.n_groups) * w.cols_pad : 0);
@@ -864,7 +995,10 @@ TileList list_of(Arena& ar, const dpa4c_grouped& l, int rows, bool rest) {
   return t;
 }
 
-int pitch_of(int cols) { return static_cast<int>(align_up(cols, 4)); }
+// entries of a row of dz: rows start at multiples of 16 bytes
+int pitch_of(const dpa4c_grouped& l) {
+  return static_cast<int>(align_up(l.n_out, l.dtype == DPA4C_F32 ? 4 : 8));
+}
 
 struct ForwardPlan {
   Weights w;
@@ -874,7 +1008,7 @@ ForwardPlan plan_forward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   ForwardPlan p;
   p.w = weights_of(ar, l, false);
-  p.tiles = list_of(ar, l, kTileRows, true);
+  p.tiles = list_of(ar, l, tile_side(l.n, l.n_out), true);
   *bytes = ar.used;
   return p;
 }
@@ -882,17 +1016,17 @@ ForwardPlan plan_forward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
 struct BackwardPlan {
   Weights w;
   TileList tiles, blocks;
-  unsigned* dz;
+  void* dz;
   float *parts, *db_parts;
 };
 BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   BackwardPlan p;
   p.w = weights_of(ar, l, true);
-  p.tiles = list_of(ar, l, kTileRows, true);
+  p.tiles = list_of(ar, l, tile_side(l.n, l.k), true);
   const int rows = outer_rows(l);
   p.blocks = list_of(ar, l, rows, false);
-  p.dz = ar.take<unsigned>(l.n * pitch_of(l.n_out));
+  p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
   const int64_t blocks = tiles_at_most(l.n, l.n_groups, rows);
   p.parts = ar.take<float>(blocks * l.k * l.n_out);
   p.db_parts = ar.take<float>(blocks * l.n_out);
@@ -932,19 +1066,27 @@ int prepare(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, con
 
 template <class T, Source S>
 int run_rows(const RowsArgs& a, const TileList& tiles, hipStream_t st) {
-  const int64_t grid = tiles_at_most(a.n, a.n_groups, tiles.rows) * (a.w.cols_pad / kTileCols);
-  grouped_rows_kernel<T, S><<<grid, kThreads, 0, st>>>(a);
+  const int64_t grid = tiles_at_most(a.n, a.n_groups, tiles.rows) * ((a.kout + tiles.rows - 1) / tiles.rows);
+  if (tiles.rows == kSide<2>)
+    grouped_rows_kernel<T, S, 2><<<grid, kThreads, 0, st>>>(a);
+  else
+    grouped_rows_kernel<T, S, 1><<<grid, kThreads, 0, st>>>(a);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }
 
-template <class T, Source SX, Source SZ>
+template <class T>
 int run_outer(const dpa4c_grouped& l, const OuterArgs& a, const TileList& blocks, hipStream_t st) {
-  const int64_t tiles = (a.dw ? (l.k + kTileRows - 1) / kTileRows : 1) *
-                        int64_t((l.n_out + kTileCols - 1) / kTileCols);
+  const int64_t tiles = (a.dw ? (l.k + kOuterTile - 1) / kOuterTile : 1) *
+                        int64_t((l.n_out + kOuterTile - 1) / kOuterTile);
   if (l.n > 0) {
     const int64_t grid = tiles_at_most(l.n, l.n_groups, blocks.rows) * tiles;
-    grouped_outer_kernel<T, SX, SZ><<<grid, kThreads, 0, st>>>(a);
+    if constexpr (sizeof(T) == 4)
+      grouped_outer_kernel<<<grid, kThreads, 0, st>>>(a);
+    else if (a.by_place)
+      grouped_outer_half_kernel<T, kPair><<<grid, kThreads, 0, st>>>(a);
+    else
+      grouped_outer_half_kernel<T, kHalf><<<grid, kThreads, 0, st>>>(a);
     DPA4C_HIP_TRY(hipGetLastError());
   }
   auto join = [&](int64_t each, const float* parts, void* out) {
@@ -1012,13 +1154,13 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
     const BackwardPlan p = plan_backward(l, work, &bytes);
     DPA4C_TRY((prepare<T, true>(l, rows ? &p.w : nullptr, rows ? &p.tiles : nullptr,
                                 outer ? &p.blocks : nullptr, st)));
-    const int pitch = pitch_of(l.n_out);
+    const int pitch = pitch_of(l);
     if (z && l.n > 0) {
-      const int64_t quads = l.n * (pitch / 4);
-      const int64_t grid = std::min<int64_t>((quads + kThreads - 1) / kThreads, 8192);
+      const int64_t each = l.n * (pitch * int64_t(sizeof(T)) / 16);
+      const int64_t grid = std::min<int64_t>((each + kThreads - 1) / kThreads, 8192);
       grouped_dz_kernel<T><<<grid, kThreads, 0, st>>>(
           l.group_ptr, l.order, l.n_groups, l.n, l.n_out, pitch, static_cast<const T*>(dy), ldy,
-          static_cast<const T*>(z), ldz, p.dz);
+          static_cast<const T*>(z), ldz, static_cast<T*>(p.dz));
       DPA4C_HIP_TRY(hipGetLastError());
     }
     if (rows) {
@@ -1030,7 +1172,7 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.n_tiles = p.tiles.count;
       a.kin = l.n_out;
       a.kout = l.k;
-      a.in = z ? static_cast<const void*>(p.dz) : dy;
+      a.in = z ? p.dz : dy;
       a.ldin = z ? pitch : ldy;
       a.by_place = z != nullptr;
       a.w = p.w;
@@ -1052,17 +1194,14 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.m = l.n_out;
       a.x = l.x;
       a.ldx = l.ldx;
-      a.dz = z ? static_cast<const void*>(p.dz) : dy;
+      a.dz = z ? p.dz : dy;
       a.lddz = z ? pitch : ldy;
       a.by_place = z != nullptr;
       a.dw = dw;
       a.db = db;
       a.parts = p.parts;
       a.db_parts = p.db_parts;
-      if (z)
-        DPA4C_TRY((run_outer<T, kOwn, kMade>(l, a, p.blocks, st)));
-      else
-        DPA4C_TRY((run_outer<T, kOwn, kOwn>(l, a, p.blocks, st)));
+      DPA4C_TRY(run_outer<T>(l, a, p.blocks, st));
     }
     return 0;
   });

@@ -2,15 +2,15 @@
 //
 // Per step and matrix (lo x hi, the shorter side first):
 //   A = X X^T                  lo lo hi flops (half of a product: A is symmetric)
-//   B = a I + A (b I + c A)    lo lo lo       (half of one)
+//   B = a I + b A + c A A      lo lo lo       (half of one)
 //   X <- B X                   2 lo lo hi
 // each a product of float16 pairs on the matrix cores (tile.h), three times
-// the above.  The identities go into the factors as they are written, C = b I +
-// c A beside A, so no product has to read another operand at its end.  The iterates keep to fixed scales, since the norms are known:
-// |X| <= 1 at the start and the iteration bounds it afterwards.  So the planes
-// are written as the next product reads them: rows of 64 reduction entries.  X
-// is the operand of A along its rows and of B X along its columns and is
-// kept in both orders; A and B, symmetric, in one.
+// the above.  The iterates keep to fixed scales, since the norms are known:
+// |X| <= 1 at the start and the iteration bounds it afterwards.  So each product
+// writes its result as planes that the next one reads without converting: rows
+// of 32 reduction entries.  X is written once, along its rows; B X reads it
+// through transposing LDS reads.  A step moves 4 bytes an entry of
+// X twice (and its write), A and B twice each (and theirs).
 //
 // All matrices of a call go through a phase in one launch: one for the
 // momentum and the norms, one for the start, three for each step, of which the
@@ -24,28 +24,27 @@ namespace dpa4c {
 namespace {
 
 constexpr int kThreads = kTileThreads;
-constexpr int64_t kChunk = 8192;   // entries of a partial sum of squares
+constexpr int64_t kChunk = 4096;   // entries of a partial sum of squares
 
-// fixed scales of the planes: entries of X, A and B (and C) below 4, 16 and 64
+// fixed scales of the planes: entries of X, A and B below 4, 16 and 64
 constexpr float kScaleX = 8192.0f, kScaleA = 2048.0f, kScaleB = 512.0f;
 
-// One stack.  A plane set is [matrix][step of 64][hi, lo][rows padded to
-// 128][64 entries].
+// One stack.  A plane set is [matrix][step of 32][hi, lo][rows padded to
+// 128][32 entries].
 struct Stack {
   const void* grad;
   void* out;
   float* momentum;
-  char* xr[2];    // rows lo, entries along hi; read and written in turn
-  char* xt[2];    // rows hi, entries along lo
-  char *a, *b, *c;   // rows lo, entries along lo
+  char* x[2];     // rows lo, entries along hi; read and written in turn
+  char *a, *b;    // rows lo, entries along lo
   double* squares;   // [matrix][chunks]
   int64_t batch;
   int rows, cols;
   int lo, hi;
-  int lo_pad, hi_pad;   // to 128
+  int lo_pad;     // to 128
   int lo_steps, hi_steps;
   int chunks;
-  int turned;   // X is the transpose of the matrix
+  int turned;     // X is the transpose of the matrix
 };
 struct Stacks {
   Stack s[kMaxStacks];
@@ -57,13 +56,13 @@ struct Shares {
 };
 
 __device__ inline int stack_of(const Shares& sh, int count, int64_t item) {
-  int i = 0;
-  while (i + 1 < count && item >= sh.first[i + 1]) ++i;
-  return i;
+  const int lane = threadIdx.x & (kWave - 1);
+  const int64_t next = sh.first[lane < kMaxStacks ? lane + 1 : 0];
+  return __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < count - 1 && item >= next)));
 }
 
 __host__ __device__ inline int64_t set_bytes(int steps, int rows_pad) {
-  return int64_t(steps) * 2 * rows_pad * 128;
+  return int64_t(steps) * 2 * rows_pad * kRowBytes;
 }
 
 // U of the update: the gradient, or with momentum (already updated) its mix
@@ -84,14 +83,34 @@ __global__ void __launch_bounds__(kThreads) newton_norm_kernel(Stacks all, Share
   const int64_t item = blockIdx.x - sh.first[i], m = item / s.chunks;
   const int64_t size = int64_t(s.rows) * s.cols, base = m * size;
   const int64_t begin = (item - m * s.chunks) * kChunk;
-  const int64_t end = begin + kChunk < size ? begin + kChunk : size;
-  double sum = 0.0;
-  for (int64_t j = begin + threadIdx.x; j < end; j += kThreads) {
-    if constexpr (Muon)
-      s.momentum[base + j] = beta * s.momentum[base + j] + to_f32(static_cast<const T*>(s.grad)[base + j]);
-    const double u = update_of<T, Muon>(s, base + j, beta, nesterov);
-    sum += u * u;
+  const int count = static_cast<int>(begin + kChunk < size ? kChunk : size - begin);
+  const T* __restrict__ grad = static_cast<const T*>(s.grad) + base + begin;
+  constexpr int kEach = kChunk / kThreads;
+  float u[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int j = threadIdx.x + k * kThreads;
+    u[k] = j < count ? to_f32(grad[j]) : 0.0f;
   }
+  if constexpr (Muon) {
+    float* momentum = s.momentum + base + begin;
+    float v[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int j = threadIdx.x + k * kThreads;
+      v[k] = j < count ? momentum[j] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int j = threadIdx.x + k * kThreads;
+      v[k] = beta * v[k] + u[k];
+      if (j < count) momentum[j] = v[k];
+      u[k] = nesterov ? u[k] + beta * v[k] : v[k];
+    }
+  }
+  double sum = 0.0;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) sum += double(u[k]) * double(u[k]);
   __shared__ double part[kThreads];
   part[threadIdx.x] = sum;
   __syncthreads();
@@ -106,6 +125,11 @@ __global__ void __launch_bounds__(kThreads) newton_norm_kernel(Stacks all, Share
 // Results in LDS (stage_at), and where they go
 // ---------------------------------------------------------------------------
 
+// byte offset of the slot of entries entry .. entry + 7 of a row of a plane set
+__device__ inline int64_t slot_of(int rows_pad, int row, int entry) {
+  return int64_t(entry / kDepth) * 2 * rows_pad * kRowBytes + slot_at(row, entry % kDepth / 8);
+}
+
 // eight values as one slot of each plane of a set
 __device__ inline void write_slot(char* set, int rows_pad, int row, int entry, const float* f, float scale) {
   u4 hi, lo;
@@ -116,40 +140,85 @@ __device__ inline void write_slot(char* set, int rows_pad, int row, int entry, c
     hi[j] = h;
     lo[j] = l;
   }
-  char* to = set + int64_t(entry / kDepth) * 2 * rows_pad * 128 + slot_at(row, entry % kDepth / 8);
+  char* to = set + slot_of(rows_pad, row, entry);
   *reinterpret_cast<u4*>(to) = hi;
-  *reinterpret_cast<u4*>(to + int64_t(rows_pad) * 128) = lo;
+  *reinterpret_cast<u4*>(to + int64_t(rows_pad) * kRowBytes) = lo;
 }
 
-// mul x the stage (+ diag on the matrix's diagonal) as rows r0 .. of a plane
-// set, entries from c0; Rows: the stage's rows
-template <int Rows>
-__device__ inline void write_rows(char* set, int rows_pad, int steps, int r0, int c0,
-                                  const float* stage, float scale, float mul = 1.0f, float diag = 0.0f) {
-#pragma unroll 4
-  for (int i = 0; i < Rows * 16 / kThreads; ++i) {
-    const int slot = threadIdx.x % 16, r = threadIdx.x / 16 + i * (kThreads / 16), c = slot * 8;
-    if ((c0 + c) / kDepth >= steps) continue;
-    float f[8];
-    *reinterpret_cast<v4f*>(f) = *reinterpret_cast<const v4f*>(stage + stage_at(r, c));
-    *reinterpret_cast<v4f*>(f + 4) = *reinterpret_cast<const v4f*>(stage + stage_at(r, c + 4));
+// What a slot of the result gets besides the stage: add x the same slot of a
+// plane set, and diag on the matrix's diagonal.
+struct Extra {
+  const char* set;
+  float add, diag;
+};
+struct Slot {
+  v8h hi, lo;
+};
+__device__ inline Slot read_slot(const char* set, int rows_pad, int row, int entry) {
+  const char* from = set + slot_of(rows_pad, row, entry);
+  return {*reinterpret_cast<const v8h*>(from),
+          *reinterpret_cast<const v8h*>(from + int64_t(rows_pad) * kRowBytes)};
+}
+__device__ inline void add_slot(const Extra& x, const Slot& s, int row, int entry, float* f) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = f[j] * mul + (r0 + r == c0 + c + j ? diag : 0.0f);
-    write_slot(set, rows_pad, r0 + r, c0 + c, f, scale);
+  for (int j = 0; j < 8; ++j) {
+    f[j] += x.add * (static_cast<float>(s.hi[j]) + static_cast<float>(s.lo[j]));
+    f[j] += row == entry + j ? x.diag : 0.0f;
   }
 }
-// the stage's columns as rows c0 .., entries from r0
-template <int Rows>
-__device__ inline void write_columns(char* set, int rows_pad, int steps, int r0, int c0,
-                                     const float* stage, float scale, float mul = 1.0f) {
-#pragma unroll 4
-  for (int i = 0; i < Rows * 16 / kThreads; ++i) {
-    const int c = threadIdx.x % kTileCols, slot = threadIdx.x / kTileCols + 2 * i;
-    if ((r0 + slot * 8) / kDepth >= steps) continue;
-    float f[8];
+constexpr int kBatch = 4;   // slots of a thread in flight
+
+// the stage (Rows of it) as rows r0 .. of a plane set, entries from c0
+template <int NB, int Rows, bool Has = false>
+__device__ inline void write_rows(char* set, int rows_pad, int steps, int r0, int c0,
+                                  const float* stage, float scale, const Extra& x = {}) {
+  constexpr int kSlots = kSide<NB> / 8, kEach = Rows * kSlots / kThreads;
+  const int c = threadIdx.x % kSlots * 8;
+  const int entry = c0 + c;
+  if (entry / kDepth >= steps) return;
+  constexpr int kGo = kEach < kBatch ? kEach : kBatch;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = stage[stage_at(slot * 8 + j, c)] * mul;
-    write_slot(set, rows_pad, c0 + c, r0 + slot * 8, f, scale);
+  for (int i0 = 0; i0 < kEach; i0 += kGo) {
+    Slot old[kGo];
+#pragma unroll
+    for (int k = 0; k < kGo; ++k)
+      if constexpr (Has)
+        old[k] = read_slot(x.set, rows_pad, r0 + int(threadIdx.x) / kSlots + (i0 + k) * (kThreads / kSlots), entry);
+#pragma unroll
+    for (int k = 0; k < kGo; ++k) {
+      const int r = threadIdx.x / kSlots + (i0 + k) * (kThreads / kSlots);
+      float f[8];
+      *reinterpret_cast<v4f*>(f) = *reinterpret_cast<const v4f*>(stage + stage_at<NB>(r, c));
+      *reinterpret_cast<v4f*>(f + 4) = *reinterpret_cast<const v4f*>(stage + stage_at<NB>(r, c + 4));
+      if constexpr (Has) add_slot(x, old[k], r0 + r, entry, f);
+      write_slot(set, rows_pad, r0 + r, entry, f, scale);
+    }
+  }
+}
+// the stage's columns as rows c0 .., entries from r0: four lanes a row of a step
+template <int NB, bool Has = false>
+__device__ inline void write_columns(char* set, int rows_pad, int steps, int r0, int c0,
+                                     const float* stage, float scale, const Extra& x = {}) {
+  constexpr int kEach = kSide<NB> * kSide<NB> / 8 / kThreads, kGo = kEach < kBatch ? kEach : kBatch;
+#pragma unroll
+  for (int i0 = 0; i0 < kEach; i0 += kGo) {
+    Slot old[kGo];
+#pragma unroll
+    for (int k = 0; k < kGo; ++k) {
+      const int i = i0 + k, c = threadIdx.x / 4 + i % NB * 64, slot = threadIdx.x % 4 + i / NB * 4;
+      if constexpr (Has)
+        if ((r0 + slot * 8) / kDepth < steps) old[k] = read_slot(x.set, rows_pad, c0 + c, r0 + slot * 8);
+    }
+#pragma unroll
+    for (int k = 0; k < kGo; ++k) {
+      const int i = i0 + k, c = threadIdx.x / 4 + i % NB * 64, slot = threadIdx.x % 4 + i / NB * 4;
+      if ((r0 + slot * 8) / kDepth >= steps) continue;
+      float f[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[j] = stage[stage_at<NB>(slot * 8 + j, c)];
+      if constexpr (Has) add_slot(x, old[k], c0 + c, r0 + slot * 8, f);
+      write_slot(set, rows_pad, c0 + c, r0 + slot * 8, f, scale);
+    }
   }
 }
 
@@ -158,19 +227,32 @@ struct Finish {
 };
 
 // the stage as the result: out = O, or the weights' update
-template <class T, bool Muon, int Rows>
+template <class T, bool Muon, int NB, int Rows>
 __device__ inline void write_result(const Stack& s, int64_t m, int r0, int c0, const float* stage,
                                     const Finish& f) {
   T* out = static_cast<T*>(s.out) + m * s.rows * s.cols;
   const float step = Muon ? f.step * sqrtf(fmaxf(1.0f, float(s.cols) / float(s.rows))) : 0.0f;
-#pragma unroll 8
-  for (int i = threadIdx.x; i < Rows * kTileCols; i += kThreads) {
-    const int r = s.turned ? i % Rows : i / kTileCols;
-    const int c = s.turned ? i / Rows : i % kTileCols;
-    if (r0 + r >= s.lo || c0 + c >= s.hi) continue;
-    const int64_t at = s.turned ? int64_t(c0 + c) * s.cols + r0 + r : int64_t(r0 + r) * s.cols + c0 + c;
-    const float o = stage[stage_at(r, c)];
-    out[at] = from_f32<T>(Muon ? f.keep * to_f32(out[at]) - step * o : o);
+  constexpr int kEach = Rows * kSide<NB> / kThreads, kGo = 8;
+#pragma unroll 1
+  for (int k0 = 0; k0 < kEach; k0 += kGo) {
+    float w[kGo];
+    int64_t at[kGo];
+#pragma unroll
+    for (int k = 0; k < kGo; ++k) {
+      const int i = threadIdx.x + (k0 + k) * kThreads;
+      const int r = s.turned ? i % Rows : i / kSide<NB>, c = s.turned ? i / Rows : i % kSide<NB>;
+      at[k] = r0 + r >= s.lo || c0 + c >= s.hi ? -1
+              : s.turned                       ? int64_t(c0 + c) * s.cols + r0 + r
+                                               : int64_t(r0 + r) * s.cols + c0 + c;
+      w[k] = Muon && at[k] >= 0 ? to_f32(out[at[k]]) : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < kGo; ++k) {
+      const int i = threadIdx.x + (k0 + k) * kThreads;
+      const int r = s.turned ? i % Rows : i / kSide<NB>, c = s.turned ? i / Rows : i % kSide<NB>;
+      const float o = stage[stage_at<NB>(r, c)];
+      if (at[k] >= 0) out[at[k]] = from_f32<T>(Muon ? f.keep * w[k] - step * o : o);
+    }
   }
 }
 
@@ -180,14 +262,28 @@ constexpr int kStartRows = 64;
 template <class T, bool Muon, bool Last>
 __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shares sh, float beta,
                                                                 int nesterov, float eps, Finish f) {
-  __shared__ __attribute__((aligned(16))) float stage[kStartRows * kTileCols];
+  constexpr int kCols = kSide<2>;
+  __shared__ __attribute__((aligned(16))) float stage[kStartRows * kCols];
   __shared__ double norm;
   const int i = stack_of(sh, all.count, blockIdx.x);
   const Stack& s = all.s[i];
   const int64_t item = blockIdx.x - sh.first[i];
-  const int tr = s.lo_pad / kStartRows, tc = s.hi_pad / kTileCols;
+  const int tr = s.lo_pad / kStartRows, tc = (s.hi + kCols - 1) / kCols;
   const int64_t m = item / (tr * tc);
-  const int r0 = static_cast<int>(item / tc % tr) * kStartRows, c0 = static_cast<int>(item % tc) * kTileCols;
+  const int r0 = static_cast<int>(item / tc % tr) * kStartRows, c0 = static_cast<int>(item % tc) * kCols;
+  const int64_t base = m * s.rows * s.cols;
+  constexpr int kEach = kStartRows * kCols / kThreads;
+  float u[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int j = threadIdx.x + k * kThreads;
+    const int r = s.turned ? j % kStartRows : j / kCols, c = s.turned ? j / kStartRows : j % kCols;
+    u[k] = 0.0f;
+    if (r0 + r < s.lo && c0 + c < s.hi)
+      u[k] = update_of<T, Muon>(
+          s, base + (s.turned ? int64_t(c0 + c) * s.cols + r0 + r : int64_t(r0 + r) * s.cols + c0 + c), beta,
+          nesterov);
+  }
   if (threadIdx.x < kWave) {
     double sum = 0.0;
     for (int j = threadIdx.x; j < s.chunks; j += kWave) sum += s.squares[m * s.chunks + j];
@@ -196,43 +292,36 @@ __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shar
   }
   __syncthreads();
   const double inv = norm;
-  const int64_t base = m * s.rows * s.cols;
-#pragma unroll 8
-  for (int j = threadIdx.x; j < kStartRows * kTileCols; j += kThreads) {
-    const int r = s.turned ? j % kStartRows : j / kTileCols;
-    const int c = s.turned ? j / kStartRows : j % kTileCols;
-    float v = 0.0f;
-    if (r0 + r < s.lo && c0 + c < s.hi) {
-      const int64_t at = s.turned ? int64_t(c0 + c) * s.cols + r0 + r : int64_t(r0 + r) * s.cols + c0 + c;
-      v = static_cast<float>(update_of<T, Muon>(s, base + at, beta, nesterov) * inv);
-    }
-    stage[stage_at(r, c)] = v;
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int j = threadIdx.x + k * kThreads;
+    const int r = s.turned ? j % kStartRows : j / kCols, c = s.turned ? j / kStartRows : j % kCols;
+    // the padding stays zero also where the norm is not finite
+    stage[stage_at<2>(r, c)] = r0 + r < s.lo && c0 + c < s.hi ? static_cast<float>(u[k] * inv) : 0.0f;
   }
   __syncthreads();
-  if constexpr (Last) {
-    write_result<T, Muon, kStartRows>(s, m, r0, c0, stage, f);
-  } else {
-    write_rows<kStartRows>(s.xr[0] + m * set_bytes(s.hi_steps, s.lo_pad), s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
-    write_columns<kStartRows>(s.xt[0] + m * set_bytes(s.lo_steps, s.hi_pad), s.hi_pad, s.lo_steps, r0, c0, stage, kScaleX);
-  }
+  if constexpr (Last)
+    write_result<T, Muon, 2, kStartRows>(s, m, r0, c0, stage, f);
+  else
+    write_rows<2, kStartRows>(s.x[0] + m * set_bytes(s.hi_steps, s.lo_pad), s.lo_pad, s.hi_steps, r0, c0,
+                              stage, kScaleX);
 }
 
 enum Phase { kGram, kPoly, kApply, kLast };
 
-// one 128 x 128 tile of a phase
-template <class T, bool Muon, Phase P>
+// one tile of a phase
+template <class T, bool Muon, Phase P, int NB>
 __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all, Shares sh, int from,
                                                                      float ca, float cb, float cc,
                                                                      Finish f) {
-  __shared__ __attribute__((aligned(16))) char lds[4 * kPlane];
-  char* la = lds;
-  char* lb = lds + 2 * kPlane;
+  constexpr bool kWide = P == kApply || P == kLast;
+  constexpr int kOne = kPlane<NB>, kTile = kSide<NB>;
+  __shared__ __attribute__((aligned(16))) char lds[8 * kOne];
   const int64_t work = xcd_block(blockIdx.x, gridDim.x);
   const int is = stack_of(sh, all.count, work);
   const Stack& s = all.s[is];
   const int64_t item = work - sh.first[is];
-  constexpr bool kWide = P == kApply || P == kLast;
-  const int tr = s.lo_pad / kTileRows, tc = kWide ? s.hi_pad / kTileCols : tr;
+  const int tr = (s.lo + kTile - 1) / kTile, tc = kWide ? (s.hi + kTile - 1) / kTile : tr;
   const int each = kWide ? tr * tc : tr * (tr + 1) / 2;
   const int64_t m = item / each;
   int ti, tj;
@@ -248,75 +337,92 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
   }
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1;
+  const int r0 = ti * kTile, c0 = tj * kTile;
 
-  const int64_t xr_bytes = set_bytes(s.hi_steps, s.lo_pad), xt_bytes = set_bytes(s.lo_steps, s.hi_pad);
-  const int64_t sq_bytes = set_bytes(s.lo_steps, s.lo_pad);
-  const char* xr = s.xr[from] + m * xr_bytes;
+  const int64_t x_bytes = set_bytes(s.hi_steps, s.lo_pad), sq_bytes = set_bytes(s.lo_steps, s.lo_pad);
+  const char* X = s.x[from] + m * x_bytes;
   const char* A = s.a + m * sq_bytes;
-  const char* left = P == kGram ? xr : P == kPoly ? A : s.b + m * sq_bytes;
-  const char* right = P == kGram ? xr : P == kPoly ? s.c + m * sq_bytes : s.xt[from] + m * xt_bytes;
+  const int64_t plane = int64_t(s.lo_pad) * kRowBytes;
   const int steps = P == kGram ? s.hi_steps : s.lo_steps;
-  const int64_t lplane = int64_t(s.lo_pad) * 128, rplane = kWide ? int64_t(s.hi_pad) * 128 : lplane;
-  left += int64_t(ti) * kPlane;
-  right += int64_t(tj) * kPlane;
+  // rows of a step follow each other, a 16-byte slot a thread
+  const char* left = (P == kGram ? X : P == kPoly ? A : s.b + m * sq_bytes) + r0 * kRowBytes;
+  const char* right = P == kGram ? X + c0 * kRowBytes : P == kPoly ? A + c0 * kRowBytes : X;
 
-  u4 ra[2][4], rb[2][4];
-  auto fetch = [&](int step) {
+  u4 ra[2][2][NB], rb[2][2][NB];
+  auto fetch = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const bool in = step < steps;   // past the end: one line
+    const int st = in ? step : 0, at = in ? tid * 16 : 0;
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ra[p][i] = *reinterpret_cast<const u4*>(left + (2 * step + p) * lplane + i * 4096 + tid * 16);
-        rb[p][i] = *reinterpret_cast<const u4*>(right + (2 * step + p) * rplane + i * 4096 + tid * 16);
+      for (int i = 0; i < NB; ++i) {
+        ra[q][p][i] = *reinterpret_cast<const u4*>(left + (2 * st + p) * plane + i * 4096 + at);
+        if constexpr (!kWide) {
+          rb[q][p][i] = *reinterpret_cast<const u4*>(right + (2 * st + p) * plane + i * 4096 + at);
+        } else {
+          // 32 rows of X of each of the tile's blocks of 32 columns; blocks
+          // past the last repeat it, and nothing of them is stored
+          int block = c0 / 32 + i * 2 + tid / 128;
+          block = block < s.hi_steps ? block : s.hi_steps - 1;
+          rb[q][p][i] = *reinterpret_cast<const u4*>(right + (2 * block + p) * plane + st * 32 * kRowBytes +
+                                                     (in ? tid % 128 * 16 : 0));
+        }
       }
   };
-  Sums acc;
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) acc.v[i][j] = v16f{};
-  fetch(0);
-  for (int step = 0; step < steps; ++step) {
-    __syncthreads();
+  auto put = [&](auto turn, int) {
+    constexpr int q = decltype(turn)::value;
+    char* to = lds + q * 4 * kOne + tid * 16;
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        *reinterpret_cast<u4*>(la + p * kPlane + i * 4096 + tid * 16) = ra[p][i];
-        *reinterpret_cast<u4*>(lb + p * kPlane + i * 4096 + tid * 16) = rb[p][i];
+      for (int i = 0; i < NB; ++i) {
+        *reinterpret_cast<u4*>(to + p * kOne + i * 4096) = ra[q][p][i];
+        *reinterpret_cast<u4*>(to + (2 + p) * kOne + i * 4096) = rb[q][p][i];
       }
-    __syncthreads();
-    if (step + 1 < steps) fetch(step + 1);
-    if (ti * kTileRows + 64 * wm < s.lo && tj * kTileCols + 64 * wn < (kWide ? s.hi : s.lo))
-      tile_step<false, 2, 2>(acc, la + wm * 64 * 128, lb + wn * 64 * 128, lane);
-  }
+  };
+  Sums<NB> acc;
+  acc.clear();
+  const bool live = r0 + kTile / 2 * wm < s.lo && c0 + kTile / 2 * wn < (kWide ? s.hi : s.lo);
+  auto multiply = [&](int step, auto&& between) {
+    const char* a = lds + (step & 1) * 4 * kOne + wm * (kTile / 2) * kRowBytes;
+    const char* b = lds + (step & 1) * 4 * kOne + 2 * kOne + wn * (kTile / 2) * kRowBytes;
+    Part<NB, 2> fa[2], fb[2];
+    if (live) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        load_part(fa[ks], a, kOne, lane, ks);
+        if constexpr (kWide)
+          load_part_turned(fb[ks], b, kOne, lane, ks);
+        else
+          load_part(fb[ks], b, kOne, lane, ks);
+      }
+      multiply_parts<false>(acc, fa[0], fb[0]);
+    }
+    between();
+    if (live) multiply_parts<false>(acc, fa[1], fb[1]);
+  };
+  run_steps(steps, fetch, put, [](int) {}, multiply);
 
   float* stage = reinterpret_cast<float*>(lds);
-  __syncthreads();
-  stage_sums(stage, acc, wm, wn, lane,
+  stage_sums(stage, acc, kTile / 2 * wm, kTile / 2 * wn, lane,
              P == kGram   ? 1.0f / (kScaleX * kScaleX)
-             : P == kPoly ? 1.0f / (kScaleA * kScaleB)
+             : P == kPoly ? cc / (kScaleA * kScaleA)
                           : 1.0f / (kScaleB * kScaleX));
   __syncthreads();
-  const int r0 = ti * kTileRows, c0 = tj * kTileCols;
   if constexpr (P == kGram) {
     char* out = s.a + m * sq_bytes;
-    char* mix = s.c + m * sq_bytes;
-    write_rows<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
-    write_rows<kTileRows>(mix, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, cc, cb);
-    if (ti != tj) {
-      write_columns<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
-      write_columns<kTileRows>(mix, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, cc);
-    }
+    write_rows<NB, kTile>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
+    if (ti != tj) write_columns<NB>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
   } else if constexpr (P == kPoly) {
     char* out = s.b + m * sq_bytes;
-    write_rows<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, 1.0f, ca);
-    if (ti != tj) write_columns<kTileRows>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB);
+    const Extra x{A, cb / kScaleA, ca};
+    write_rows<NB, kTile, true>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, x);
+    if (ti != tj) write_columns<NB, true>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, x);
   } else if constexpr (P == kApply) {
-    write_rows<kTileRows>(s.xr[from ^ 1] + m * xr_bytes, s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
-    write_columns<kTileRows>(s.xt[from ^ 1] + m * xt_bytes, s.hi_pad, s.lo_steps, r0, c0, stage, kScaleX);
+    write_rows<NB, kTile>(s.x[from ^ 1] + m * x_bytes, s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
   } else {
-    write_result<T, Muon, kTileRows>(s, m, r0, c0, stage, f);
+    write_result<T, Muon, NB, kTile>(s, m, r0, c0, stage, f);
   }
 }
 
@@ -335,18 +441,13 @@ Stacks lay_out(int count, const NewtonStack* in, void* work, int64_t* bytes) {
     s.turned = s.rows > s.cols;
     s.lo = s.turned ? s.cols : s.rows;
     s.hi = s.turned ? s.rows : s.cols;
-    s.lo_pad = static_cast<int>(align_up(s.lo, kTileRows));
-    s.hi_pad = static_cast<int>(align_up(s.hi, kTileCols));
+    s.lo_pad = static_cast<int>(align_up(s.lo, kPad));
     s.lo_steps = (s.lo + kDepth - 1) / kDepth;
     s.hi_steps = (s.hi + kDepth - 1) / kDepth;
     s.chunks = static_cast<int>((int64_t(s.rows) * s.cols + kChunk - 1) / kChunk);
-    for (int k = 0; k < 2; ++k) {
-      s.xr[k] = ar.take<char>(s.batch * set_bytes(s.hi_steps, s.lo_pad));
-      s.xt[k] = ar.take<char>(s.batch * set_bytes(s.lo_steps, s.hi_pad));
-    }
+    for (int k = 0; k < 2; ++k) s.x[k] = ar.take<char>(s.batch * set_bytes(s.hi_steps, s.lo_pad));
     s.a = ar.take<char>(s.batch * set_bytes(s.lo_steps, s.lo_pad));
     s.b = ar.take<char>(s.batch * set_bytes(s.lo_steps, s.lo_pad));
-    s.c = ar.take<char>(s.batch * set_bytes(s.lo_steps, s.lo_pad));
     s.squares = ar.take<double>(s.batch * s.chunks);
   }
   *bytes = ar.used;
@@ -360,20 +461,41 @@ Shares share(const Stacks& all, Fn&& of) {
   for (int i = 0; i < all.count; ++i) sh.first[i + 1] = sh.first[i] + all.s[i].batch * of(all.s[i]);
   return sh;
 }
+Shares share_square(const Stacks& all, int side) {
+  return share(all, [&](const Stack& s) {
+    const int64_t t = (s.lo + side - 1) / side;
+    return t * (t + 1) / 2;
+  });
+}
+Shares share_wide(const Stacks& all, int side) {
+  return share(all, [&](const Stack& s) {
+    return int64_t((s.lo + side - 1) / side) * ((s.hi + side - 1) / side);
+  });
+}
+
+template <class T, bool Muon, Phase P>
+int product(const Stacks& all, const Shares (&sh)[2], int from, const dpa4c_newton& how, const Finish& f,
+            hipStream_t st) {
+  // Tiles of 128 x 128 once they fill the chip's 256 compute units, of 64 x 64
+  // below.
+  const int64_t large = sh[1].first[all.count];
+  if (large >= 256)
+    newton_product_kernel<T, Muon, P, 2><<<large, kThreads, 0, st>>>(all, sh[1], from, how.a, how.b, how.c, f);
+  else
+    newton_product_kernel<T, Muon, P, 1>
+        <<<sh[0].first[all.count], kThreads, 0, st>>>(all, sh[0], from, how.a, how.b, how.c, f);
+  DPA4C_HIP_TRY(hipGetLastError());
+  return 0;
+}
 
 template <class T, bool Muon>
 int run(const Stacks& all, const dpa4c_newton& how, const MuonStep& mu, hipStream_t st) {
   const Shares norms = share(all, [](const Stack& s) { return int64_t(s.chunks); });
   const Shares starts = share(all, [](const Stack& s) {
-    return int64_t(s.lo_pad / kStartRows) * (s.hi_pad / kTileCols);
+    return int64_t(s.lo_pad / kStartRows) * ((s.hi + kSide<2> - 1) / kSide<2>);
   });
-  const Shares squares = share(all, [](const Stack& s) {
-    const int64_t t = s.lo_pad / kTileRows;
-    return t * (t + 1) / 2;
-  });
-  const Shares wides = share(all, [](const Stack& s) {
-    return int64_t(s.lo_pad / kTileRows) * (s.hi_pad / kTileCols);
-  });
+  const Shares squares[2] = {share_square(all, kSide<1>), share_square(all, kSide<2>)};
+  const Shares wides[2] = {share_wide(all, kSide<1>), share_wide(all, kSide<2>)};
   const Finish f{1.0f - mu.lr * mu.decay, mu.lr};
   newton_norm_kernel<T, Muon><<<norms.first[all.count], kThreads, 0, st>>>(all, norms, mu.momentum, mu.nesterov);
   DPA4C_HIP_TRY(hipGetLastError());
@@ -383,16 +505,13 @@ int run(const Stacks& all, const dpa4c_newton& how, const MuonStep& mu, hipStrea
   else
     newton_start_kernel<T, Muon, false><<<tiles, kThreads, 0, st>>>(all, starts, mu.momentum, mu.nesterov, how.eps, f);
   DPA4C_HIP_TRY(hipGetLastError());
-  const int64_t square = squares.first[all.count], wide = wides.first[all.count];
   for (int step = 0; step < how.steps; ++step) {
-    const int from = step & 1;
-    newton_product_kernel<float, false, kGram><<<square, kThreads, 0, st>>>(all, squares, from, how.a, how.b, how.c, f);
-    newton_product_kernel<float, false, kPoly><<<square, kThreads, 0, st>>>(all, squares, from, how.a, how.b, how.c, f);
+    DPA4C_TRY((product<float, false, kGram>(all, squares, step & 1, how, f, st)));
+    DPA4C_TRY((product<float, false, kPoly>(all, squares, step & 1, how, f, st)));
     if (step + 1 < how.steps)
-      newton_product_kernel<float, false, kApply><<<wide, kThreads, 0, st>>>(all, wides, from, how.a, how.b, how.c, f);
+      DPA4C_TRY((product<float, false, kApply>(all, wides, step & 1, how, f, st)));
     else
-      newton_product_kernel<T, Muon, kLast><<<wide, kThreads, 0, st>>>(all, wides, from, how.a, how.b, how.c, f);
-    DPA4C_HIP_TRY(hipGetLastError());
+      DPA4C_TRY((product<T, Muon, kLast>(all, wides, step & 1, how, f, st)));
   }
   return 0;
 }

@@ -1,16 +1,23 @@
-// The 128 x 128 product tile that the fitting operators share.
+// The product tile that the fitting operators share.
 //
 // A workgroup of four waves multiplies two operands that lie in LDS as rows of
-// 64 reduction entries, [row][64] of 16-bit numbers; a wave forms 64 x 64 of the
-// outputs from v_mfma_f32_32x32x16, the instruction with the fewest LDS bytes
-// for its work.  float32 operands are pairs of float16 planes, x 2^e = hi + lo
-// with both rounded to nearest (2^-24 of x 2^e or 2^-25 absolute), and a product
-// is hi hi + hi lo + lo hi; a half-type factor may come as such a pair too (two
-// products).  Three float16 products take 3 x 32 cycles for what
-// v_mfma_f32_32x32x2_f32 takes 512 cycles for.
+// 32 reduction entries, [row][32] of 16-bit numbers, into 64 NB x 64 NB outputs; a
+// wave forms 32 NB x 32 NB of them from v_mfma_f32_32x32x16, the instruction with
+// the fewest LDS bytes for its work.  float32 operands are pairs of float16
+// planes, x 2^e = hi + lo with both rounded to nearest (2^-24 of x 2^e or 2^-25
+// absolute), and a product is hi hi + hi lo + lo hi; a half-type factor may
+// come as such a pair too (two products).  Three float16 products take 3 x 32
+// cycles for what v_mfma_f32_32x32x2_f32 takes 512 cycles for.
 //
-// The 16-byte slots of a row are exchanged by the row's low three bits, so that
-// the eight lanes of one LDS cycle, eight rows at one slot, meet all banks.
+// A step of 32 entries is 768 matrix-core cycles of a wave for float32 at NB =
+// 2.  Its loads are issued two steps before their use, into registers; they go
+// to the other half of LDS while this step's half is read, so a step has one
+// barrier.  NB = 2 halves the traffic; NB = 1 gives four times as many
+// workgroups with a quarter of the latency of a step, for work that does not
+// fill the chip.
+//
+// The 16-byte slots of a row are exchanged by bits of the row, so that the
+// eight lanes of one LDS cycle, eight rows at one slot, meet all banks.
 #pragma once
 
 #include "train.h"
@@ -26,12 +33,19 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTileThreads = 256;
-constexpr int kTileRows = 128, kTileCols = 128;   // outputs of a workgroup
-constexpr int kDepth = 64;                        // reduction entries of a step
-constexpr int kPlane = kTileRows * kDepth * 2;    // bytes of one operand's plane
+constexpr int kDepth = 32;                        // reduction entries of a step
+constexpr int kRowBytes = kDepth * 2;
+constexpr int kPad = 128;                         // rows of a laid-out operand are padded to this
+
+template <int NB>
+constexpr int kSide = 64 * NB;                    // rows and columns of a tile
+template <int NB>
+constexpr int kPlane = kSide<NB> * kRowBytes;     // bytes of one operand's plane of a step
 
 // byte offset of slot (8 reduction entries) ``slot`` of row ``row`` in a plane
-__device__ inline int slot_at(int row, int slot) { return row * 128 + ((slot ^ (row & 7)) << 4); }
+__device__ inline int slot_at(int row, int slot) {
+  return row * kRowBytes + ((slot ^ (row >> 1 & 3)) << 4);
+}
 
 template <bool Bf16>
 __device__ inline v16f mfma(u4 a, u4 b, v16f c) {
@@ -70,62 +84,126 @@ __device__ inline int exp_for(float m) {
   return e > kFirstExp ? kFirstExp : e;
 }
 
-// sums of a wave: acc[i][j] holds the 32 x 32 outputs at (32 i, 32 j) of its
-// 64 x 64; lane l has column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4
+// sums of a wave: v[i][j] holds the 32 x 32 outputs at (32 i, 32 j) of its part;
+// lane l has column l % 32 and rows 8 (r / 4) + 4 (l / 32) + r % 4
+template <int NB>
 struct Sums {
-  v16f v[2][2];
+  v16f v[NB][NB];
+  __device__ inline void clear() {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) v[i][j] = v16f{};
+  }
 };
 __device__ inline int sum_row(int lane, int r) { return 8 * (r / 4) + 4 * (lane / 32) + r % 4; }
 
-// acc += A B^T over one step; a, b: the operands' planes in LDS at the wave's
-// first row
-template <bool Bf16, int PA, int PB>
-__device__ inline void tile_step(Sums& acc, const char* a, const char* b, int lane) {
-  const int row = lane & 31, half = lane >> 5;
+// a wave's part of one operand for 16 entries of a step
+template <int NB, int P>
+struct Part {
+  u4 v[NB][P];
+};
+// from planes ``plane`` bytes apart in LDS, at the wave's first row
+template <int NB, int P>
+__device__ inline void load_part(Part<NB, P>& f, const char* a, int plane, int lane, int ks) {
 #pragma unroll
-  for (int ks = 0; ks < kDepth / 16; ++ks) {
-    u4 fa[2][PA], fb[2][PB];
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int p = 0; p < P; ++p)
+      f.v[i][p] = *reinterpret_cast<const u4*>(a + p * plane + slot_at(32 * i + (lane & 31), 2 * ks + (lane >> 5)));
+}
+// The same of an operand whose rows are the reduction entries: blocks of 32
+// columns, [block][entry 32][32 columns], slots exchanged as above.  One
+// transposing read gives a lane four entries of its column: the lanes 4 j + q of
+// sixteen point at columns 4 q .. 4 q + 3 of entry j.
+template <int NB, int P>
+__device__ inline void load_part_turned(Part<NB, P>& f, const char* a, int plane, int lane, int ks) {
+  typedef short v4s __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) v4s* Lds;
+  const int group = lane >> 4, entry = 16 * ks + 8 * (group >> 1) + (lane >> 2 & 3);
+  const int col = 16 * (group & 1) + 4 * (lane & 3);
 #pragma unroll
-      for (int p = 0; p < PA; ++p)
-        fa[i][p] = *reinterpret_cast<const u4*>(a + p * kPlane + slot_at(32 * i + row, 2 * ks + half));
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-      for (int p = 0; p < PB; ++p)
-        fb[i][p] = *reinterpret_cast<const u4*>(b + p * kPlane + slot_at(32 * i + row, 2 * ks + half));
+    for (int p = 0; p < P; ++p) {
+      v4s h[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        h[k] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (Lds)(a + p * plane + i * 32 * kRowBytes + slot_at(entry + 4 * k, col >> 3) + (col & 7) * 2));
+      __builtin_memcpy(&f.v[i][p], h, 16);
     }
-#pragma unroll
-    for (int p = PA + PB - 2; p >= 0; --p)   // the small products first; lo lo is left out
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if (PA == 2 && PB == 2) {
-            if (p == 2) acc.v[i][j] = mfma<Bf16>(fa[i][PA - 1], fb[j][0], acc.v[i][j]);
-            if (p == 1) acc.v[i][j] = mfma<Bf16>(fa[i][0], fb[j][PB - 1], acc.v[i][j]);
-            if (p == 0) acc.v[i][j] = mfma<Bf16>(fa[i][0], fb[j][0], acc.v[i][j]);
-          } else {
-            acc.v[i][j] = mfma<Bf16>(fa[i][PA == 2 ? p : 0], fb[j][PB == 2 ? p : 0], acc.v[i][j]);
-          }
-        }
-  }
 }
 
-// The tile's outputs pass through LDS once, 128 x 128 float32 in the operands'
-// place; the 16-byte chunks of a row are exchanged by the row's low three bits,
-// so that reads along rows and along columns both meet all banks.
-constexpr int kStageBytes = kTileRows * kTileCols * 4;
-__device__ inline int stage_at(int row, int col) { return row * kTileCols + (col ^ ((row & 7) << 2)); }
+// acc += A B^T over 16 entries
+template <bool Bf16, int NB, int PA, int PB>
+__device__ inline void multiply_parts(Sums<NB>& acc, const Part<NB, PA>& a, const Part<NB, PB>& b) {
+#pragma unroll
+  for (int p = PA + PB - 2; p >= 0; --p)   // the small products first; lo lo is left out
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        if (PA == 2 && PB == 2) {
+          if (p == 2) acc.v[i][j] = mfma<Bf16>(a.v[i][PA - 1], b.v[j][0], acc.v[i][j]);
+          if (p == 1) acc.v[i][j] = mfma<Bf16>(a.v[i][0], b.v[j][PB - 1], acc.v[i][j]);
+          if (p == 0) acc.v[i][j] = mfma<Bf16>(a.v[i][0], b.v[j][0], acc.v[i][j]);
+        } else {
+          acc.v[i][j] = mfma<Bf16>(a.v[i][PA == 2 ? p : 0], b.v[j][PB == 2 ? p : 0], acc.v[i][j]);
+        }
+      }
+}
 
-// this wave's sums, scaled, into the stage; a barrier has to come before and after
-__device__ inline void stage_sums(float* stage, const Sums& acc, int wm, int wn, int lane, float scale) {
+// The steps of a tile.  fetch(turn, s) issues the loads of step s into register
+// set ``turn`` (a constant 0 or 1; s may be past the end, where it loads
+// anything that is cheap: loads under a condition would make the compiler wait
+// for all of them at every put), put(turn, s) writes that set to half s % 2 of LDS,
+// before(s) runs when step s - 1's sums are complete, and multiply(s, between)
+// adds step s, with ``between`` called halfway.
+template <class Fetch, class Put, class Before, class Multiply>
+__device__ inline void run_steps(int steps, Fetch&& fetch, Put&& put, Before&& before, Multiply&& multiply) {
+  using Even = std::integral_constant<int, 0>;
+  using Odd = std::integral_constant<int, 1>;
+  fetch(Even{}, 0);
+  fetch(Odd{}, 1);
+  put(Even{}, 0);
+  fetch(Even{}, 2);
+  __syncthreads();
+  auto step = [&](auto other, int s) {
+    before(s);
+    multiply(s, [&] {
+      if (s + 1 < steps) put(other, s + 1);
+      fetch(other, s + 3);
+    });
+    __syncthreads();
+  };
+  int s = 0;
+  for (; s + 1 < steps; s += 2) {
+    step(Odd{}, s);
+    step(Even{}, s + 1);
+  }
+  if (s < steps) step(Odd{}, s);
+}
+
+// The tile's outputs pass through LDS as float32, in the operands' place; the
+// 16-byte chunks of a row are exchanged by bits of the row, so that reads along
+// rows and along columns, sixteen columns of four slots of rows too, meet all banks.
+template <int NB>
+__device__ inline int stage_at(int row, int col) {
+  return row * kSide<NB> + (col ^ ((row & 7) << 2) ^ ((row >> 3 & 3) << 4));
+}
+
+// this wave's sums, scaled, into the stage at its row ``row0`` and column
+// ``col0``; a barrier has to come before and after
+template <int NB>
+__device__ inline void stage_sums(float* stage, const Sums<NB>& acc, int row0, int col0, int lane, float scale) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        stage[stage_at(64 * wm + 32 * i + sum_row(lane, r), 64 * wn + 32 * j + (lane & 31))] =
+        stage[stage_at<NB>(row0 + 32 * i + sum_row(lane, r), col0 + 32 * j + (lane & 31))] =
             acc.v[i][j][r] * scale;
 }
 
