@@ -223,7 +223,19 @@ __global__ void __launch_bounds__(kPrepThreads) grouped_prepare_kernel(PrepArgs 
   lay_weights<T, Back>(a, static_cast<int>(b / col_blocks), static_cast<int>(b % col_blocks) * kPrepCols);
 }
 
-// dz = dy act'(z) by place: float32 as it is, half types as a plane of their own
+// Rows of fewer than eight entries, eight entries apart, so that loads of eight
+// stay inside.
+constexpr int kLeastWidth = 8;
+template <class T>
+__global__ void __launch_bounds__(kThreads) grouped_widen_kernel(int64_t n, int width, const T* __restrict__ in,
+                                                                 int64_t ld, T* __restrict__ out) {
+  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  if (i >= n * kLeastWidth) return;
+  const int c = static_cast<int>(i % kLeastWidth);
+  out[i] = c < width ? in[i / kLeastWidth * ld + c] : from_f32<T>(0.0f);
+}
+
+// dz = dy act'(z) (z = null: dy) by place: float32 as it is, half types as a plane of their own
 // type and one of what that leaves, hi + lo (16 or 22 bits: dz is an intermediate;
 // rounded to its 8 or 11 bits it would add as much error to dx and dW as their own
 // rounding does)
@@ -244,18 +256,19 @@ __global__ void __launch_bounds__(kThreads) grouped_dz_kernel(
     if (row >= 0) {
       if (c + kEach <= cols) {
         a = *reinterpret_cast<const Pack<T, kEach>*>(dy + row * ldy + c);
-        b = *reinterpret_cast<const Pack<T, kEach>*>(z + row * ldz + c);
+        if (z) b = *reinterpret_cast<const Pack<T, kEach>*>(z + row * ldz + c);
       } else {
         for (int j = 0; j < kEach; ++j)
           if (c + j < cols) {
             a.v[j] = dy[row * ldy + c + j];
-            b.v[j] = z[row * ldz + c + j];
+            if (z) b.v[j] = z[row * ldz + c + j];
           }
       }
     }
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-      float v = to_f32(a.v[j]) * silu_slope(to_f32(b.v[j]));
+      float v = to_f32(a.v[j]);
+      if (z) v *= silu_slope(to_f32(b.v[j]));
       // v as one value: fused with the product, the two conversions below could
       // round it to neighbouring hi at a tie
       asm("" : "+v"(v));
@@ -299,44 +312,59 @@ struct RowsArgs {
   void* zout;
 };
 
-// eight entries of a row as they come
+// Eight entries of a row as they come.  A load takes eight entries whatever the
+// row's length, without a condition (loads under one would make the compiler
+// wait for all that are in flight): ``last`` is the largest k at which eight entries
+// lie inside the array, and trim() puts the entries from there in their place
+// and zeros in that of those past the row.
 template <Source S>
 struct Raw {
   u4 v[planes_of<S>];
 };
+// entries of an array of n rows of ``width``, ``ld`` apart, from row ``row`` to its end
+__host__ __device__ inline int last_of(int64_t n, int64_t ld, int width, int64_t row) {
+  const int64_t left = (n - 1 - row) * ld + width - 8;
+  return left > (1 << 30) ? 1 << 30 : static_cast<int>(left);
+}
 
-// entries k .. k + 7 of a row, zeros from kin on; ``row`` starts at any multiple
-// of an entry's size
+// from ``row``, which starts at any multiple of an entry's size, at entry ``k``
 template <Source S>
-__device__ inline void load_raw(Raw<S>& r, const char* row, int64_t plane, int k, int kin) {
-  if (k + 8 <= kin) {
-    if constexpr (S == kFloat) {
-      const Pack<unsigned, 8> p = *reinterpret_cast<const Pack<unsigned, 8>*>(row + int64_t(k) * 4);
-      __builtin_memcpy(&r, &p, sizeof(r));
-    } else {
-#pragma unroll
-      for (int i = 0; i < planes_of<S>; ++i) {
-        const Pack<unsigned short, 8> p =
-            *reinterpret_cast<const Pack<unsigned short, 8>*>(row + i * plane + int64_t(k) * 2);
-        __builtin_memcpy(&r.v[i], &p, 16);
-      }
-    }
+__device__ inline void load_raw(Raw<S>& r, const char* row, int64_t plane, int k) {
+  if constexpr (S == kFloat) {
+    const Pack<unsigned, 8> p = *reinterpret_cast<const Pack<unsigned, 8>*>(row + int64_t(k) * 4);
+    __builtin_memcpy(&r, &p, sizeof(r));
   } else {
-    const u4 none = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < planes_of<S>; ++i) r.v[i] = none;
+    for (int i = 0; i < planes_of<S>; ++i) {
+      const Pack<unsigned short, 8> p =
+          *reinterpret_cast<const Pack<unsigned short, 8>*>(row + i * plane + int64_t(k) * 2);
+      __builtin_memcpy(&r.v[i], &p, 16);
+    }
+  }
+}
+// what was loaded at min(k, last) as the entries k .. k + 7 of a row of ``width``
+template <Source S>
+__device__ inline void trim(Raw<S>& r, int k, int last, int width) {
+  const int off = k < last ? 0 : k - last, keep = width - k;
+  if constexpr (S == kFloat) {
+    unsigned e[8];
+    __builtin_memcpy(e, &r, 32);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (k + j < kin) {
-        if constexpr (S == kFloat) {
-          r.v[j / 4][j % 4] = reinterpret_cast<const unsigned*>(row)[k + j];
-        } else {
+    for (int bit = 1; bit < 8; bit *= 2)
 #pragma unroll
-          for (int i = 0; i < planes_of<S>; ++i)
-            r.v[i][j / 2] |= unsigned(reinterpret_cast<const unsigned short*>(row + i * plane)[k + j])
-                             << (16 * (j & 1));
-        }
-      }
+      for (int j = 0; j < 8; ++j) e[j] = !(off & bit) ? e[j] : j + bit < 8 ? e[j + bit] : 0u;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = j < keep && off < 8 ? e[j] : 0u;
+    __builtin_memcpy(&r, e, 32);
+  } else {
+#pragma unroll
+    for (int p = 0; p < planes_of<S>; ++p) {
+      unsigned __int128 x;
+      __builtin_memcpy(&x, &r.v[p], 16);
+      x = off >= 8 || keep <= 0 ? 0 : x >> (16 * off);
+      if (keep < 8 && keep > 0) x &= ((unsigned __int128)1 << (16 * keep)) - 1;
+      __builtin_memcpy(&r.v[p], &x, 16);
+    }
   }
 }
 
@@ -381,6 +409,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
   // past the tile repeat its last one, and nothing of them is stored
   const int sub = tid & 3, own = tid / 4;
   const char* rows[NB];
+  int last[NB];
 #pragma unroll
   for (int i = 0; i < NB; ++i) {
     int r = 64 * i + own;
@@ -389,25 +418,26 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     if (sub == 0) row_of[64 * i + own] = 64 * i + own < t.count ? static_cast<int32_t>(to) : -1;
     const int64_t row = a.by_place ? t.first + r : to < 0 ? 0 : to;
     rows[i] = static_cast<const char*>(a.in) + row * a.ldin * bytes_of<S>;
+    last[i] = last_of(a.n, a.ldin, a.by_place ? static_cast<int>(a.ldin) : a.kin, row);
   }
   const int64_t in_plane = a.n * a.ldin * bytes_of<S>;
   const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
   const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
 
-  Raw<S> ra[2][NB];
+  constexpr int kFar = 4;
+  Raw<S> ra[kFar][NB];
   u4 rb[2][PB][NB];
-  auto fetch = [&](auto turn, int step) {
+  auto far = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
     const bool in = step < a.w.steps;   // past the end: one line of the weights
-    const int k = in ? step * kDepth + sub * 8 : 0;
-    if (!in || (step + 1) * kDepth <= a.kin) {
+    const int k = step * kDepth + sub * 8;
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-        load_raw<S>(ra[q][i], in ? rows[i] : wsrc, in ? in_plane : 0, k, 1 << 30);
-    } else {
-#pragma unroll
-      for (int i = 0; i < NB; ++i) load_raw<S>(ra[q][i], rows[i], in_plane, k, a.kin);
-    }
+    for (int i = 0; i < NB; ++i)
+      load_raw<S>(ra[q][i], in ? rows[i] : wsrc, in ? in_plane : 0, !in ? 0 : k < last[i] ? k : last[i]);
+  };
+  auto near = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const bool in = step < a.w.steps;
     const char* src = in ? wsrc + step * a.w.step_bytes() + tid * 16 : wsrc;
 #pragma unroll
     for (int p = 0; p < PB; ++p)
@@ -428,8 +458,8 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     __syncthreads();
   }
 
-  auto put = [&](auto turn, int step) {
-    constexpr int q = decltype(turn)::value;
+  auto put = [&](auto turn, auto far_turn, int step) {
+    constexpr int q = decltype(turn)::value, f = decltype(far_turn)::value;
     char* la = lds + q * kHalfLds;
     char* lb = la + PA * kOne;
 #pragma unroll
@@ -437,6 +467,9 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
 #pragma unroll
       for (int i = 0; i < NB; ++i)
         *reinterpret_cast<u4*>(lb + p * kOne + i * 4096 + tid * 16) = rb[q][p][i];
+    if ((step + 1) * kDepth > a.kin)
+#pragma unroll
+      for (int i = 0; i < NB; ++i) trim<S>(ra[f][i], step * kDepth + sub * 8, last[i], a.kin);
     if constexpr (S == kFloat) {
       if (tid == 0) flag[(step + 1) % 3] = 0;
       if (changed[q]) {   // two steps ago; its readers are past it
@@ -445,16 +478,16 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
           if (changed[q] >> i & 1) change[q][64 * i + own] = 0;
         changed[q] = 0;
       }
-      float f[NB][8];
+      float v[NB][8];
       bool over = false;
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         float m = 0.0f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const unsigned bits = ra[q][i].v[j / 4][j % 4];
-          f[i][j] = __builtin_bit_cast(float, bits);
-          m = fmaxf(m, fabsf(f[i][j]));
+          const unsigned bits = ra[f][i].v[j / 4][j % 4];
+          v[i][j] = __builtin_bit_cast(float, bits);
+          m = fmaxf(m, fabsf(v[i][j]));
         }
         over |= m * exp2_of(e[i]) > kLimit;
       }
@@ -463,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
         for (int i = 0; i < NB; ++i) {
           float m = 0.0f;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[i][j]));
+          for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(v[i][j]));
           m = fmaxf(m, __shfl_xor(m, 1));
           m = fmaxf(m, __shfl_xor(m, 2));
           if (m * exp2_of(e[i]) > kLimit) {
@@ -484,7 +517,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           unsigned h, l;
-          split2(f[i][2 * j] * scale, f[i][2 * j + 1] * scale, &h, &l);
+          split2(v[i][2 * j] * scale, v[i][2 * j + 1] * scale, &h, &l);
           hi[j] = h;
           lo[j] = l;
         }
@@ -497,7 +530,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
       for (int i = 0; i < NB; ++i)
 #pragma unroll
         for (int p = 0; p < PA; ++p)
-          *reinterpret_cast<u4*>(la + p * kOne + slot_at(64 * i + own, sub)) = ra[q][i].v[p];
+          *reinterpret_cast<u4*>(la + p * kOne + slot_at(64 * i + own, sub)) = ra[f][i].v[p];
     }
   };
   auto before = [&](int step) {
@@ -531,7 +564,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     between();
     if (live) multiply_parts<kBf>(acc, fa[1], fb[1]);
   };
-  run_steps(a.w.steps, fetch, put, before, multiply);
+  run_steps<kFar>(a.w.steps, near, far, put, before, multiply);
 
   // outputs through LDS, so that rows are written in one piece
   if (S == kFloat && sub == 0)
@@ -693,22 +726,25 @@ struct Column {
   float v[kDepth];
 };
 
-// Column ``col`` of the places first .. first + 31 (zeros from ``end`` on).  The
-// row is the same for all lanes, so its address is scalar work: a lane holds the
-// row of one place, and each load takes its own from there.
-__device__ inline void load_column(Column& r, const float* base, int64_t ld, const int32_t* order,
-                                   int64_t n, int64_t first, int64_t end, int col) {
+// the row of place first + lane % 32, -1 past ``end``
+__device__ inline int look_up(const int32_t* order, int64_t n, int64_t first, int64_t end) {
   const int64_t place = first + (threadIdx.x & 31);
-  int64_t mine = -1;
-  if (place < end) mine = row_at(order, place, n);
-  const bool whole = __ballot(mine < 0) == 0;
-  const int row = static_cast<int>(mine < 0 ? 0 : mine);
+  const int64_t at = place < end ? place : end - 1;
+  const int64_t row = order ? order[at] : at;   // without a condition
+  return place < end && row >= 0 && row < n ? static_cast<int>(row) : -1;
+}
+// Column ``col`` of 32 rows, a lane holding the number of one.  The row of a load
+// is the same for all lanes, so its address is scalar work.
+__device__ inline void load_column(Column& r, const float* base, int64_t ld, int row, int col) {
+  const int at = row < 0 ? 0 : row;
 #pragma unroll
-  for (int i = 0; i < kDepth; ++i) r.v[i] = (base + __builtin_amdgcn_readlane(row, i) * ld)[col];
-  if (!whole)
+  for (int i = 0; i < kDepth; ++i) r.v[i] = (base + __builtin_amdgcn_readlane(at, i) * ld)[col];
+}
+// zeros for the rows that are not there
+__device__ inline void clear_column(Column& r, int row) {
+  if (__ballot(row < 0) == 0) return;
 #pragma unroll
-    for (int i = 0; i < kDepth; ++i)
-      r.v[i] = __builtin_amdgcn_readlane(static_cast<int>(mine < 0), i) ? 0.0f : r.v[i];
+  for (int i = 0; i < kDepth; ++i) r.v[i] = __builtin_amdgcn_readlane(row, i) < 0 ? 0.0f : r.v[i];
 }
 
 __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a) {
@@ -735,13 +771,17 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
   const int steps = (o.t.count + kDepth - 1) / kDepth;
   const bool sums_bias = a.db && o.r0 == 0 && !of_x;
 
+  // The rows of a step are looked up one fetch before its loads, and before
+  // that fetch's own: loads arrive in order, so they are there in time without
+  // the columns having to be.
   Column c[2];
+  int row[2], next = look_up(order, a.n, o.t.first, end);
   auto fetch = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
-    // past the end: the first row's first entry
-    const bool in = step < steps;
-    load_column(c[q], base, in ? ld : 0, in ? order : nullptr, a.n,
-                in ? o.t.first + int64_t(step) * kDepth : 0, in ? end : kDepth, in ? col : 0);
+    row[q] = next;
+    next = look_up(order, a.n, o.t.first + int64_t(step + 1) * kDepth, end);
+    const bool in = step < steps;   // past the end: one entry
+    load_column(c[q], base, in ? ld : 0, row[q], in ? col : 0);
   };
   Sums<2> acc;
   acc.clear();
@@ -751,8 +791,9 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
   change[0][tid] = change[1][tid] = 0;
   if (tid < 3) flag[tid] = 0;
   __syncthreads();
-  auto put = [&](auto turn, int step) {
+  auto put = [&](auto turn, auto, int step) {
     constexpr int q = decltype(turn)::value;
+    clear_column(c[q], row[q]);
     if (sums_bias)
 #pragma unroll
       for (int i = 0; i < kDepth; ++i) bias += c[q].v[i];
@@ -817,7 +858,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
     between();
     if (live) multiply_parts<false>(acc, fa[1], fb[1]);
   };
-  run_steps(steps, fetch, put, before, multiply);
+  run_steps<2>(steps, fetch, [](auto, int) {}, put, before, multiply);
 
   if (a.dw) {
     exps[tid] = e;
@@ -848,43 +889,52 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   const int xc = o.r0 + 8 * cg, zc = o.c0 + 8 * cg;
   const int64_t z_plane = a.n * a.lddz * 2;
 
-  // the row of each place, one step ahead of its use
-  int64_t row[2];
-  auto look_up = [&](int step) {
+  // the rows of a step, looked up one fetch before its loads, and before that
+  // fetch's own (see above)
+  int64_t next[2];
+  auto look = [&](int step) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int64_t place = o.t.first + int64_t(step) * kDepth + 16 * i + own;
-      row[i] = place < end ? row_at(a.order, place, a.n) : -1;
+      const int64_t at = place < end ? place : end - 1;
+      const int64_t row = a.order ? a.order[at] : at;   // without a condition
+      next[i] = place < end && row >= 0 && row < a.n ? row : -1;
     }
   };
   Raw<kHalf> rx[2][2];
   Raw<SZ> rz[2][2];
+  int x_last[2][2], z_last[2][2];
   bool there[2][2];
-  look_up(0);
+  look(0);
   auto fetch = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
+    int64_t row[2] = {next[0], next[1]};
+    look(step + 1);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       // places past the end: row 0, put as zeros
       there[q][i] = row[i] >= 0;
-      const int64_t rx_row = there[q][i] ? row[i] : 0;
-      const int64_t rz_row =
+      const int64_t x_row = there[q][i] ? row[i] : 0;
+      const int64_t z_row =
           !there[q][i] ? 0 : a.by_place ? o.t.first + int64_t(step) * kDepth + 16 * i + own : row[i];
-      const char* px = static_cast<const char*>(a.x) + rx_row * a.ldx * 2;
-      const char* pz = static_cast<const char*>(a.dz) + rz_row * a.lddz * 2;
-      load_raw<kHalf>(rx[q][i], px, 0, xc, a.k);
-      load_raw<SZ>(rz[q][i], pz, z_plane, zc, a.m);
+      x_last[q][i] = last_of(a.n, a.ldx, a.k, x_row);
+      z_last[q][i] = last_of(a.n, a.lddz, a.by_place ? static_cast<int>(a.lddz) : a.m, z_row);
+      const char* px = static_cast<const char*>(a.x) + x_row * a.ldx * 2;
+      const char* pz = static_cast<const char*>(a.dz) + z_row * a.lddz * 2;
+      load_raw<kHalf>(rx[q][i], px, 0, xc < x_last[q][i] ? xc : x_last[q][i]);
+      load_raw<SZ>(rz[q][i], pz, z_plane, zc < z_last[q][i] ? zc : z_last[q][i]);
     }
-    look_up(step + 1);
   };
   float bias[8] = {};
-  auto put = [&](auto turn, int) {
+  auto put = [&](auto turn, auto, int) {
     constexpr int q = decltype(turn)::value;
     const u4 none = {0, 0, 0, 0};
     char* to = lds + q * kHalfLds + cg / 4 * 32 * kRowBytes;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int at = slot_at(16 * i + own, cg % 4);
+      if (o.r0 + kOuterTile > a.k) trim<kHalf>(rx[q][i], xc, x_last[q][i], a.k);
+      if (o.c0 + kOuterTile > a.m) trim<SZ>(rz[q][i], zc, z_last[q][i], a.m);
       *reinterpret_cast<u4*>(to + at) = there[q][i] ? rx[q][i].v[0] : none;
 #pragma unroll
       for (int p = 0; p < PB; ++p) {
@@ -918,7 +968,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
     between();
     if (live) multiply_parts<kBf>(acc, fa[1], fb[1]);
   };
-  run_steps(steps, fetch, put, [](int) {}, multiply);
+  run_steps<2>(steps, fetch, [](auto, int) {}, put, [](int) {}, multiply);
 
   if (a.dw) store_outer<T>(a, o, acc, nullptr);
   if (sums_bias) {
@@ -933,19 +983,35 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   }
 }
 
-// the blocks of a group added up in their order; zeros for groups without rows
+// The blocks of a group added up in their order, dW then db (null: not formed);
+// zeros for groups without rows.
 template <class T>
 __global__ void __launch_bounds__(kThreads) grouped_join_kernel(const int32_t* __restrict__ first_of,
-                                                                int64_t each,
-                                                                const float* __restrict__ parts,
-                                                                T* __restrict__ out) {
+                                                                int64_t each_w, int64_t each_b,
+                                                                const float* __restrict__ parts_w,
+                                                                const float* __restrict__ parts_b,
+                                                                T* __restrict__ dw, T* __restrict__ db) {
   const int g = blockIdx.y;
-  const int64_t first = first_of[g], count = first_of[g + 1] - first;
+  const int first = first_of[g], count = first_of[g + 1] - first;
   if (count == 1) return;
-  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= each) return;
+  int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t of_w = dw ? each_w : 0;
+  const bool w = i < of_w;
+  i = w ? i : i - of_w;
+  const int64_t each = w ? each_w : each_b;
+  T* out = w ? dw : db;
+  if (!out || i >= each) return;
+  const float* part = (w ? parts_w : parts_b) + first * each + i;
   float s = 0.0f;
-  for (int64_t b = 0; b < count; ++b) s += parts[(first + b) * each + i];
+  int b = 0;
+  for (; b + 8 <= count; b += 8) {   // eight loads in flight
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = part[(b + k) * each];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += v[k];
+  }
+  for (; b < count; ++b) s += part[b * each];
   out[g * each + i] = from_f32<T>(s);
 }
 
@@ -996,19 +1062,38 @@ TileList list_of(Arena& ar, const dpa4c_grouped& l, int rows, bool rest) {
 }
 
 // entries of a row of dz: rows start at multiples of 16 bytes
-int pitch_of(const dpa4c_grouped& l) {
-  return static_cast<int>(align_up(l.n_out, l.dtype == DPA4C_F32 ? 4 : 8));
+int pitch_of(const dpa4c_grouped& l) { return static_cast<int>(align_up(l.n_out, 8)); }
+
+// x with rows of at least eight entries
+struct Input {
+  const void* at;
+  int64_t ld;
+};
+int64_t wide_bytes(const dpa4c_grouped& l) {
+  return l.k < kLeastWidth ? l.n * kLeastWidth * (l.dtype == DPA4C_F32 ? 4 : 2) : 0;
+}
+template <class T>
+int widen(const dpa4c_grouped& l, void* room, Input* in, hipStream_t st) {
+  *in = {l.x, l.ldx};
+  if (l.k >= kLeastWidth) return 0;
+  grouped_widen_kernel<T><<<(l.n * kLeastWidth + kThreads - 1) / kThreads, kThreads, 0, st>>>(
+      l.n, l.k, static_cast<const T*>(l.x), l.ldx, static_cast<T*>(room));
+  DPA4C_HIP_TRY(hipGetLastError());
+  *in = {room, kLeastWidth};
+  return 0;
 }
 
 struct ForwardPlan {
   Weights w;
   TileList tiles;
+  void* wide;
 };
 ForwardPlan plan_forward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   ForwardPlan p;
   p.w = weights_of(ar, l, false);
   p.tiles = list_of(ar, l, tile_side(l.n, l.n_out), true);
+  p.wide = ar.take<char>(wide_bytes(l));
   *bytes = ar.used;
   return p;
 }
@@ -1016,7 +1101,7 @@ ForwardPlan plan_forward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
 struct BackwardPlan {
   Weights w;
   TileList tiles, blocks;
-  void* dz;
+  void *dz, *wide;
   float *parts, *db_parts;
 };
 BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
@@ -1027,6 +1112,7 @@ BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   const int rows = outer_rows(l);
   p.blocks = list_of(ar, l, rows, false);
   p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
+  p.wide = ar.take<char>(wide_bytes(l));
   const int64_t blocks = tiles_at_most(l.n, l.n_groups, rows);
   p.parts = ar.take<float>(blocks * l.k * l.n_out);
   p.db_parts = ar.take<float>(blocks * l.n_out);
@@ -1089,12 +1175,10 @@ int run_outer(const dpa4c_grouped& l, const OuterArgs& a, const TileList& blocks
       grouped_outer_half_kernel<T, kHalf><<<grid, kThreads, 0, st>>>(a);
     DPA4C_HIP_TRY(hipGetLastError());
   }
-  auto join = [&](int64_t each, const float* parts, void* out) {
-    const dim3 grid((each + kThreads - 1) / kThreads, l.n_groups);
-    grouped_join_kernel<T><<<grid, kThreads, 0, st>>>(blocks.first_of, each, parts, static_cast<T*>(out));
-  };
-  if (a.dw) join(int64_t(l.k) * l.n_out, a.parts, a.dw);
-  if (a.db) join(l.n_out, a.db_parts, a.db);
+  const int64_t each_w = int64_t(l.k) * l.n_out, all = (a.dw ? each_w : 0) + (a.db ? l.n_out : 0);
+  const dim3 grid((all + kThreads - 1) / kThreads, l.n_groups);
+  grouped_join_kernel<T><<<grid, kThreads, 0, st>>>(blocks.first_of, each_w, l.n_out, a.parts, a.db_parts,
+                                                    static_cast<T*>(a.dw), static_cast<T*>(a.db));
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }
@@ -1121,6 +1205,8 @@ int launch_grouped_forward(const dpa4c_grouped& l, const void* bias, bool silu, 
     int64_t bytes;
     const ForwardPlan p = plan_forward(l, work, &bytes);
     DPA4C_TRY((prepare<T, false>(l, &p.w, &p.tiles, nullptr, st)));
+    Input in;
+    DPA4C_TRY(widen<T>(l, p.wide, &in, st));
     RowsArgs a{};
     a.order = l.order;
     a.n_groups = l.n_groups;
@@ -1129,8 +1215,8 @@ int launch_grouped_forward(const dpa4c_grouped& l, const void* bias, bool silu, 
     a.n_tiles = p.tiles.count;
     a.kin = l.k;
     a.kout = l.n_out;
-    a.in = l.x;
-    a.ldin = l.ldx;
+    a.in = in.at;
+    a.ldin = in.ld;
     a.w = p.w;
     a.bias = bias;
     a.silu = silu;
@@ -1155,7 +1241,8 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
     DPA4C_TRY((prepare<T, true>(l, rows ? &p.w : nullptr, rows ? &p.tiles : nullptr,
                                 outer ? &p.blocks : nullptr, st)));
     const int pitch = pitch_of(l);
-    if (z && l.n > 0) {
+    const bool made = z || l.n_out < kLeastWidth;   // dz is formed, by place
+    if (made && l.n > 0) {
       const int64_t each = l.n * (pitch * int64_t(sizeof(T)) / 16);
       const int64_t grid = std::min<int64_t>((each + kThreads - 1) / kThreads, 8192);
       grouped_dz_kernel<T><<<grid, kThreads, 0, st>>>(
@@ -1172,14 +1259,14 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.n_tiles = p.tiles.count;
       a.kin = l.n_out;
       a.kout = l.k;
-      a.in = z ? p.dz : dy;
-      a.ldin = z ? pitch : ldy;
-      a.by_place = z != nullptr;
+      a.in = made ? p.dz : dy;
+      a.ldin = made ? pitch : ldy;
+      a.by_place = made;
       a.w = p.w;
       a.residual = residual ? dy : nullptr;
       a.ldres = ldy;
       a.out = dx;
-      if (z)
+      if (made)
         DPA4C_TRY((run_rows<T, kMade>(a, p.tiles, st)));
       else
         DPA4C_TRY((run_rows<T, kOwn>(a, p.tiles, st)));
@@ -1192,11 +1279,13 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.n_blocks = p.blocks.count;
       a.k = l.k;
       a.m = l.n_out;
-      a.x = l.x;
-      a.ldx = l.ldx;
-      a.dz = z ? p.dz : dy;
-      a.lddz = z ? pitch : ldy;
-      a.by_place = z != nullptr;
+      Input in{l.x, l.ldx};
+      if (l.n > 0) DPA4C_TRY(widen<T>(l, p.wide, &in, st));
+      a.x = in.at;
+      a.ldx = in.ld;
+      a.dz = made ? p.dz : dy;
+      a.lddz = made ? pitch : ldy;
+      a.by_place = made;
       a.dw = dw;
       a.db = db;
       a.parts = p.parts;

@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
         }
       }
   };
-  auto put = [&](auto turn, int) {
+  auto put = [&](auto turn, auto, int) {
     constexpr int q = decltype(turn)::value;
     char* to = lds + q * 4 * kOne + tid * 16;
 #pragma unroll
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
     between();
     if (live) multiply_parts<false>(acc, fa[1], fb[1]);
   };
-  run_steps(steps, fetch, put, [](int) {}, multiply);
+  run_steps<2>(steps, fetch, [](auto, int) {}, put, [](int) {}, multiply);
 
   float* stage = reinterpret_cast<float*>(lds);
   stage_sums(stage, acc, kTile / 2 * wm, kTile / 2 * wn, lane,

@@ -10,9 +10,9 @@
 // cycles for what v_mfma_f32_32x32x2_f32 takes 512 cycles for.
 //
 // A step of 32 entries is 768 matrix-core cycles of a wave for float32 at NB =
-// 2.  Its loads are issued two steps before their use, into registers; they go
-// to the other half of LDS while this step's half is read, so a step has one
-// barrier.  NB = 2 halves the traffic; NB = 1 gives four times as many
+// 2.  Its loads are issued two steps (from HBM four) before their use, into
+// registers; they go to the other half of LDS while this step's half is read, so a
+// step has one barrier.  NB = 2 halves the traffic; NB = 1 gives four times as many
 // workgroups with a quarter of the latency of a step, for work that does not
 // fill the chip.
 //
@@ -154,35 +154,56 @@ __device__ inline void multiply_parts(Sums<NB>& acc, const Part<NB, PA>& a, cons
       }
 }
 
-// The steps of a tile.  fetch(turn, s) issues the loads of step s into register
-// set ``turn`` (a constant 0 or 1; s may be past the end, where it loads
-// anything that is cheap: loads under a condition would make the compiler wait
-// for all of them at every put), put(turn, s) writes that set to half s % 2 of LDS,
-// before(s) runs when step s - 1's sums are complete, and multiply(s, between)
-// adds step s, with ``between`` called halfway.
-template <class Fetch, class Put, class Before, class Multiply>
-__device__ inline void run_steps(int steps, Fetch&& fetch, Put&& put, Before&& before, Multiply&& multiply) {
-  using Even = std::integral_constant<int, 0>;
-  using Odd = std::integral_constant<int, 1>;
-  fetch(Even{}, 0);
-  fetch(Odd{}, 1);
-  put(Even{}, 0);
-  fetch(Even{}, 2);
+// The steps of a tile.  near(turn, s) and far(turn, s) issue the loads of step s
+// into register set ``turn`` (a constant) of 2 and of Far sets: operands from L2,
+// two steps ahead, and operands from HBM, Far ahead (s may be past the end, where
+// they load anything that is cheap: loads under a condition would make the
+// compiler wait for all of them at every put).  put(n, f, s) writes sets n and f to
+// half s % 2 of LDS, before(s) runs when step s - 1's sums are complete, and
+// multiply(s, between) adds step s, with ``between`` called halfway.  Loads arrive
+// in the order of their issue, so the near ones go first.
+template <int K>
+using Const = std::integral_constant<int, K>;
+template <int Far, class Near, class FarFn, class Put, class Before, class Multiply>
+__device__ inline void run_steps(int steps, Near&& near, FarFn&& far, Put&& put, Before&& before,
+                                 Multiply&& multiply) {
+  static_assert(Far == 2 || Far == 4, "the steps are unrolled by Far");
+  near(Const<0>{}, 0);
+  far(Const<0>{}, 0);
+  near(Const<1>{}, 1);
+  far(Const<1>{}, 1);
+  if constexpr (Far == 4) {
+    far(Const<2>{}, 2);
+    far(Const<3>{}, 3);
+  }
+  put(Const<0>{}, Const<0>{}, 0);
+  near(Const<0>{}, 2);
+  far(Const<0>{}, Far);
   __syncthreads();
-  auto step = [&](auto other, int s) {
+  auto step = [&](auto next, int s) {   // next = (s + 1) % Far
+    constexpr int f = decltype(next)::value;
     before(s);
     multiply(s, [&] {
-      if (s + 1 < steps) put(other, s + 1);
-      fetch(other, s + 3);
+      if (s + 1 < steps) put(Const<f & 1>{}, next, s + 1);
+      near(Const<f & 1>{}, s + 3);
+      far(next, s + 1 + Far);
     });
     __syncthreads();
   };
   int s = 0;
-  for (; s + 1 < steps; s += 2) {
-    step(Odd{}, s);
-    step(Even{}, s + 1);
+  for (; s + Far <= steps; s += Far) {
+    step(Const<1>{}, s);
+    if constexpr (Far == 4) {
+      step(Const<2>{}, s + 1);
+      step(Const<3>{}, s + 2);
+    }
+    step(Const<0>{}, s + Far - 1);
   }
-  if (s < steps) step(Odd{}, s);
+  if (s < steps) step(Const<1>{}, s);
+  if constexpr (Far == 4) {
+    if (s + 1 < steps) step(Const<2>{}, s + 1);
+    if (s + 2 < steps) step(Const<3>{}, s + 2);
+  }
 }
 
 // The tile's outputs pass through LDS as float32, in the operands' place; the
