@@ -640,6 +640,282 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// Many rows times weights: 128 rows x up to 384 columns a workgroup
+// ---------------------------------------------------------------------------
+
+// Rows come from HBM with some 2 us of latency, and a compute unit needs 37 KB of
+// them in flight for its share of the bandwidth.  Tiles of 128 columns each fetch
+// the same rows; here a workgroup of eight waves, one a compute unit, fetches a row
+// once for up to 384 columns.  A wave forms 64 x 96 outputs, so LDS is read 2/3 as
+// often for a product too, and a float32 step is 1 us of the matrix cores, three
+// of which cover the latency.
+constexpr int kWideThreads = 512, kWideRows = 128, kWideBlocks = 12;   // blocks of 32 columns
+
+template <class T, Source S>
+__global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs a) {
+  constexpr int PA = planes_of<S>, PB = S == kFloat ? 2 : 1, NT = kWideBlocks / 4;
+  constexpr bool kBf = std::is_same<T, __bf16>::value;
+  constexpr int kOneA = kWideRows * kRowBytes, kOneB = kWideBlocks * 32 * kRowBytes;
+  constexpr int kHalfLds = PA * kOneA + PB * kOneB;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
+  __shared__ int32_t row_of[kWideRows];      // -1: nothing is stored
+  __shared__ int32_t change[2][kWideRows];   // exponent that a row's sums are to move by
+  __shared__ int32_t row_exp[kWideRows];
+  __shared__ int32_t flag[3];
+
+  const int all_blocks = (a.kout + 31) / 32;
+  const int col_tiles = (all_blocks + kWideBlocks - 1) / kWideBlocks;
+  const int each = (all_blocks + col_tiles - 1) / col_tiles;   // blocks of a tile
+  const int64_t total = int64_t(*a.n_tiles) * col_tiles;
+  if (blockIdx.x >= total) return;
+  const int64_t work = xcd_block(blockIdx.x, total);
+  const RowTile t = a.tiles[work / col_tiles];
+  const int b0 = static_cast<int>(work % col_tiles) * each, c0 = b0 * 32;
+  const int blocks = all_blocks - b0 < each ? all_blocks - b0 : each;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
+  T* out = static_cast<T*>(a.out);
+  T* zout = static_cast<T*>(a.zout);
+
+  if (t.group == a.n_groups) {   // rows of no group
+    const int width = a.kout - c0 < blocks * 32 ? a.kout - c0 : blocks * 32;
+    for (int i = tid; i < t.count * width; i += kWideThreads) {
+      const int64_t row = row_at(a.order, t.first + i / width, a.n);
+      if (row < 0) continue;
+      out[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
+      if (zout) zout[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
+    }
+    return;
+  }
+
+  // this thread's row and its eight entries of a step; rows past the tile repeat
+  // its last one, and nothing of them is stored
+  const int sub = tid & 3, own = tid / 4;
+  const char* row_p;
+  int last;
+  {
+    const int r = own < t.count ? own : t.count - 1;
+    const int64_t to = row_at(a.order, t.first + r, a.n);
+    if (sub == 0) row_of[own] = own < t.count ? static_cast<int32_t>(to) : -1;
+    const int64_t row = a.by_place ? t.first + r : to < 0 ? 0 : to;
+    row_p = static_cast<const char*>(a.in) + row * a.ldin * bytes_of<S>;
+    last = last_of(a.n, a.ldin, a.by_place ? static_cast<int>(a.ldin) : a.kin, row);
+  }
+  const int64_t in_plane = a.n * a.ldin * bytes_of<S>;
+  const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
+  const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
+
+  constexpr int kFar = 4;
+  Raw<S> ra[kFar];
+  u4 rb[2][PB][NT];
+  auto far = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const bool in = step < a.w.steps;   // past the end: one line of the weights
+    const int k = step * kDepth + sub * 8;
+    load_raw<S>(ra[q], in ? row_p : wsrc, in ? in_plane : 0, !in ? 0 : k < last ? k : last);
+  };
+  // slots i 512 + tid of the tile's columns; those past them: one line
+  unsigned slot_of_b[NT];
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const unsigned idx = i * kWideThreads + tid;
+    slot_of_b[i] = idx < unsigned(blocks) * 128 ? idx * 16 : 0;
+  }
+  auto near = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const bool in = step < a.w.steps;
+    const char* src = in ? wsrc + step * a.w.step_bytes() : wsrc;
+#pragma unroll
+    for (int p = 0; p < PB; ++p)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        rb[q][p][i] = *reinterpret_cast<const u4*>(src + p * wplane + size_t(in ? slot_of_b[i] : 0));
+  };
+
+  v16f acc[2][NT];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = v16f{};
+  int e = kFirstExp;
+  bool changed[2] = {false, false};
+  if (S == kFloat) {
+    if (tid < 2 * kWideRows) change[tid / kWideRows][tid % kWideRows] = 0;
+    if (tid < 3) flag[tid] = 0;
+    __syncthreads();
+  }
+
+  auto put = [&](auto turn, auto far_turn, int step) {
+    constexpr int q = decltype(turn)::value, f = decltype(far_turn)::value;
+    char* la = lds + q * kHalfLds;
+    char* lb = la + PA * kOneA;
+#pragma unroll
+    for (int p = 0; p < PB; ++p)
+#pragma unroll
+      for (int i = 0; i < NT; ++i)
+        *reinterpret_cast<u4*>(lb + p * kOneB + (i * kWideThreads + tid) * 16) = rb[q][p][i];
+    if ((step + 1) * kDepth > a.kin) trim<S>(ra[f], step * kDepth + sub * 8, last, a.kin);
+    const int at = slot_at(own, sub);
+    if constexpr (S == kFloat) {
+      if (tid == 0) flag[(step + 1) % 3] = 0;
+      if (changed[q]) {   // two steps ago; its readers are past it
+        change[q][own] = 0;
+        changed[q] = false;
+      }
+      float v[8];
+      float m = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const unsigned bits = ra[f].v[j / 4][j % 4];
+        v[j] = __builtin_bit_cast(float, bits);
+        m = fmaxf(m, fabsf(v[j]));
+      }
+      if (__ballot(m * exp2_of(e) > kLimit) != 0) {   // a row has outgrown its scale: rare past the first step
+        m = fmaxf(m, __shfl_xor(m, 1));
+        m = fmaxf(m, __shfl_xor(m, 2));
+        if (m * exp2_of(e) > kLimit) {
+          const int now = exp_for(m);
+          if (sub == 0) {
+            change[q][own] = now - e;
+            changed[q] = true;
+            flag[step % 3] = 1;
+          }
+          e = now;
+        }
+      }
+      const float scale = exp2_of(e);
+      u4 hi, lo;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        unsigned h, l;
+        split2(v[2 * j] * scale, v[2 * j + 1] * scale, &h, &l);
+        hi[j] = h;
+        lo[j] = l;
+      }
+      *reinterpret_cast<u4*>(la + at) = hi;
+      *reinterpret_cast<u4*>(la + kOneA + at) = lo;
+    } else {
+#pragma unroll
+      for (int p = 0; p < PA; ++p) *reinterpret_cast<u4*>(la + p * kOneA + at) = ra[f].v[p];
+    }
+  };
+  auto before = [&](int step) {
+    if constexpr (S == kFloat) {
+      if (flag[step % 3]) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int d = change[step & 1][64 * wm + 32 * i + sum_row(lane, r)];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j][r] = ldexpf(acc[i][j][r], d);
+          }
+      }
+    }
+  };
+  // this wave's blocks wn, wn + 4, ..
+  const int mine = 64 * wm >= t.count || wn >= blocks ? 0 : (blocks - wn + 3) / 4;
+  auto multiply = [&](int step, auto&& between) {
+    const char* la = lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes;
+    const char* lb = lds + (step & 1) * kHalfLds + PA * kOneA + wn * 32 * kRowBytes;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      if (mine > 0) {
+        Part<2, PA> fa;
+        load_part(fa, la, kOneA, lane, ks);
+        Part<1, PB> fb[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) load_part(fb[j], lb + j * 128 * kRowBytes, kOneB, lane, ks);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int p = PA + PB - 2; p >= 0; --p)   // the small products first
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int pa = PA == 2 && PB == 2 ? (p == 2 ? 1 : 0) : PA == 2 ? p : 0;
+              const int pb = PA == 2 && PB == 2 ? (p == 1 ? 1 : 0) : PB == 2 ? p : 0;
+              acc[i][j] = mfma<kBf>(fa.v[i][pa], fb[j].v[0][pb], acc[i][j]);
+            }
+      }
+      if (ks == 0) between();
+    }
+  };
+  run_steps<kFar>(a.w.steps, near, far, put, before, multiply);
+
+  if (S == kFloat) {
+    if (sub == 0) row_exp[own] = e;
+    __syncthreads();
+  }
+  // Outputs from the registers: a lane has a column, 32 of them are 128 bytes of a
+  // row; half types go out two columns a lane, the even lanes with the row of sum
+  // r and the odd ones with that of sum r + 1.
+  const T* bias = a.bias ? static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
+  const T* res = static_cast<const T*>(a.residual);
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    if (j >= mine) continue;
+    const int c = c0 + (wn + 4 * j) * 32 + (lane & 31);
+    const bool in = c < a.kout;
+    const int cc = in ? c : a.kout - 1;
+    const float bv = bias ? to_f32(bias[cc]) : 0.0f;
+    const int ec = S == kFloat ? a.w.exps[int64_t(t.group) * a.w.cols_pad + c] : 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      int row[16];
+      float rv[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) row[r] = row_of[64 * wm + 32 * i + sum_row(lane, r)];
+      if (res)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) rv[r] = to_f32(res[int64_t(row[r] < 0 ? 0 : row[r]) * a.ldres + cc]);
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        float y[2], z[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          z[q] = acc[i][j][r + q];
+          if (S == kFloat) z[q] = ldexpf(z[q], -row_exp[64 * wm + 32 * i + sum_row(lane, r + q)] - ec);
+          z[q] += bv;
+          y[q] = a.silu ? z[q] * logistic(z[q]) : z[q];
+          if (res) y[q] += rv[r + q];
+        }
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (in && row[r + q] >= 0) {
+              out[int64_t(row[r + q]) * a.kout + c] = y[q];
+              if (zout) zout[int64_t(row[r + q]) * a.kout + c] = z[q];
+            }
+        } else {
+          const bool odd = lane & 1;
+          const int to = odd ? row[r + 1] : row[r], at = odd ? c - 1 : c;
+          auto pack = [&](const float* v) {
+            const unsigned mine2 = unsigned(__builtin_bit_cast(unsigned short, from_f32<T>(v[0]))) |
+                                   unsigned(__builtin_bit_cast(unsigned short, from_f32<T>(v[1]))) << 16;
+            // the neighbour's two rows of its column
+            const unsigned other = __builtin_amdgcn_mov_dpp(mine2, 0xB1, 0xf, 0xf, true);
+            return odd ? __builtin_amdgcn_perm(mine2, other, 0x07060302u)
+                       : __builtin_amdgcn_perm(other, mine2, 0x05040100u);
+          };
+          const unsigned yy = pack(y), zz = zout ? pack(z) : 0;
+          if (to >= 0) {
+            T* po = out + int64_t(to) * a.kout + at;
+            T* pz = zout + int64_t(to) * a.kout + at;
+            if (at + 1 < a.kout) {
+              *reinterpret_cast<Pack<T, 2>*>(po) = __builtin_bit_cast(Pack<T, 2>, yy);
+              if (zout) *reinterpret_cast<Pack<T, 2>*>(pz) = __builtin_bit_cast(Pack<T, 2>, zz);
+            } else if (at < a.kout) {
+              *po = __builtin_bit_cast(T, static_cast<unsigned short>(yy & 0xffff));
+              if (zout) *pz = __builtin_bit_cast(T, static_cast<unsigned short>(zz & 0xffff));
+            }
+          }
+        }
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Gradients of the weights
 // ---------------------------------------------------------------------------
 
@@ -1023,11 +1299,9 @@ int64_t tiles_at_most(int64_t n, int n_groups, int64_t rows) {
   return n / rows + (n < n_groups + 1 ? n : n_groups + 1);
 }
 
-// Rows (and columns) of a tile: 128 once such tiles fill the chip's 256 compute
-// units, 64 below.
-int tile_side(int64_t n, int cols) {
-  return (n / 128) * ((cols + 127) / 128) >= 256 ? 128 : 64;
-}
+// Rows of a tile: 128, with up to 384 columns, from half as many such tiles as
+// there are compute units on, 64 and 64 columns below.
+int tile_rows(int64_t n) { return n >= 128 * 128 ? kWideRows : kSide<1>; }
 
 // Rows of a block of dW: 4,096 workgroups in all, some rounds of the chip's 512
 // resident ones, but no fewer than 512 rows, so that a block's sums are small
@@ -1092,7 +1366,7 @@ ForwardPlan plan_forward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   ForwardPlan p;
   p.w = weights_of(ar, l, false);
-  p.tiles = list_of(ar, l, tile_side(l.n, l.n_out), true);
+  p.tiles = list_of(ar, l, tile_rows(l.n), true);
   p.wide = ar.take<char>(wide_bytes(l));
   *bytes = ar.used;
   return p;
@@ -1108,7 +1382,7 @@ BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   BackwardPlan p;
   p.w = weights_of(ar, l, true);
-  p.tiles = list_of(ar, l, tile_side(l.n, l.k), true);
+  p.tiles = list_of(ar, l, tile_rows(l.n), true);
   const int rows = outer_rows(l);
   p.blocks = list_of(ar, l, rows, false);
   p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
@@ -1152,11 +1426,14 @@ int prepare(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, con
 
 template <class T, Source S>
 int run_rows(const RowsArgs& a, const TileList& tiles, hipStream_t st) {
-  const int64_t grid = tiles_at_most(a.n, a.n_groups, tiles.rows) * ((a.kout + tiles.rows - 1) / tiles.rows);
-  if (tiles.rows == kSide<2>)
-    grouped_rows_kernel<T, S, 2><<<grid, kThreads, 0, st>>>(a);
-  else
-    grouped_rows_kernel<T, S, 1><<<grid, kThreads, 0, st>>>(a);
+  const int64_t most = tiles_at_most(a.n, a.n_groups, tiles.rows);
+  if (tiles.rows == kWideRows) {
+    const int64_t cols = ((a.kout + 31) / 32 + kWideBlocks - 1) / kWideBlocks;
+    grouped_wide_kernel<T, S><<<most * cols, kWideThreads, 0, st>>>(a);
+  } else {
+    const int64_t cols = (a.kout + kSide<1> - 1) / kSide<1>;
+    grouped_rows_kernel<T, S, 1><<<most * cols, kThreads, 0, st>>>(a);
+  }
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }
