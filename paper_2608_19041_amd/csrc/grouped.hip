@@ -424,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
   const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
   const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
 
-  constexpr int kFar = 4;
+  constexpr int kFar = S == kFloat && NB == 2 ? 2 : 4;   // what the registers hold
   Raw<S> ra[kFar][NB];
   u4 rb[2][PB][NB];
   auto far = [&](auto turn, int step) {
@@ -548,23 +548,19 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     }
   };
   const bool live = c0 + kTile / 2 * wn < a.kout && kTile / 2 * wm < t.count;
-  auto multiply = [&](int step, auto&& between) {
-    const char* la = lds + (step & 1) * kHalfLds + wm * (kTile / 2) * kRowBytes;
-    const char* lb = lds + (step & 1) * kHalfLds + PA * kOne + wn * (kTile / 2) * kRowBytes;
-    Part<NB, PA> fa[2];
-    Part<NB, PB> fb[2];
-    if (live) {
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        load_part(fa[ks], la, kOne, lane, ks);
-        load_part(fb[ks], lb, kOne, lane, ks);
-      }
-      multiply_parts<kBf>(acc, fa[0], fb[0]);
-    }
-    between();
-    if (live) multiply_parts<kBf>(acc, fa[1], fb[1]);
+  Part<NB, PA> fa[2];
+  Part<NB, PB> fb[2];
+  auto read = [&](auto half, int step) {
+    constexpr int ks = decltype(half)::value;
+    if (!live) return;
+    load_part(fa[ks], lds + (step & 1) * kHalfLds + wm * (kTile / 2) * kRowBytes, kOne, lane, ks);
+    load_part(fb[ks], lds + (step & 1) * kHalfLds + PA * kOne + wn * (kTile / 2) * kRowBytes, kOne, lane, ks);
   };
-  run_steps<kFar>(a.w.steps, near, far, put, before, multiply);
+  auto multiply = [&](auto half) {
+    constexpr int ks = decltype(half)::value;
+    if (live) multiply_parts<kBf>(acc, fa[ks], fb[ks]);
+  };
+  run_steps<2, kFar>(a.w.steps, near, far, put, read, before, multiply);
 
   // outputs through LDS, so that rows are written in one piece
   if (S == kFloat && sub == 0)
@@ -705,9 +701,9 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
   const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
   const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
 
-  constexpr int kFar = 4;
+  constexpr int kFar = 2;
   Raw<S> ra[kFar];
-  u4 rb[2][PB][NT];
+  u4 rb[PB][NT];
   auto far = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
     const bool in = step < a.w.steps;   // past the end: one line of the weights
@@ -721,15 +717,14 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
     const unsigned idx = i * kWideThreads + tid;
     slot_of_b[i] = idx < unsigned(blocks) * 128 ? idx * 16 : 0;
   }
-  auto near = [&](auto turn, int step) {
-    constexpr int q = decltype(turn)::value;
+  auto near = [&](auto, int step) {
     const bool in = step < a.w.steps;
     const char* src = in ? wsrc + step * a.w.step_bytes() : wsrc;
 #pragma unroll
     for (int p = 0; p < PB; ++p)
 #pragma unroll
       for (int i = 0; i < NT; ++i)
-        rb[q][p][i] = *reinterpret_cast<const u4*>(src + p * wplane + size_t(in ? slot_of_b[i] : 0));
+        rb[p][i] = *reinterpret_cast<const u4*>(src + p * wplane + size_t(in ? slot_of_b[i] : 0));
   };
 
   v16f acc[2][NT];
@@ -745,15 +740,15 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
     __syncthreads();
   }
 
-  auto put = [&](auto turn, auto far_turn, int step) {
-    constexpr int q = decltype(turn)::value, f = decltype(far_turn)::value;
+  auto put = [&](auto, auto far_turn, int step) {
+    constexpr int f = decltype(far_turn)::value, q = f & 1;   // q: step % 2
     char* la = lds + q * kHalfLds;
     char* lb = la + PA * kOneA;
 #pragma unroll
     for (int p = 0; p < PB; ++p)
 #pragma unroll
       for (int i = 0; i < NT; ++i)
-        *reinterpret_cast<u4*>(lb + p * kOneB + (i * kWideThreads + tid) * 16) = rb[q][p][i];
+        *reinterpret_cast<u4*>(lb + p * kOneB + (i * kWideThreads + tid) * 16) = rb[p][i];
     if ((step + 1) * kDepth > a.kin) trim<S>(ra[f], step * kDepth + sub * 8, last, a.kin);
     const int at = slot_at(own, sub);
     if constexpr (S == kFloat) {
@@ -815,103 +810,94 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
   };
   // this wave's blocks wn, wn + 4, ..
   const int mine = 64 * wm >= t.count || wn >= blocks ? 0 : (blocks - wn + 3) / 4;
-  auto multiply = [&](int step, auto&& between) {
+  Part<2, PA> fa[2];
+  Part<1, PB> fb[2][NT];
+  auto read = [&](auto half, int step) {
+    constexpr int ks = decltype(half)::value;
+    if (mine == 0) return;
     const char* la = lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes;
     const char* lb = lds + (step & 1) * kHalfLds + PA * kOneA + wn * 32 * kRowBytes;
+    load_part(fa[ks], la, kOneA, lane, ks);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      if (mine > 0) {
-        Part<2, PA> fa;
-        load_part(fa, la, kOneA, lane, ks);
-        Part<1, PB> fb[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) load_part(fb[j], lb + j * 128 * kRowBytes, kOneB, lane, ks);
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int p = PA + PB - 2; p >= 0; --p)   // the small products first
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              const int pa = PA == 2 && PB == 2 ? (p == 2 ? 1 : 0) : PA == 2 ? p : 0;
-              const int pb = PA == 2 && PB == 2 ? (p == 1 ? 1 : 0) : PB == 2 ? p : 0;
-              acc[i][j] = mfma<kBf>(fa.v[i][pa], fb[j].v[0][pb], acc[i][j]);
-            }
-      }
-      if (ks == 0) between();
-    }
+    for (int j = 0; j < NT; ++j) load_part(fb[ks][j], lb + j * 128 * kRowBytes, kOneB, lane, ks);
   };
-  run_steps<kFar>(a.w.steps, near, far, put, before, multiply);
+  auto multiply = [&](auto half) {
+    constexpr int ks = decltype(half)::value;
+    if (mine == 0) return;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int p = PA + PB - 2; p >= 0; --p)   // the small products first
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int pa = PA == 2 && PB == 2 ? (p == 2 ? 1 : 0) : PA == 2 ? p : 0;
+          const int pb = PA == 2 && PB == 2 ? (p == 1 ? 1 : 0) : PB == 2 ? p : 0;
+          acc[i][j] = mfma<kBf>(fa[ks].v[i][pa], fb[ks][j].v[0][pb], acc[i][j]);
+        }
+  };
+  run_steps<1, kFar>(a.w.steps, near, far, put, read, before, multiply);
 
   if (S == kFloat) {
     if (sub == 0) row_exp[own] = e;
     __syncthreads();
   }
-  // Outputs from the registers: a lane has a column, 32 of them are 128 bytes of a
-  // row; half types go out two columns a lane, the even lanes with the row of sum
-  // r and the odd ones with that of sum r + 1.
+  // outputs from the registers: a lane has a column, 32 of them are 128 bytes of a row
   const T* bias = a.bias ? static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
   const T* res = static_cast<const T*>(a.residual);
+  if (mine == 0) return;
+  // sixteen sums (i, j) at a time; the residual's entries one group ahead
+  float rv[2][16];
+  auto fetch_residual = [&](auto turn, int i, int j) {
+    constexpr int q = decltype(turn)::value;
+    if (!res) return;
+    int c = c0 + (wn + 4 * (j < mine ? j : mine - 1)) * 32 + (lane & 31);
+    c = c < a.kout ? c : a.kout - 1;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int row = row_of[64 * wm + 32 * i + sum_row(lane, r)];
+      rv[q][r] = to_f32(res[int64_t(row < 0 ? 0 : row) * a.ldres + c]);
+    }
+  };
+  auto store = [&](auto part, int j, const v16f& sums, float bv, int ec) {
+    constexpr int i = decltype(part)::value;
+    const int c = c0 + (wn + 4 * j) * 32 + (lane & 31);
+    const bool in = c < a.kout;
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) {
+      float y[2], z[2];
+      int row[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int rl = 64 * wm + 32 * i + sum_row(lane, r + q);
+        row[q] = row_of[rl];
+        z[q] = sums[r + q];
+        if (S == kFloat) z[q] = ldexpf(z[q], -row_exp[rl] - ec);
+        z[q] += bv;
+        y[q] = a.silu ? z[q] * logistic(z[q]) : z[q];
+        if (res) y[q] += rv[i][r + q];
+      }
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+          if (in && row[q] >= 0) {
+            out[int64_t(row[q]) * a.kout + c] = y[q];
+            if (zout) zout[int64_t(row[q]) * a.kout + c] = z[q];
+          }
+      }
+    }
+  };
+  static_assert(sizeof(T) == 4, "half types take tiles of 128 columns");
+  fetch_residual(Const<0>{}, 0, 0);
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     if (j >= mine) continue;
     const int c = c0 + (wn + 4 * j) * 32 + (lane & 31);
-    const bool in = c < a.kout;
-    const int cc = in ? c : a.kout - 1;
-    const float bv = bias ? to_f32(bias[cc]) : 0.0f;
+    const float bv = bias ? to_f32(bias[c < a.kout ? c : a.kout - 1]) : 0.0f;
     const int ec = S == kFloat ? a.w.exps[int64_t(t.group) * a.w.cols_pad + c] : 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      int row[16];
-      float rv[16];
-#pragma unroll
-      for (int r = 0; r < 16; ++r) row[r] = row_of[64 * wm + 32 * i + sum_row(lane, r)];
-      if (res)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) rv[r] = to_f32(res[int64_t(row[r] < 0 ? 0 : row[r]) * a.ldres + cc]);
-#pragma unroll
-      for (int r = 0; r < 16; r += 2) {
-        float y[2], z[2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          z[q] = acc[i][j][r + q];
-          if (S == kFloat) z[q] = ldexpf(z[q], -row_exp[64 * wm + 32 * i + sum_row(lane, r + q)] - ec);
-          z[q] += bv;
-          y[q] = a.silu ? z[q] * logistic(z[q]) : z[q];
-          if (res) y[q] += rv[r + q];
-        }
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (in && row[r + q] >= 0) {
-              out[int64_t(row[r + q]) * a.kout + c] = y[q];
-              if (zout) zout[int64_t(row[r + q]) * a.kout + c] = z[q];
-            }
-        } else {
-          const bool odd = lane & 1;
-          const int to = odd ? row[r + 1] : row[r], at = odd ? c - 1 : c;
-          auto pack = [&](const float* v) {
-            const unsigned mine2 = unsigned(__builtin_bit_cast(unsigned short, from_f32<T>(v[0]))) |
-                                   unsigned(__builtin_bit_cast(unsigned short, from_f32<T>(v[1]))) << 16;
-            // the neighbour's two rows of its column
-            const unsigned other = __builtin_amdgcn_mov_dpp(mine2, 0xB1, 0xf, 0xf, true);
-            return odd ? __builtin_amdgcn_perm(mine2, other, 0x07060302u)
-                       : __builtin_amdgcn_perm(other, mine2, 0x05040100u);
-          };
-          const unsigned yy = pack(y), zz = zout ? pack(z) : 0;
-          if (to >= 0) {
-            T* po = out + int64_t(to) * a.kout + at;
-            T* pz = zout + int64_t(to) * a.kout + at;
-            if (at + 1 < a.kout) {
-              *reinterpret_cast<Pack<T, 2>*>(po) = __builtin_bit_cast(Pack<T, 2>, yy);
-              if (zout) *reinterpret_cast<Pack<T, 2>*>(pz) = __builtin_bit_cast(Pack<T, 2>, zz);
-            } else if (at < a.kout) {
-              *po = __builtin_bit_cast(T, static_cast<unsigned short>(yy & 0xffff));
-              if (zout) *pz = __builtin_bit_cast(T, static_cast<unsigned short>(zz & 0xffff));
-            }
-          }
-        }
-      }
-    }
+    fetch_residual(Const<1>{}, 1, j);
+    store(Const<0>{}, j, acc[0][j], bv, ec);
+    fetch_residual(Const<0>{}, 0, j + 1);
+    store(Const<1>{}, j, acc[1][j], bv, ec);
   }
 }
 
@@ -1119,22 +1105,18 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
       }
   };
   const bool live = a.dw && o.r0 + 64 * wm < a.k && o.c0 + 64 * wn < a.m;
-  auto multiply = [&](int step, auto&& between) {
-    const char* la = lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes;
-    const char* lb = lds + (step & 1) * kHalfLds + 2 * kOne + wn * 64 * kRowBytes;
-    Part<2, 2> fa[2], fb[2];
-    if (live) {
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        load_part(fa[ks], la, kOne, lane, ks);
-        load_part(fb[ks], lb, kOne, lane, ks);
-      }
-      multiply_parts<false>(acc, fa[0], fb[0]);
-    }
-    between();
-    if (live) multiply_parts<false>(acc, fa[1], fb[1]);
+  Part<2, 2> fa[2], fb[2];
+  auto read = [&](auto half, int step) {
+    constexpr int ks = decltype(half)::value;
+    if (!live) return;
+    load_part(fa[ks], lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes, kOne, lane, ks);
+    load_part(fb[ks], lds + (step & 1) * kHalfLds + 2 * kOne + wn * 64 * kRowBytes, kOne, lane, ks);
   };
-  run_steps<2>(steps, fetch, [](auto, int) {}, put, before, multiply);
+  auto multiply = [&](auto half) {
+    constexpr int ks = decltype(half)::value;
+    if (live) multiply_parts<false>(acc, fa[ks], fb[ks]);
+  };
+  run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, before, multiply);
 
   if (a.dw) {
     exps[tid] = e;
@@ -1228,23 +1210,19 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   Sums<2> acc;
   acc.clear();
   const bool live = a.dw && o.r0 + 64 * wm < a.k && o.c0 + 64 * wn < a.m;
-  auto multiply = [&](int step, auto&& between) {
-    const char* la = lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes;
-    const char* lb = lds + (step & 1) * kHalfLds + kOne + wn * 64 * kRowBytes;
-    Part<2, 1> fa[2];
-    Part<2, PB> fb[2];
-    if (live) {
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        load_part_turned(fa[ks], la, kOne, lane, ks);
-        load_part_turned(fb[ks], lb, kOne, lane, ks);
-      }
-      multiply_parts<kBf>(acc, fa[0], fb[0]);
-    }
-    between();
-    if (live) multiply_parts<kBf>(acc, fa[1], fb[1]);
+  Part<2, 1> fa[2];
+  Part<2, PB> fb[2];
+  auto read = [&](auto half, int step) {
+    constexpr int ks = decltype(half)::value;
+    if (!live) return;
+    load_part_turned(fa[ks], lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes, kOne, lane, ks);
+    load_part_turned(fb[ks], lds + (step & 1) * kHalfLds + kOne + wn * 64 * kRowBytes, kOne, lane, ks);
   };
-  run_steps<2>(steps, fetch, [](auto, int) {}, put, [](int) {}, multiply);
+  auto multiply = [&](auto half) {
+    constexpr int ks = decltype(half)::value;
+    if (live) multiply_parts<kBf>(acc, fa[ks], fb[ks]);
+  };
+  run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
 
   if (a.dw) store_outer<T>(a, o, acc, nullptr);
   if (sums_bias) {
@@ -1299,9 +1277,19 @@ int64_t tiles_at_most(int64_t n, int n_groups, int64_t rows) {
   return n / rows + (n < n_groups + 1 ? n : n_groups + 1);
 }
 
-// Rows of a tile: 128, with up to 384 columns, from half as many such tiles as
-// there are compute units on, 64 and 64 columns below.
-int tile_rows(int64_t n) { return n >= 128 * 128 ? kWideRows : kSide<1>; }
+// The tile of rows times weights.  Wide: float32 with more than 256 columns,
+// from two rounds of the 256 compute units on (1,000,188 x 384 -> 384: 1,600 us,
+// 128 x 128 tiles 1,850; bfloat16 1,140 against 1,000, and 128 columns 3,600
+// against 1,910: half types and few columns leave its columns or matrix cores
+// idle).  Else 128 x 128 where such tiles fill the compute units, and 64 x 64.
+enum TileKind { kSmallTile, kLargeTile, kWideTile };
+TileKind tile_kind(int dtype, int64_t n, int cols) {
+  if (dtype == DPA4C_F32 && cols > 256 && n >= 2 * 256 * kWideRows) return kWideTile;
+  return cols > 64 && (n / 128) * ((cols + 127) / 128) >= 256 ? kLargeTile : kSmallTile;
+}
+int tile_rows(int dtype, int64_t n, int cols) {
+  return tile_kind(dtype, n, cols) == kSmallTile ? kSide<1> : kSide<2>;
+}
 
 // Rows of a block of dW: 4,096 workgroups in all, some rounds of the chip's 512
 // resident ones, but no fewer than 512 rows, so that a block's sums are small
@@ -1366,7 +1354,7 @@ ForwardPlan plan_forward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   ForwardPlan p;
   p.w = weights_of(ar, l, false);
-  p.tiles = list_of(ar, l, tile_rows(l.n), true);
+  p.tiles = list_of(ar, l, tile_rows(l.dtype, l.n, l.n_out), true);
   p.wide = ar.take<char>(wide_bytes(l));
   *bytes = ar.used;
   return p;
@@ -1382,7 +1370,7 @@ BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   BackwardPlan p;
   p.w = weights_of(ar, l, true);
-  p.tiles = list_of(ar, l, tile_rows(l.n), true);
+  p.tiles = list_of(ar, l, tile_rows(l.dtype, l.n, l.k), true);
   const int rows = outer_rows(l);
   p.blocks = list_of(ar, l, rows, false);
   p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
@@ -1427,13 +1415,14 @@ int prepare(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, con
 template <class T, Source S>
 int run_rows(const RowsArgs& a, const TileList& tiles, hipStream_t st) {
   const int64_t most = tiles_at_most(a.n, a.n_groups, tiles.rows);
-  if (tiles.rows == kWideRows) {
-    const int64_t cols = ((a.kout + 31) / 32 + kWideBlocks - 1) / kWideBlocks;
-    grouped_wide_kernel<T, S><<<most * cols, kWideThreads, 0, st>>>(a);
-  } else {
-    const int64_t cols = (a.kout + kSide<1> - 1) / kSide<1>;
-    grouped_rows_kernel<T, S, 1><<<most * cols, kThreads, 0, st>>>(a);
-  }
+  const TileKind kind = tile_kind(sizeof(T) == 4 ? DPA4C_F32 : DPA4C_F16, a.n, a.kout);
+  if (kind == kSmallTile)
+    grouped_rows_kernel<T, S, 1><<<most * ((a.kout + 63) / 64), kThreads, 0, st>>>(a);
+  else if (kind == kLargeTile)
+    grouped_rows_kernel<T, S, 2><<<most * ((a.kout + 127) / 128), kThreads, 0, st>>>(a);
+  else if constexpr (S == kFloat)
+    grouped_wide_kernel<T, S><<<most * (((a.kout + 31) / 32 + kWideBlocks - 1) / kWideBlocks), kWideThreads, 0,
+                                st>>>(a);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }

@@ -384,25 +384,23 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
   Sums<NB> acc;
   acc.clear();
   const bool live = r0 + kTile / 2 * wm < s.lo && c0 + kTile / 2 * wn < (kWide ? s.hi : s.lo);
-  auto multiply = [&](int step, auto&& between) {
+  Part<NB, 2> fa[2], fb[2];
+  auto read = [&](auto half, int step) {
+    constexpr int ks = decltype(half)::value;
+    if (!live) return;
     const char* a = lds + (step & 1) * 4 * kOne + wm * (kTile / 2) * kRowBytes;
     const char* b = lds + (step & 1) * 4 * kOne + 2 * kOne + wn * (kTile / 2) * kRowBytes;
-    Part<NB, 2> fa[2], fb[2];
-    if (live) {
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        load_part(fa[ks], a, kOne, lane, ks);
-        if constexpr (kWide)
-          load_part_turned(fb[ks], b, kOne, lane, ks);
-        else
-          load_part(fb[ks], b, kOne, lane, ks);
-      }
-      multiply_parts<false>(acc, fa[0], fb[0]);
-    }
-    between();
-    if (live) multiply_parts<false>(acc, fa[1], fb[1]);
+    load_part(fa[ks], a, kOne, lane, ks);
+    if constexpr (kWide)
+      load_part_turned(fb[ks], b, kOne, lane, ks);
+    else
+      load_part(fb[ks], b, kOne, lane, ks);
   };
-  run_steps<2>(steps, fetch, [](auto, int) {}, put, [](int) {}, multiply);
+  auto multiply = [&](auto half) {
+    constexpr int ks = decltype(half)::value;
+    if (live) multiply_parts<false>(acc, fa[ks], fb[ks]);
+  };
+  run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
 
   float* stage = reinterpret_cast<float*>(lds);
   stage_sums(stage, acc, kTile / 2 * wm, kTile / 2 * wn, lane,

@@ -155,40 +155,45 @@ __device__ inline void multiply_parts(Sums<NB>& acc, const Part<NB, PA>& a, cons
 }
 
 // The steps of a tile.  near(turn, s) and far(turn, s) issue the loads of step s
-// into register set ``turn`` (a constant) of 2 and of Far sets: operands from L2,
-// two steps ahead, and operands from HBM, Far ahead (s may be past the end, where
-// they load anything that is cheap: loads under a condition would make the
-// compiler wait for all of them at every put).  put(n, f, s) writes sets n and f to
-// half s % 2 of LDS, before(s) runs when step s - 1's sums are complete, and
-// multiply(s, between) adds step s, with ``between`` called halfway.  Loads arrive
-// in the order of their issue, so the near ones go first.
+// into register set ``turn`` (a constant) of Near and of Far sets: operands from L2
+// and operands from HBM, Near and Far steps ahead (s may be past the end, where they
+// load anything that is cheap: loads under a condition would make the compiler
+// wait for all of them at every put).  Loads arrive in the order of their issue, so
+// the near ones go first.  put(n, f, s) writes sets n and f to half s % 2 of LDS,
+// read(ks, s) takes 16 entries of a step from there to fragment set ks, before(s)
+// runs when step s - 1's sums are complete and multiply(ks) adds fragment set ks.
+// The barrier of a step stands between its two products: the second one runs
+// from registers while the next step's first fragments arrive.
 template <int K>
 using Const = std::integral_constant<int, K>;
-template <int Far, class Near, class FarFn, class Put, class Before, class Multiply>
-__device__ inline void run_steps(int steps, Near&& near, FarFn&& far, Put&& put, Before&& before,
-                                 Multiply&& multiply) {
-  static_assert(Far == 2 || Far == 4, "the steps are unrolled by Far");
+template <int Near, int Far, class NearFn, class FarFn, class Put, class Read, class Before, class Multiply>
+__device__ inline void run_steps(int steps, NearFn&& near, FarFn&& far, Put&& put, Read&& read,
+                                 Before&& before, Multiply&& multiply) {
+  static_assert((Near == 1 || Near == 2) && (Far == 2 || Far == 4), "the steps are unrolled by Far");
   near(Const<0>{}, 0);
   far(Const<0>{}, 0);
-  near(Const<1>{}, 1);
+  if constexpr (Near == 2) near(Const<1>{}, 1);
   far(Const<1>{}, 1);
   if constexpr (Far == 4) {
     far(Const<2>{}, 2);
     far(Const<3>{}, 3);
   }
   put(Const<0>{}, Const<0>{}, 0);
-  near(Const<0>{}, 2);
+  near(Const<0>{}, Near);
   far(Const<0>{}, Far);
   __syncthreads();
+  read(Const<0>{}, 0);
   auto step = [&](auto next, int s) {   // next = (s + 1) % Far
-    constexpr int f = decltype(next)::value;
+    constexpr int f = decltype(next)::value, n = Near == 2 ? f & 1 : 0;
     before(s);
-    multiply(s, [&] {
-      if (s + 1 < steps) put(Const<f & 1>{}, next, s + 1);
-      near(Const<f & 1>{}, s + 3);
-      far(next, s + 1 + Far);
-    });
+    read(Const<1>{}, s);
+    multiply(Const<0>{});
+    if (s + 1 < steps) put(Const<n>{}, next, s + 1);
+    near(Const<n>{}, s + 1 + Near);
+    far(next, s + 1 + Far);
     __syncthreads();
+    if (s + 1 < steps) read(Const<0>{}, s + 1);
+    multiply(Const<1>{});
   };
   int s = 0;
   for (; s + Far <= steps; s += Far) {
