@@ -134,14 +134,23 @@ struct PrepArgs {
   int depth, cols;   // entries of a column and columns; W is [depth][cols], or [cols][depth]
   Weights out;
   TileList tiles, blocks;   // the row tiles; the row blocks of dW (list = null: none)
-  int list_blocks;          // workgroups that list tiles, after those of the weights
+  // gradients: zeros for the groups without rows (null: not formed), and dz
+  void *dw, *db;
+  const int32_t* order;
+  const void *dy, *z;       // dy = null: dz is not formed
+  int64_t ldy, ldz;
+  int pitch;
+  void* dz;
+  // the workgroups of each kind, in this order
+  int64_t list_blocks, weight_blocks, clear_blocks, dz_blocks;
 };
 
-// 32 columns of one group's weights by a workgroup of 512 threads.  The entries
-// of the columns are read along the rows of W: 32 columns of one entry, or (Back,
-// a column is a row of W) 64 entries of one column a wave.  float32 columns
-// are read twice, for the largest entry and for the planes (from L2).
-constexpr int kPrepThreads = 512, kPrepCols = 32;
+// 32 columns of one group's weights by a workgroup of 512 threads, which holds them
+// in registers between finding the largest entry and writing the planes (columns
+// of more than kHeld x 128 entries are read twice, from L2).  The entries are
+// read along the rows of W: 32 columns of one entry, or (Back, a column is a row of
+// W) eight entries a lane.
+constexpr int kPrepThreads = 512, kPrepCols = 32, kHeld = 6;
 
 template <class T, bool Back>
 __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
@@ -151,39 +160,23 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
   constexpr bool kSplit = sizeof(T) == 4;
   __shared__ float most[kPrepThreads / kPrepCols][kPrepCols];
   __shared__ int32_t exps[kPrepCols];
-  auto at = [&](int c, int k) {
-    return to_f32(Back ? w[int64_t(c) * a.depth + k] : w[int64_t(k) * a.cols + c]);
-  };
-  if (kSplit) {
-    // column c0 + r, entries q, q + 16, ..; Back: eight neighbours q a lane
-    const int r = Back ? threadIdx.x / 16 : threadIdx.x % kPrepCols;
-    const int q = Back ? threadIdx.x % 16 : threadIdx.x / kPrepCols;
-    float m = 0.0f;
-    if (c0 + r < a.cols) {
-#pragma unroll 8
-      for (int k = q; k < a.depth; k += 16) m = fmaxf(m, fabsf(at(c0 + r, k)));
-    }
-    most[q][r] = m;
-    __syncthreads();
-    if (threadIdx.x < kPrepCols) {
-      for (int i = 0; i < 16; ++i) m = i ? fmaxf(m, most[i][threadIdx.x]) : most[0][threadIdx.x];
-      const int e = m > 0.0f ? exp_for(m) : 0;
-      exps[threadIdx.x] = e;
-      a.out.exps[int64_t(g) * a.out.cols_pad + c0 + threadIdx.x] = e;
-    }
-    __syncthreads();
-  }
-  // slots (column, 8 entries)
+  // slots (column c0 + r, entries 8 sl ..), sl = first, first + 16, ..
   constexpr int kSlots = kDepth / 8;
   const int r = Back ? threadIdx.x / 16 : threadIdx.x % kPrepCols;
   const int first = Back ? threadIdx.x % 16 : threadIdx.x / kPrepCols;
-  const int c = c0 + r;
-  const float scale = kSplit ? exp2_of(exps[r]) : 1.0f;
-#pragma unroll 2
-  for (int sl = first; sl < a.out.steps * kSlots; sl += 16) {
-    float f[8];
+  const int c = c0 + r, slots = a.out.steps * kSlots;
+  auto load = [&](int sl, T* f) {
+    const int k = sl * 8;
+    if (Back && c < a.cols && k + 8 <= a.depth) {
+      *reinterpret_cast<Pack<T, 8>*>(f) = *reinterpret_cast<const Pack<T, 8>*>(w + int64_t(c) * a.depth + k);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = c < a.cols && sl * 8 + j < a.depth ? at(c, sl * 8 + j) : 0.0f;
+      for (int j = 0; j < 8; ++j)
+        f[j] = c < a.cols && k + j < a.depth ? w[Back ? int64_t(c) * a.depth + k + j : int64_t(k + j) * a.cols + c]
+                                             : from_f32<T>(0.0f);
+    }
+  };
+  auto write = [&](int sl, const T* f, float scale) {
     u4 hi, lo;
     if constexpr (kSplit) {
 #pragma unroll
@@ -195,32 +188,84 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const T x = from_f32<T>(f[2 * j]), y = from_f32<T>(f[2 * j + 1]);
-        hi[j] = unsigned(__builtin_bit_cast(unsigned short, x)) |
-                unsigned(__builtin_bit_cast(unsigned short, y)) << 16;
-      }
+      for (int j = 0; j < 4; ++j)
+        hi[j] = unsigned(__builtin_bit_cast(unsigned short, f[2 * j])) |
+                unsigned(__builtin_bit_cast(unsigned short, f[2 * j + 1])) << 16;
     }
     char* to = a.out.planes + (int64_t(g) * a.out.steps + sl / kSlots) * a.out.step_bytes() +
                slot_at(c, sl % kSlots);
     *reinterpret_cast<u4*>(to) = hi;
     if (kSplit) *reinterpret_cast<u4*>(to + int64_t(a.out.cols_pad) * kRowBytes) = lo;
+  };
+  const bool held = slots <= kHeld * 16;
+  T f[kHeld][8];
+  if (held) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (first + 16 * i < slots) load(first + 16 * i, f[i]);
+  }
+  float scale = 1.0f;
+  if constexpr (kSplit) {
+    float m = 0.0f;
+    if (held) {
+#pragma unroll
+      for (int i = 0; i < kHeld; ++i)
+        if (first + 16 * i < slots)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[i][j]));
+    } else {
+      for (int sl = first; sl < slots; sl += 16) {
+        load(sl, f[0]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, fabsf(f[0][j]));
+      }
+    }
+    most[first][r] = m;
+    __syncthreads();
+    if (threadIdx.x < kPrepCols) {
+      float top = 0.0f;
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, most[i][threadIdx.x]);
+      const int e = top > 0.0f ? exp_for(top) : 0;
+      exps[threadIdx.x] = e;
+      a.out.exps[int64_t(g) * a.out.cols_pad + c0 + threadIdx.x] = e;
+    }
+    __syncthreads();
+    scale = exp2_of(exps[r]);
+  }
+  if (held) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (first + 16 * i < slots) write(first + 16 * i, f[i], scale);
+  } else {
+    for (int sl = first; sl < slots; sl += 16) {
+      load(sl, f[0]);
+      write(sl, f[0], scale);
+    }
   }
 }
 
-template <class T, bool Back>
-__global__ void __launch_bounds__(kPrepThreads) grouped_prepare_kernel(PrepArgs a) {
-  extern __shared__ int32_t starts[];
-  // the lists first: the other workgroups' work hides theirs
-  if (blockIdx.x < unsigned(a.list_blocks)) {
-    if (a.tiles.list) list_tiles(a.tiles, a.ptr, a.n_groups, a.n, blockIdx.x, a.list_blocks, starts);
-    __syncthreads();
-    if (a.blocks.list) list_tiles(a.blocks, a.ptr, a.n_groups, a.n, blockIdx.x, a.list_blocks, starts);
-    return;
+// a part of the zeros of one group without rows
+constexpr int64_t kClear = 1 << 16;   // entries of a workgroup
+template <class T>
+__device__ inline void clear_gradients(const PrepArgs& a, int g, int64_t part) {
+  const Span s = span_of(a.ptr, g, a.n_groups, a.n);
+  if (s.begin != s.end) return;
+  constexpr int kEach = 16 / sizeof(T);
+  const Pack<T, kEach> none = {};
+  const int64_t each = int64_t(a.depth) * a.cols;   // k n_out either way
+  if (a.dw) {
+    T* out = static_cast<T*>(a.dw) + g * each;
+    const int64_t end = (part + 1) * kClear < each ? (part + 1) * kClear : each;
+    for (int64_t i = part * kClear + threadIdx.x * kEach; i < end; i += kPrepThreads * kEach) {
+      if (i + kEach <= end)
+        *reinterpret_cast<Pack<T, kEach>*>(out + i) = none;
+      else
+        for (int64_t j = i; j < end; ++j) out[j] = none.v[0];
+    }
   }
-  const int col_blocks = a.out.cols_pad / kPrepCols;
-  const int64_t b = int64_t(blockIdx.x) - a.list_blocks;
-  lay_weights<T, Back>(a, static_cast<int>(b / col_blocks), static_cast<int>(b % col_blocks) * kPrepCols);
+  if (a.db && part == 0)
+    for (int i = threadIdx.x; i < a.depth; i += kPrepThreads)
+      static_cast<T*>(a.db)[int64_t(g) * a.depth + i] = none.v[0];   // Back: depth = n_out
 }
 
 // Rows of fewer than eight entries, eight entries apart, so that loads of eight
@@ -240,18 +285,19 @@ __global__ void __launch_bounds__(kThreads) grouped_widen_kernel(int64_t n, int 
 // rounded to its 8 or 11 bits it would add as much error to dx and dW as their own
 // rounding does)
 template <class T>
-__global__ void __launch_bounds__(kThreads) grouped_dz_kernel(
-    const int64_t* __restrict__ ptr, const int32_t* __restrict__ order, int n_groups, int64_t n,
-    int cols, int pitch, const T* __restrict__ dy, int64_t ldy, const T* __restrict__ z, int64_t ldz,
-    T* __restrict__ dz) {
+__device__ inline void form_dz(const PrepArgs& p, int64_t block, int64_t blocks) {
   constexpr int kEach = 16 / sizeof(T);
-  const int64_t live = clamp_place(ptr[n_groups], n);
+  const int64_t n = p.n, ldy = p.ldy, ldz = p.ldz;
+  const int cols = p.depth, pitch = p.pitch;   // Back: depth = n_out
+  const T* dy = static_cast<const T*>(p.dy);
+  const T* z = static_cast<const T*>(p.z);
+  T* dz = static_cast<T*>(p.dz);
+  const int64_t live = clamp_place(p.ptr[p.n_groups], n);
   const int each = pitch / kEach;
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < live * each;
-       i += int64_t(gridDim.x) * kThreads) {
+  for (int64_t i = block * kPrepThreads + threadIdx.x; i < live * each; i += blocks * kPrepThreads) {
     const int64_t place = i / each;
     const int c = static_cast<int>(i - place * each) * kEach;
-    const int64_t row = row_at(order, place, n);
+    const int64_t row = row_at(p.order, place, n);
     Pack<T, kEach> a = {}, b = {}, hi, lo;
     if (row >= 0) {
       if (c + kEach <= cols) {
@@ -278,6 +324,35 @@ __global__ void __launch_bounds__(kThreads) grouped_dz_kernel(
     typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
     *reinterpret_cast<V*>(dz + place * pitch + c) = __builtin_bit_cast(V, hi);
     if (sizeof(T) == 2) *reinterpret_cast<V*>(dz + (n + place) * pitch + c) = __builtin_bit_cast(V, lo);
+  }
+}
+
+// What the products of a call need first, each piece by workgroups of its own.
+template <class T, bool Back>
+__global__ void __launch_bounds__(kPrepThreads) grouped_prepare_kernel(PrepArgs a) {
+  extern __shared__ int32_t starts[];
+  int64_t b = blockIdx.x;
+  if (b < a.list_blocks) {
+    const int block = static_cast<int>(b), blocks = static_cast<int>(a.list_blocks);
+    if (a.tiles.list) list_tiles(a.tiles, a.ptr, a.n_groups, a.n, block, blocks, starts);
+    __syncthreads();
+    if (a.blocks.list) list_tiles(a.blocks, a.ptr, a.n_groups, a.n, block, blocks, starts);
+    return;
+  }
+  b -= a.list_blocks;
+  if (b < a.weight_blocks) {
+    const int64_t each = a.weight_blocks / a.n_groups;
+    lay_weights<T, Back>(a, static_cast<int>(b / each), static_cast<int>(b % each) * kPrepCols);
+    return;
+  }
+  if constexpr (Back) {
+    b -= a.weight_blocks;
+    if (b < a.clear_blocks) {
+      const int64_t each = a.clear_blocks / a.n_groups;
+      clear_gradients<T>(a, static_cast<int>(b / each), b % each);
+      return;
+    }
+    form_dz<T>(a, b - a.clear_blocks, a.dz_blocks);
   }
 }
 
@@ -1237,8 +1312,8 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   }
 }
 
-// The blocks of a group added up in their order, dW then db (null: not formed);
-// zeros for groups without rows.
+// The blocks of the groups that have several, added up in their order: dW, then db
+// (null: not formed).
 template <class T>
 __global__ void __launch_bounds__(kThreads) grouped_join_kernel(const int32_t* __restrict__ first_of,
                                                                 int64_t each_w, int64_t each_b,
@@ -1247,7 +1322,7 @@ __global__ void __launch_bounds__(kThreads) grouped_join_kernel(const int32_t* _
                                                                 T* __restrict__ dw, T* __restrict__ db) {
   const int g = blockIdx.y;
   const int first = first_of[g], count = first_of[g + 1] - first;
-  if (count == 1) return;
+  if (count < 2) return;
   int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
   const int64_t of_w = dw ? each_w : 0;
   const bool w = i < of_w;
@@ -1382,20 +1457,20 @@ BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   return p;
 }
 
-template <class T, bool Back>
-int prepare(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, const TileList* blocks,
-            hipStream_t st) {
+// the arguments of the preparing launch: the lists and, with ``w``, the weights
+template <bool Back>
+PrepArgs prepare_args(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, const TileList* blocks) {
   PrepArgs a{};
   a.ptr = l.group_ptr;
   a.n_groups = l.n_groups;
   a.n = l.n;
   a.depth = Back ? l.n_out : l.k;
   a.cols = Back ? l.k : l.n_out;
-  int64_t grid = 0, list = 0;
+  int64_t list = 0;
   if (w) {
     a.w = l.weight;
     a.out = *w;
-    grid = int64_t(l.n_groups) * (w->cols_pad / kPrepCols);
+    a.weight_blocks = int64_t(l.n_groups) * (w->cols_pad / kPrepCols);
   }
   if (tiles) {
     a.tiles = *tiles;
@@ -1405,9 +1480,14 @@ int prepare(const dpa4c_grouped& l, const Weights* w, const TileList* tiles, con
     a.blocks = *blocks;
     list = std::max(list, tiles_at_most(l.n, l.n_groups, blocks->rows));
   }
-  a.list_blocks = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(64, list / kPrepThreads)));
+  a.list_blocks = std::max<int64_t>(1, std::min<int64_t>(64, list / kPrepThreads));
+  return a;
+}
+template <class T, bool Back>
+int prepare(const PrepArgs& a, hipStream_t st) {
+  const int64_t grid = a.list_blocks + a.weight_blocks + a.clear_blocks + a.dz_blocks;
   grouped_prepare_kernel<T, Back>
-      <<<grid + a.list_blocks, kPrepThreads, (l.n_groups + 2) * sizeof(int32_t), st>>>(a);
+      <<<grid, kPrepThreads, (a.n_groups + 2) * sizeof(int32_t), st>>>(a);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }
@@ -1470,7 +1550,7 @@ int launch_grouped_forward(const dpa4c_grouped& l, const void* bias, bool silu, 
     using T = typename Elem<decltype(d)::value>::T;
     int64_t bytes;
     const ForwardPlan p = plan_forward(l, work, &bytes);
-    DPA4C_TRY((prepare<T, false>(l, &p.w, &p.tiles, nullptr, st)));
+    DPA4C_TRY((prepare<T, false>(prepare_args<false>(l, &p.w, &p.tiles, nullptr), st)));
     Input in;
     DPA4C_TRY(widen<T>(l, p.wide, &in, st));
     RowsArgs a{};
@@ -1504,18 +1584,28 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
     constexpr Source kOwn = sizeof(T) == 4 ? kFloat : kHalf, kMade = sizeof(T) == 4 ? kFloat : kPair;
     int64_t bytes;
     const BackwardPlan p = plan_backward(l, work, &bytes);
-    DPA4C_TRY((prepare<T, true>(l, rows ? &p.w : nullptr, rows ? &p.tiles : nullptr,
-                                outer ? &p.blocks : nullptr, st)));
     const int pitch = pitch_of(l);
-    const bool made = z || l.n_out < kLeastWidth;   // dz is formed, by place
-    if (made && l.n > 0) {
-      const int64_t each = l.n * (pitch * int64_t(sizeof(T)) / 16);
-      const int64_t grid = std::min<int64_t>((each + kThreads - 1) / kThreads, 8192);
-      grouped_dz_kernel<T><<<grid, kThreads, 0, st>>>(
-          l.group_ptr, l.order, l.n_groups, l.n, l.n_out, pitch, static_cast<const T*>(dy), ldy,
-          static_cast<const T*>(z), ldz, static_cast<T*>(p.dz));
-      DPA4C_HIP_TRY(hipGetLastError());
+    const bool made = l.n > 0 && (z || l.n_out < kLeastWidth);   // dz is formed, by place
+    PrepArgs pre = prepare_args<true>(l, rows ? &p.w : nullptr, rows ? &p.tiles : nullptr,
+                                      outer ? &p.blocks : nullptr);
+    if (outer) {
+      pre.dw = dw;
+      pre.db = db;
+      const int64_t each = dw ? int64_t(l.k) * l.n_out : 1;
+      pre.clear_blocks = int64_t(l.n_groups) * ((each + kClear - 1) / kClear);
     }
+    if (made) {
+      pre.order = l.order;
+      pre.dy = dy;
+      pre.ldy = ldy;
+      pre.z = z;
+      pre.ldz = ldz;
+      pre.pitch = pitch;
+      pre.dz = p.dz;
+      const int64_t each = l.n * (pitch * int64_t(sizeof(T)) / 16);
+      pre.dz_blocks = std::min<int64_t>((each + kPrepThreads - 1) / kPrepThreads, 4096);
+    }
+    DPA4C_TRY((prepare<T, true>(pre, st)));
     if (rows) {
       RowsArgs a{};
       a.order = l.order;
