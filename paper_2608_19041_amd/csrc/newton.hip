@@ -65,12 +65,10 @@ __host__ __device__ inline int64_t set_bytes(int steps, int rows_pad) {
   return int64_t(steps) * 2 * rows_pad * kRowBytes;
 }
 
-// U of the update: the gradient, or with momentum (already updated) its mix
-template <class T, bool Muon>
-__device__ inline float update_of(const Stack& s, int64_t at, float beta, int nesterov) {
-  const float g = to_f32(static_cast<const T*>(s.grad)[at]);
+// U of the update: the gradient, or with momentum m (already updated) its mix
+template <bool Muon>
+__device__ inline float update_of(float g, float m, float beta, int nesterov) {
   if constexpr (!Muon) return g;
-  const float m = s.momentum[at];
   return nesterov ? g + beta * m : m;
 }
 
@@ -86,31 +84,33 @@ __global__ void __launch_bounds__(kThreads) newton_norm_kernel(Stacks all, Share
   const int count = static_cast<int>(begin + kChunk < size ? kChunk : size - begin);
   const T* __restrict__ grad = static_cast<const T*>(s.grad) + base + begin;
   constexpr int kEach = kChunk / kThreads;
+  // past the chunk its last entry is read again, and counts as zero
+  T g[kEach];
   float u[kEach];
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) {
-    const int j = threadIdx.x + k * kThreads;
-    u[k] = j < count ? to_f32(grad[j]) : 0.0f;
-  }
+  for (int k = 0; k < kEach; ++k) g[k] = grad[min(int(threadIdx.x) + k * kThreads, count - 1)];
   if constexpr (Muon) {
     float* momentum = s.momentum + base + begin;
     float v[kEach];
 #pragma unroll
-    for (int k = 0; k < kEach; ++k) {
-      const int j = threadIdx.x + k * kThreads;
-      v[k] = j < count ? momentum[j] : 0.0f;
-    }
+    for (int k = 0; k < kEach; ++k) v[k] = momentum[min(int(threadIdx.x) + k * kThreads, count - 1)];
+    __syncthreads();   // read before the last entry is written
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       const int j = threadIdx.x + k * kThreads;
+      u[k] = to_f32(g[k]);
       v[k] = beta * v[k] + u[k];
       if (j < count) momentum[j] = v[k];
-      u[k] = nesterov ? u[k] + beta * v[k] : v[k];
+      u[k] = update_of<true>(u[k], v[k], beta, nesterov);
     }
+  } else {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) u[k] = to_f32(g[k]);
   }
   double sum = 0.0;
 #pragma unroll
-  for (int k = 0; k < kEach; ++k) sum += double(u[k]) * double(u[k]);
+  for (int k = 0; k < kEach; ++k)
+    sum += threadIdx.x + k * kThreads < unsigned(count) ? double(u[k]) * double(u[k]) : 0.0;
   __shared__ double part[kThreads];
   part[threadIdx.x] = sum;
   __syncthreads();
@@ -235,34 +235,35 @@ __device__ inline void write_result(const Stack& s, int64_t m, int r0, int c0, c
   constexpr int kEach = Rows * kSide<NB> / kThreads, kGo = 8;
 #pragma unroll 1
   for (int k0 = 0; k0 < kEach; k0 += kGo) {
-    float w[kGo];
+    // the weights of the place, or past the matrix of its last row or column
+    T w[kGo];
     int64_t at[kGo];
 #pragma unroll
     for (int k = 0; k < kGo; ++k) {
       const int i = threadIdx.x + (k0 + k) * kThreads;
-      const int r = s.turned ? i % Rows : i / kSide<NB>, c = s.turned ? i / Rows : i % kSide<NB>;
-      at[k] = r0 + r >= s.lo || c0 + c >= s.hi ? -1
-              : s.turned                       ? int64_t(c0 + c) * s.cols + r0 + r
-                                               : int64_t(r0 + r) * s.cols + c0 + c;
-      w[k] = Muon && at[k] >= 0 ? to_f32(out[at[k]]) : 0.0f;
+      const int r = min(r0 + (s.turned ? i % Rows : i / kSide<NB>), s.lo - 1);
+      const int c = min(c0 + (s.turned ? i / Rows : i % kSide<NB>), s.hi - 1);
+      at[k] = s.turned ? int64_t(c) * s.cols + r : int64_t(r) * s.cols + c;
+      if constexpr (Muon) w[k] = out[at[k]];
     }
 #pragma unroll
     for (int k = 0; k < kGo; ++k) {
       const int i = threadIdx.x + (k0 + k) * kThreads;
       const int r = s.turned ? i % Rows : i / kSide<NB>, c = s.turned ? i / Rows : i % kSide<NB>;
       const float o = stage[stage_at<NB>(r, c)];
-      if (at[k] >= 0) out[at[k]] = from_f32<T>(Muon ? f.keep * w[k] - step * o : o);
+      if (r0 + r < s.lo && c0 + c < s.hi)
+        out[at[k]] = from_f32<T>(Muon ? f.keep * to_f32(w[k]) - step * o : o);
     }
   }
 }
 
-constexpr int kStartRows = 64;
+constexpr int kStartRows = 64, kStartSide = 1;
 
-// X = U / (|U| + eps), 64 x 128 a workgroup
+// X = U / (|U| + eps), 64 x 64 a workgroup
 template <class T, bool Muon, bool Last>
 __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shares sh, float beta,
                                                                 int nesterov, float eps, Finish f) {
-  constexpr int kCols = kSide<2>;
+  constexpr int kCols = kSide<kStartSide>;
   __shared__ __attribute__((aligned(16))) float stage[kStartRows * kCols];
   __shared__ double norm;
   const int i = stack_of(sh, all.count, blockIdx.x);
@@ -273,16 +274,17 @@ __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shar
   const int r0 = static_cast<int>(item / tc % tr) * kStartRows, c0 = static_cast<int>(item % tc) * kCols;
   const int64_t base = m * s.rows * s.cols;
   constexpr int kEach = kStartRows * kCols / kThreads;
-  float u[kEach];
+  // past the matrix the last entry is read again: no load waits for another's value
+  T g[kEach];
+  float mom[kEach];
 #pragma unroll
   for (int k = 0; k < kEach; ++k) {
     const int j = threadIdx.x + k * kThreads;
-    const int r = s.turned ? j % kStartRows : j / kCols, c = s.turned ? j / kStartRows : j % kCols;
-    u[k] = 0.0f;
-    if (r0 + r < s.lo && c0 + c < s.hi)
-      u[k] = update_of<T, Muon>(
-          s, base + (s.turned ? int64_t(c0 + c) * s.cols + r0 + r : int64_t(r0 + r) * s.cols + c0 + c), beta,
-          nesterov);
+    const int r = min(r0 + (s.turned ? j % kStartRows : j / kCols), s.lo - 1);
+    const int c = min(c0 + (s.turned ? j / kStartRows : j % kCols), s.hi - 1);
+    const int64_t at = base + (s.turned ? int64_t(c) * s.cols + r : int64_t(r) * s.cols + c);
+    g[k] = static_cast<const T*>(s.grad)[at];
+    if constexpr (Muon) mom[k] = s.momentum[at];
   }
   if (threadIdx.x < kWave) {
     double sum = 0.0;
@@ -296,14 +298,15 @@ __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shar
   for (int k = 0; k < kEach; ++k) {
     const int j = threadIdx.x + k * kThreads;
     const int r = s.turned ? j % kStartRows : j / kCols, c = s.turned ? j / kStartRows : j % kCols;
+    const float u = update_of<Muon>(to_f32(g[k]), Muon ? mom[k] : 0.0f, beta, nesterov);
     // the padding stays zero also where the norm is not finite
-    stage[stage_at<2>(r, c)] = r0 + r < s.lo && c0 + c < s.hi ? static_cast<float>(u[k] * inv) : 0.0f;
+    stage[stage_at<kStartSide>(r, c)] = r0 + r < s.lo && c0 + c < s.hi ? static_cast<float>(u * inv) : 0.0f;
   }
   __syncthreads();
   if constexpr (Last)
-    write_result<T, Muon, 2, kStartRows>(s, m, r0, c0, stage, f);
+    write_result<T, Muon, kStartSide, kStartRows>(s, m, r0, c0, stage, f);
   else
-    write_rows<2, kStartRows>(s.x[0] + m * set_bytes(s.hi_steps, s.lo_pad), s.lo_pad, s.hi_steps, r0, c0,
+    write_rows<kStartSide, kStartRows>(s.x[0] + m * set_bytes(s.hi_steps, s.lo_pad), s.lo_pad, s.hi_steps, r0, c0,
                               stage, kScaleX);
 }
 
@@ -490,7 +493,7 @@ template <class T, bool Muon>
 int run(const Stacks& all, const dpa4c_newton& how, const MuonStep& mu, hipStream_t st) {
   const Shares norms = share(all, [](const Stack& s) { return int64_t(s.chunks); });
   const Shares starts = share(all, [](const Stack& s) {
-    return int64_t(s.lo_pad / kStartRows) * ((s.hi + kSide<2> - 1) / kSide<2>);
+    return int64_t(s.lo_pad / kStartRows) * ((s.hi + kSide<kStartSide> - 1) / kSide<kStartSide>);
   });
   const Shares squares[2] = {share_square(all, kSide<1>), share_square(all, kSide<2>)};
   const Shares wides[2] = {share_wide(all, kSide<1>), share_wide(all, kSide<2>)};

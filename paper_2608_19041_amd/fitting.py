@@ -13,8 +13,8 @@ caller's stream, and scratch comes from torch's allocator on that stream.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 import math
 
 from . import _check, _ptr, _require, library
@@ -49,12 +49,18 @@ class _Newton(ctypes.Structure):
                 ("c", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
+@functools.lru_cache(maxsize=None)
+def _codes():
+    import torch
+    return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
 def _dtype_code(t, name):
     import torch
-    codes = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in codes:
+    code = _codes().get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if code is None:
         raise ValueError(f"{name} must be a CUDA tensor of float32, float16 or bfloat16")
-    return codes[t.dtype]
+    return code
 
 
 def _rows(t, dtype, shape, device, name):
@@ -62,7 +68,7 @@ def _rows(t, dtype, shape, device, name):
     import torch
     if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be a tensor of {dtype} on {device}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have unit stride within a row")
@@ -73,22 +79,38 @@ def _rows(t, dtype, shape, device, name):
 
 
 def _same(t, dtype, shape, device, name):
-    _require(t, dtype, shape, name)
+    _require(t, dtype, None, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}")
 
 
-@contextlib.contextmanager
-def _launch(device, stream):
-    """The stream's handle, with ``device`` current and torch's allocator on that stream."""
-    import torch
-    if stream is None and device.index == torch.cuda.current_device():
-        yield ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
-        return
-    with torch.cuda.device(device):
-        stream = stream if stream is not None else torch.cuda.current_stream()
-        with torch.cuda.stream(stream):
-            yield ctypes.c_void_p(stream.cuda_stream)
+class _launch:
+    """The stream's handle, with ``device`` current and torch's allocator on that stream.
+
+    The common call, on the current device's current stream, only looks the handle up.
+    """
+
+    def __init__(self, device, stream):
+        import torch
+        self._guards = ()
+        if stream is None and device.index == torch.cuda.current_device():
+            self._handle = torch._C._cuda_getCurrentRawStream(device.index)
+            return
+        if stream is None:
+            stream = torch.cuda.current_stream(device)
+        self._guards = (torch.cuda.device(device), torch.cuda.stream(stream))
+        self._handle = stream.cuda_stream
+
+    def __enter__(self):
+        for guard in self._guards:
+            guard.__enter__()
+        return self._handle
+
+    def __exit__(self, *error):
+        for guard in reversed(self._guards):
+            guard.__exit__(*error)
 
 
 def _scratch(size_of, device):
@@ -208,18 +230,21 @@ def _stack_list(name, tensors):
             raise ValueError(f"{name} must be contiguous matrices or stacks of matrices")
         if t.dtype != tensors[0].dtype or t.device != tensors[0].device:
             raise ValueError(f"{name} must share one type and one device")
-        if t.shape[-1] < 1 or t.shape[-2] < 1:
+        shape = t.shape
+        if shape[-1] < 1 or shape[-2] < 1:
             raise ValueError(f"{name} must not have empty matrices")
     return tensors
+
+
+def _shape(t):
+    """batch, rows, cols of a matrix or a stack of them"""
+    *batch, rows, cols = t.shape
+    return math.prod(batch), rows, cols
 
 
 def _newton(steps, coefficients, eps):
     a, b, c = (float(v) for v in coefficients)
     return _Newton(int(steps), a, b, c, float(eps))
-
-
-def _batch(t):
-    return math.prod(t.shape[:-2])
 
 
 def orthogonalize(matrices, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps: float = 1e-7,
@@ -240,7 +265,7 @@ def orthogonalize(matrices, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps:
         for at in range(0, len(matrices), MAX_STACKS):
             part = matrices[at:at + MAX_STACKS]
             stacks = (_Stack * len(part))(*[
-                _Stack(t.data_ptr(), o.data_ptr(), _batch(t), t.shape[-2], t.shape[-1])
+                _Stack(t.data_ptr(), o.data_ptr(), *_shape(t))
                 for t, o in zip(part, out[at:at + MAX_STACKS])])
             work, size = _scratch(
                 lambda need: lib.dpa4c_orthogonalize_work(len(part), stacks, need), dev)
@@ -260,8 +285,7 @@ def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nestero
     ``momenta``: float32 tensors of the same shapes.
     """
     import torch
-    params, grads = _stack_list("params", params), _stack_list("grads", grads)
-    momenta = _stack_list("momenta", momenta)
+    params, grads, momenta = _stack_list("params", params), list(grads), list(momenta)
     if not len(params) == len(grads) == len(momenta):
         raise ValueError("params, grads and momenta must have the same length")
     if not params:
@@ -276,8 +300,7 @@ def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nestero
             cut = slice(at, at + MAX_STACKS)
             part = params[cut]
             ups = (_Update * len(part))(*[
-                _Update(w.data_ptr(), g.data_ptr(), m.data_ptr(), _batch(w), w.shape[-2],
-                        w.shape[-1])
+                _Update(w.data_ptr(), g.data_ptr(), m.data_ptr(), *_shape(w))
                 for w, g, m in zip(part, grads[cut], momenta[cut])])
             work, size = _scratch(lambda need: lib.dpa4c_muon_step_work(len(part), ups, need), dev)
             _check(lib.dpa4c_muon_step(_dtype_code(part[0], "params"), len(part), ups,
