@@ -1312,8 +1312,46 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   }
 }
 
-// The blocks of the groups that have several, added up in their order: dW, then db
-// (null: not formed).
+// Entries i .. of the sum of a group's blocks in their order, kJoin a thread.
+constexpr int kJoin = 4;
+template <class T>
+__device__ inline void join_parts(const float* part, int count, int64_t each, int64_t i, T* out) {
+  if (i + kJoin > each) {   // the last entries once more, as one vector (or each < kJoin)
+    if (each < kJoin) {
+      for (; i < each; ++i) {
+        float s = 0.0f;
+        for (int b = 0; b < count; ++b) s += part[b * each + i];
+        out[i] = from_f32<T>(s);
+      }
+      return;
+    }
+    i = each - kJoin;
+  }
+  part += i;
+  float s[kJoin] = {};
+  int b = 0;
+  for (; b + 8 <= count; b += 8) {   // eight loads in flight
+    Pack<float, kJoin> v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = *reinterpret_cast<const Pack<float, kJoin>*>(part + (b + k) * each);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+#pragma unroll
+      for (int j = 0; j < kJoin; ++j) s[j] += v[k].v[j];
+  }
+  for (; b < count; ++b) {
+    const Pack<float, kJoin> v = *reinterpret_cast<const Pack<float, kJoin>*>(part + b * each);
+#pragma unroll
+    for (int j = 0; j < kJoin; ++j) s[j] += v.v[j];
+  }
+  Pack<T, kJoin> r;
+#pragma unroll
+  for (int j = 0; j < kJoin; ++j) r.v[j] = from_f32<T>(s[j]);
+  *reinterpret_cast<Pack<T, kJoin>*>(out + i) = r;
+}
+
+// The blocks of the groups that have several, added up: dW, then db (null: not
+// formed).
 template <class T>
 __global__ void __launch_bounds__(kThreads) grouped_join_kernel(const int32_t* __restrict__ first_of,
                                                                 int64_t each_w, int64_t each_b,
@@ -1321,27 +1359,15 @@ __global__ void __launch_bounds__(kThreads) grouped_join_kernel(const int32_t* _
                                                                 const float* __restrict__ parts_b,
                                                                 T* __restrict__ dw, T* __restrict__ db) {
   const int g = blockIdx.y;
-  const int first = first_of[g], count = first_of[g + 1] - first;
+  const int64_t first = first_of[g];
+  const int count = static_cast<int>(first_of[g + 1] - first);
   if (count < 2) return;
-  int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t of_w = dw ? each_w : 0;
-  const bool w = i < of_w;
-  i = w ? i : i - of_w;
-  const int64_t each = w ? each_w : each_b;
-  T* out = w ? dw : db;
-  if (!out || i >= each) return;
-  const float* part = (w ? parts_w : parts_b) + first * each + i;
-  float s = 0.0f;
-  int b = 0;
-  for (; b + 8 <= count; b += 8) {   // eight loads in flight
-    float v[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = part[(b + k) * each];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) s += v[k];
-  }
-  for (; b < count; ++b) s += part[b * each];
-  out[g * each + i] = from_f32<T>(s);
+  int64_t i = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * kJoin;
+  const int64_t of_w = dw ? align_up(each_w, kJoin) : 0;
+  if (i < of_w)
+    join_parts(parts_w + first * each_w, count, each_w, i, dw + g * each_w);
+  else if (db && i - of_w < each_b)
+    join_parts(parts_b + first * each_b, count, each_b, i - of_w, db + g * each_b);
 }
 
 // ---------------------------------------------------------------------------
@@ -1372,6 +1398,7 @@ int tile_rows(int dtype, int64_t n, int cols) {
 // straight to dW.  Where even that gives fewer than 512 workgroups, 256.
 int outer_rows(const dpa4c_grouped& l) {
   const int64_t tiles = ((l.k + kOuterTile - 1) / kOuterTile) * int64_t((l.n_out + kOuterTile - 1) / kOuterTile);
+  if (l.n * tiles < 256 * 256) return 128;
   if (l.n * tiles < 512 * 512) return 256;
   const int64_t rows = align_up((l.n * tiles + 4095) / 4096, kDepth);
   return static_cast<int>(rows < 512 ? 512 : rows > 16384 ? 16384 : rows);
@@ -1521,8 +1548,9 @@ int run_outer(const dpa4c_grouped& l, const OuterArgs& a, const TileList& blocks
       grouped_outer_half_kernel<T, kHalf><<<grid, kThreads, 0, st>>>(a);
     DPA4C_HIP_TRY(hipGetLastError());
   }
-  const int64_t each_w = int64_t(l.k) * l.n_out, all = (a.dw ? each_w : 0) + (a.db ? l.n_out : 0);
-  const dim3 grid((all + kThreads - 1) / kThreads, l.n_groups);
+  const int64_t each_w = int64_t(l.k) * l.n_out;
+  const int64_t all = (a.dw ? align_up(each_w, kJoin) : 0) + (a.db ? l.n_out : 0);
+  const dim3 grid((all + kThreads * kJoin - 1) / (kThreads * kJoin), l.n_groups);
   grouped_join_kernel<T><<<grid, kThreads, 0, st>>>(blocks.first_of, each_w, l.n_out, a.parts, a.db_parts,
                                                     static_cast<T*>(a.dw), static_cast<T*>(a.db));
   DPA4C_HIP_TRY(hipGetLastError());
