@@ -7,11 +7,13 @@
 // A wave takes 64 rows at a time in row order.  Lanes with equal keys find each
 // other by one ballot for each bit of the key, so a lane's rank among its peers
 // is a population count, and no atomic's order enters the result.  A workgroup
-// counts the keys of its rows, a wave at a time, turns the counts into starts
-// and places the rows in a second pass over them (from L2).  More than one
-// workgroup's rows are counted by a first launch; every workgroup of the second
-// adds up the counts of those before it by itself, which costs the chip one
-// more read of 4 (n_groups + 1) bytes a workgroup but no third launch.
+// ranks its rows, a wave's stretch at a time, turns the counts into starts and
+// places the rows, whose keys and ranks stay in registers in between (up to
+// kMostBlocks workgroups; beyond, stretches grow and are read again from L2).
+// More than one workgroup's rows are counted by a first launch; every workgroup
+// of the second adds up the counts of those before it by itself, which costs the
+// chip one more read of 4 (n_groups + 1) bytes a pair of workgroups but no third
+// launch.
 #include <hip/hip_runtime.h>
 
 #include "train.h"
@@ -22,19 +24,17 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / kWave;
 // Rows of a workgroup.  Up to kOneBlock one workgroup takes all of them in one
-// launch; beyond, as many as keep 256 compute units busy at a million rows.
-constexpr int64_t kBlockRows = 4096, kOneBlock = 8192;
+// launch; beyond, as many as keep 256 compute units busy at a million rows, and
+// more from kMostBlocks workgroups on: the pairs of workgroups grow as their square.
+constexpr int64_t kBlockRows = 4096, kOneBlock = 8192, kMostBlocks = 1024;
+constexpr int kStrips = static_cast<int>(kBlockRows / (kWaves * kWave));     // of a wave, in registers
+constexpr int kOneStrips = static_cast<int>(kOneBlock / (kWaves * kWave));
 
-__host__ __device__ inline int64_t sort_blocks(int64_t n) {
-  return n <= kOneBlock ? 1 : (n + kBlockRows - 1) / kBlockRows;
+int64_t rows_of_block(int64_t n) {
+  if (n <= kOneBlock) return n;
+  return kBlockRows * ((n + kBlockRows * kMostBlocks - 1) / (kBlockRows * kMostBlocks));
 }
-
-// the group of a row; n_groups for ids outside the range
-__device__ inline int key_of(const int32_t* group, int64_t r, int64_t n, int n_groups) {
-  if (r >= n) return -1;
-  const int g = group[r];
-  return g >= 0 && g < n_groups ? g : n_groups;
-}
+int64_t sort_blocks(int64_t n) { return n <= kOneBlock ? 1 : (n + rows_of_block(n) - 1) / rows_of_block(n); }
 
 // lanes of this wave with the same key (bits: enough for every key)
 __device__ inline uint64_t peers_of(int key, int bits) {
@@ -62,28 +62,52 @@ __device__ inline void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// counts of this wave's keys into cnt[key]
-__device__ inline void count_rows(const int32_t* group, int64_t n, int n_groups, int bits,
-                                  int64_t first, int64_t last, int32_t* cnt) {
+// S strips of rows from r0: their keys (the group; n_groups for ids outside the
+// range; -1 past ``last``) and their ranks, counted on in cnt[key]
+template <int S>
+__device__ inline void rank_rows(const int32_t* group, int n_groups, int bits, int64_t r0, int64_t last,
+                                 int32_t* cnt, int (&key)[S], int (&rank)[S]) {
+  if (r0 >= last) {
+#pragma unroll
+    for (int i = 0; i < S; ++i) key[i] = -1;
+    return;
+  }
   const int lane = threadIdx.x & (kWave - 1);
-  for (int64_t r = first; r < last; r += kWave) {
-    const int key = key_of(group, r + lane, last, n_groups);
-    const uint64_t m = peers_of(key, bits);
-    if (key >= 0 && lane == __builtin_ctzll(m)) cnt[key] += __popcll(m);
+#pragma unroll
+  for (int i = 0; i < S; ++i) {   // all in flight; past the last row it is read again
+    const int64_t r = r0 + i * kWave + lane;
+    key[i] = group[r < last ? r : last - 1];
+  }
+#pragma unroll
+  for (int i = 0; i < S; ++i) {
+    if (r0 + i * kWave >= last) {
+      key[i] = -1;
+      continue;
+    }
+    key[i] = r0 + i * kWave + lane >= last ? -1 : key[i] >= 0 && key[i] < n_groups ? key[i] : n_groups;
+    const uint64_t m = peers_of(key[i], bits);
+    if (key[i] >= 0) {
+      const int before = cnt[key[i]], mine = __popcll(m & ((uint64_t(1) << lane) - 1));
+      rank[i] = before + mine;
+      if (mine == 0) cnt[key[i]] = before + __popcll(m);
+    }
     wave_sync();
   }
 }
 
 __global__ void __launch_bounds__(kThreads) group_count_kernel(const int32_t* __restrict__ group,
                                                                int64_t n, int n_groups, int bits,
+                                                               int64_t per_block,
                                                                int32_t* __restrict__ counts) {
   extern __shared__ int32_t sh[];   // [kWaves][n_groups + 1]
   const int g1 = n_groups + 1, wave = threadIdx.x / kWave;
   for (int i = threadIdx.x; i < kWaves * g1; i += kThreads) sh[i] = 0;
   __syncthreads();
   int64_t first, last;
-  wave_rows(n, kBlockRows, blockIdx.x, wave, &first, &last);
-  count_rows(group, n, n_groups, bits, first, last, sh + wave * g1);
+  wave_rows(n, per_block, blockIdx.x, wave, &first, &last);
+  int key[kStrips], rank[kStrips];
+  for (int64_t r = first; r < last; r += kStrips * kWave)
+    rank_rows(group, n_groups, bits, r, last, sh + wave * g1, key, rank);
   __syncthreads();
   for (int g = threadIdx.x; g < g1; g += kThreads) {
     int c = 0;
@@ -94,6 +118,7 @@ __global__ void __launch_bounds__(kThreads) group_count_kernel(const int32_t* __
 
 // places the rows of a workgroup; counts = null: there is one workgroup only,
 // which counts its rows first
+template <int S>
 __global__ void __launch_bounds__(kThreads) group_place_kernel(
     const int32_t* __restrict__ group, int64_t n, int n_groups, int bits, int64_t per_block,
     const int32_t* __restrict__ counts, int64_t* __restrict__ group_ptr,
@@ -107,17 +132,30 @@ __global__ void __launch_bounds__(kThreads) group_place_kernel(
   __syncthreads();
   int64_t first, last;
   wave_rows(n, per_block, blockIdx.x, wave, &first, &last);
-  count_rows(group, n, n_groups, bits, first, last, sh + wave * g1);
+  int32_t* at = sh + wave * g1;
+  const bool held = per_block <= S * kWaves * kWave;
+  int key[S], rank[S];
+  rank_rows(group, n_groups, bits, first, last, at, key, rank);
+  for (int64_t r = first + S * kWave; r < last; r += S * kWave)
+    rank_rows(group, n_groups, bits, r, last, at, key, rank);
   __syncthreads();
   // the rows of each group before this workgroup and in all (whole numbers:
   // the order of the additions does not matter)
   if (counts)
     for (int g = lane; g < g1; g += kWave) {
       int bef = 0, all = 0;
-      for (int64_t b = wave; b < gridDim.x; b += kWaves) {
-        const int c = counts[b * g1 + g];
-        bef += b < blockIdx.x ? c : 0;
-        all += c;
+      constexpr int kFlight = 16;
+      for (int b0 = wave; b0 < int(gridDim.x); b0 += kFlight * kWaves) {
+        int c[kFlight];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k)
+          c[k] = counts[int64_t(min(b0 + k * kWaves, int(gridDim.x) - 1)) * g1 + g];
+#pragma unroll
+        for (int k = 0; k < kFlight; ++k) {
+          const int b = b0 + k * kWaves;
+          bef += b < int(blockIdx.x) ? c[k] : 0;
+          all += b < int(gridDim.x) ? c[k] : 0;
+        }
       }
       atomicAdd(&before[g], bef);
       atomicAdd(&total[g], all);
@@ -152,17 +190,14 @@ __global__ void __launch_bounds__(kThreads) group_place_kernel(
   __syncthreads();
   if (blockIdx.x == 0)
     for (int g = threadIdx.x; g < g1; g += kThreads) group_ptr[g] = total[g];
-  int32_t* at = sh + wave * g1;
-  for (int64_t r = first; r < last; r += kWave) {
-    const int key = key_of(group, r + lane, last, n_groups);
-    const uint64_t m = peers_of(key, bits);
-    if (key >= 0) {
-      const int rank = __popcll(m & ((uint64_t(1) << lane) - 1));
-      const int base = at[key];
-      order[total[key] + base + rank] = static_cast<int32_t>(r + lane);
-      if (rank == 0) at[key] = base + __popcll(m);
-    }
-    wave_sync();
+  // held: a row's rank in its wave's stretch; else its place in the group, in a
+  // second pass over the stretch
+  for (int64_t r = first; r < last; r += S * kWave) {
+    if (!held) rank_rows(group, n_groups, bits, r, last, at, key, rank);
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+      if (key[i] >= 0)
+        order[total[key[i]] + (held ? at[key[i]] : 0) + rank[i]] = static_cast<int32_t>(r + i * kWave + lane);
   }
 }
 
@@ -180,14 +215,17 @@ int launch_group_rows(const int32_t* group, int64_t n, int n_groups, int64_t* gr
   const int64_t blocks = sort_blocks(n);
   const size_t lds = size_t(kWaves + 2) * (n_groups + 1) * 4;
   int32_t* counts = nullptr;
+  const int64_t rows = rows_of_block(n);
   if (blocks > 1) {
     counts = static_cast<int32_t*>(work);
-    group_count_kernel<<<blocks, kThreads, lds, st>>>(group, n, n_groups, bits, counts);
+    group_count_kernel<<<blocks, kThreads, lds, st>>>(group, n, n_groups, bits, rows, counts);
     DPA4C_HIP_TRY(hipGetLastError());
+    group_place_kernel<kStrips><<<blocks, kThreads, lds, st>>>(group, n, n_groups, bits, rows, counts,
+                                                               group_ptr, order);
+  } else {
+    group_place_kernel<kOneStrips><<<1, kThreads, lds, st>>>(group, n, n_groups, bits, rows, nullptr,
+                                                             group_ptr, order);
   }
-  group_place_kernel<<<blocks, kThreads, lds, st>>>(group, n, n_groups, bits,
-                                                    blocks > 1 ? kBlockRows : n, counts, group_ptr,
-                                                    order);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }

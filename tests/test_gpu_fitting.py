@@ -43,6 +43,16 @@ def test_group_rows_is_a_stable_sort(n, groups):
     assert np.array_equal(order.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("n,groups", [(1000188, 118), (4194304, 3), (4194305, 118), (9000001, 512)])
+def test_group_rows_of_many_workgroups(n, groups):
+    ids = np.random.default_rng(n).integers(-1, groups + 1, n).astype(np.int32)
+    ids[n // 3:n // 2] = 1
+    ptr, order = dp.group_rows(torch.tensor(ids, device="cuda"), groups)
+    key = np.where((ids >= 0) & (ids < groups), ids, groups).astype(np.int16)
+    assert ptr.cpu().tolist() == [0] + np.cumsum(np.bincount(key, minlength=groups + 1)[:groups]).tolist()
+    assert np.array_equal(order.cpu().numpy(), np.argsort(key, kind="stable"))
+
+
 def test_group_rows_extreme_ids():
     ids = torch.tensor([2 ** 31 - 1, -2 ** 31, 3, 0, 118, 117], dtype=torch.int32, device="cuda")
     ptr, order = dp.group_rows(ids, 118)
