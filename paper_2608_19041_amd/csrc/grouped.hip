@@ -368,6 +368,16 @@ constexpr int planes_of = S == kHalf ? 1 : 2;
 template <Source S>
 constexpr int bytes_of = S == kFloat ? 4 : 2;
 
+// How a product reads the weights.  Half types take them as they are: the rows of W
+// are the reduction entries of x W (read through transposing LDS reads) and the
+// columns of dz W^T.  float32 weights are laid out as planes first, and so are
+// rows of fewer than eight entries and, since the planes are quicker to fetch, the
+// weights of kLaidRows rows a group and more.  (bfloat16, 541 -> 384, us: forward of
+// 31,250 rows in 118 groups 60 as they are, 80 laid out; of 1,000,188 rows in 5 groups
+// 1,250 against 1,200, and dx of those 1,410 against 1,290.)
+enum WeightForm { kLaid, kEntries, kColumns };
+constexpr int kLaidRows = 4096;
+
 struct RowsArgs {
   const int32_t* order;
   int n_groups;
@@ -379,6 +389,7 @@ struct RowsArgs {
   int64_t ldin;
   int by_place;     // ``in`` is in group order; its second plane n ldin entries on
   Weights w;
+  const void* weight;   // as they are, unless kLaid
   const void* bias;
   int silu;
   const void* residual;   // rows of kout entries, ldres apart, or null
@@ -443,8 +454,9 @@ __device__ inline void trim(Raw<S>& r, int k, int last, int width) {
   }
 }
 
-template <class T, Source S, int NB>
+template <class T, Source S, int NB, WeightForm W>
 __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
+  static_assert(S != kFloat || W == kLaid, "float32 weights are split into planes first");
   constexpr int PA = planes_of<S>, PB = S == kFloat ? 2 : 1;
   constexpr bool kBf = std::is_same<T, __bf16>::value;
   constexpr int kTile = kSide<NB>, kOne = kPlane<NB>;
@@ -496,12 +508,38 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     last[i] = last_of(a.n, a.ldin, a.by_place ? static_cast<int>(a.ldin) : a.kin, row);
   }
   const int64_t in_plane = a.n * a.ldin * bytes_of<S>;
-  const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
+  // laid out: from c0 of the first step; as they are: of the group
+  const char* wsrc =
+      W == kLaid ? a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes
+                 : static_cast<const char*>(a.weight) + int64_t(t.group) * a.kin * a.kout * sizeof(T);
   const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
+  // kColumns: this thread's NB columns (rows of W, as those of ``in``); columns past
+  // the last repeat it
+  const char* wrow[NB];
+  int wlast[NB];
+  if constexpr (W == kColumns) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int c = c0 + 64 * i + own < a.kout ? c0 + 64 * i + own : a.kout - 1;
+      wrow[i] = wsrc + int64_t(c) * a.kin * sizeof(T);
+      wlast[i] = last_of(int64_t(a.n_groups) * a.kout, a.kin, a.kin, int64_t(t.group) * a.kout + c);
+    }
+  }
+  // kEntries: eight columns of entry tid / kTileSlots (+ 16) of a step; from ``wleft`` on, in
+  // the group, eight entries would reach past the last group's end
+  constexpr int kTileSlots = kTile / 8;
+  const int wentry = tid / kTileSlots, wslot = tid % kTileSlots;
+  const int64_t wleft = (int64_t(a.n_groups) - t.group) * a.kin * a.kout - 8;
+  auto entry_at = [&](int step, int i) {
+    const int k = step * kDepth + wentry + 16 * i;
+    return int64_t(k < a.kin ? k : a.kin - 1) * a.kout + c0 + wslot * 8;
+  };
 
   constexpr int kFar = S == kFloat && NB == 2 ? 2 : 4;   // what the registers hold
+  // weights as they are come from HBM too
+  constexpr int kNear = W == kLaid || S == kPair ? 2 : kFar;
   Raw<S> ra[kFar][NB];
-  u4 rb[2][PB][NB];
+  u4 rb[kNear][PB][NB];
   auto far = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
     const bool in = step < a.w.steps;   // past the end: one line of the weights
@@ -513,12 +551,27 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
   auto near = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
     const bool in = step < a.w.steps;
-    const char* src = in ? wsrc + step * a.w.step_bytes() + tid * 16 : wsrc;
+    if constexpr (W == kLaid) {
+      const char* src = in ? wsrc + step * a.w.step_bytes() + tid * 16 : wsrc;
 #pragma unroll
-    for (int p = 0; p < PB; ++p)
+      for (int p = 0; p < PB; ++p)
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-        rb[q][p][i] = *reinterpret_cast<const u4*>(src + (in ? p * wplane + i * 4096 : 0));
+        for (int i = 0; i < NB; ++i)
+          rb[q][p][i] = *reinterpret_cast<const u4*>(src + (in ? p * wplane + i * 4096 : 0));
+    } else {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        Raw<kHalf> r;
+        if constexpr (W == kColumns) {
+          const int k = step * kDepth + sub * 8;
+          load_raw<kHalf>(r, in ? wrow[i] : wsrc, 0, !in ? 0 : k < wlast[i] ? k : wlast[i]);
+        } else {
+          const int64_t at = entry_at(step, i);
+          load_raw<kHalf>(r, wsrc + (!in ? 0 : at < wleft ? at : wleft) * sizeof(T), 0, 0);
+        }
+        rb[q][0][i] = r.v[0];
+      }
+    }
   };
 
   Sums<NB> acc;
@@ -534,14 +587,34 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
   }
 
   auto put = [&](auto turn, auto far_turn, int step) {
-    constexpr int q = decltype(turn)::value, f = decltype(far_turn)::value;
+    constexpr int n = decltype(turn)::value, f = decltype(far_turn)::value, q = f & 1;
     char* la = lds + q * kHalfLds;
     char* lb = la + PA * kOne;
+    if constexpr (W == kLaid) {
 #pragma unroll
-    for (int p = 0; p < PB; ++p)
+      for (int p = 0; p < PB; ++p)
 #pragma unroll
-      for (int i = 0; i < NB; ++i)
-        *reinterpret_cast<u4*>(lb + p * kOne + i * 4096 + tid * 16) = rb[q][p][i];
+        for (int i = 0; i < NB; ++i)
+          *reinterpret_cast<u4*>(lb + p * kOne + i * 4096 + tid * 16) = rb[n][p][i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        if ((step + 1) * kDepth >= a.kin) {   // the last step
+          Raw<kHalf> r{{rb[n][0][i]}};
+          if constexpr (W == kColumns) {
+            trim<kHalf>(r, step * kDepth + sub * 8, wlast[i], a.kin);
+          } else {
+            const int64_t past = entry_at(step, i) - wleft;
+            const int off = past > 0 ? static_cast<int>(past) : 0;
+            trim<kHalf>(r, off, 0, step * kDepth + wentry + 16 * i < a.kin ? off + 8 : off);
+          }
+          rb[n][0][i] = r.v[0];
+        }
+        const int at = W == kColumns ? slot_at(64 * i + own, sub)
+                                     : wslot / 4 * kDepth * kRowBytes + slot_at(wentry + 16 * i, wslot % 4);
+        *reinterpret_cast<u4*>(lb + at) = rb[n][0][i];
+      }
+    }
     if ((step + 1) * kDepth > a.kin)
 #pragma unroll
       for (int i = 0; i < NB; ++i) trim<S>(ra[f][i], step * kDepth + sub * 8, last[i], a.kin);
@@ -629,13 +702,17 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     constexpr int ks = decltype(half)::value;
     if (!live) return;
     load_part(fa[ks], lds + (step & 1) * kHalfLds + wm * (kTile / 2) * kRowBytes, kOne, lane, ks);
-    load_part(fb[ks], lds + (step & 1) * kHalfLds + PA * kOne + wn * (kTile / 2) * kRowBytes, kOne, lane, ks);
+    const char* lb = lds + (step & 1) * kHalfLds + PA * kOne + wn * (kTile / 2) * kRowBytes;
+    if constexpr (W == kEntries)
+      load_part_turned(fb[ks], lb, kOne, lane, ks);
+    else
+      load_part(fb[ks], lb, kOne, lane, ks);
   };
   auto multiply = [&](auto half) {
     constexpr int ks = decltype(half)::value;
     if (live) multiply_parts<kBf>(acc, fa[ks], fb[ks]);
   };
-  run_steps<2, kFar>(a.w.steps, near, far, put, read, before, multiply);
+  run_steps<kNear, kFar>(a.w.steps, near, far, put, read, before, multiply);
 
   // outputs through LDS, so that rows are written in one piece
   if (S == kFloat && sub == 0)
@@ -1383,13 +1460,19 @@ int64_t tiles_at_most(int64_t n, int n_groups, int64_t rows) {
 // 128 x 128 tiles 1,850; bfloat16 1,140 against 1,000, and 128 columns 3,600
 // against 1,910: half types and few columns leave its columns or matrix cores
 // idle).  Else 128 x 128 where such tiles fill the compute units, and 64 x 64.
-enum TileKind { kSmallTile, kLargeTile, kWideTile };
-TileKind tile_kind(int dtype, int64_t n, int cols) {
-  if (dtype == DPA4C_F32 && cols > 256 && n >= 2 * 256 * kWideRows) return kWideTile;
-  return cols > 64 && (n / 128) * ((cols + 127) / 128) >= 256 ? kLargeTile : kSmallTile;
+// whether products read planes of the weights, not the weights (WeightForm)
+bool laid_out(const dpa4c_grouped& l) {
+  return l.dtype == DPA4C_F32 || l.n_out < kLeastWidth || l.n >= int64_t(kLaidRows) * l.n_groups;
 }
-int tile_rows(int dtype, int64_t n, int cols) {
-  return tile_kind(dtype, n, cols) == kSmallTile ? kSide<1> : kSide<2>;
+
+enum TileKind { kSmallTile, kLargeTile, kWideTile };
+TileKind tile_kind(const dpa4c_grouped& l, bool back) {
+  const int cols = back ? l.k : l.n_out;
+  if (l.dtype == DPA4C_F32 && cols > 256 && l.n >= 2 * 256 * kWideRows) return kWideTile;
+  return cols > 64 && (l.n / 128) * ((cols + 127) / 128) >= 256 ? kLargeTile : kSmallTile;
+}
+int tile_rows(const dpa4c_grouped& l, bool back) {
+  return tile_kind(l, back) == kSmallTile ? kSide<1> : kSide<2>;
 }
 
 // Rows of a block of dW: 4,096 workgroups in all, some rounds of the chip's 512
@@ -1405,11 +1488,12 @@ int outer_rows(const dpa4c_grouped& l) {
 }
 
 Weights weights_of(Arena& ar, const dpa4c_grouped& l, bool back) {
-  Weights w;
+  Weights w{};
   const int depth = back ? l.n_out : l.k, cols = back ? l.k : l.n_out;
   w.steps = (depth + kDepth - 1) / kDepth;
   w.cols_pad = static_cast<int>(align_up(cols, kPad));
   w.planes_n = l.dtype == DPA4C_F32 ? 2 : 1;
+  if (!laid_out(l)) return w;
   w.planes = ar.take<char>(int64_t(l.n_groups) * w.steps * w.step_bytes());
   w.exps = ar.take<int32_t>(l.dtype == DPA4C_F32 ? int64_t(l.n_groups) * w.cols_pad : 0);
   return w;
@@ -1456,7 +1540,7 @@ ForwardPlan plan_forward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   ForwardPlan p;
   p.w = weights_of(ar, l, false);
-  p.tiles = list_of(ar, l, tile_rows(l.dtype, l.n, l.n_out), true);
+  p.tiles = list_of(ar, l, tile_rows(l, false), true);
   p.wide = ar.take<char>(wide_bytes(l));
   *bytes = ar.used;
   return p;
@@ -1472,7 +1556,7 @@ BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   BackwardPlan p;
   p.w = weights_of(ar, l, true);
-  p.tiles = list_of(ar, l, tile_rows(l.dtype, l.n, l.k), true);
+  p.tiles = list_of(ar, l, tile_rows(l, true), true);
   const int rows = outer_rows(l);
   p.blocks = list_of(ar, l, rows, false);
   p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
@@ -1494,7 +1578,7 @@ PrepArgs prepare_args(const dpa4c_grouped& l, const Weights* w, const TileList* 
   a.depth = Back ? l.n_out : l.k;
   a.cols = Back ? l.k : l.n_out;
   int64_t list = 0;
-  if (w) {
+  if (w && laid_out(l)) {
     a.w = l.weight;
     a.out = *w;
     a.weight_blocks = int64_t(l.n_groups) * (w->cols_pad / kPrepCols);
@@ -1519,14 +1603,20 @@ int prepare(const PrepArgs& a, hipStream_t st) {
   return 0;
 }
 
-template <class T, Source S>
-int run_rows(const RowsArgs& a, const TileList& tiles, hipStream_t st) {
+template <class T, Source S, bool Back>
+int run_rows(const dpa4c_grouped& l, const RowsArgs& a, const TileList& tiles, hipStream_t st) {
+  constexpr WeightForm W = S == kFloat ? kLaid : Back ? kColumns : kEntries;
   const int64_t most = tiles_at_most(a.n, a.n_groups, tiles.rows);
-  const TileKind kind = tile_kind(sizeof(T) == 4 ? DPA4C_F32 : DPA4C_F16, a.n, a.kout);
-  if (kind == kSmallTile)
-    grouped_rows_kernel<T, S, 1><<<most * ((a.kout + 63) / 64), kThreads, 0, st>>>(a);
+  const int64_t small = most * ((a.kout + 63) / 64), large = most * ((a.kout + 127) / 128);
+  const TileKind kind = tile_kind(l, Back);
+  if (kind == kSmallTile && laid_out(l))
+    grouped_rows_kernel<T, S, 1, kLaid><<<small, kThreads, 0, st>>>(a);
+  else if (kind == kSmallTile)
+    grouped_rows_kernel<T, S, 1, W><<<small, kThreads, 0, st>>>(a);
+  else if (kind == kLargeTile && laid_out(l))
+    grouped_rows_kernel<T, S, 2, kLaid><<<large, kThreads, 0, st>>>(a);
   else if (kind == kLargeTile)
-    grouped_rows_kernel<T, S, 2><<<most * ((a.kout + 127) / 128), kThreads, 0, st>>>(a);
+    grouped_rows_kernel<T, S, 2, W><<<large, kThreads, 0, st>>>(a);
   else if constexpr (S == kFloat)
     grouped_wide_kernel<T, S><<<most * (((a.kout + 31) / 32 + kWideBlocks - 1) / kWideBlocks), kWideThreads, 0,
                                 st>>>(a);
@@ -1592,13 +1682,14 @@ int launch_grouped_forward(const dpa4c_grouped& l, const void* bias, bool silu, 
     a.in = in.at;
     a.ldin = in.ld;
     a.w = p.w;
+    a.weight = l.weight;
     a.bias = bias;
     a.silu = silu;
     a.residual = residual ? l.x : nullptr;
     a.ldres = l.ldx;
     a.out = y;
     a.zout = z;
-    return run_rows<T, sizeof(T) == 4 ? kFloat : kHalf>(a, p.tiles, st);
+    return run_rows<T, sizeof(T) == 4 ? kFloat : kHalf, false>(l, a, p.tiles, st);
   });
 }
 
@@ -1647,13 +1738,14 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.ldin = made ? pitch : ldy;
       a.by_place = made;
       a.w = p.w;
+      a.weight = l.weight;
       a.residual = residual ? dy : nullptr;
       a.ldres = ldy;
       a.out = dx;
       if (made)
-        DPA4C_TRY((run_rows<T, kMade>(a, p.tiles, st)));
+        DPA4C_TRY((run_rows<T, kMade, true>(l, a, p.tiles, st)));
       else
-        DPA4C_TRY((run_rows<T, kOwn>(a, p.tiles, st)));
+        DPA4C_TRY((run_rows<T, kOwn, true>(l, a, p.tiles, st)));
     }
     if (outer) {
       OuterArgs a{};

@@ -169,13 +169,16 @@ using Const = std::integral_constant<int, K>;
 template <int Near, int Far, class NearFn, class FarFn, class Put, class Read, class Before, class Multiply>
 __device__ inline void run_steps(int steps, NearFn&& near, FarFn&& far, Put&& put, Read&& read,
                                  Before&& before, Multiply&& multiply) {
-  static_assert((Near == 1 || Near == 2) && (Far == 2 || Far == 4), "the steps are unrolled by Far");
+  static_assert((Near == 1 || Near == 2 || Near == Far) && (Far == 2 || Far == 4),
+                "the steps are unrolled by Far");
   near(Const<0>{}, 0);
   far(Const<0>{}, 0);
-  if constexpr (Near == 2) near(Const<1>{}, 1);
+  if constexpr (Near >= 2) near(Const<1>{}, 1);
   far(Const<1>{}, 1);
   if constexpr (Far == 4) {
+    if constexpr (Near == 4) near(Const<2>{}, 2);
     far(Const<2>{}, 2);
+    if constexpr (Near == 4) near(Const<3>{}, 3);
     far(Const<3>{}, 3);
   }
   put(Const<0>{}, Const<0>{}, 0);
@@ -184,7 +187,7 @@ __device__ inline void run_steps(int steps, NearFn&& near, FarFn&& far, Put&& pu
   __syncthreads();
   read(Const<0>{}, 0);
   auto step = [&](auto next, int s) {   // next = (s + 1) % Far
-    constexpr int f = decltype(next)::value, n = Near == 2 ? f & 1 : 0;
+    constexpr int f = decltype(next)::value, n = f % Near;
     before(s);
     read(Const<1>{}, s);
     multiply(Const<0>{});
