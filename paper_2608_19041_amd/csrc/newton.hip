@@ -195,9 +195,10 @@ __device__ inline void write_rows(char* set, int rows_pad, int steps, int r0, in
     }
   }
 }
-// the stage's columns as rows c0 .., entries from r0: four lanes a row of a step
+// the stage's columns as rows c0 .., entries from r0: four lanes a row of a step;
+// with ``mirror`` its rows are added (a tile on the diagonal)
 template <int NB, bool Has = false>
-__device__ inline void write_columns(char* set, int rows_pad, int steps, int r0, int c0,
+__device__ inline void write_columns(char* set, int rows_pad, int steps, int r0, int c0, bool mirror,
                                      const float* stage, float scale, const Extra& x = {}) {
   constexpr int kEach = kSide<NB> * kSide<NB> / 8 / kThreads, kGo = kEach < kBatch ? kEach : kBatch;
 #pragma unroll
@@ -216,6 +217,15 @@ __device__ inline void write_columns(char* set, int rows_pad, int steps, int r0,
       float f[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) f[j] = stage[stage_at<NB>(slot * 8 + j, c)];
+      if (mirror) {
+        const v4f u = *reinterpret_cast<const v4f*>(stage + stage_at<NB>(c, slot * 8));
+        const v4f v = *reinterpret_cast<const v4f*>(stage + stage_at<NB>(c, slot * 8 + 4));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          f[j] += u[j];
+          f[4 + j] += v[j];
+        }
+      }
       if constexpr (Has) add_slot(x, old[k], c0 + c, r0 + slot * 8, f);
       write_slot(set, rows_pad, c0 + c, r0 + slot * 8, f, scale);
     }
@@ -312,7 +322,10 @@ __global__ void __launch_bounds__(kThreads) newton_start_kernel(Stacks all, Shar
 
 enum Phase { kGram, kPoly, kApply, kLast };
 
-// one tile of a phase
+// One tile of a phase.  In a tile on the diagonal of A = X X^T (or of A A) both
+// operands are the same rows, and with S = hi hi^T / 2 + hi lo^T the sum of its
+// three products is S + S^T: two products, with lo doubled and the sums halved, which
+// is exact, and the sum with the transpose on the way out.
 template <class T, bool Muon, Phase P, int NB>
 __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all, Shares sh, int from,
                                                                      float ca, float cb, float cc,
@@ -341,6 +354,7 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1;
   const int r0 = ti * kTile, c0 = tj * kTile;
+  const bool same = !kWide && ti == tj;
 
   const int64_t x_bytes = set_bytes(s.hi_steps, s.lo_pad), sq_bytes = set_bytes(s.lo_steps, s.lo_pad);
   const char* X = s.x[from] + m * x_bytes;
@@ -351,75 +365,102 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
   const char* left = (P == kGram ? X : P == kPoly ? A : s.b + m * sq_bytes) + r0 * kRowBytes;
   const char* right = P == kGram ? X + c0 * kRowBytes : P == kPoly ? A + c0 * kRowBytes : X;
 
-  u4 ra[2][2][NB], rb[2][2][NB];
-  auto fetch = [&](auto turn, int step) {
-    constexpr int q = decltype(turn)::value;
-    const bool in = step < steps;   // past the end: one line
-    const int st = in ? step : 0, at = in ? tid * 16 : 0;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        ra[q][p][i] = *reinterpret_cast<const u4*>(left + (2 * st + p) * plane + i * 4096 + at);
-        if constexpr (!kWide) {
-          rb[q][p][i] = *reinterpret_cast<const u4*>(right + (2 * st + p) * plane + i * 4096 + at);
-        } else {
-          // 32 rows of X of each of the tile's blocks of 32 columns; blocks
-          // past the last repeat it, and nothing of them is stored
-          int block = c0 / 32 + i * 2 + tid / 128;
-          block = block < s.hi_steps ? block : s.hi_steps - 1;
-          rb[q][p][i] = *reinterpret_cast<const u4*>(right + (2 * block + p) * plane + st * 32 * kRowBytes +
-                                                     (in ? tid % 128 * 16 : 0));
-        }
-      }
-  };
-  auto put = [&](auto turn, auto, int) {
-    constexpr int q = decltype(turn)::value;
-    char* to = lds + q * 4 * kOne + tid * 16;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        *reinterpret_cast<u4*>(to + p * kOne + i * 4096) = ra[q][p][i];
-        *reinterpret_cast<u4*>(to + (2 + p) * kOne + i * 4096) = rb[q][p][i];
-      }
-  };
   Sums<NB> acc;
   acc.clear();
   const bool live = r0 + kTile / 2 * wm < s.lo && c0 + kTile / 2 * wn < (kWide ? s.hi : s.lo);
-  Part<NB, 2> fa[2], fb[2];
-  auto read = [&](auto half, int step) {
-    constexpr int ks = decltype(half)::value;
-    if (!live) return;
-    const char* a = lds + (step & 1) * 4 * kOne + wm * (kTile / 2) * kRowBytes;
-    const char* b = lds + (step & 1) * 4 * kOne + 2 * kOne + wn * (kTile / 2) * kRowBytes;
-    load_part(fa[ks], a, kOne, lane, ks);
-    if constexpr (kWide)
-      load_part_turned(fb[ks], b, kOne, lane, ks);
+  auto run = [&](auto diagonal) {   // a constant: no branch inside the steps
+    constexpr bool kSame = decltype(diagonal)::value;
+    u4 ra[2][2][NB], rb[2][2][NB];
+    Part<NB, 2> fa[2], fb[2];
+    auto fetch = [&](auto turn, int step) {
+      constexpr int q = decltype(turn)::value;
+      const bool in = step < steps;   // past the end: one line
+      const int st = in ? step : 0, at = in ? tid * 16 : 0;
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          ra[q][p][i] = *reinterpret_cast<const u4*>(left + (2 * st + p) * plane + i * 4096 + at);
+          if constexpr (kWide) {
+            // 32 rows of X of each of the tile's blocks of 32 columns; blocks
+            // past the last repeat it, and nothing of them is stored
+            int block = c0 / 32 + i * 2 + tid / 128;
+            block = block < s.hi_steps ? block : s.hi_steps - 1;
+            rb[q][p][i] = *reinterpret_cast<const u4*>(right + (2 * block + p) * plane + st * 32 * kRowBytes +
+                                                       (in ? tid % 128 * 16 : 0));
+          } else if constexpr (!kSame) {
+            rb[q][p][i] = *reinterpret_cast<const u4*>(right + (2 * st + p) * plane + i * 4096 + at);
+          }
+        }
+    };
+    auto put = [&](auto turn, auto, int) {
+      constexpr int q = decltype(turn)::value;
+      char* to = lds + q * 4 * kOne + tid * 16;
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          if constexpr (kSame) {
+            const v8h x = __builtin_bit_cast(v8h, ra[q][p][i]);
+            *reinterpret_cast<v8h*>(to + p * kOne + i * 4096) = p == 0 ? x : x + x;
+          } else {
+            *reinterpret_cast<u4*>(to + p * kOne + i * 4096) = ra[q][p][i];
+            *reinterpret_cast<u4*>(to + (2 + p) * kOne + i * 4096) = rb[q][p][i];
+          }
+        }
+    };
+    auto read = [&](auto half, int step) {
+      constexpr int ks = decltype(half)::value;
+      if (!live) return;
+      const char* a = lds + (step & 1) * 4 * kOne + wm * (kTile / 2) * kRowBytes;
+      const char* b = lds + (step & 1) * 4 * kOne + (kSame ? 0 : 2 * kOne) + wn * (kTile / 2) * kRowBytes;
+      load_part(fa[ks], a, kOne, lane, ks);
+      if constexpr (kWide)
+        load_part_turned(fb[ks], b, kOne, lane, ks);
+      else
+        load_part(fb[ks], b, kOne, lane, ks);
+    };
+    auto multiply = [&](auto half) {
+      constexpr int ks = decltype(half)::value;
+      if (!live) return;
+      if constexpr (kSame) {
+#pragma unroll
+        for (int p = 1; p >= 0; --p)
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+              acc.v[i][j] = mfma<false>(fa[ks].v[i][0], fb[ks].v[j][p], acc.v[i][j]);
+      } else {
+        multiply_parts<false>(acc, fa[ks], fb[ks]);
+      }
+    };
+    run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
+  };
+  if constexpr (kWide) {
+    run(std::false_type{});
+  } else {
+    if (same)
+      run(std::true_type{});
     else
-      load_part(fb[ks], b, kOne, lane, ks);
-  };
-  auto multiply = [&](auto half) {
-    constexpr int ks = decltype(half)::value;
-    if (live) multiply_parts<false>(acc, fa[ks], fb[ks]);
-  };
-  run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
+      run(std::false_type{});
+  }
 
   float* stage = reinterpret_cast<float*>(lds);
   stage_sums(stage, acc, kTile / 2 * wm, kTile / 2 * wn, lane,
-             P == kGram   ? 1.0f / (kScaleX * kScaleX)
-             : P == kPoly ? cc / (kScaleA * kScaleA)
-                          : 1.0f / (kScaleB * kScaleX));
+             (same ? 0.5f : 1.0f) * (P == kGram   ? 1.0f / (kScaleX * kScaleX)
+                                     : P == kPoly ? cc / (kScaleA * kScaleA)
+                                                  : 1.0f / (kScaleB * kScaleX)));
   __syncthreads();
   if constexpr (P == kGram) {
     char* out = s.a + m * sq_bytes;
-    write_rows<NB, kTile>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
-    if (ti != tj) write_columns<NB>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
+    if (!same) write_rows<NB, kTile>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleA);
+    write_columns<NB>(out, s.lo_pad, s.lo_steps, r0, c0, same, stage, kScaleA);
   } else if constexpr (P == kPoly) {
     char* out = s.b + m * sq_bytes;
     const Extra x{A, cb / kScaleA, ca};
-    write_rows<NB, kTile, true>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, x);
-    if (ti != tj) write_columns<NB, true>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, x);
+    if (!same) write_rows<NB, kTile, true>(out, s.lo_pad, s.lo_steps, r0, c0, stage, kScaleB, x);
+    write_columns<NB, true>(out, s.lo_pad, s.lo_steps, r0, c0, same, stage, kScaleB, x);
   } else if constexpr (P == kApply) {
     write_rows<NB, kTile>(s.x[from ^ 1] + m * x_bytes, s.lo_pad, s.hi_steps, r0, c0, stage, kScaleX);
   } else {
