@@ -518,14 +518,18 @@ Shares share_wide(const Stacks& all, int side) {
 template <class T, bool Muon, Phase P>
 int product(const Stacks& all, const Shares (&sh)[2], int from, const dpa4c_newton& how, const Finish& f,
             hipStream_t st) {
-  // Tiles of 128 x 128 once they fill the chip's 256 compute units, of 64 x 64
-  // below.
-  const int64_t large = sh[1].first[all.count];
-  if (large >= 256)
+  // Tiles of 128 x 128 once they make two rounds of the 512 workgroups that the
+  // 256 compute units hold, and unless they cover a quarter more than tiles of
+  // 64 x 64 do.  (Five steps, us: 118 matrices of 541 x 384, whose squares are
+  // 708 large tiles, 1,030 with small ones for them, 1,070 without; 100 of 192 x 144
+  // 167 with small tiles, 187 with large ones; products of 236 of 384 x 384,
+  // A 90 with large tiles and 101 with small ones, B X 141 and 174.)
+  const int64_t large = sh[1].first[all.count], small = sh[0].first[all.count];
+  if (large >= 1024 && 16 * large <= 5 * small)
     newton_product_kernel<T, Muon, P, 2><<<large, kThreads, 0, st>>>(all, sh[1], from, how.a, how.b, how.c, f);
   else
     newton_product_kernel<T, Muon, P, 1>
-        <<<sh[0].first[all.count], kThreads, 0, st>>>(all, sh[0], from, how.a, how.b, how.c, f);
+        <<<small, kThreads, 0, st>>>(all, sh[0], from, how.a, how.b, how.c, f);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }
