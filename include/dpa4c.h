@@ -395,7 +395,8 @@ int dpa4c_group_rows(const int32_t* group, int64_t n, int n_groups, int64_t* gro
  * are passed over.
  *   x       [n][k] of ``dtype``, rows ldx entries apart (0: one row for all)
  *   weight  [n_groups][k][n_out], contiguous
- * 0 <= n < 2^31; 1 <= k, n_out <= 65536; 1 <= n_groups <= 4096 (UNSUPPORTED above).
+ * 0 <= n < 2^31; 1 <= k, n_out <= 65536; 1 <= n_groups <= 4096 (UNSUPPORTED above,
+ * and where a product's 64 x 64 tiles reach 2^24, the most of one launch).
  * ``dtype`` is the type of every array of a call.  Products are accumulated in
  * float32 and each output is rounded once.  float32 operands are carried as
  * pairs of float16 under power-of-two scales, which hold them to about 2^-23

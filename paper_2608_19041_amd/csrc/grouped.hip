@@ -1649,6 +1649,17 @@ int run_outer(const dpa4c_grouped& l, const OuterArgs& a, const TileList& blocks
 
 }  // namespace
 
+bool grouped_fits(const dpa4c_grouped& l) {
+  auto up = [](int64_t x, int64_t by) { return (x + by - 1) / by; };
+  const int64_t most = std::max(l.k, l.n_out);
+  const int64_t prep = 64 + 4096 + l.n_groups * (up(most, kPad) * (kPad / kPrepCols) +
+                                                 up(int64_t(l.k) * l.n_out, kClear));
+  const int64_t rows = tiles_at_most(l.n, l.n_groups, kSide<1>) * up(most, kSide<1>);
+  const int64_t outer = tiles_at_most(l.n, l.n_groups, outer_rows(l)) * up(l.k, kOuterTile) * up(l.n_out, kOuterTile);
+  return grid_fits(prep, kPrepThreads) && grid_fits(rows, kThreads) && grid_fits(outer, kThreads) &&
+         grid_fits(up(l.n * kLeastWidth, kThreads), kThreads);
+}
+
 int64_t grouped_forward_work(const dpa4c_grouped& l) {
   int64_t bytes;
   plan_forward(l, nullptr, &bytes);

@@ -515,6 +515,15 @@ Shares share_wide(const Stacks& all, int side) {
   });
 }
 
+Shares share_norms(const Stacks& all) {
+  return share(all, [](const Stack& s) { return int64_t(s.chunks); });
+}
+Shares share_starts(const Stacks& all) {
+  return share(all, [](const Stack& s) {
+    return int64_t(s.lo_pad / kStartRows) * ((s.hi + kSide<kStartSide> - 1) / kSide<kStartSide>);
+  });
+}
+
 template <class T, bool Muon, Phase P>
 int product(const Stacks& all, const Shares (&sh)[2], int from, const dpa4c_newton& how, const Finish& f,
             hipStream_t st) {
@@ -536,10 +545,7 @@ int product(const Stacks& all, const Shares (&sh)[2], int from, const dpa4c_newt
 
 template <class T, bool Muon>
 int run(const Stacks& all, const dpa4c_newton& how, const MuonStep& mu, hipStream_t st) {
-  const Shares norms = share(all, [](const Stack& s) { return int64_t(s.chunks); });
-  const Shares starts = share(all, [](const Stack& s) {
-    return int64_t(s.lo_pad / kStartRows) * ((s.hi + kSide<kStartSide> - 1) / kSide<kStartSide>);
-  });
+  const Shares norms = share_norms(all), starts = share_starts(all);
   const Shares squares[2] = {share_square(all, kSide<1>), share_square(all, kSide<2>)};
   const Shares wides[2] = {share_wide(all, kSide<1>), share_wide(all, kSide<2>)};
   const Finish f{1.0f - mu.lr * mu.decay, mu.lr};
@@ -563,6 +569,14 @@ int run(const Stacks& all, const dpa4c_newton& how, const MuonStep& mu, hipStrea
 }
 
 }  // namespace
+
+bool newton_fits(int count, const NewtonStack* s) {
+  int64_t bytes;
+  const Stacks all = lay_out(count, s, nullptr, &bytes);
+  // the most workgroups: a product's small tiles are no more than the start's
+  return grid_fits(share_norms(all).first[all.count], kThreads) &&
+         grid_fits(share_starts(all).first[all.count], kThreads);
+}
 
 int64_t newton_work(int count, const NewtonStack* s) {
   int64_t bytes;

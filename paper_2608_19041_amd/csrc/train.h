@@ -26,10 +26,14 @@ struct Arena {
   }
 };
 
+// a launch of so many workgroups can be made: HIP takes fewer than 2^32 threads
+constexpr bool grid_fits(int64_t blocks, int threads) { return blocks * threads < (int64_t(1) << 32); }
+
 int64_t group_rows_work(int64_t n, int n_groups);
 int launch_group_rows(const int32_t* group, int64_t n, int n_groups, int64_t* group_ptr,
                       int32_t* order, void* work, hipStream_t st);
 
+bool grouped_fits(const dpa4c_grouped& l);   // every launch of either direction
 int64_t grouped_forward_work(const dpa4c_grouped& l);
 int launch_grouped_forward(const dpa4c_grouped& l, const void* bias, bool silu, bool residual,
                            void* y, void* z, void* work, hipStream_t st);
@@ -52,6 +56,7 @@ struct MuonStep {
   float lr, momentum, decay;
   bool nesterov;
 };
+bool newton_fits(int count, const NewtonStack* s);
 int64_t newton_work(int count, const NewtonStack* s);
 int launch_newton(int dtype, int count, const NewtonStack* s, const dpa4c_newton& how,
                   const MuonStep* muon, void* work, hipStream_t st);

@@ -40,6 +40,10 @@ int check_layer(const char* who, const dpa4c_grouped* l, bool all) {
   DPA4C_TRY(check_rows(who, l->n, l->n_groups, kMaxGroups));
   if (l->k < 1 || l->n_out < 1 || l->k > kMaxWidth || l->n_out > kMaxWidth)
     return invalid(std::string(who) + ": widths must be 1 .. 65536");
+  if (!grouped_fits(*l)) {
+    set_error(std::string(who) + ": more tiles than one launch takes");
+    return DPA4C_ERR_UNSUPPORTED;
+  }
   if (!all) return 0;
   if (!l->group_ptr || !l->weight || (l->n > 0 && !l->x))
     return invalid(std::string(who) + ": null pointer");
@@ -47,23 +51,11 @@ int check_layer(const char* who, const dpa4c_grouped* l, bool all) {
   return 0;
 }
 
-int check_newton(const char* who, int dtype, int count, const dpa4c_newton* how) {
+int check_newton(const char* who, int dtype, const dpa4c_newton* how) {
   if (dtype < DPA4C_F32 || dtype > DPA4C_BF16) return invalid(std::string(who) + ": unknown dtype");
   if (!how || how->steps < 0 || how->steps > 100 || !(how->eps > 0) || !std::isfinite(how->eps) ||
       !std::isfinite(how->a) || !std::isfinite(how->b) || !std::isfinite(how->c))
     return invalid(std::string(who) + ": needs 0 <= steps <= 100, eps > 0, finite coefficients");
-  (void)count;
-  return 0;
-}
-
-template <class S>
-int check_stacks(const char* who, int count, const S* s) {
-  if (count < 0 || count > kMaxStacks || (count > 0 && !s))
-    return invalid(std::string(who) + ": 0 to " + std::to_string(kMaxStacks) + " stacks a call");
-  for (int i = 0; i < count; ++i)
-    if (s[i].rows < 1 || s[i].cols < 1 || s[i].rows > kMaxWidth || s[i].cols > kMaxWidth ||
-        s[i].batch < 0 || s[i].batch > INT32_MAX / (int64_t(s[i].rows) + s[i].cols))
-      return invalid(std::string(who) + ": stack " + std::to_string(i) + " has an unusable shape");
   return 0;
 }
 
@@ -78,6 +70,21 @@ std::vector<NewtonStack> stacks_of(int count, const dpa4c_update* s) {
   for (int i = 0; i < count; ++i)
     v.push_back({s[i].grad, s[i].param, s[i].momentum_buf, s[i].batch, s[i].rows, s[i].cols});
   return v;
+}
+
+template <class S>
+int check_stacks(const char* who, int count, const S* s) {
+  if (count < 0 || count > kMaxStacks || (count > 0 && !s))
+    return invalid(std::string(who) + ": 0 to " + std::to_string(kMaxStacks) + " stacks a call");
+  for (int i = 0; i < count; ++i)
+    if (s[i].rows < 1 || s[i].cols < 1 || s[i].rows > kMaxWidth || s[i].cols > kMaxWidth ||
+        s[i].batch < 0 || s[i].batch > INT32_MAX / (int64_t(s[i].rows) + s[i].cols))
+      return invalid(std::string(who) + ": stack " + std::to_string(i) + " has an unusable shape");
+  if (!newton_fits(count, stacks_of(count, s).data())) {
+    set_error(std::string(who) + ": more tiles than one launch takes");
+    return DPA4C_ERR_UNSUPPORTED;
+  }
+  return 0;
 }
 
 // no C++ exception leaves an entry point
@@ -183,7 +190,7 @@ int dpa4c_orthogonalize(int dtype, int count, const dpa4c_stack* stacks, const d
                         void* work, int64_t work_bytes, void* stream) {
   return guarded([&] {
     const char* who = "dpa4c_orthogonalize";
-    DPA4C_TRY(check_newton(who, dtype, count, how));
+    DPA4C_TRY(check_newton(who, dtype, how));
     DPA4C_TRY(check_stacks(who, count, stacks));
     const std::vector<NewtonStack> s = stacks_of(count, stacks);
     for (const NewtonStack& x : s)
@@ -208,7 +215,7 @@ int dpa4c_muon_step(int dtype, int count, const dpa4c_update* updates, const dpa
                     int64_t work_bytes, void* stream) {
   return guarded([&] {
     const char* who = "dpa4c_muon_step";
-    DPA4C_TRY(check_newton(who, dtype, count, how));
+    DPA4C_TRY(check_newton(who, dtype, how));
     DPA4C_TRY(check_stacks(who, count, updates));
     if (!std::isfinite(lr) || !std::isfinite(momentum) || !std::isfinite(weight_decay))
       return invalid("dpa4c_muon_step: lr, momentum and weight_decay must be finite");

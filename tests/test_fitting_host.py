@@ -98,3 +98,32 @@ def test_update_refused():
     u[0].momentum_buf = 256
     assert call(0, 1, u, ctypes.byref(how), float("nan"), 0.9, 1, 0.0, 256, 1 << 40, None) == INVALID
     assert call(0, 1, u, None, 0.1, 0.9, 1, 0.0, 256, 1 << 40, None) == INVALID
+
+
+@pytest.mark.parametrize("change,rc", [(dict(n=2 ** 31 - 1), UNSUPPORTED), (dict(n=2 ** 28), 0),
+                                       (dict(n=2 ** 24, k=65536, ldx=65536), UNSUPPORTED),
+                                       (dict(n_groups=4096, k=1, n_out=65536), UNSUPPORTED),
+                                       (dict(n_groups=512, k=1, n_out=65536), 0)])
+def test_layers_beyond_a_launch(change, rc):
+    lib, l, need = dp.library(), layer(**change), ctypes.c_int64(-1)
+    assert lib.dpa4c_grouped_linear_work(ctypes.byref(l), ctypes.byref(need)) == rc
+    assert lib.dpa4c_grouped_linear_backward_work(ctypes.byref(l), ctypes.byref(need)) == rc
+    if rc:
+        big = 1 << 60
+        assert lib.dpa4c_grouped_linear(ctypes.byref(l), None, 0, 0, 256, None, 256, big, None) == rc
+        assert lib.dpa4c_grouped_linear_backward(ctypes.byref(l), 256, l.n_out, None, 0, 0, 256, 256, 256,
+                                                 256, big, None) == rc
+
+
+@pytest.mark.parametrize("batch,rows,cols,rc", [(2 ** 24, 1, 1, UNSUPPORTED), (2 ** 22, 1, 1, 0),
+                                                (20, 65536, 65536, UNSUPPORTED), (1, 65536, 65536, 0)])
+def test_matrices_beyond_a_launch(batch, rows, cols, rc):
+    lib, need, how = dp.library(), ctypes.c_int64(-1), newton()
+    s = (ft._Stack * 1)(ft._Stack(256, 256, batch, rows, cols))
+    assert lib.dpa4c_orthogonalize_work(1, s, ctypes.byref(need)) == rc
+    u = (ft._Update * 1)(ft._Update(256, 256, 256, batch, rows, cols))
+    assert lib.dpa4c_muon_step_work(1, u, ctypes.byref(need)) == rc
+    if rc:
+        big = 1 << 60
+        assert lib.dpa4c_orthogonalize(0, 1, s, ctypes.byref(how), 256, big, None) == rc
+        assert lib.dpa4c_muon_step(0, 1, u, ctypes.byref(how), 0.1, 0.9, 1, 0.0, 256, big, None) == rc

@@ -211,6 +211,70 @@ def test_backward(n, k, m, groups, kind, act, dtype):
     assert (dx.cpu()[ids < 0] == 0).all()
 
 
+# rows and columns enough for the larger tiles, and for weights read as they are and
+# laid out
+MANY = [
+    (17000, 541, 384, 118, "few"), (16400, 130, 260, 3, "all"), (16500, 384, 384, 2, "all"),
+    (40000, 5, 130, 9, "few"), (40000, 130, 5, 9, "few"), (65600, 33, 541, 118, "few"),
+    (66000, 290, 290, 5, "one"),
+]
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("n,k,m,groups,kind", MANY)
+def test_many_rows(n, k, m, groups, kind, dtype):
+    test_forward(n, k, m, groups, kind, dtype)
+    test_backward(n, k, m, groups, kind, True, dtype)
+
+
+def test_scales_and_nonfinite_rows_of_many():
+    # a million outputs a column tile: rows of all sizes, rows that grow, rows of NaN
+    n, k, m, groups = 66000, 100, 280, 3
+    ids, x, w, b, _, _ = frame(n, k, m, groups, "fp32", seed=20)
+    g = torch.Generator().manual_seed(21)
+    x = x * torch.logspace(-30, 30, n)[torch.randperm(n, generator=g)][:, None]
+    x[::3] = torch.randn(x[::3].shape, generator=g) * torch.exp2(torch.linspace(-20, 20, k))
+    x[::6, :50] = 0
+    w = w * torch.logspace(-6, 6, m)
+    ptr, order = sorted_rows(ids, groups)
+    y = dp.grouped_linear(x.cuda(), w.cuda(), ptr, order)
+    want, mag = product(x.to(F64), w.to(F64), ids)
+    check(y, want, depth("fp32", k) * mag, "fp32")
+    bad = x.clone()
+    hit = (ids >= 0).nonzero().flatten()[[0, 700, 50000]]
+    bad[ids < 0] = float("nan")
+    bad[hit[0], 3], bad[hit[1], 99], bad[hit[2], 64] = float("nan"), float("inf"), float("-inf")
+    z = dp.grouped_linear(bad.cuda(), w.cuda(), ptr, order)
+    same = torch.ones(n, dtype=torch.bool)
+    same[hit] = False
+    assert torch.equal(z.cpu()[same], y.cpu()[same])
+    assert not torch.isfinite(z.cpu()[hit]).any()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_weights_next_to_nan(dtype):
+    # half-type weights are read where they lie: nothing of a neighbouring group's or
+    # of what follows the array enters
+    for n, k, m, groups in ((300, 37, 45, 4), (20000, 37, 141, 4), (20000, 37, 141, 8), (300, 1, 9, 3), (200, 3, 8, 1)):
+        ids, x, w, b, dy, z = frame(n, k, m, groups, dtype, seed=22)
+        ids[ids == 1] = 0
+        ptr, order = sorted_rows(ids, groups)
+        args = (x.cuda(), ptr, order)
+
+        def layer(w):
+            y = dp.grouped_linear(args[0], w, *args[1:])
+            return (y,) + dp.grouped_linear_backward(dy.cuda(), args[0], w, *args[1:], preact=z.cuda())
+
+        clean = layer(w.cuda())
+        room = torch.full((w.numel() + 64,), float("nan"), dtype=DT[dtype], device="cuda")
+        inside = room[32:32 + w.numel()].view(w.shape)
+        inside.copy_(w)
+        if groups > 1:
+            inside[1] = float("nan")
+        for a, c in zip(clean, layer(inside)):
+            assert torch.equal(a, c)
+
+
 def test_backward_is_the_difference_quotient():
     # L = sum dy * y; a central difference along a direction d with step h is off by
     # h^2 L'''/6 and by the rounding of two sums over h
@@ -418,6 +482,15 @@ def test_orthogonalize(shape, dtype):
     (o,) = dp.orthogonalize([m.cuda()])
     assert o.dtype == m.dtype and o.shape == m.shape
     assert off(o, newton(m)) < NS_BOUND + (0 if dtype == "fp32" else ROUND[dtype])
+
+
+@pytest.mark.parametrize("batch,rows,cols", [(175, 541, 384), (200, 380, 384)])
+def test_orthogonalize_many(batch, rows, cols):
+    g = torch.Generator(device="cuda").manual_seed(batch)
+    m = torch.randn(batch, rows, cols, generator=g, device="cuda") * 1e-3
+    (o,) = dp.orthogonalize([m])
+    want = newton(m).cpu()
+    assert off(o, want) < NS_BOUND
 
 
 def test_orthogonalize_sets_and_stacks():
