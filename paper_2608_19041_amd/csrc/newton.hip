@@ -365,8 +365,15 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
   const char* left = (P == kGram ? X : P == kPoly ? A : s.b + m * sq_bytes) + r0 * kRowBytes;
   const char* right = P == kGram ? X + c0 * kRowBytes : P == kPoly ? A + c0 * kRowBytes : X;
 
-  Sums<NB> acc;
+  // For float32 results, small tiles have registers for sums of their own of the
+  // small products, so that the large ones' are rounded a third as often, and form
+  // the fourth, lo lo, of tiles on the diagonal, where it only ever adds up.  (16
+  // matrices of 3 x 179: off by 1.1e-6, by 1.5e-6 without.)  Large tiles serve large
+  // matrices, whose errors are other terms'.
+  constexpr bool kFull = NB == 1 && sizeof(T) == 4;
+  Sums<NB> acc, low;
   acc.clear();
+  if constexpr (kFull) low.clear();
   const bool live = r0 + kTile / 2 * wm < s.lo && c0 + kTile / 2 * wn < (kWide ? s.hi : s.lo);
   auto run = [&](auto diagonal) {   // a constant: no branch inside the steps
     constexpr bool kSame = decltype(diagonal)::value;
@@ -402,7 +409,7 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
         for (int i = 0; i < NB; ++i) {
           if constexpr (kSame) {
             const v8h x = __builtin_bit_cast(v8h, ra[q][p][i]);
-            *reinterpret_cast<v8h*>(to + p * kOne + i * 4096) = p == 0 ? x : x + x;
+            *reinterpret_cast<v8h*>(to + p * kOne + i * 4096) = p == 0 || kFull ? x : x + x;
           } else {
             *reinterpret_cast<u4*>(to + p * kOne + i * 4096) = ra[q][p][i];
             *reinterpret_cast<u4*>(to + (2 + p) * kOne + i * 4096) = rb[q][p][i];
@@ -423,7 +430,16 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
     auto multiply = [&](auto half) {
       constexpr int ks = decltype(half)::value;
       if (!live) return;
-      if constexpr (kSame) {
+      if constexpr (kFull) {
+        const u4 ah = fa[ks].v[0][0], al = fa[ks].v[0][1], bh = fb[ks].v[0][0], bl = fb[ks].v[0][1];
+        v16f &big = acc.v[0][0], &small = low.v[0][0];
+        if constexpr (kSame)
+          big = mfma<false>(al, bl, big);
+        else
+          small = mfma<false>(al, bh, small);
+        small = mfma<false>(ah, bl, small);
+        big = mfma<false>(ah, bh, big);
+      } else if constexpr (kSame) {
 #pragma unroll
         for (int p = 1; p >= 0; --p)
 #pragma unroll
@@ -447,6 +463,8 @@ __global__ void __launch_bounds__(kThreads, 2) newton_product_kernel(Stacks all,
   }
 
   float* stage = reinterpret_cast<float*>(lds);
+  if constexpr (kFull)
+    for (int r = 0; r < 16; ++r) acc.v[0][0][r] += (same ? 2.0f : 1.0f) * low.v[0][0][r];
   stage_sums(stage, acc, kTile / 2 * wm, kTile / 2 * wn, lane,
              (same ? 0.5f : 1.0f) * (P == kGram   ? 1.0f / (kScaleX * kScaleX)
                                      : P == kPoly ? cc / (kScaleA * kScaleA)
@@ -557,11 +575,12 @@ int run(const Stacks& all, const dpa4c_newton& how, const MuonStep& mu, hipStrea
   else
     newton_start_kernel<T, Muon, false><<<tiles, kThreads, 0, st>>>(all, starts, mu.momentum, mu.nesterov, how.eps, f);
   DPA4C_HIP_TRY(hipGetLastError());
+  using P = std::conditional_t<sizeof(T) == 4, float, _Float16>;   // of the phases between
   for (int step = 0; step < how.steps; ++step) {
-    DPA4C_TRY((product<float, false, kGram>(all, squares, step & 1, how, f, st)));
-    DPA4C_TRY((product<float, false, kPoly>(all, squares, step & 1, how, f, st)));
+    DPA4C_TRY((product<P, false, kGram>(all, squares, step & 1, how, f, st)));
+    DPA4C_TRY((product<P, false, kPoly>(all, squares, step & 1, how, f, st)));
     if (step + 1 < how.steps)
-      DPA4C_TRY((product<float, false, kApply>(all, wides, step & 1, how, f, st)));
+      DPA4C_TRY((product<P, false, kApply>(all, wides, step & 1, how, f, st)));
     else
       DPA4C_TRY((product<T, Muon, kLast>(all, wides, step & 1, how, f, st)));
   }

@@ -493,6 +493,22 @@ def test_orthogonalize_many(batch, rows, cols):
     assert off(o, want) < NS_BOUND
 
 
+@pytest.mark.parametrize("rows,cols", [(3, 179), (16, 20), (69, 31)])
+def test_orthogonalize_is_as_exact_as_float32(rows, cols):
+    # a spectrum that falls off, as a gradient's; half again what the formula is off in float32
+    g = torch.Generator().manual_seed(rows)
+    m = torch.randn(256, rows, cols, generator=g) * torch.arange(1.0, cols + 1).pow(-0.5) * 1e-3
+    x = m / (torch.linalg.matrix_norm(m, keepdim=True) + 1e-7)
+    x = x.mT if rows > cols else x
+    for _ in range(5):
+        p = x @ x.mT
+        x = ABC[0] * x + (ABC[1] * p + ABC[2] * (p @ p)) @ x
+    x = x.mT if rows > cols else x
+    want = newton(m)
+    (o,) = dp.orthogonalize([m.cuda()])
+    assert (o.cpu().to(F64) - want).norm() < 1.5 * (x.to(F64) - want).norm()
+
+
 def test_orthogonalize_sets_and_stacks():
     g = torch.Generator().manual_seed(1)
     shapes = [(5, 7), (70, 30), (0, 8, 8), (2, 3, 40, 41), (11, 128, 64)] + [(3, 9, 5)] * 40
