@@ -249,6 +249,35 @@ __device__ inline void write_result(const Stack& s, int64_t m, int r0, int c0, c
                                     const Finish& f) {
   T* out = static_cast<T*>(s.out) + m * s.rows * s.cols;
   const float step = Muon ? f.step * sqrtf(fmaxf(1.0f, float(s.cols) / float(s.rows))) : 0.0f;
+  if (r0 + Rows <= s.lo && c0 + kSide<NB> <= s.hi) {   // inside: four entries a lane
+    constexpr int kQuads = Rows * kSide<NB> / 4 / kThreads, kGo = 4;
+#pragma unroll 1
+    for (int k0 = 0; k0 < kQuads; k0 += kGo) {
+      Pack<T, 4> w[kGo];
+      int64_t at[kGo];
+#pragma unroll
+      for (int k = 0; k < kGo; ++k) {
+        const int i = threadIdx.x + (k0 + k) * kThreads;
+        const int r = s.turned ? i % (Rows / 4) * 4 : i / (kSide<NB> / 4);
+        const int c = s.turned ? i / (Rows / 4) : i % (kSide<NB> / 4) * 4;
+        at[k] = s.turned ? int64_t(c0 + c) * s.cols + r0 + r : int64_t(r0 + r) * s.cols + c0 + c;
+        if constexpr (Muon) w[k] = *reinterpret_cast<const Pack<T, 4>*>(out + at[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kGo; ++k) {
+        const int i = threadIdx.x + (k0 + k) * kThreads;
+        Pack<T, 4> p;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float o = s.turned ? stage[stage_at<NB>(i % (Rows / 4) * 4 + j, i / (Rows / 4))]
+                                   : stage[stage_at<NB>(i / (kSide<NB> / 4), i % (kSide<NB> / 4) * 4 + j)];
+          p.v[j] = from_f32<T>(Muon ? f.keep * to_f32(w[k].v[j]) - step * o : o);
+        }
+        *reinterpret_cast<Pack<T, 4>*>(out + at[k]) = p;
+      }
+    }
+    return;
+  }
   constexpr int kEach = Rows * kSide<NB> / kThreads, kGo = 8;
 #pragma unroll 1
   for (int k0 = 0; k0 < kEach; k0 += kGo) {
