@@ -63,37 +63,41 @@ struct RowTile {
 
 // Tiles of at most ``rows`` places of all groups, in group order, into list;
 // *count of them, first_of[g] the first of group g.  With ``rest`` group
-// n_groups stands for the rows of no group.  The work of one workgroup of
-// ``blocks``; starts: LDS of n_groups + 2 words.
+// n_groups stands for the rows of no group.  No more than ``room`` tiles are listed,
+// the most that a group_ptr can have that does not decrease: what one that does
+// would add is left out.  The work of one workgroup of ``blocks``; starts: LDS of
+// n_groups + 2 words.
 struct TileList {
   RowTile* list;
   int32_t* first_of;   // [n_groups + 2]
   int32_t* count;
   int rows;
   int rest;
+  int room;
 };
 __device__ inline void list_tiles(const TileList& tl, const int64_t* ptr, int n_groups, int64_t n,
                                   int block, int blocks, int32_t* starts) {
   const int groups = n_groups + (tl.rest ? 1 : 0);
   if (threadIdx.x < kWave) {
     const int lane = threadIdx.x;
-    int run = 0;
+    const int64_t room = tl.room;
+    int64_t run = 0;
     for (int g0 = 0; g0 < groups; g0 += kWave) {
       const int g = g0 + lane;
-      int mine = 0;
+      int64_t mine = 0;
       if (g < groups) {
         const Span s = span_of(ptr, g, n_groups, n);
-        mine = static_cast<int>((s.end - s.begin + tl.rows - 1) / tl.rows);
+        mine = (s.end - s.begin + tl.rows - 1) / tl.rows;
       }
-      int sum = mine;
+      int64_t sum = mine;
       for (int d = 1; d < kWave; d *= 2) {
-        const int v = __shfl_up(sum, d);
+        const int64_t v = __shfl_up(sum, d);
         sum += lane >= d ? v : 0;
       }
-      if (g < groups) starts[g] = run + sum - mine;
+      if (g < groups) starts[g] = static_cast<int>(run + sum - mine < room ? run + sum - mine : room);
       run += __shfl(sum, kWave - 1);
     }
-    if (lane == 0) starts[groups] = run;
+    if (lane == 0) starts[groups] = static_cast<int>(run < room ? run : room);
   }
   __syncthreads();
   const int total = starts[groups];
@@ -1525,7 +1529,8 @@ Weights weights_of(Arena& ar, const dpa4c_grouped& l, bool back) {
 
 TileList list_of(Arena& ar, const dpa4c_grouped& l, int rows, bool rest) {
   TileList t;
-  t.list = ar.take<RowTile>(tiles_at_most(l.n, l.n_groups, rows));
+  t.room = static_cast<int>(tiles_at_most(l.n, l.n_groups, rows));
+  t.list = ar.take<RowTile>(t.room);
   t.first_of = ar.take<int32_t>(l.n_groups + 2);
   t.count = ar.take<int32_t>(1);
   t.rows = rows;

@@ -389,6 +389,24 @@ def test_gradients_on_request():
             assert (part[j] is None) if j != i else torch.equal(part[j], full[j])
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_group_ptr_that_decreases_stays_in_bounds(dtype):
+    # what it gives is nobody's, but nothing else is touched and the next call is right
+    n, k, m, groups = 1000, 40, 72, 30
+    ids, x, w, b, dy, z = (t.cuda() for t in frame(n, k, m, groups, dtype, seed=30))
+    ptr, order = dp.group_rows(ids, groups)
+    want = (dp.grouped_linear(x, w, ptr, order),) + dp.grouped_linear_backward(dy, x, w, ptr, order, preact=z)
+    torch.cuda.synchronize()
+    for bad in (torch.tensor([0, n] * 16)[:groups + 1], torch.tensor([n, -5] * 16)[:groups + 1],
+                torch.tensor([2 ** 62, -2 ** 62] * 16)[:groups + 1]):
+        dp.grouped_linear(x, w, bad.cuda(), order)
+        dp.grouped_linear_backward(dy, x, w, bad.cuda(), order, preact=z)
+        torch.cuda.synchronize()
+    got = (dp.grouped_linear(x, w, ptr, order),) + dp.grouped_linear_backward(dy, x, w, ptr, order, preact=z)
+    for a, c in zip(want, got):
+        assert torch.equal(a, c)
+
+
 def test_no_rows():
     w = torch.randn(3, 5, 7, device="cuda")
     ids = torch.empty(0, dtype=torch.int32, device="cuda")
