@@ -17,11 +17,11 @@
 // last writes the result or the weights itself.
 //
 // Measured, a step's three products and what they come to in float16 products:
-// 118 matrices of 541 x 384 64 + 52 + 109 us (0.50 PFLOP/s), 236 of 384 x 384
+// 118 matrices of 541 x 384 64 + 52 + 109 us (0.47 PFLOP/s), 236 of 384 x 384
 // 90 + 107 + 142 us (0.47).  Matrix cores, at the clock that random operands leave
-// them, and the last workgroups of each launch.  One 688 x 768 with fourteen
-// smaller ones 18 + 13 + 17 us: too few tiles for the chip, each a chain of steps whose
-// latencies nothing hides.  Twelve matrices up to 192 x 192 take 6 to 7 us a launch.
+// them, and the last workgroups of each launch.  Twelve matrices up to
+// 688 x 768 18 + 13 + 17 us: too few tiles for the chip, each a chain of steps whose
+// latencies nothing hides.  Eleven up to 192 x 192 take 6 to 7 us a launch.
 #include <hip/hip_runtime.h>
 
 #include "tile.h"
