@@ -227,6 +227,51 @@ def test_many_rows(n, k, m, groups, kind, dtype):
     test_backward(n, k, m, groups, kind, True, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_offsets_beyond_32_bits(dtype):
+    # 2.25e9 entries a matrix: rows on both sides of 2^31, and sums over all of them
+    n, k, groups = 5630001, 400, 3
+    g = torch.Generator(device="cuda").manual_seed(40)
+    dt = DT[dtype]
+
+    def normal(*shape):
+        return torch.empty(*shape, dtype=dt, device="cuda").normal_(generator=g)
+
+    x, dy, w, b = normal(n, k), normal(n, k), normal(groups, k, k) * k ** -0.5, normal(groups, k)
+    ids = torch.randint(-1, groups, (n,), generator=g, device="cuda", dtype=torch.int32)
+    ptr, order = dp.group_rows(ids, groups)
+    y, z = dp.grouped_linear(x, w, ptr, order, bias=b, activation="silu", residual=True, preact=True)
+    dx, dw, db = dp.grouped_linear_backward(dy, x, w, ptr, order, preact=z, residual=True)
+    at = torch.cat([torch.arange(50), 2 ** 31 // k + torch.arange(-50, 50), torch.arange(n - 50, n)]).cuda()
+    few, xs, ws = ids[at].cpu(), x[at].cpu().to(F64), w.cpu().to(F64)
+    live = (few >= 0).to(F64)[:, None]
+    want, mag = product(xs, ws, few)
+    want = want + live * b.cpu().to(F64)[few.clamp(min=0).long()]
+    slack = depth(dtype, k) * mag + 2 * U * want.abs()
+    check(z[at], want, slack, dtype)
+    check(y[at], silu(want) + live * xs, 1.1 * slack + 8 * U * (silu(want).abs() + xs.abs()), dtype)
+    rel = 0 if dtype == "fp32" else 2.0 ** -15
+    wx, mx, sx = backward_reference(few, x[at].cpu(), w.cpu(), dy[at].cpu(), z[at].cpu(), True)[:3]
+    check(dx[at], wx, (depth(dtype, k) + rel) * mx + 16 * U * sx + 2 * U * wx.abs(), dtype)
+    # sums of all rows, of eight columns: in 64 bits, a stretch at a time
+    ww = torch.zeros(groups, k, 8, dtype=F64, device="cuda")
+    mw, wb, mb = torch.zeros_like(ww), ww[:, 0].clone(), ww[:, 0].clone()
+    for i in range(0, n, 200000):
+        part = slice(i, i + 200000)
+        dz = dy[part, :8].to(F64) * slope(z[part, :8].to(F64))
+        for t in range(groups):
+            mine = dz * (ids[part] == t)[:, None]
+            ww[t] += x[part].to(F64).t() @ mine
+            mw[t] += x[part].to(F64).abs().t() @ mine.abs()
+            wb[t] += mine.sum(0)
+            mb[t] += mine.abs().sum(0)
+    rows = int((ptr[1:] - ptr[:-1]).max())
+    check(dw[:, :, :8], ww.cpu(), ((depth(dtype, rows) + rel + 16 * U) * mw).cpu(), dtype)
+    check(db[:, :8], wb.cpu(), ((depth(dtype, rows) + rel + 16 * U) * mb).cpu(), dtype)
+    del x, dy, y, z, dx
+    torch.cuda.empty_cache()
+
+
 def test_scales_and_nonfinite_rows_of_many():
     # a million outputs a column tile: rows of all sizes, rows that grow, rows of NaN
     n, k, m, groups = 66000, 100, 280, 3
