@@ -5,6 +5,8 @@ element type), the gradients of such a layer, and the Newton-Schulz update of
 the weights (the Muon optimiser).  Argument marshalling only, as in the rest
 of the binding: every step runs in the HIP kernels of the library, on the
 caller's stream, and scratch comes from torch's allocator on that stream.
+Nothing here is recorded by autograd: a layer's gradients come from
+``grouped_linear_backward``.
 
     ptr, order = group_rows(species, 118)
     y, z = grouped_linear(x, w, ptr, order, bias=b, activation="silu", preact=True)
@@ -113,13 +115,18 @@ class _launch:
             guard.__exit__(*error)
 
 
-def _scratch(size_of, device):
-    """(tensor or None, bytes) for a call whose scratch ``size_of`` writes to its argument."""
+def _scratch(device, *sizes_of):
+    """(tensor or None, bytes) for calls that follow each other.
+
+    Each of ``sizes_of`` writes a call's scratch to its argument, and refuses
+    what the call would refuse by its sizes.
+    """
     import torch
-    need = ctypes.c_int64(0)
-    _check(size_of(ctypes.byref(need)))
-    work = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
-    return work, need.value
+    most, need = 0, ctypes.c_int64(0)
+    for size_of in sizes_of:
+        _check(size_of(ctypes.byref(need)))
+        most = max(most, need.value)
+    return torch.empty(most, dtype=torch.uint8, device=device) if most else None, most
 
 
 def group_rows(group, n_groups: int, stream=None):
@@ -134,8 +141,8 @@ def group_rows(group, n_groups: int, stream=None):
         raise ValueError("group must have one dimension")
     n, lib = group.shape[0], library()
     with _launch(group.device, stream) as st:
-        work, size = _scratch(lambda need: lib.dpa4c_group_rows_work(n, int(n_groups), need),
-                              group.device)
+        work, size = _scratch(group.device,
+                              lambda need: lib.dpa4c_group_rows_work(n, int(n_groups), need))
         ptr = torch.empty(int(n_groups) + 1, dtype=torch.int64, device=group.device)
         order = torch.empty(n, dtype=torch.int32, device=group.device)
         _check(lib.dpa4c_group_rows(_ptr(group), n, int(n_groups), _ptr(ptr), _ptr(order),
@@ -182,8 +189,8 @@ def grouped_linear(x, weight, group_ptr, order=None, bias=None, activation=None,
         _same(bias, weight.dtype, (layer.n_groups, layer.n_out), weight.device, "bias")
     lib = library()
     with _launch(weight.device, stream) as st:
-        work, size = _scratch(lambda need: lib.dpa4c_grouped_linear_work(ctypes.byref(layer), need),
-                              weight.device)
+        work, size = _scratch(weight.device,
+                              lambda need: lib.dpa4c_grouped_linear_work(ctypes.byref(layer), need))
         y = torch.empty(layer.n, layer.n_out, dtype=weight.dtype, device=weight.device)
         z = torch.empty_like(y) if preact else None
         _check(lib.dpa4c_grouped_linear(ctypes.byref(layer), _ptr(bias), ACTIVATIONS[activation],
@@ -209,7 +216,7 @@ def grouped_linear_backward(dy, x, weight, group_ptr, order=None, preact=None, r
     lib = library()
     with _launch(dev, stream) as st:
         work, size = _scratch(
-            lambda want: lib.dpa4c_grouped_linear_backward_work(ctypes.byref(layer), want), dev)
+            dev, lambda want: lib.dpa4c_grouped_linear_backward_work(ctypes.byref(layer), want))
         dx = torch.empty(n, layer.k, dtype=weight.dtype, device=dev) if need[0] else None
         dw = torch.empty_like(weight) if need[1] else None
         db = torch.empty(layer.n_groups, m, dtype=weight.dtype, device=dev) if need[2] else None
@@ -242,6 +249,13 @@ def _shape(t):
     return math.prod(batch), rows, cols
 
 
+def _calls(struct, *tensors):
+    """The matching tensors of all lists as arrays of ``struct``, MAX_STACKS at a time."""
+    every = [struct(*(t.data_ptr() for t in ts), *_shape(ts[0])) for ts in zip(*tensors)]
+    return [(struct * len(part))(*part)
+            for part in (every[at:at + MAX_STACKS] for at in range(0, len(every), MAX_STACKS))]
+
+
 def _newton(steps, coefficients, eps):
     a, b, c = (float(v) for v in coefficients)
     return _Newton(int(steps), a, b, c, float(eps))
@@ -260,17 +274,14 @@ def orthogonalize(matrices, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps:
     if not matrices:
         return []
     how, lib, dev = _newton(steps, coefficients, eps), library(), matrices[0].device
+    code = _dtype_code(matrices[0], "matrices")
     with _launch(dev, stream) as st:
         out = [torch.empty_like(t) for t in matrices]
-        for at in range(0, len(matrices), MAX_STACKS):
-            part = matrices[at:at + MAX_STACKS]
-            stacks = (_Stack * len(part))(*[
-                _Stack(t.data_ptr(), o.data_ptr(), *_shape(t))
-                for t, o in zip(part, out[at:at + MAX_STACKS])])
-            work, size = _scratch(
-                lambda need: lib.dpa4c_orthogonalize_work(len(part), stacks, need), dev)
-            _check(lib.dpa4c_orthogonalize(_dtype_code(part[0], "matrices"), len(part), stacks,
-                                           ctypes.byref(how), _ptr(work), size, st))
+        calls = _calls(_Stack, matrices, out)
+        work, size = _scratch(dev, *(
+            functools.partial(lib.dpa4c_orthogonalize_work, len(c), c) for c in calls))
+        for c in calls:
+            _check(lib.dpa4c_orthogonalize(code, len(c), c, ctypes.byref(how), _ptr(work), size, st))
     return out
 
 
@@ -294,16 +305,13 @@ def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nestero
     for w, g, m in zip(params, grads, momenta):
         _same(g, w.dtype, w.shape, dev, "grads")
         _same(m, torch.float32, w.shape, dev, "momenta")
-    how, lib = _newton(steps, coefficients, eps), library()
+    how, lib, code = _newton(steps, coefficients, eps), library(), _dtype_code(params[0], "params")
     with _launch(dev, stream) as st:
-        for at in range(0, len(params), MAX_STACKS):
-            cut = slice(at, at + MAX_STACKS)
-            part = params[cut]
-            ups = (_Update * len(part))(*[
-                _Update(w.data_ptr(), g.data_ptr(), m.data_ptr(), *_shape(w))
-                for w, g, m in zip(part, grads[cut], momenta[cut])])
-            work, size = _scratch(lambda need: lib.dpa4c_muon_step_work(len(part), ups, need), dev)
-            _check(lib.dpa4c_muon_step(_dtype_code(part[0], "params"), len(part), ups,
-                                       ctypes.byref(how), float(lr), float(momentum),
-                                       int(bool(nesterov)), float(weight_decay), _ptr(work), size,
-                                       st))
+        # the sizes of all calls are checked before the first changes a weight
+        calls = _calls(_Update, params, grads, momenta)
+        work, size = _scratch(dev, *(
+            functools.partial(lib.dpa4c_muon_step_work, len(c), c) for c in calls))
+        for c in calls:
+            _check(lib.dpa4c_muon_step(code, len(c), c, ctypes.byref(how), float(lr),
+                                       float(momentum), int(bool(nesterov)), float(weight_decay),
+                                       _ptr(work), size, st))

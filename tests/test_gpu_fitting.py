@@ -691,3 +691,29 @@ def test_refusals():
                  lambda: dp.muon_step([w], [w], [w.clone()], lr=float("inf"))):
         with pytest.raises(dp.DPA4CError):
             call()
+
+
+def test_a_refused_update_changes_nothing():
+    f = dict(device="cuda")
+    ws = [torch.randn(4, 4, **f) for _ in range(33)] + [torch.randn(1, 65537, **f)]
+    ms = [torch.randn_like(w) for w in ws]
+    before = [t.clone() for t in ws + ms]
+    with pytest.raises(dp.DPA4CError):   # the last matrix is too wide, in the second call of the library
+        dp.muon_step(ws, [torch.randn_like(w) for w in ws], ms, lr=0.1)
+    for t, old in zip(ws + ms, before):
+        assert torch.equal(t, old)
+
+
+def test_more_matrices_than_one_call_takes():
+    g = torch.Generator().manual_seed(3)
+    ws = [torch.randn(3 + i % 7, 5 + i % 4, generator=g).cuda() for i in range(67)]
+    gs, ms = [w.flip(0).contiguous() for w in ws], [torch.zeros_like(w) for w in ws]
+    alone = [dp.orthogonalize([w])[0] for w in ws]
+    for a, b in zip(alone, dp.orthogonalize(ws)):
+        assert torch.equal(a, b)
+    one_w, one_m = [w.clone() for w in ws], [m.clone() for m in ms]
+    for w, gr, m in zip(one_w, gs, one_m):
+        dp.muon_step([w], [gr], [m], lr=0.1)
+    dp.muon_step(ws, gs, ms, lr=0.1)
+    for a, b in zip(one_w + one_m, ws + ms):
+        assert torch.equal(a, b)
