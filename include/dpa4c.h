@@ -436,6 +436,9 @@ int dpa4c_grouped_linear(const dpa4c_grouped* layer, const void* bias, int activ
  *     dW_g = sum_r x_r^T dz_r,   db_g = sum_r dz_r.
  * dx [n][k], dw [n_groups][k][n_out], db [n_groups][n_out], contiguous; each
  * may be NULL (not formed).  Groups without rows get zeros.
+ * dz of a half type with z is carried as a pair of numbers of that type: of bfloat16
+ * to 2^-16 of itself; of float16 under a power-of-two scale, to 2^-22 of itself or
+ * 2^-39 of the largest finite dz, of its row for dx and db and of its group for dW.
  */
 int dpa4c_grouped_linear_backward_work(const dpa4c_grouped* layer, int64_t* bytes);
 int dpa4c_grouped_linear_backward(const dpa4c_grouped* layer, const void* dy, int64_t ldy,

@@ -12,7 +12,8 @@
 // the product tile reads them where that pays (WeightForm), forms dz by place and
 // clears the gradients of the groups without rows.  dx and dW then read dz with
 // plain rows.  Sums are float32 and every output rounds once; dz of a half type is
-// kept as a pair of halves (2^-15 of itself), not rounded to one.
+// kept as a pair of them (16 bits of bfloat16, 22 of float16 under a scale of its row),
+// not rounded to one.
 //
 // The launches of a call depend on each other, so a call of few rows is bound by
 // the latencies of two (forward) or four (backward) kernels: 108 rows of 144 -> 192
@@ -150,6 +151,7 @@ struct PrepArgs {
   int64_t ldy, ldz;
   int pitch;
   void* dz;
+  int32_t* dz_exps;   // float16: the exponent of each place's row
   // the workgroups of each kind, in this order
   int64_t list_blocks, weight_blocks, clear_blocks, dz_blocks;
 };
@@ -290,9 +292,9 @@ __global__ void __launch_bounds__(kThreads) grouped_widen_kernel(int64_t n, int 
 }
 
 // dz = dy act'(z) (z = null: dy) by place: float32 as it is, half types as a plane of their own
-// type and one of what that leaves, hi + lo (16 or 22 bits: dz is an intermediate;
-// rounded to its 8 or 11 bits it would add as much error to dx and dW as their own
-// rounding does)
+// type and one of what that leaves, hi + lo (16 or, of float16 below, 22 bits: dz is an
+// intermediate; rounded to its 8 or 11 bits it would add as much error to dx and dW as their
+// own rounding does)
 template <class T>
 __device__ inline void form_dz(const PrepArgs& p, int64_t block, int64_t blocks) {
   constexpr int kEach = 16 / sizeof(T);
@@ -336,6 +338,84 @@ __device__ inline void form_dz(const PrepArgs& p, int64_t block, int64_t blocks)
   }
 }
 
+// The same of float16, whose exponents end too early for what a gradient can be: a
+// row is multiplied by 2^e first, so that its largest finite entry lies in [2^14, 2^15).
+// hi + lo then holds an entry to 2^-22 of itself or 2^-39 of that largest one, and
+// nothing overflows.  A row of zeros has kNoExp.  lanes_of_dz(pitch) lanes take a row,
+// eight entries each; longer rows are formed twice.  (1,000,188 rows of 384: the
+// launch 705 us, of bfloat16 620, and dW 1,970 against 1,780.)
+constexpr int kDzTop = 14, kNoExp = 100;
+__host__ __device__ inline int lanes_of_dz(int pitch) {
+  int lanes = 1;
+  while (lanes < kWave && lanes * 8 < pitch) lanes *= 2;
+  return lanes;
+}
+__device__ inline void form_dz_scaled(const PrepArgs& p, int64_t block, int64_t blocks) {
+  using T = _Float16;
+  const int64_t n = p.n;
+  const int cols = p.depth, pitch = p.pitch;   // Back: depth = n_out
+  const T* dy = static_cast<const T*>(p.dy);
+  const T* z = static_cast<const T*>(p.z);
+  T* dz = static_cast<T*>(p.dz);
+  const int64_t live = clamp_place(p.ptr[p.n_groups], n);
+  const int lanes = lanes_of_dz(pitch), sub = threadIdx.x & (lanes - 1);
+  const int rows = kPrepThreads / lanes;
+  for (int64_t place = block * rows + int(threadIdx.x) / lanes; place < live; place += blocks * rows) {
+    const int64_t row = row_at(p.order, place, n);
+    float v[8];
+    auto form = [&](int c) {
+      Pack<T, 8> a = {}, b = {};
+      if (row >= 0) {
+        if (c + 8 <= cols) {
+          a = *reinterpret_cast<const Pack<T, 8>*>(dy + row * p.ldy + c);
+          if (z) b = *reinterpret_cast<const Pack<T, 8>*>(z + row * p.ldz + c);
+        } else {
+          for (int j = 0; j < 8; ++j)
+            if (c + j < cols) {
+              a.v[j] = dy[row * p.ldy + c + j];
+              if (z) b.v[j] = z[row * p.ldz + c + j];
+            }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = to_f32(a.v[j]);
+        if (z) v[j] *= silu_slope(to_f32(b.v[j]));
+      }
+    };
+    float m = 0.0f;
+    for (int c = sub * 8; c < pitch; c += lanes * 8) {
+      form(c);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float size = fabsf(v[j]);
+        m = size < INFINITY ? fmaxf(m, size) : m;   // neither infinities nor NaN
+      }
+    }
+    for (int d = lanes / 2; d > 0; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
+    const int top = kDzTop - (static_cast<int>(__builtin_bit_cast(unsigned, m) >> 23) - 127);
+    const int e = top < kNoExp ? top : kNoExp;   // m = 0 too
+    if (sub == 0) p.dz_exps[place] = e;
+    const float scale = exp2_of(e);
+    for (int c = sub * 8; c < pitch; c += lanes * 8) {
+      if (pitch > lanes * 8) form(c);
+      u4 hi, lo;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // one value each: as in form_dz
+        float x = v[2 * j] * scale, y = v[2 * j + 1] * scale;
+        asm("" : "+v"(x), "+v"(y));
+        unsigned h, l;
+        split2(x, y, &h, &l);
+        hi[j] = h;
+        lo[j] = l;
+      }
+      *reinterpret_cast<u4*>(dz + place * pitch + c) = hi;
+      *reinterpret_cast<u4*>(dz + (n + place) * pitch + c) = lo;
+    }
+  }
+}
+
 // What the products of a call need first, each piece by workgroups of its own, since
 // all of it is bound by HBM: 31,250 rows of 541 -> 384 in 118 groups move 340 MB in
 // 65 us (5.2 TB/s, reads of dy and z that the last-level cache holds among them), dz
@@ -364,7 +444,10 @@ __global__ void __launch_bounds__(kPrepThreads) grouped_prepare_kernel(PrepArgs 
       clear_gradients<T>(a, static_cast<int>(b / each), b % each);
       return;
     }
-    form_dz<T>(a, b - a.clear_blocks, a.dz_blocks);
+    if constexpr (std::is_same<T, _Float16>::value)
+      form_dz_scaled(a, b - a.clear_blocks, a.dz_blocks);
+    else
+      form_dz<T>(a, b - a.clear_blocks, a.dz_blocks);
   }
 }
 
@@ -379,6 +462,9 @@ template <Source S>
 constexpr int planes_of = S == kHalf ? 1 : 2;
 template <Source S>
 constexpr int bytes_of = S == kFloat ? 4 : 2;
+// a pair of float16 has an exponent of its row
+template <class T, Source S>
+constexpr bool row_scaled = S == kPair && std::is_same<T, _Float16>::value;
 
 // How a product reads the weights.  Half types take them as they are: the rows of W
 // are the reduction entries of x W (read through transposing LDS reads) and the
@@ -400,6 +486,7 @@ struct RowsArgs {
   const void* in;   // rows of kin entries, ldin apart
   int64_t ldin;
   int by_place;     // ``in`` is in group order; its second plane n ldin entries on
+  const int32_t* in_exps;   // row_scaled: the rows' exponents, by place
   Weights w;
   const void* weight;   // as they are, unless kLaid
   const void* bias;
@@ -523,6 +610,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
     r = r < t.count ? r : t.count - 1;
     const int64_t to = row_at(a.order, t.first + r, a.n);
     if (sub == 0) row_of[64 * i + own] = 64 * i + own < t.count ? static_cast<int32_t>(to) : -1;
+    if (row_scaled<T, S> && sub == 0) row_exp[64 * i + own] = a.in_exps[t.first + r];
     const int64_t row = a.by_place ? t.first + r : to < 0 ? 0 : to;
     rows[i] = static_cast<const char*>(a.in) + row * a.ldin * bytes_of<S>;
     last[i] = last_of(a.n, a.ldin, a.by_place ? static_cast<int>(a.ldin) : a.kin, row);
@@ -780,11 +868,11 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
         if (row[k] < 0) continue;
         const int r = r0 + kRowsOnce * k;
         const v4f s = *reinterpret_cast<const v4f*>(stage + stage_at<NB>(r, quad * 4));
-        const int er = S == kFloat ? row_exp[h + r] : 0;
+        const int er = S == kFloat || row_scaled<T, S> ? row_exp[h + r] : 0;
         Pack<T, 4> py, pz;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          float z = S == kFloat ? ldexpf(s[j], -er - eq[j]) : s[j];
+          float z = S == kFloat || row_scaled<T, S> ? ldexpf(s[j], -er - eq[j]) : s[j];
           z += bq[j];
           float y = a.silu ? z * logistic(z) : z;
           if (a.residual) y += to_f32(res[k].v[j]);
@@ -1090,6 +1178,7 @@ struct OuterArgs {
   const void* dz;     // by row, or by place (its second plane n lddz entries on)
   int64_t lddz;
   int by_place;
+  const int32_t* dz_exps;   // row_scaled: the rows' exponents, by place
   void* dw;           // null: not formed
   void* db;
   float* parts;       // [block][k][m] where a group has several blocks
@@ -1119,11 +1208,11 @@ __device__ inline bool outer_tile(const OuterArgs& a, OuterTile& o) {
   return true;
 }
 
-// sums of a tile, scaled by 2^-(row exponent + column exponent), to dW where no
-// other block adds to the group, else to the block's own sums
+// sums of a tile, scaled by 2^-(row exponent + column exponent) or by 2^-e_all, to dW
+// where no other block adds to the group, else to the block's own sums
 template <class T>
 __device__ inline void store_outer(const OuterArgs& a, const OuterTile& o, const Sums<2>& acc,
-                                   const int32_t* exps) {
+                                   const int32_t* exps, int e_all = 0) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
   const bool whole = o.t.parts == 1;
   T* dw = static_cast<T*>(a.dw) + int64_t(o.t.group) * a.k * a.m;
@@ -1139,7 +1228,7 @@ __device__ inline void store_outer(const OuterArgs& a, const OuterTile& o, const
         const int rl = 64 * wm + 32 * i + sum_row(lane, r), row = o.r0 + rl;
         if (row >= a.k || c >= a.m) continue;
         float v = acc.v[i][j][r];
-        if (exps) v = ldexpf(v, -exps[rl] - ec);
+        v = ldexpf(v, exps ? -exps[rl] - ec : -e_all);
         if (whole)
           dw[int64_t(row) * a.m + c] = from_f32<T>(v);
         else
@@ -1303,11 +1392,15 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
   if (sums_bias) store_bias<float>(a, o, mine, bias);
 }
 
-// Half types need no scale, so the rows go to LDS as they come, eight columns a
+// Half types need no scale of their columns, so the rows go to LDS as they come, eight columns a
 // lane, and transposing reads turn them: 6 loads a lane and step for dz in two
 // planes, where a column a lane would take 64 loads of 2 or 4 bytes.  1,000,188
-// rows of 541 x 384 in two planes: 1,780 us, 0.47 PFLOP/s; five tiles across read dz
+// bfloat16 rows of 541 x 384 in two planes: 1,780 us, 0.47 PFLOP/s; five tiles across read dz
 // five times and three x three times, from L2 as they run side by side.
+//
+// Rows of dz with exponents of their own are brought to the least one of the block on
+// the way to LDS, by powers of two: exact, but for what falls below 2^-39 of the block's
+// largest entry.
 template <class T, Source SZ>
 __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterArgs a) {
   constexpr int PB = planes_of<SZ>, kOne = kPlane<2>, kHalfLds = (1 + PB) * kOne;
@@ -1321,6 +1414,17 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   const int64_t end = o.t.first + o.t.count;
   const int steps = (o.t.count + kDepth - 1) / kDepth;
   const bool sums_bias = a.db && o.r0 == 0;
+  constexpr bool kScaled = row_scaled<T, SZ>;
+  int e_all = 0;
+  if constexpr (kScaled) {
+    __shared__ int32_t least[kThreads / kWave];
+    e_all = kNoExp;
+    for (int i = tid; i < o.t.count; i += kThreads) e_all = min(e_all, a.dz_exps[o.t.first + i]);
+    for (int d = kWave / 2; d > 0; d /= 2) e_all = min(e_all, __shfl_xor(e_all, d));
+    if (lane == 0) least[wave] = e_all;
+    __syncthreads();
+    for (int i = 0; i < kThreads / kWave; ++i) e_all = min(e_all, least[i]);
+  }
   // places tid / 16 and tid / 16 + 16 of a step, columns 8 (tid % 16) .. of both operands
   const int own = tid / 16, cg = tid % 16;
   const int xc = o.r0 + 8 * cg, zc = o.c0 + 8 * cg;
@@ -1329,6 +1433,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   // the rows of a step, looked up one fetch before its loads, and before that
   // fetch's own (see above)
   int64_t next[2];
+  int next_exp[2] = {}, exps[2][2];
   auto look = [&](int step) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -1336,6 +1441,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
       const int64_t at = place < end ? place : end - 1;
       const int64_t row = a.order ? a.order[at] : at;   // without a condition
       next[i] = place < end && row >= 0 && row < a.n ? row : -1;
+      if constexpr (kScaled) next_exp[i] = a.dz_exps[at];
     }
   };
   Raw<kHalf> rx[2][2];
@@ -1346,6 +1452,8 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   auto fetch = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
     int64_t row[2] = {next[0], next[1]};
+    exps[q][0] = next_exp[0];
+    exps[q][1] = next_exp[1];
     look(step + 1);
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -1373,16 +1481,26 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
       if (o.r0 + kOuterTile > a.k) trim<kHalf>(rx[q][i], xc, x_last[q][i], a.k);
       if (o.c0 + kOuterTile > a.m) trim<SZ>(rz[q][i], zc, z_last[q][i], a.m);
       *reinterpret_cast<u4*>(to + at) = there[q][i] ? rx[q][i].v[0] : none;
+      const int d = kScaled ? e_all - exps[q][i] : 0;   // never above 0
+      const float own_scale = kScaled ? exp2_of(-exps[q][i]) : 1.0f;
 #pragma unroll
       for (int p = 0; p < PB; ++p) {
-        const u4 v = there[q][i] ? rz[q][i].v[p] : none;
-        *reinterpret_cast<u4*>(to + (1 + p) * kOne + at) = v;
+        u4 v = there[q][i] ? rz[q][i].v[p] : none;
         if (sums_bias)
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             const unsigned w = v[j / 2];
-            bias[j] += to_f32(__builtin_bit_cast(T, static_cast<unsigned short>(j & 1 ? w >> 16 : w & 0xffff)));
+            bias[j] += own_scale *
+                       to_f32(__builtin_bit_cast(T, static_cast<unsigned short>(j & 1 ? w >> 16 : w & 0xffff)));
           }
+        if constexpr (kScaled) {
+          // 2^-24 is the least power that float16 has: the rest in a second product
+          v8h f = __builtin_bit_cast(v8h, v) * static_cast<_Float16>(exp2_of(max(d, -24)));
+          if (__ballot(d < -24) != 0)
+            f *= static_cast<_Float16>(d < -48 ? 0.0f : exp2_of(min(d + 24, 0)));
+          v = __builtin_bit_cast(u4, f);
+        }
+        *reinterpret_cast<u4*>(to + (1 + p) * kOne + at) = v;
       }
     }
   };
@@ -1403,7 +1521,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   };
   run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
 
-  if (a.dw) store_outer<T>(a, o, acc, nullptr);
+  if (a.dw) store_outer<T>(a, o, acc, nullptr, e_all);
   if (sums_bias) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) bias_part[own][8 * cg + j] = bias[j];
@@ -1579,6 +1697,7 @@ struct BackwardPlan {
   Weights w;
   TileList tiles, blocks;
   void *dz, *wide;
+  int32_t* dz_exps;
   float *parts, *db_parts;
 };
 BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
@@ -1589,6 +1708,7 @@ BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   const int rows = outer_rows(l);
   p.blocks = list_of(ar, l, rows, false);
   p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
+  p.dz_exps = ar.take<int32_t>(l.dtype == DPA4C_F16 ? l.n : 0);
   p.wide = ar.take<char>(wide_bytes(l));
   const int64_t blocks = tiles_at_most(l.n, l.n_groups, rows);
   p.parts = ar.take<float>(blocks * l.k * l.n_out);
@@ -1761,7 +1881,9 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       pre.ldz = ldz;
       pre.pitch = pitch;
       pre.dz = p.dz;
-      const int64_t each = l.n * (pitch * int64_t(sizeof(T)) / 16);
+      pre.dz_exps = p.dz_exps;
+      const int64_t each =
+          l.n * (l.dtype == DPA4C_F16 ? lanes_of_dz(pitch) : pitch * int64_t(sizeof(T)) / 16);
       pre.dz_blocks = std::min<int64_t>((each + kPrepThreads - 1) / kPrepThreads, 4096);
     }
     DPA4C_TRY((prepare<T, true>(pre, st)));
@@ -1777,6 +1899,7 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.in = made ? p.dz : dy;
       a.ldin = made ? pitch : ldy;
       a.by_place = made;
+      a.in_exps = p.dz_exps;
       a.w = p.w;
       a.weight = l.weight;
       a.residual = residual ? dy : nullptr;
@@ -1802,6 +1925,7 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.dz = made ? p.dz : dy;
       a.lddz = made ? pitch : ldy;
       a.by_place = made;
+      a.dz_exps = p.dz_exps;
       a.dw = dw;
       a.db = db;
       a.parts = p.parts;
