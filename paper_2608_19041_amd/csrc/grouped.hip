@@ -1265,6 +1265,14 @@ __device__ inline void load_column(Column& r, const float* base, int64_t ld, int
 #pragma unroll
   for (int i = 0; i < kDepth; ++i) r.v[i] = (base + __builtin_amdgcn_readlane(at, i) * ld)[col];
 }
+// the sum of N entries as a tree
+template <int N>
+__device__ inline float tree_sum(const float* v) {
+  if constexpr (N == 1)
+    return v[0];
+  else
+    return tree_sum<N / 2>(v) + tree_sum<N / 2>(v + N / 2);
+}
 // zeros for the rows that are not there
 __device__ inline void clear_column(Column& r, int row) {
   if (__ballot(row < 0) == 0) return;
@@ -1315,16 +1323,14 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
   acc.clear();
   int e = kFirstExp;
   bool changed[2] = {false, false};
-  float bias = 0.0f;
+  double bias = 0.0;   // a step's sum at a time: roundings of many rows can all go one way
   change[0][tid] = change[1][tid] = 0;
   if (tid < 3) flag[tid] = 0;
   __syncthreads();
   auto put = [&](auto turn, auto, int step) {
     constexpr int q = decltype(turn)::value;
     clear_column(c[q], row[q]);
-    if (sums_bias)
-#pragma unroll
-      for (int i = 0; i < kDepth; ++i) bias += c[q].v[i];
+    if (sums_bias) bias += tree_sum<kDepth>(c[q].v);
     if (!a.dw) return;
     if (tid == 0) flag[(step + 1) % 3] = 0;
     if (changed[q]) {   // two steps ago; its readers are past it
@@ -1389,7 +1395,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
     __syncthreads();
     store_outer<float>(a, o, acc, exps);
   }
-  if (sums_bias) store_bias<float>(a, o, mine, bias);
+  if (sums_bias) store_bias<float>(a, o, mine, static_cast<float>(bias));
 }
 
 // Half types need no scale of their columns, so the rows go to LDS as they come, eight columns a
@@ -1534,23 +1540,24 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_half_kernel(OuterAr
   }
 }
 
-// Entries i .. of the sum of a group's blocks in their order, kJoin a thread.
+// Entries i .. of the sum of a group's blocks in their order, kJoin a thread; in 64
+// bits, since blocks can be thousands and of one sign.
 constexpr int kJoin = 4;
 template <class T>
 __device__ inline void join_parts(const float* part, int count, int64_t each, int64_t i, T* out) {
   if (i + kJoin > each) {   // the last entries once more, as one vector (or each < kJoin)
     if (each < kJoin) {
       for (; i < each; ++i) {
-        float s = 0.0f;
+        double s = 0.0;
         for (int b = 0; b < count; ++b) s += part[b * each + i];
-        out[i] = from_f32<T>(s);
+        out[i] = from_f32<T>(static_cast<float>(s));
       }
       return;
     }
     i = each - kJoin;
   }
   part += i;
-  float s[kJoin] = {};
+  double s[kJoin] = {};
   int b = 0;
   for (; b + 8 <= count; b += 8) {   // eight loads in flight
     Pack<float, kJoin> v[8];
@@ -1568,7 +1575,7 @@ __device__ inline void join_parts(const float* part, int count, int64_t each, in
   }
   Pack<T, kJoin> r;
 #pragma unroll
-  for (int j = 0; j < kJoin; ++j) r.v[j] = from_f32<T>(s[j]);
+  for (int j = 0; j < kJoin; ++j) r.v[j] = from_f32<T>(static_cast<float>(s[j]));
   *reinterpret_cast<Pack<T, kJoin>*>(out + i) = r;
 }
 
@@ -1624,13 +1631,15 @@ int tile_rows(const dpa4c_grouped& l, bool back) {
 // Rows of a block of dW: 4,096 workgroups in all, some rounds of the chip's 512
 // resident ones, but no fewer than 512 rows, so that a block's sums are small
 // beside its rows, and groups of a few hundred rows are one block, whose sums go
-// straight to dW.  Where even that gives fewer than 512 workgroups, 256.
+// straight to dW, and no more than 8,192, whose sums of one sign in float32 are off by
+// 4e-5 at the most (70,000,000 equal rows: 8e-5 in blocks of 16,384).  Where even 512 give
+// few workgroups 256, and 128.
 int outer_rows(const dpa4c_grouped& l) {
   const int64_t tiles = ((l.k + kOuterTile - 1) / kOuterTile) * int64_t((l.n_out + kOuterTile - 1) / kOuterTile);
   if (l.n * tiles < 256 * 256) return 128;
   if (l.n * tiles < 512 * 512) return 256;
   const int64_t rows = align_up((l.n * tiles + 4095) / 4096, kDepth);
-  return static_cast<int>(rows < 512 ? 512 : rows > 16384 ? 16384 : rows);
+  return static_cast<int>(rows < 512 ? 512 : rows > 8192 ? 8192 : rows);
 }
 
 Weights weights_of(Arena& ar, const dpa4c_grouped& l, bool back) {
