@@ -127,13 +127,15 @@ __device__ inline void list_tiles(const TileList& tl, const int64_t* ptr, int n_
 // Weights as the product tile reads them
 // ---------------------------------------------------------------------------
 
-// [group][step of 32][plane][columns padded to 128][32 entries], and for
-// float32 the exponent of each column
+// [set][step of 32][plane][columns padded to 128][32 entries], and for float32 the
+// exponent of each column.  A set for every group or, with fewer rows than groups, for
+// every row: that of a group with rows is then the place of its first one.
 struct Weights {
   char* planes;
   int32_t* exps;
-  int steps, cols_pad, planes_n;
+  int steps, cols_pad, planes_n, by_start;
   __host__ __device__ int64_t step_bytes() const { return int64_t(planes_n) * cols_pad * kRowBytes; }
+  __device__ int64_t set_of(int group, int64_t begin) const { return by_start ? begin : group; }
 };
 
 struct PrepArgs {
@@ -168,6 +170,7 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
   const Span s = span_of(a.ptr, g, a.n_groups, a.n);
   if (s.begin == s.end) return;
   const T* w = static_cast<const T*>(a.w) + int64_t(g) * a.depth * a.cols;
+  const int64_t set = a.out.set_of(g, s.begin);
   constexpr bool kSplit = sizeof(T) == 4;
   __shared__ float most[kPrepThreads / kPrepCols][kPrepCols];
   __shared__ int32_t exps[kPrepCols];
@@ -203,7 +206,7 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
         hi[j] = unsigned(__builtin_bit_cast(unsigned short, f[2 * j])) |
                 unsigned(__builtin_bit_cast(unsigned short, f[2 * j + 1])) << 16;
     }
-    char* to = a.out.planes + (int64_t(g) * a.out.steps + sl / kSlots) * a.out.step_bytes() +
+    char* to = a.out.planes + (set * a.out.steps + sl / kSlots) * a.out.step_bytes() +
                slot_at(c, sl % kSlots);
     *reinterpret_cast<u4*>(to) = hi;
     if (kSplit) *reinterpret_cast<u4*>(to + int64_t(a.out.cols_pad) * kRowBytes) = lo;
@@ -238,7 +241,7 @@ __device__ inline void lay_weights(const PrepArgs& a, int g, int c0) {
       for (int i = 0; i < 16; ++i) top = fmaxf(top, most[i][threadIdx.x]);
       const int e = top > 0.0f ? exp_for(top) : 0;
       exps[threadIdx.x] = e;
-      a.out.exps[int64_t(g) * a.out.cols_pad + c0 + threadIdx.x] = e;
+      a.out.exps[set * a.out.cols_pad + c0 + threadIdx.x] = e;
     }
     __syncthreads();
     scale = exp2_of(exps[r]);
@@ -617,8 +620,9 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
   }
   const int64_t in_plane = a.n * a.ldin * bytes_of<S>;
   // laid out: from c0 of the first step; as they are: of the group
+  const int64_t set = a.w.set_of(t.group, t.first - int64_t(t.part) * kTile);
   const char* wsrc =
-      W == kLaid ? a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes
+      W == kLaid ? a.w.planes + set * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes
                  : static_cast<const char*>(a.weight) + int64_t(t.group) * a.kin * a.kout * sizeof(T);
   const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
   // kColumns: this thread's NB columns (rows of W, as those of ``in``); columns past
@@ -835,7 +839,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     bq[j] = bias && c + j < a.kout ? to_f32(bias[c + j]) : 0.0f;
-    if (S == kFloat) eq[j] = a.w.exps[int64_t(t.group) * a.w.cols_pad + c + j];
+    if (S == kFloat) eq[j] = a.w.exps[set * a.w.cols_pad + c + j];
   }
   const bool whole = c + 4 <= a.kout;
 #pragma unroll 1
@@ -960,7 +964,8 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
     last = last_of(a.n, a.ldin, a.by_place ? static_cast<int>(a.ldin) : a.kin, row);
   }
   const int64_t in_plane = a.n * a.ldin * bytes_of<S>;
-  const char* wsrc = a.w.planes + int64_t(t.group) * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
+  const int64_t set = a.w.set_of(t.group, t.first - int64_t(t.part) * kWideRows);
+  const char* wsrc = a.w.planes + set * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
   const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
 
   constexpr int kFar = 2;
@@ -1155,7 +1160,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
     if (j >= mine) continue;
     const int c = c0 + (wn + 4 * j) * 32 + (lane & 31);
     const float bv = bias ? to_f32(bias[c < a.kout ? c : a.kout - 1]) : 0.0f;
-    const int ec = S == kFloat ? a.w.exps[int64_t(t.group) * a.w.cols_pad + c] : 0;
+    const int ec = S == kFloat ? a.w.exps[set * a.w.cols_pad + c] : 0;
     fetch_residual(Const<1>{}, 1, j);
     store(Const<0>{}, j, acc[0][j], bv, ec);
     fetch_residual(Const<0>{}, 0, j + 1);
@@ -1166,6 +1171,17 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
 // ---------------------------------------------------------------------------
 // Gradients of the weights
 // ---------------------------------------------------------------------------
+
+// The slot of a block's sums: its number or, where that takes less room, the number that
+// its group would start at in blocks of half as many rows, and on from there.  Groups of
+// several blocks, P over more than (P - 1) ``rows`` places, then do not meet, and end
+// below 2 n / rows.
+struct Slots {
+  int rows, by_start;
+  __host__ __device__ int64_t of(int64_t begin, int part) const {
+    return static_cast<uint32_t>(2 * begin) / static_cast<uint32_t>(rows) + int64_t(part);
+  }
+};
 
 struct OuterArgs {
   const int32_t* order;
@@ -1181,8 +1197,9 @@ struct OuterArgs {
   const int32_t* dz_exps;   // row_scaled: the rows' exponents, by place
   void* dw;           // null: not formed
   void* db;
-  float* parts;       // [block][k][m] where a group has several blocks
-  float* db_parts;    // [block][m]
+  float* parts;       // [slot][k][m] where a group has several blocks
+  float* db_parts;    // [slot][m]
+  Slots slots;
 };
 
 constexpr int kOuterTile = kSide<2>;
@@ -1191,7 +1208,7 @@ constexpr int kOuterTile = kSide<2>;
 // false past the last
 struct OuterTile {
   RowTile t;
-  int64_t block;
+  int64_t slot;
   int r0, c0;
 };
 __device__ inline bool outer_tile(const OuterArgs& a, OuterTile& o) {
@@ -1201,8 +1218,9 @@ __device__ inline bool outer_tile(const OuterArgs& a, OuterTile& o) {
   if (blockIdx.x >= total) return false;
   // the tiles of a block of rows follow each other on one XCD
   const int64_t work = xcd_block(blockIdx.x, total);
-  o.block = work / (row_tiles * col_tiles);
-  o.t = a.blocks[o.block];
+  const int64_t block = work / (row_tiles * col_tiles);
+  o.t = a.blocks[block];
+  o.slot = a.slots.by_start ? a.slots.of(o.t.first - int64_t(o.t.part) * a.slots.rows, o.t.part) : block;
   o.r0 = static_cast<int>(work / col_tiles % row_tiles) * kOuterTile;
   o.c0 = static_cast<int>(work % col_tiles) * kOuterTile;
   return true;
@@ -1216,7 +1234,7 @@ __device__ inline void store_outer(const OuterArgs& a, const OuterTile& o, const
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1;
   const bool whole = o.t.parts == 1;
   T* dw = static_cast<T*>(a.dw) + int64_t(o.t.group) * a.k * a.m;
-  float* part = a.parts + o.block * a.k * a.m;
+  float* part = a.parts + o.slot * a.k * a.m;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -1242,7 +1260,7 @@ __device__ inline void store_bias(const OuterArgs& a, const OuterTile& o, int co
   if (o.t.parts == 1)
     static_cast<T*>(a.db)[int64_t(o.t.group) * a.m + o.c0 + col] = from_f32<T>(v);
   else
-    a.db_parts[o.block * a.m + o.c0 + col] = v;
+    a.db_parts[o.slot * a.m + o.c0 + col] = v;
 }
 
 // float32.  A wave fetches 64 columns of one operand, so a lane has a column of a
@@ -1584,14 +1602,16 @@ __device__ inline void join_parts(const float* part, int count, int64_t each, in
 // 203 MB in 54 us), by its launch else (4,000 rows: 8 us).
 template <class T>
 __global__ void __launch_bounds__(kThreads) grouped_join_kernel(const int32_t* __restrict__ first_of,
-                                                                int64_t each_w, int64_t each_b,
+                                                                const int64_t* __restrict__ ptr, int64_t n,
+                                                                Slots slots, int64_t each_w, int64_t each_b,
                                                                 const float* __restrict__ parts_w,
                                                                 const float* __restrict__ parts_b,
                                                                 T* __restrict__ dw, T* __restrict__ db) {
   const int g = blockIdx.y;
-  const int64_t first = first_of[g];
-  const int count = static_cast<int>(first_of[g + 1] - first);
+  const int64_t begin = clamp_place(ptr[g], n);   // beside the loads of first_of
+  const int count = first_of[g + 1] - first_of[g];
   if (count < 2) return;
+  const int64_t first = slots.by_start ? slots.of(begin, 0) : first_of[g];
   int64_t i = (int64_t(blockIdx.x) * kThreads + threadIdx.x) * kJoin;
   const int64_t of_w = dw ? align_up(each_w, kJoin) : 0;
   if (i < of_w)
@@ -1648,9 +1668,11 @@ Weights weights_of(Arena& ar, const dpa4c_grouped& l, bool back) {
   w.steps = (depth + kDepth - 1) / kDepth;
   w.cols_pad = static_cast<int>(align_up(cols, kPad));
   w.planes_n = l.dtype == DPA4C_F32 ? 2 : 1;
+  w.by_start = l.n < l.n_groups;
   if (!laid_out(l)) return w;
-  w.planes = ar.take<char>(int64_t(l.n_groups) * w.steps * w.step_bytes());
-  w.exps = ar.take<int32_t>(l.dtype == DPA4C_F32 ? int64_t(l.n_groups) * w.cols_pad : 0);
+  const int64_t sets = std::min<int64_t>(l.n, l.n_groups);
+  w.planes = ar.take<char>(sets * w.steps * w.step_bytes());
+  w.exps = ar.take<int32_t>(l.dtype == DPA4C_F32 ? sets * w.cols_pad : 0);
   return w;
 }
 
@@ -1708,6 +1730,7 @@ struct BackwardPlan {
   void *dz, *wide;
   int32_t* dz_exps;
   float *parts, *db_parts;
+  Slots slots;
 };
 BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
@@ -1719,9 +1742,11 @@ BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
   p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
   p.dz_exps = ar.take<int32_t>(l.dtype == DPA4C_F16 ? l.n : 0);
   p.wide = ar.take<char>(wide_bytes(l));
-  const int64_t blocks = tiles_at_most(l.n, l.n_groups, rows);
-  p.parts = ar.take<float>(blocks * l.k * l.n_out);
-  p.db_parts = ar.take<float>(blocks * l.n_out);
+  // only groups of more than ``rows`` rows have several blocks
+  const int64_t blocks = tiles_at_most(l.n, l.n_groups, rows), ends = l.n > rows ? (2 * l.n + rows - 1) / rows : 0;
+  p.slots = {rows, ends < blocks};
+  p.parts = ar.take<float>(std::min(blocks, ends) * l.k * l.n_out);
+  p.db_parts = ar.take<float>(std::min(blocks, ends) * l.n_out);
   *bytes = ar.used;
   return p;
 }
@@ -1799,7 +1824,7 @@ int run_outer(const dpa4c_grouped& l, const OuterArgs& a, const TileList& blocks
   const int64_t each_w = int64_t(l.k) * l.n_out;
   const int64_t all = (a.dw ? align_up(each_w, kJoin) : 0) + (a.db ? l.n_out : 0);
   const dim3 grid((all + kThreads * kJoin - 1) / (kThreads * kJoin), l.n_groups);
-  grouped_join_kernel<T><<<grid, kThreads, 0, st>>>(blocks.first_of, each_w, l.n_out, a.parts, a.db_parts,
+  grouped_join_kernel<T><<<grid, kThreads, 0, st>>>(blocks.first_of, l.group_ptr, l.n, a.slots, each_w, l.n_out, a.parts, a.db_parts,
                                                     static_cast<T*>(a.dw), static_cast<T*>(a.db));
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
@@ -1939,6 +1964,7 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
       a.db = db;
       a.parts = p.parts;
       a.db_parts = p.db_parts;
+      a.slots = p.slots;
       DPA4C_TRY(run_outer<T>(l, a, p.blocks, st));
     }
     return 0;
