@@ -441,6 +441,9 @@ int dpa4c_grouped_linear(const dpa4c_grouped* layer, const void* bias, int activ
  * 2^-39 of the largest finite dz, of its row for dx and db and of its group for dW.
  */
 int dpa4c_grouped_linear_backward_work(const dpa4c_grouped* layer, int64_t* bytes);
+/* what a call needs that has z, dx, dw and db (non-zero) or NULL in their place; the above is with all */
+int dpa4c_grouped_linear_backward_work_of(const dpa4c_grouped* layer, int z, int dx, int dw, int db,
+                                          int64_t* bytes);
 int dpa4c_grouped_linear_backward(const dpa4c_grouped* layer, const void* dy, int64_t ldy,
                                   const void* z, int64_t ldz, int residual, void* dx, void* dw,
                                   void* db, void* work, int64_t work_bytes, void* stream);

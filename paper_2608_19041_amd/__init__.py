@@ -71,6 +71,7 @@ def library():
             "dpa4c_grouped_linear_work": (i32, [vp, vp]),
             "dpa4c_grouped_linear": (i32, [vp, vp, i32, i32, vp, vp, vp, i64, vp]),
             "dpa4c_grouped_linear_backward_work": (i32, [vp, vp]),
+            "dpa4c_grouped_linear_backward_work_of": (i32, [vp, i32, i32, i32, i32, vp]),
             "dpa4c_grouped_linear_backward": (i32, [vp, vp, i64, vp, i64, i32, vp, vp, vp, vp, i64,
                                                     vp]),
             "dpa4c_orthogonalize_work": (i32, [i32, vp, vp]),
@@ -95,7 +96,7 @@ def exported_symbols() -> list[str]:
             "dpa4c_get_timings", "dpa4c_stage_name", "dpa4c_debug_gemm",
             "dpa4c_group_rows_work", "dpa4c_group_rows", "dpa4c_grouped_linear_work",
             "dpa4c_grouped_linear", "dpa4c_grouped_linear_backward_work",
-            "dpa4c_grouped_linear_backward", "dpa4c_orthogonalize_work", "dpa4c_orthogonalize",
+            "dpa4c_grouped_linear_backward_work_of", "dpa4c_grouped_linear_backward", "dpa4c_orthogonalize_work", "dpa4c_orthogonalize",
             "dpa4c_muon_step_work", "dpa4c_muon_step", "dpa4c_last_error"]
 
 

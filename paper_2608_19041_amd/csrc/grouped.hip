@@ -1732,21 +1732,26 @@ struct BackwardPlan {
   float *parts, *db_parts;
   Slots slots;
 };
-BackwardPlan plan_backward(const dpa4c_grouped& l, void* work, int64_t* bytes) {
+// dz is formed, by place
+bool makes_dz(const dpa4c_grouped& l, bool z) { return l.n > 0 && (z || l.n_out < kLeastWidth); }
+BackwardPlan plan_backward(const dpa4c_grouped& l, const Wanted& want, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
-  BackwardPlan p;
-  p.w = weights_of(ar, l, true);
-  p.tiles = list_of(ar, l, tile_rows(l, true), true);
+  BackwardPlan p{};
+  const bool outer = want.dw || want.db, made = makes_dz(l, want.z) && (want.dx || outer);
+  if (want.dx) {
+    p.w = weights_of(ar, l, true);
+    p.tiles = list_of(ar, l, tile_rows(l, true), true);
+  }
   const int rows = outer_rows(l);
-  p.blocks = list_of(ar, l, rows, false);
-  p.dz = ar.take<float>(l.n * pitch_of(l));   // or two planes of a half type
-  p.dz_exps = ar.take<int32_t>(l.dtype == DPA4C_F16 ? l.n : 0);
-  p.wide = ar.take<char>(wide_bytes(l));
+  if (outer) p.blocks = list_of(ar, l, rows, false);
+  p.dz = ar.take<float>(made ? l.n * pitch_of(l) : 0);   // or two planes of a half type
+  p.dz_exps = ar.take<int32_t>(made && l.dtype == DPA4C_F16 ? l.n : 0);
+  p.wide = ar.take<char>(outer ? wide_bytes(l) : 0);
   // only groups of more than ``rows`` rows have several blocks
   const int64_t blocks = tiles_at_most(l.n, l.n_groups, rows), ends = l.n > rows ? (2 * l.n + rows - 1) / rows : 0;
   p.slots = {rows, ends < blocks};
-  p.parts = ar.take<float>(std::min(blocks, ends) * l.k * l.n_out);
-  p.db_parts = ar.take<float>(std::min(blocks, ends) * l.n_out);
+  p.parts = ar.take<float>(want.dw ? std::min(blocks, ends) * l.k * l.n_out : 0);
+  p.db_parts = ar.take<float>(want.db ? std::min(blocks, ends) * l.n_out : 0);
   *bytes = ar.used;
   return p;
 }
@@ -1849,9 +1854,9 @@ int64_t grouped_forward_work(const dpa4c_grouped& l) {
   return bytes;
 }
 
-int64_t grouped_backward_work(const dpa4c_grouped& l) {
+int64_t grouped_backward_work(const dpa4c_grouped& l, const Wanted& want) {
   int64_t bytes;
-  plan_backward(l, nullptr, &bytes);
+  plan_backward(l, want, nullptr, &bytes);
   return bytes;
 }
 
@@ -1896,9 +1901,9 @@ int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy,
     using T = typename Elem<decltype(d)::value>::T;
     constexpr Source kOwn = sizeof(T) == 4 ? kFloat : kHalf, kMade = sizeof(T) == 4 ? kFloat : kPair;
     int64_t bytes;
-    const BackwardPlan p = plan_backward(l, work, &bytes);
+    const BackwardPlan p = plan_backward(l, {z != nullptr, dx != nullptr, dw != nullptr, db != nullptr}, work, &bytes);
     const int pitch = pitch_of(l);
-    const bool made = l.n > 0 && (z || l.n_out < kLeastWidth);   // dz is formed, by place
+    const bool made = makes_dz(l, z);
     PrepArgs pre = prepare_args<true>(l, rows ? &p.w : nullptr, rows ? &p.tiles : nullptr,
                                       outer ? &p.blocks : nullptr);
     if (outer) {

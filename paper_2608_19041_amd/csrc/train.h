@@ -37,7 +37,10 @@ bool grouped_fits(const dpa4c_grouped& l);   // every launch of either direction
 int64_t grouped_forward_work(const dpa4c_grouped& l);
 int launch_grouped_forward(const dpa4c_grouped& l, const void* bias, bool silu, bool residual,
                            void* y, void* z, void* work, hipStream_t st);
-int64_t grouped_backward_work(const dpa4c_grouped& l);
+struct Wanted {   // of a backward call: whether z is given and what is formed
+  bool z, dx, dw, db;
+};
+int64_t grouped_backward_work(const dpa4c_grouped& l, const Wanted& want);
 int launch_grouped_backward(const dpa4c_grouped& l, const void* dy, int64_t ldy, const void* z,
                             int64_t ldz, bool residual, void* dx, void* dw, void* db, void* work,
                             hipStream_t st);

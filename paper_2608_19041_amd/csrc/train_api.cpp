@@ -155,7 +155,17 @@ int dpa4c_grouped_linear_backward_work(const dpa4c_grouped* layer, int64_t* byte
   return guarded([&] {
     DPA4C_TRY(check_layer("dpa4c_grouped_linear_backward_work", layer, false));
     if (!bytes) return invalid("dpa4c_grouped_linear_backward_work: null pointer");
-    *bytes = grouped_backward_work(*layer);
+    *bytes = grouped_backward_work(*layer, {true, true, true, true});
+    return 0;
+  });
+}
+
+int dpa4c_grouped_linear_backward_work_of(const dpa4c_grouped* layer, int z, int dx, int dw, int db,
+                                          int64_t* bytes) {
+  return guarded([&] {
+    DPA4C_TRY(check_layer("dpa4c_grouped_linear_backward_work_of", layer, false));
+    if (!bytes) return invalid("dpa4c_grouped_linear_backward_work_of: null pointer");
+    *bytes = grouped_backward_work(*layer, {z != 0, dx != 0, dw != 0, db != 0});
     return 0;
   });
 }
@@ -171,7 +181,8 @@ int dpa4c_grouped_linear_backward(const dpa4c_grouped* layer, const void* dy, in
     if (layer->n > 0 && !dy) return invalid("dpa4c_grouped_linear_backward: null pointer");
     if ((ldy != 0 && ldy < layer->n_out) || (z && ldz != 0 && ldz < layer->n_out))
       return invalid("dpa4c_grouped_linear_backward: ldy or ldz below n_out");
-    DPA4C_TRY(check_work(who, work, work_bytes, grouped_backward_work(*layer)));
+    const Wanted want{z != nullptr, dx != nullptr, dw != nullptr, db != nullptr};
+    DPA4C_TRY(check_work(who, work, work_bytes, grouped_backward_work(*layer, want)));
     return launch_grouped_backward(*layer, dy, ldy, z, ldz, residual != 0, dx, dw, db, work,
                                    static_cast<hipStream_t>(stream));
   });

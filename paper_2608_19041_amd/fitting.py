@@ -215,8 +215,8 @@ def grouped_linear_backward(dy, x, weight, group_ptr, order=None, preact=None, r
     ldz = 0 if preact is None else _rows(preact, weight.dtype, (n, m), dev, "preact")
     lib = library()
     with _launch(dev, stream) as st:
-        work, size = _scratch(
-            dev, lambda want: lib.dpa4c_grouped_linear_backward_work(ctypes.byref(layer), want))
+        work, size = _scratch(dev, lambda size: lib.dpa4c_grouped_linear_backward_work_of(
+            ctypes.byref(layer), preact is not None, *(bool(w) for w in need), size))
         dx = torch.empty(n, layer.k, dtype=weight.dtype, device=dev) if need[0] else None
         dw = torch.empty_like(weight) if need[1] else None
         db = torch.empty(layer.n_groups, m, dtype=weight.dtype, device=dev) if need[2] else None

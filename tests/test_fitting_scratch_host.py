@@ -43,3 +43,28 @@ def test_scratch_is_what_rows_can_use(n, k, m, groups, dtype):
     dz = n * (up(m, 8) * 4 + 4)
     blocks = 2 * n // 128 + 1 if n > 128 else 0
     assert backward <= planes(n, m, k, groups, dtype) + widened + dz + blocks * (k + 1) * m * 4 + 8 * groups
+
+
+def test_scratch_of_what_is_formed():
+    lib, need, n, k, m = dp.library(), ctypes.c_int64(-1), 20000, 384, 256
+    l = layer(n, k, m, 118)
+
+    def of(*want):
+        assert lib.dpa4c_grouped_linear_backward_work_of(ctypes.byref(l), *want, ctypes.byref(need)) == 0
+        return need.value
+
+    assert lib.dpa4c_grouped_linear_backward_work(ctypes.byref(l), ctypes.byref(need)) == 0
+    assert need.value == of(1, 1, 1, 1)
+    weights, dz = 118 * k * m * 4, n * m * 4
+    assert of(1, 1, 0, 0) >= weights + dz
+    assert of(0, 1, 0, 0) < weights + 8 * n + 2 ** 20          # no dz, no sums of blocks
+    assert dz < of(1, 0, 0, 1) < dz + 2 ** 20                  # no weights, no sums of dW
+    assert of(0, 0, 0, 1) < 2 ** 20 and of(1, 0, 0, 0) < 2 ** 10
+    assert of(1, 0, 1, 0) < dz + 2 * n // 128 * k * m * 4 + 2 ** 20
+    # a call takes what it needs, and no less
+    some = of(0, 1, 0, 0)
+    back = lib.dpa4c_grouped_linear_backward
+    assert back(ctypes.byref(l), 256, m, None, 0, 0, 256, None, None, 256, some - 1, None) == dp.ERR_INVALID_ARG
+    assert back(ctypes.byref(l), 256, m, 256, m, 0, 256, None, None, 256, some, None) == dp.ERR_INVALID_ARG
+    assert lib.dpa4c_grouped_linear_backward_work_of(ctypes.byref(l), 1, 1, 1, 1, None) == dp.ERR_INVALID_ARG
+    assert lib.dpa4c_grouped_linear_backward_work_of(None, 1, 1, 1, 1, ctypes.byref(need)) == dp.ERR_INVALID_ARG
