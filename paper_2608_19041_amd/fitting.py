@@ -6,7 +6,9 @@ the weights (the Muon optimiser).  Argument marshalling only, as in the rest
 of the binding: every step runs in the HIP kernels of the library, on the
 caller's stream, and scratch comes from torch's allocator on that stream.
 Nothing here is recorded by autograd: a layer's gradients come from
-``grouped_linear_backward``.
+``grouped_linear_backward``, and tensors that autograd would have to follow are
+refused (where it records, i.e. not under ``torch.no_grad()`` or within the
+methods of a ``torch.autograd.Function``).
 
     ptr, order = group_rows(species, 118)
     y, z = grouped_linear(x, w, ptr, order, bias=b, activation="silu", preact=True)
@@ -86,6 +88,16 @@ def _same(t, dtype, shape, device, name):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} must be on {device}")
+
+
+def _unrecorded(**tensors):
+    """Refuses tensors whose gradients autograd would silently lose here."""
+    import torch
+    if torch.is_grad_enabled():
+        for name, t in tensors.items():
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{name} requires a gradient, which nothing here records: "
+                                 "call under torch.no_grad() or detach it")
 
 
 class _launch:
@@ -187,6 +199,7 @@ def grouped_linear(x, weight, group_ptr, order=None, bias=None, activation=None,
         raise ValueError("a residual needs as many outputs as inputs")
     if bias is not None:
         _same(bias, weight.dtype, (layer.n_groups, layer.n_out), weight.device, "bias")
+    _unrecorded(x=x, weight=weight, bias=bias)
     lib = library()
     with _launch(weight.device, stream) as st:
         work, size = _scratch(weight.device,
@@ -213,6 +226,7 @@ def grouped_linear_backward(dy, x, weight, group_ptr, order=None, preact=None, r
         raise ValueError("a residual needs as many outputs as inputs")
     ldy = _rows(dy, weight.dtype, (n, m), dev, "dy")
     ldz = 0 if preact is None else _rows(preact, weight.dtype, (n, m), dev, "preact")
+    _unrecorded(dy=dy, x=x, weight=weight, preact=preact)
     lib = library()
     with _launch(dev, stream) as st:
         work, size = _scratch(dev, lambda size: lib.dpa4c_grouped_linear_backward_work_of(
@@ -273,6 +287,8 @@ def orthogonalize(matrices, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps:
     matrices = _stack_list("matrices", matrices)
     if not matrices:
         return []
+    for t in matrices:
+        _unrecorded(matrices=t)
     how, lib, dev = _newton(steps, coefficients, eps), library(), matrices[0].device
     code = _dtype_code(matrices[0], "matrices")
     with _launch(dev, stream) as st:
@@ -293,7 +309,8 @@ def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nestero
     M <- momentum M + G; U = G + momentum M (``nesterov``) or M;
     W <- (1 - lr weight_decay) W - lr sqrt(max(1, cols / rows)) NS(U).
     ``params``, ``grads``: lists of contiguous matrices or stacks of one type;
-    ``momenta``: float32 tensors of the same shapes.
+    ``momenta``: float32 tensors of the same shapes.  As an optimiser's step does,
+    this writes parameters that require a gradient; autograd notices the write.
     """
     import torch
     params, grads, momenta = _stack_list("params", params), list(grads), list(momenta)
@@ -311,6 +328,7 @@ def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nestero
         calls = _calls(_Update, params, grads, momenta)
         work, size = _scratch(dev, *(
             functools.partial(lib.dpa4c_muon_step_work, len(c), c) for c in calls))
+        torch.autograd.graph.increment_version(params + momenta)
         for c in calls:
             _check(lib.dpa4c_muon_step(code, len(c), c, ctypes.byref(how), float(lr),
                                        float(momentum), int(bool(nesterov)), float(weight_decay),
