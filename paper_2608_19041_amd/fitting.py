@@ -59,6 +59,11 @@ def _codes():
     return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 
+def _int(v):
+    """``v`` as the library takes it: beyond 32 bits the nearest, which it refuses."""
+    return max(-2 ** 31, min(int(v), 2 ** 31 - 1))
+
+
 def _dtype_code(t, name):
     import torch
     code = _codes().get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
@@ -151,14 +156,14 @@ def group_rows(group, n_groups: int, stream=None):
     _require(group, torch.int32, None, "group")
     if group.dim() != 1:
         raise ValueError("group must have one dimension")
-    n, lib = group.shape[0], library()
+    n, n_groups, lib = group.shape[0], _int(n_groups), library()
     with _launch(group.device, stream) as st:
         work, size = _scratch(group.device,
-                              lambda need: lib.dpa4c_group_rows_work(n, int(n_groups), need))
-        ptr = torch.empty(int(n_groups) + 1, dtype=torch.int64, device=group.device)
+                              lambda need: lib.dpa4c_group_rows_work(n, n_groups, need))
+        ptr = torch.empty(n_groups + 1, dtype=torch.int64, device=group.device)
         order = torch.empty(n, dtype=torch.int32, device=group.device)
-        _check(lib.dpa4c_group_rows(_ptr(group), n, int(n_groups), _ptr(ptr), _ptr(order),
-                                    _ptr(work), size, st))
+        _check(lib.dpa4c_group_rows(_ptr(group), n, n_groups, _ptr(ptr), _ptr(order), _ptr(work), size,
+                                    st))
     return ptr, order
 
 
@@ -175,7 +180,7 @@ def _layer(x, weight, group_ptr, order):
     _same(group_ptr, torch.int64, (groups + 1,), weight.device, "group_ptr")
     if order is not None:
         _same(order, torch.int32, (n,), weight.device, "order")
-    return _Grouped(code, groups, k, n_out, n, group_ptr.data_ptr(),
+    return _Grouped(code, _int(groups), _int(k), _int(n_out), n, group_ptr.data_ptr(),
                     None if order is None else order.data_ptr(), x.data_ptr(), ldx,
                     weight.data_ptr())
 
@@ -260,7 +265,7 @@ def _stack_list(name, tensors):
 def _shape(t):
     """batch, rows, cols of a matrix or a stack of them"""
     *batch, rows, cols = t.shape
-    return math.prod(batch), rows, cols
+    return math.prod(batch), _int(rows), _int(cols)
 
 
 def _calls(struct, *tensors):
@@ -272,7 +277,7 @@ def _calls(struct, *tensors):
 
 def _newton(steps, coefficients, eps):
     a, b, c = (float(v) for v in coefficients)
-    return _Newton(int(steps), a, b, c, float(eps))
+    return _Newton(_int(steps), a, b, c, float(eps))
 
 
 def orthogonalize(matrices, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps: float = 1e-7,

@@ -1,0 +1,19 @@
+"""Sizes beyond 32 bits reach the library as sizes that it refuses (no GPU)."""
+import ctypes
+
+import torch
+
+import paper_2608_19041_amd as dp
+from paper_2608_19041_amd import fitting as ft
+
+
+def test_sizes_beyond_32_bits():
+    lib, need = dp.library(), ctypes.c_int64(-1)
+    for shape in ((2 ** 32 + 8, 1), (3, 5, 2 ** 32 + 8)):
+        stack = (ft._Stack * 1)(ft._Stack(256, 256, *ft._shape(torch.empty(shape, device="meta"))))
+        assert lib.dpa4c_orthogonalize_work(1, stack, ctypes.byref(need)) == dp.ERR_INVALID_ARG
+    stack = (ft._Stack * 1)(ft._Stack(256, 256, *ft._shape(torch.empty(2, 5, 6, device="meta"))))
+    assert (stack[0].batch, stack[0].rows, stack[0].cols) == (2, 5, 6)
+    for steps in (2 ** 32 + 5, -2 ** 32 + 5):
+        how = ft._newton(steps, ft.MUON_COEFFICIENTS, 1e-7)
+        assert lib.dpa4c_orthogonalize(0, 1, stack, ctypes.byref(how), 256, 1 << 40, None) == dp.ERR_INVALID_ARG
