@@ -61,7 +61,8 @@ def _codes():
 
 def _int(v):
     """``v`` as the library takes it: beyond 32 bits the nearest, which it refuses."""
-    return max(-2 ** 31, min(int(v), 2 ** 31 - 1))
+    v = int(v)
+    return v if -2 ** 31 <= v < 2 ** 31 else (2 ** 31 - 1 if v > 0 else -2 ** 31)
 
 
 def _dtype_code(t, name):
@@ -265,12 +266,17 @@ def _stack_list(name, tensors):
 def _shape(t):
     """batch, rows, cols of a matrix or a stack of them"""
     *batch, rows, cols = t.shape
-    return math.prod(batch), _int(rows), _int(cols)
+    return math.prod(batch), rows if rows < 2 ** 31 else _int(rows), cols if cols < 2 ** 31 else _int(cols)
 
 
-def _calls(struct, *tensors):
-    """The matching tensors of all lists as arrays of ``struct``, MAX_STACKS at a time."""
-    every = [struct(*(t.data_ptr() for t in ts), *_shape(ts[0])) for ts in zip(*tensors)]
+def _pointers(tensors):
+    """Where the tensors are; 0 for those without entries."""
+    return [t.data_ptr() for t in tensors]
+
+
+def _calls(struct, tensors, *pointers):
+    """Tensors of these shapes at the matching pointers as arrays of ``struct``, MAX_STACKS at a time."""
+    every = [struct(*at, *_shape(t)) for t, *at in zip(tensors, *pointers)]
     return [(struct * len(part))(*part)
             for part in (every[at:at + MAX_STACKS] for at in range(0, len(every), MAX_STACKS))]
 
@@ -298,7 +304,7 @@ def orthogonalize(matrices, steps: int = 5, coefficients=MUON_COEFFICIENTS, eps:
     code = _dtype_code(matrices[0], "matrices")
     with _launch(dev, stream) as st:
         out = [torch.empty_like(t) for t in matrices]
-        calls = _calls(_Stack, matrices, out)
+        calls = _calls(_Stack, matrices, _pointers(matrices), _pointers(out))
         work, size = _scratch(dev, *(
             functools.partial(lib.dpa4c_orthogonalize_work, len(c), c) for c in calls))
         for c in calls:
@@ -314,7 +320,7 @@ def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nestero
     M <- momentum M + G; U = G + momentum M (``nesterov``) or M;
     W <- (1 - lr weight_decay) W - lr sqrt(max(1, cols / rows)) NS(U).
     ``params``, ``grads``: lists of contiguous matrices or stacks of one type;
-    ``momenta``: float32 tensors of the same shapes.  As an optimiser's step does,
+    ``momenta``: float32 tensors of the same shapes; each tensor once.  As an optimiser's step does,
     this writes parameters that require a gradient; autograd notices the write.
     """
     import torch
@@ -327,10 +333,15 @@ def muon_step(params, grads, momenta, lr: float, momentum: float = 0.95, nestero
     for w, g, m in zip(params, grads, momenta):
         _same(g, w.dtype, w.shape, dev, "grads")
         _same(m, torch.float32, w.shape, dev, "momenta")
+    # all matrices are updated together: one listed twice would be written by both
+    at_w, at_g, at_m = (_pointers(ts) for ts in (params, grads, momenta))
+    written = [p for p in at_w + at_m if p]
+    if len(set(written)) < len(written) or not set(at_m).isdisjoint(filter(None, at_g)):
+        raise ValueError("params and momenta must not share memory with each other, nor momenta with grads")
     how, lib, code = _newton(steps, coefficients, eps), library(), _dtype_code(params[0], "params")
     with _launch(dev, stream) as st:
         # the sizes of all calls are checked before the first changes a weight
-        calls = _calls(_Update, params, grads, momenta)
+        calls = _calls(_Update, params, at_w, at_g, at_m)
         work, size = _scratch(dev, *(
             functools.partial(lib.dpa4c_muon_step_work, len(c), c) for c in calls))
         torch.autograd.graph.increment_version(params + momenta)
