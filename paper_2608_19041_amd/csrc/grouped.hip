@@ -288,10 +288,11 @@ constexpr int kLeastWidth = 8;
 template <class T>
 __global__ void __launch_bounds__(kThreads) grouped_widen_kernel(int64_t n, int width, const T* __restrict__ in,
                                                                  int64_t ld, T* __restrict__ out) {
-  const int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x;
-  if (i >= n * kLeastWidth) return;
-  const int c = static_cast<int>(i % kLeastWidth);
-  out[i] = c < width ? in[i / kLeastWidth * ld + c] : from_f32<T>(0.0f);
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n * kLeastWidth;
+       i += int64_t(gridDim.x) * kThreads) {
+    const int c = static_cast<int>(i % kLeastWidth);
+    out[i] = c < width ? in[i / kLeastWidth * ld + c] : from_f32<T>(0.0f);
+  }
 }
 
 // dz = dy act'(z) (z = null: dy) by place: float32 as it is, half types as a plane of their own
@@ -1702,7 +1703,8 @@ template <class T>
 int widen(const dpa4c_grouped& l, void* room, Input* in, hipStream_t st) {
   *in = {l.x, l.ldx};
   if (l.k >= kLeastWidth) return 0;
-  grouped_widen_kernel<T><<<(l.n * kLeastWidth + kThreads - 1) / kThreads, kThreads, 0, st>>>(
+  const int64_t grid = std::min<int64_t>((l.n * kLeastWidth + kThreads - 1) / kThreads, 1 << 20);
+  grouped_widen_kernel<T><<<grid, kThreads, 0, st>>>(
       l.n, l.k, static_cast<const T*>(l.x), l.ldx, static_cast<T*>(room));
   DPA4C_HIP_TRY(hipGetLastError());
   *in = {room, kLeastWidth};
@@ -1844,8 +1846,7 @@ bool grouped_fits(const dpa4c_grouped& l) {
                                                  up(int64_t(l.k) * l.n_out, kClear));
   const int64_t rows = tiles_at_most(l.n, l.n_groups, kSide<1>) * up(most, kSide<1>);
   const int64_t outer = tiles_at_most(l.n, l.n_groups, outer_rows(l)) * up(l.k, kOuterTile) * up(l.n_out, kOuterTile);
-  return grid_fits(prep, kPrepThreads) && grid_fits(rows, kThreads) && grid_fits(outer, kThreads) &&
-         grid_fits(up(l.n * kLeastWidth, kThreads), kThreads);
+  return grid_fits(prep, kPrepThreads) && grid_fits(rows, kThreads) && grid_fits(outer, kThreads);
 }
 
 int64_t grouped_forward_work(const dpa4c_grouped& l) {

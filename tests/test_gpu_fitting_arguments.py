@@ -33,3 +33,33 @@ def test_an_update_that_would_meet_itself():
     alone = before[0].clone(), before[3].clone()
     dp.muon_step([alone[0]], [g], [alone[1]], lr=0.1)
     assert torch.equal(alone[0], w) and torch.equal(alone[1], m)
+
+
+@pytest.mark.parametrize("k", [3, 8])
+def test_more_rows_than_2_to_the_29(k):
+    n, m, groups = 2 ** 29 + 77, 2, 2
+    x = torch.empty(n, k, dtype=torch.bfloat16, device="cuda").normal_()
+    w = torch.randn(groups, k, m, device="cuda").bfloat16()
+    ptr = torch.tensor([0, n // 3, n - 5], device="cuda")
+    y = dp.grouped_linear(x, w, ptr)
+    at = torch.cat([torch.arange(a - 60, a + 60) for a in (60, n // 3, 2 ** 29, n - 60)]).cuda()
+    group = (at >= n // 3).long()
+    want = (x[at].double()[:, :, None] * w.double()[group]).sum(1) * (at < n - 5)[:, None]
+    # rounded once to 8 bits, and a sum of 8 in float32 whose terms are below 32
+    assert ((y[at].double() - want).abs() <= 2.0 ** -8 * want.abs() + 8 * 32 * 2.0 ** -24).all()
+    _, dw, db = dp.grouped_linear_backward(y, x, w, ptr, need=(False, True, True))
+    for t, (a, b) in enumerate(((0, n // 3), (n // 3, n - 5))):
+        want, size = (torch.zeros(k + 1, m, dtype=torch.float64, device="cuda") for _ in range(2))
+        for at in range(a, b, 2 ** 25):
+            part = slice(at, min(b, at + 2 ** 25))
+            for i in range(k + 1):
+                for j in range(m):
+                    term = y[part, j].double() * (x[part, i].double() if i < k else 1)
+                    want[i, j] += term.sum()
+                    size[i, j] += term.abs().sum()
+        got = torch.cat([dw[t], db[t][None]]).double()
+        # blocks of 8,192 rows in float32: 2^-14 of the sum of magnitudes at the most
+        assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -14 * size).all()
+        assert (want[:k].abs() > 2.0 ** -9 * size[:k]).any()
+    del x, y
+    torch.cuda.empty_cache()
