@@ -901,7 +901,7 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
 }
 
 // ---------------------------------------------------------------------------
-// Many rows times weights: 128 rows x up to 384 columns a workgroup
+// Many float32 rows times weights: 128 rows x up to 384 columns a workgroup
 // ---------------------------------------------------------------------------
 
 // Rows come from HBM with some 2 us of latency, and a compute unit needs 37 KB of
@@ -914,12 +914,10 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
 // rows, read again from HBM, are 340 us; on zeros, which draw less power, 1,300.
 constexpr int kWideThreads = 512, kWideRows = 128, kWideBlocks = 12;   // blocks of 32 columns
 
-template <class T, Source S>
 __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs a) {
-  constexpr int PA = planes_of<S>, PB = S == kFloat ? 2 : 1, NT = kWideBlocks / 4;
-  constexpr bool kBf = std::is_same<T, __bf16>::value;
+  constexpr int NT = kWideBlocks / 4;
   constexpr int kOneA = kWideRows * kRowBytes, kOneB = kWideBlocks * 32 * kRowBytes;
-  constexpr int kHalfLds = PA * kOneA + PB * kOneB;
+  constexpr int kHalfLds = 2 * kOneA + 2 * kOneB;
   __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
   __shared__ int32_t row_of[kWideRows];      // -1: nothing is stored
   __shared__ int32_t change[2][kWideRows];   // exponent that a row's sums are to move by
@@ -937,16 +935,16 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
   const int blocks = all_blocks - b0 < each ? all_blocks - b0 : each;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
-  T* out = static_cast<T*>(a.out);
-  T* zout = static_cast<T*>(a.zout);
+  float* out = static_cast<float*>(a.out);
+  float* zout = static_cast<float*>(a.zout);
 
   if (t.group == a.n_groups) {   // rows of no group
     const int width = a.kout - c0 < blocks * 32 ? a.kout - c0 : blocks * 32;
     for (int i = tid; i < t.count * width; i += kWideThreads) {
       const int64_t row = row_at(a.order, t.first + i / width, a.n);
       if (row < 0) continue;
-      out[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
-      if (zout) zout[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
+      out[row * a.kout + c0 + i % width] = 0.0f;
+      if (zout) zout[row * a.kout + c0 + i % width] = 0.0f;
     }
     return;
   }
@@ -961,22 +959,21 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
     const int64_t to = row_at(a.order, t.first + r, a.n);
     if (sub == 0) row_of[own] = own < t.count ? static_cast<int32_t>(to) : -1;
     const int64_t row = a.by_place ? t.first + r : to < 0 ? 0 : to;
-    row_p = static_cast<const char*>(a.in) + row * a.ldin * bytes_of<S>;
+    row_p = static_cast<const char*>(a.in) + row * a.ldin * 4;
     last = last_of(a.n, a.ldin, a.by_place ? static_cast<int>(a.ldin) : a.kin, row);
   }
-  const int64_t in_plane = a.n * a.ldin * bytes_of<S>;
   const int64_t set = a.w.set_of(t.group, t.first - int64_t(t.part) * kWideRows);
   const char* wsrc = a.w.planes + set * a.w.steps * a.w.step_bytes() + int64_t(c0) * kRowBytes;
   const int64_t wplane = int64_t(a.w.cols_pad) * kRowBytes;
 
   constexpr int kFar = 2;
-  Raw<S> ra[kFar];
-  u4 rb[PB][NT];
+  Raw<kFloat> ra[kFar];
+  u4 rb[2][NT];
   auto far = [&](auto turn, int step) {
     constexpr int q = decltype(turn)::value;
     const bool in = step < a.w.steps;   // past the end: one line of the weights
     const int k = step * kDepth + sub * 8;
-    load_raw<S>(ra[q], in ? row_p : wsrc, in ? in_plane : 0, !in ? 0 : k < last ? k : last);
+    load_raw<kFloat>(ra[q], in ? row_p : wsrc, 0, !in ? 0 : k < last ? k : last);
   };
   // slots i 512 + tid of the tile's columns; those past them: one line
   unsigned slot_of_b[NT];
@@ -989,7 +986,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
     const bool in = step < a.w.steps;
     const char* src = in ? wsrc + step * a.w.step_bytes() : wsrc;
 #pragma unroll
-    for (int p = 0; p < PB; ++p)
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
       for (int i = 0; i < NT; ++i)
         rb[p][i] = *reinterpret_cast<const u4*>(src + p * wplane + size_t(in ? slot_of_b[i] : 0));
@@ -1002,89 +999,79 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
     for (int j = 0; j < NT; ++j) acc[i][j] = v16f{};
   int e = kFirstExp;
   bool changed[2] = {false, false};
-  if (S == kFloat) {
-    if (tid < 2 * kWideRows) change[tid / kWideRows][tid % kWideRows] = 0;
-    if (tid < 3) flag[tid] = 0;
-    __syncthreads();
-  }
+  if (tid < 2 * kWideRows) change[tid / kWideRows][tid % kWideRows] = 0;
+  if (tid < 3) flag[tid] = 0;
+  __syncthreads();
 
   auto put = [&](auto, auto far_turn, int step) {
     constexpr int f = decltype(far_turn)::value, q = f & 1;   // q: step % 2
     char* la = lds + q * kHalfLds;
-    char* lb = la + PA * kOneA;
+    char* lb = la + 2 * kOneA;
 #pragma unroll
-    for (int p = 0; p < PB; ++p)
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
       for (int i = 0; i < NT; ++i)
         *reinterpret_cast<u4*>(lb + p * kOneB + (i * kWideThreads + tid) * 16) = rb[p][i];
-    if ((step + 1) * kDepth > a.kin) trim<S>(ra[f], step * kDepth + sub * 8, last, a.kin);
+    if ((step + 1) * kDepth > a.kin) trim<kFloat>(ra[f], step * kDepth + sub * 8, last, a.kin);
     const int at = slot_at(own, sub);
-    if constexpr (S == kFloat) {
-      if (tid == 0) flag[(step + 1) % 3] = 0;
-      if (changed[q]) {   // two steps ago; its readers are past it
-        change[q][own] = 0;
-        changed[q] = false;
-      }
-      float v[8];
-      float m = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned bits = ra[f].v[j / 4][j % 4];
-        v[j] = __builtin_bit_cast(float, bits);
-        m = fmaxf(m, fabsf(v[j]));
-      }
-      if (__ballot(m * exp2_of(e) > kLimit) != 0) {   // a row has outgrown its scale: rare past the first step
-        m = fmaxf(m, __shfl_xor(m, 1));
-        m = fmaxf(m, __shfl_xor(m, 2));
-        if (m * exp2_of(e) > kLimit) {
-          const int now = exp_for(m);
-          if (sub == 0) {
-            change[q][own] = now - e;
-            changed[q] = true;
-            flag[step % 3] = 1;
-          }
-          e = now;
-        }
-      }
-      const float scale = exp2_of(e);
-      u4 hi, lo;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        unsigned h, l;
-        split2(v[2 * j] * scale, v[2 * j + 1] * scale, &h, &l);
-        hi[j] = h;
-        lo[j] = l;
-      }
-      *reinterpret_cast<u4*>(la + at) = hi;
-      *reinterpret_cast<u4*>(la + kOneA + at) = lo;
-    } else {
-#pragma unroll
-      for (int p = 0; p < PA; ++p) *reinterpret_cast<u4*>(la + p * kOneA + at) = ra[f].v[p];
+    if (tid == 0) flag[(step + 1) % 3] = 0;
+    if (changed[q]) {   // two steps ago; its readers are past it
+      change[q][own] = 0;
+      changed[q] = false;
     }
+    float v[8];
+    float m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned bits = ra[f].v[j / 4][j % 4];
+      v[j] = __builtin_bit_cast(float, bits);
+      m = fmaxf(m, fabsf(v[j]));
+    }
+    if (__ballot(m * exp2_of(e) > kLimit) != 0) {   // a row has outgrown its scale: rare past the first step
+      m = fmaxf(m, __shfl_xor(m, 1));
+      m = fmaxf(m, __shfl_xor(m, 2));
+      if (m * exp2_of(e) > kLimit) {
+        const int now = exp_for(m);
+        if (sub == 0) {
+          change[q][own] = now - e;
+          changed[q] = true;
+          flag[step % 3] = 1;
+        }
+        e = now;
+      }
+    }
+    const float scale = exp2_of(e);
+    u4 hi, lo;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      unsigned h, l;
+      split2(v[2 * j] * scale, v[2 * j + 1] * scale, &h, &l);
+      hi[j] = h;
+      lo[j] = l;
+    }
+    *reinterpret_cast<u4*>(la + at) = hi;
+    *reinterpret_cast<u4*>(la + kOneA + at) = lo;
   };
   auto before = [&](int step) {
-    if constexpr (S == kFloat) {
-      if (flag[step % 3]) {
+    if (!flag[step % 3]) return;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int d = change[step & 1][64 * wm + 32 * i + sum_row(lane, r)];
+      for (int r = 0; r < 16; ++r) {
+        const int d = change[step & 1][64 * wm + 32 * i + sum_row(lane, r)];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j][r] = ldexpf(acc[i][j][r], d);
-          }
+        for (int j = 0; j < NT; ++j) acc[i][j][r] = ldexpf(acc[i][j][r], d);
       }
-    }
   };
   // this wave's blocks wn, wn + 4, ..
   const int mine = 64 * wm >= t.count || wn >= blocks ? 0 : (blocks - wn + 3) / 4;
-  Part<2, PA> fa[2];
-  Part<1, PB> fb[2][NT];
+  Part<2, 2> fa[2];
+  Part<1, 2> fb[2][NT];
   auto read = [&](auto half, int step) {
     constexpr int ks = decltype(half)::value;
     if (mine == 0) return;
     const char* la = lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes;
-    const char* lb = lds + (step & 1) * kHalfLds + PA * kOneA + wn * 32 * kRowBytes;
+    const char* lb = lds + (step & 1) * kHalfLds + 2 * kOneA + wn * 32 * kRowBytes;
     load_part(fa[ks], la, kOneA, lane, ks);
 #pragma unroll
     for (int j = 0; j < NT; ++j) load_part(fb[ks][j], lb + j * 128 * kRowBytes, kOneB, lane, ks);
@@ -1095,23 +1082,18 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int p = PA + PB - 2; p >= 0; --p)   // the small products first
+      for (int p = 2; p >= 0; --p)   // the small products first
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int pa = PA == 2 && PB == 2 ? (p == 2 ? 1 : 0) : PA == 2 ? p : 0;
-          const int pb = PA == 2 && PB == 2 ? (p == 1 ? 1 : 0) : PB == 2 ? p : 0;
-          acc[i][j] = mfma<kBf>(fa[ks].v[i][pa], fb[ks][j].v[0][pb], acc[i][j]);
-        }
+        for (int i = 0; i < 2; ++i)
+          acc[i][j] = mfma<false>(fa[ks].v[i][p == 2], fb[ks][j].v[0][p == 1], acc[i][j]);
   };
   run_steps<1, kFar>(a.w.steps, near, far, put, read, before, multiply);
 
-  if (S == kFloat) {
-    if (sub == 0) row_exp[own] = e;
-    __syncthreads();
-  }
+  if (sub == 0) row_exp[own] = e;
+  __syncthreads();
   // outputs from the registers: a lane has a column, 32 of them are 128 bytes of a row
-  const T* bias = a.bias ? static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
-  const T* res = static_cast<const T*>(a.residual);
+  const float* bias = a.bias ? static_cast<const float*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
+  const float* res = static_cast<const float*>(a.residual);
   if (mine == 0) return;
   // sixteen sums (i, j) at a time; the residual's entries one group ahead
   float rv[2][16];
@@ -1123,7 +1105,7 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int row = row_of[64 * wm + 32 * i + sum_row(lane, r)];
-      rv[q][r] = to_f32(res[int64_t(row < 0 ? 0 : row) * a.ldres + c]);
+      rv[q][r] = res[int64_t(row < 0 ? 0 : row) * a.ldres + c];
     }
   };
   auto store = [&](auto part, int j, const v16f& sums, float bv, int ec) {
@@ -1138,30 +1120,25 @@ __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs 
       for (int q = 0; q < 2; ++q) {
         const int rl = 64 * wm + 32 * i + sum_row(lane, r + q);
         row[q] = row_of[rl];
-        z[q] = sums[r + q];
-        if (S == kFloat) z[q] = ldexpf(z[q], -row_exp[rl] - ec);
-        z[q] += bv;
+        z[q] = ldexpf(sums[r + q], -row_exp[rl] - ec) + bv;
         y[q] = a.silu ? z[q] * logistic(z[q]) : z[q];
         if (res) y[q] += rv[i][r + q];
       }
-      if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
-          if (in && row[q] >= 0) {
-            out[int64_t(row[q]) * a.kout + c] = y[q];
-            if (zout) zout[int64_t(row[q]) * a.kout + c] = z[q];
-          }
-      }
+      for (int q = 0; q < 2; ++q)
+        if (in && row[q] >= 0) {
+          out[int64_t(row[q]) * a.kout + c] = y[q];
+          if (zout) zout[int64_t(row[q]) * a.kout + c] = z[q];
+        }
     }
   };
-  static_assert(sizeof(T) == 4, "half types take tiles of 128 columns");
   fetch_residual(Const<0>{}, 0, 0);
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
     if (j >= mine) continue;
     const int c = c0 + (wn + 4 * j) * 32 + (lane & 31);
-    const float bv = bias ? to_f32(bias[c < a.kout ? c : a.kout - 1]) : 0.0f;
-    const int ec = S == kFloat ? a.w.exps[set * a.w.cols_pad + c] : 0;
+    const float bv = bias ? bias[c < a.kout ? c : a.kout - 1] : 0.0f;
+    const int ec = a.w.exps[set * a.w.cols_pad + c];
     fetch_residual(Const<1>{}, 1, j);
     store(Const<0>{}, j, acc[0][j], bv, ec);
     fetch_residual(Const<0>{}, 0, j + 1);
@@ -1629,16 +1606,16 @@ int64_t tiles_at_most(int64_t n, int n_groups, int64_t rows) {
   return n / rows + (n < n_groups + 1 ? n : n_groups + 1);
 }
 
-// The tile of rows times weights.  Wide: float32 with more than 256 columns,
-// from two rounds of the 256 compute units on (1,000,188 x 384 -> 384: 1,600 us,
-// 128 x 128 tiles 1,850; bfloat16 1,140 against 1,000, and 128 columns 3,600
-// against 1,910: half types and few columns leave its columns or matrix cores
-// idle).  Else 128 x 128 where such tiles fill the compute units, and 64 x 64.
 // whether products read planes of the weights, not the weights (WeightForm)
 bool laid_out(const dpa4c_grouped& l) {
   return l.dtype == DPA4C_F32 || l.n_out < kLeastWidth || l.n >= int64_t(kLaidRows) * l.n_groups;
 }
 
+// The tile of rows times weights.  Wide: float32 with more than 256 columns,
+// from two rounds of the 256 compute units on (1,000,188 x 384 -> 384: 1,600 us,
+// 128 x 128 tiles 1,850; bfloat16 1,140 against 1,000, and 128 columns 3,600
+// against 1,910: half types and few columns leave its columns or matrix cores
+// idle).  Else 128 x 128 where such tiles fill the compute units, and 64 x 64.
 enum TileKind { kSmallTile, kLargeTile, kWideTile };
 TileKind tile_kind(const dpa4c_grouped& l, bool back) {
   const int cols = back ? l.k : l.n_out;
@@ -1808,8 +1785,7 @@ int run_rows(const dpa4c_grouped& l, const RowsArgs& a, const TileList& tiles, h
   else if (kind == kLargeTile)
     grouped_rows_kernel<T, S, 2, W><<<large, kThreads, 0, st>>>(a);
   else if constexpr (S == kFloat)
-    grouped_wide_kernel<T, S><<<most * (((a.kout + 31) / 32 + kWideBlocks - 1) / kWideBlocks), kWideThreads, 0,
-                                st>>>(a);
+    grouped_wide_kernel<<<most * (((a.kout + 31) / 32 + kWideBlocks - 1) / kWideBlocks), kWideThreads, 0, st>>>(a);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
 }
