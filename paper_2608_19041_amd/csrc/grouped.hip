@@ -17,7 +17,7 @@
 //
 // The launches of a call depend on each other, so a call of few rows is bound by
 // the latencies of two (forward) or four (backward) kernels: 108 rows of 144 -> 192
-// take 5 + 10 us, 4,000 rows of 384 -> 384 backward 16 + 18 + 27 + 8.
+// take 5 + 10 us, 4,000 rows of 384 -> 384 backward 17 + 18 + 27 + 8.
 #include <hip/hip_runtime.h>
 
 #include "tile.h"
@@ -347,7 +347,7 @@ __device__ inline void form_dz(const PrepArgs& p, int64_t block, int64_t blocks)
 // hi + lo then holds an entry to 2^-22 of itself or 2^-39 of that largest one, and
 // nothing overflows.  A row of zeros has kNoExp.  lanes_of_dz(pitch) lanes take a row,
 // eight entries each; longer rows are formed twice.  (1,000,188 rows of 384: the
-// launch 705 us, of bfloat16 620, and dW 1,970 against 1,780.)
+// launch 710 us, of bfloat16 640 on the same card, and dW of 541 columns 1,975 against 1,715.)
 constexpr int kDzTop = 14, kNoExp = 100;
 __host__ __device__ inline int lanes_of_dz(int pitch) {
   int lanes = 1;
@@ -423,7 +423,7 @@ __device__ inline void form_dz_scaled(const PrepArgs& p, int64_t block, int64_t 
 // What the products of a call need first, each piece by workgroups of its own, since
 // all of it is bound by HBM: 31,250 rows of 541 -> 384 in 118 groups move 340 MB in
 // 65 us (5.2 TB/s, reads of dy and z that the last-level cache holds among them), dz
-// of a million bfloat16 rows 3.1 GB in 620 us (5.0 TB/s).
+// of a million bfloat16 rows 3.1 GB in 624 us (5.0 TB/s).
 template <class T, bool Back>
 __global__ void __launch_bounds__(kPrepThreads) grouped_prepare_kernel(PrepArgs a) {
   extern __shared__ int32_t starts[];
@@ -474,9 +474,12 @@ constexpr bool row_scaled = S == kPair && std::is_same<T, _Float16>::value;
 // are the reduction entries of x W (read through transposing LDS reads) and the
 // columns of dz W^T.  float32 weights are laid out as planes first, and so are
 // rows of fewer than eight entries and, since the planes are quicker to fetch, the
-// weights of kLaidRows rows a group and more.  (bfloat16, 541 -> 384, us: forward of
-// 31,250 rows in 118 groups 60 as they are, 80 laid out; of 1,000,188 rows in 5 groups
-// 1,250 against 1,200, and dx of those 1,410 against 1,290.)
+// weights under kLaidRows rows and more for each group of the table: how many of its
+// groups have rows only the device knows, and what laying out costs grows with them.
+// (bfloat16, 541 -> 384, 118 groups, us, as they are and laid out.  Forward with z, all
+// groups present: 31,250 rows 60, 80; 250,000 378, 405; 1,000,188 1,421, 1,435.  Five
+// present: 58, 62; 366, 370; 1,408, 1,398.  dx of dy and z, all: 94, 105; 577, 586; 2,173,
+// 2,158; five: 87, 85; 562, 555; 2,154, 2,118.  Of 144 -> 192 1,000,188 rows 588, 571.)
 enum WeightForm { kLaid, kEntries, kColumns };
 constexpr int kLaidRows = 4096;
 
@@ -560,11 +563,11 @@ __device__ inline void trim(Raw<S>& r, int k, int last, int width) {
 // A tile of rows times weights, by run_steps(); rows and unlaid weights are the far
 // operands, laid out weights (from L2) the near one.  A float32 row has a running
 // scale, so it is read once.  31,250 rows of 541 -> 384 in 118 groups: bfloat16
-// forward 55 us for 131 MB (2.4 TB/s: one step of loads is 0.3 us of products, so the
-// tiles of a compute unit wait on HBM), float32 dx 126 us (0.31 PFLOP/s of float16
-// products, with half of the row tiles short).  dx of 1,000,188 bfloat16 rows in two
-// planes 1,725 us (0.48 PFLOP/s): matrix cores, whose clock falls with the power
-// that products of random operands draw.
+// forward 55 to 57 us for 140 MB (2.5 TB/s, matrix cores busy 10 %: one step of loads is
+// 0.3 us of products, so the tiles of a compute unit wait for them), float32 dx 123 us
+// (0.32 PFLOP/s of float16 products, 16 %, with half of the row tiles short).  dx of
+// 1,000,188 bfloat16 rows in two planes 1,640 us (0.51 PFLOP/s): matrix cores 22 %, LDS
+// 29 %, 1.6 TB/s; a step's loads, LDS writes and barrier with two waves to a SIMD.
 template <class T, Source S, int NB, WeightForm W>
 __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
   static_assert(S != kFloat || W == kLaid, "float32 weights are split into planes first");
@@ -910,8 +913,10 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_rows_kernel(RowsArgs a) {
 // once for up to 384 columns.  A wave forms 64 x 96 outputs, so LDS is read 2/3 as
 // often for a product too, and a float32 step is 1 us of the matrix cores, three
 // of which cover the latency.  1,000,188 rows of 384 -> 384 with SiLU, z and a residual:
-// 1,600 us, 0.55 PFLOP/s of float16 products and 2.9 TB/s, of which the residual's
-// rows, read again from HBM, are 340 us; on zeros, which draw less power, 1,300.
+// 1,660 us (1,570 to 1,750), 0.53 PFLOP/s of float16 products, 6.3 GB at 3.6 TB/s, of
+// which the residual's rows, read again from HBM, are 340 us.  Matrix cores are busy
+// 25 %, LDS 24 %, vector instructions 40 %, and the clock is 1.92 GHz; on zeros, which
+// draw less power, 1,300 us.
 constexpr int kWideThreads = 512, kWideRows = 128, kWideBlocks = 12;   // blocks of 32 columns
 
 __global__ void __launch_bounds__(kWideThreads, 2) grouped_wide_kernel(RowsArgs a) {
@@ -1276,8 +1281,8 @@ __device__ inline void clear_column(Column& r, int row) {
   for (int i = 0; i < kDepth; ++i) r.v[i] = __builtin_amdgcn_readlane(row, i) < 0 ? 0.0f : r.v[i];
 }
 
-// float32: 31,250 rows of 541 x 384 in 118 groups 141 us (0.28 PFLOP/s of float16
-// products; a block's 15 tiles read x three and dz five times, from L2), 4,000 rows in
+// float32: 31,250 rows of 541 x 384 in 118 groups 143 us (0.27 PFLOP/s of float16
+// products, matrix cores busy 12 %; a block's 15 tiles read x three and dz five times, from L2), 4,000 rows in
 // 5 groups 27 us for four steps a tile: the latencies of its start and end.
 __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a) {
   constexpr int kOne = kPlane<2>, kHalfLds = 4 * kOne;
@@ -1397,7 +1402,8 @@ __global__ void __launch_bounds__(kThreads, 2) grouped_outer_kernel(OuterArgs a)
 // Half types need no scale of their columns, so the rows go to LDS as they come, eight columns a
 // lane, and transposing reads turn them: 6 loads a lane and step for dz in two
 // planes, where a column a lane would take 64 loads of 2 or 4 bytes.  1,000,188
-// bfloat16 rows of 541 x 384 in two planes: 1,780 us, 0.47 PFLOP/s; five tiles across read dz
+// bfloat16 rows of 541 x 384 in two planes: 1,690 us, 0.49 PFLOP/s, matrix cores busy
+// 21 %, LDS 26 %, 7.7 GB past the L2s at 4.5 TB/s; five tiles across read dz
 // five times and three x three times, from L2 as they run side by side.
 //
 // Rows of dz with exponents of their own are brought to the least one of the block on
@@ -1577,7 +1583,7 @@ __device__ inline void join_parts(const float* part, int count, int64_t each, in
 
 // The blocks of the groups that have several, added up: dW, then db (null: not
 // formed).  Bound by HBM where blocks are many (a million rows, 541 x 384: 244 blocks,
-// 203 MB in 54 us), by its launch else (4,000 rows: 8 us).
+// 230 MB in 47 us), by its launch else (4,000 rows: 8 us).
 template <class T>
 __global__ void __launch_bounds__(kThreads) grouped_join_kernel(const int32_t* __restrict__ first_of,
                                                                 const int64_t* __restrict__ ptr, int64_t n,

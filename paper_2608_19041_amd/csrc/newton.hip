@@ -17,10 +17,11 @@
 // last writes the result or the weights itself.
 //
 // Measured, a step's three products and what they come to in float16 products:
-// 118 matrices of 541 x 384 64 + 52 + 109 us (0.47 PFLOP/s), 236 of 384 x 384
-// 90 + 107 + 142 us (0.47).  Matrix cores, at the clock that random operands leave
-// them, and the last workgroups of each launch.  Twelve matrices up to
-// 688 x 768 18 + 13 + 17 us: too few tiles for the chip, each a chain of steps whose
+// 118 matrices of 541 x 384 55 + 45 + 93 us (0.54 PFLOP/s), 236 of 384 x 384
+// 81 + 94 + 125 us (0.54).  Matrix cores are busy 20 to 28 %, LDS 25 to 30 % (50 in tiles
+// of 64 x 64) and 3.1 to 4.4 TB/s come past the L2s: the loads and barriers of a step,
+// and the last workgroups of each launch.  Twelve matrices up to
+// 688 x 768 17 + 12 + 16 us: too few tiles for the chip, each a chain of steps whose
 // latencies nothing hides.  Eleven up to 192 x 192 take 6 to 7 us a launch.
 #include <hip/hip_runtime.h>
 
