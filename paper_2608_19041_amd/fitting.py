@@ -120,6 +120,8 @@ class _launch:
             return
         if stream is None:
             stream = torch.cuda.current_stream(device)
+        elif stream.device != device:
+            raise ValueError(f"the stream is of {stream.device}, the tensors are on {device}")
         self._guards = (torch.cuda.device(device), torch.cuda.stream(stream))
         self._handle = stream.cuda_stream
 

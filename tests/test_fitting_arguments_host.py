@@ -1,6 +1,8 @@
-"""Sizes beyond 32 bits reach the library as sizes that it refuses (no GPU)."""
+"""Sizes that the library refuses and streams that the binding does (no GPU)."""
 import ctypes
+import types
 
+import pytest
 import torch
 
 import paper_2608_19041_amd as dp
@@ -27,3 +29,9 @@ def test_rows_up_to_what_a_launch_takes():
         layer = ft._Grouped(1, 3, k, m, n, 256, None, 512, k, 1024)
         assert lib.dpa4c_grouped_linear_work(ctypes.byref(layer), ctypes.byref(need)) == rc, n
         assert lib.dpa4c_grouped_linear_backward_work(ctypes.byref(layer), ctypes.byref(need)) == rc, n
+
+
+def test_a_stream_of_another_device():
+    stream = types.SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0)
+    with pytest.raises(ValueError, match="cuda:1"):
+        ft._launch(torch.device("cuda", 0), stream)
