@@ -500,6 +500,153 @@ int dpa4c_muon_step(int dtype, int count, const dpa4c_update* updates, const dpa
                     float lr, float momentum, int nesterov, float weight_decay, void* work,
                     int64_t work_bytes, void* stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * A residual block of an energy head, its product in 8 bits
+ * ---------------------------------------------------------------------------
+ *     h' = h + dropout(act(Q(norm(h)) Q(W_g) + b_g))
+ * Root-mean-square norm of rows, rows and weights in 8 bits with scales, layers of those
+ * and their gradients, and dropout.  As above: asynchronous on ``stream``, no
+ * allocation, nothing read back, may be captured, scratch of the caller's, outputs
+ * that overlap neither inputs nor each other, the same bits from repeated calls.
+ */
+
+/*
+ * Rows of 8-bit numbers with a scale for each block of 128 entries of a row.
+ *   values  [n] rows of k bytes, ld bytes apart: ld and the address multiples of 16; the
+ *           bytes from k up to the next multiple of 16 are there, and hold any values
+ *           (rows written here have zeros in them)
+ *   scales  [n][ceil(k / 128)] bytes, rows ld_scales apart: 2^(byte - 127), 255 is NaN
+ * e4m3 has 3 fraction bits and ends at 448, e5m2 has 2 and ends at 57,344; both have NaN, and
+ * no infinity is written.  A block gets the least scale with which its largest finite entry
+ * fits, 2^-127 at the least, and its entries are rounded to nearest even.  A block of
+ * zeros has scale 2^-127; a block with an infinity or NaN is NaN as a whole.
+ */
+#define DPA4C_E4M3 0
+#define DPA4C_E5M2 1
+
+typedef struct dpa4c_rows8 {
+  int format;
+  int k;
+  int64_t n;
+  void* values;
+  int64_t ld;
+  void* scales;
+  int64_t ld_scales;
+} dpa4c_rows8;
+
+/* x [n][k] of ``dtype``, rows ldx entries apart (0: one row for all), to ``out``;
+ * and what rows stand for, contiguous [n][k] of ``dtype``.  0 <= n < 2^31, 1 <= k <= 65536. */
+int dpa4c_quantize_rows(int dtype, const void* x, int64_t ldx, const dpa4c_rows8* out, void* stream);
+int dpa4c_dequantize_rows(const dpa4c_rows8* in, int dtype, void* out, void* stream);
+
+/*
+ * Weights [n_groups][k][n_out] in e4m3, with a scale for each block of 128 x 128 of a
+ * group; contiguous, 16-byte aligned.
+ *   values  [n_groups][k][n_out padded to a multiple of 16], which gradients of rows read
+ *   turned  [n_groups][n_out][k padded to a multiple of 16], which the forward pass reads
+ *   scales  [n_groups][ceil(k / 128)][ceil(n_out / 128)] bytes as above
+ * dpa4c_quantize_weights writes those of values and turned that are not NULL.
+ */
+typedef struct dpa4c_weights8 {
+  int n_groups;
+  int k;
+  int n_out;
+  void* values;
+  void* turned;
+  void* scales;
+} dpa4c_weights8;
+
+int dpa4c_quantize_weights(int dtype, const void* w, const dpa4c_weights8* out, void* stream);
+int dpa4c_dequantize_weights(const dpa4c_weights8* in, int dtype, void* out, void* stream);
+
+/*
+ * Rows and gains of a norm.  group_ptr and order as in dpa4c_grouped; group_ptr NULL: one group
+ * of all rows, n_groups = 1.  gain [n_groups][k], contiguous, of the rows' ``dtype``.
+ * Limits as there: n_groups <= 4096, k <= 65536.
+ */
+typedef struct dpa4c_norm {
+  int dtype;
+  int n_groups;
+  int k;
+  int64_t n;
+  const int64_t* group_ptr;
+  const int32_t* order;
+  const void* gain;
+} dpa4c_norm;
+
+/*
+ * h = x + residual (x without one), s = 1 / sqrt(mean_c h_c^2 + eps), y = h s gain_g.
+ * x, residual: rows ldx and ldr entries apart (0: one row for all); eps > 0.
+ *   y     [n][k] contiguous, or NULL and y8 is given: y in 8 bits (y8->n = n, y8->k = k)
+ *   rstd  float32 [n] out: s; zero for rows of no group; or NULL
+ *   h     [n][k] contiguous out, of all rows; given with a residual, NULL without
+ * y is formed from h before its rounding, s in float64; rows of no group give zeros.
+ */
+int dpa4c_rms_norm(const dpa4c_norm* norm, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                   float eps, void* y, const dpa4c_rows8* y8, float* rstd, void* h, void* stream);
+
+/*
+ * From dy = dL/dy, h and rstd as the forward pass left them (h = x without a residual), and dh,
+ * the gradient that reaches h past the norm, or NULL:
+ *     dx_r = s dy gain - h s^3 mean_c(dy gain h) + dh   (also the residual's gradient)
+ *     dgain_g = sum_r dy h s
+ * Rows lddy, ldh, lddh entries apart (0: one row for all).  dx [n][k], dgain [n_groups][k], contiguous;
+ * either may be NULL.  Rows of no group pass dh on.  Sums are float64, outputs round once.
+ */
+int dpa4c_rms_norm_backward_work(const dpa4c_norm* norm, int dgain, int64_t* bytes);
+int dpa4c_rms_norm_backward(const dpa4c_norm* norm, const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                            const float* rstd, const void* dh, int64_t lddh, void* dx, void* dgain, void* work,
+                            int64_t work_bytes, void* stream);
+
+/*
+ * A layer of 8-bit rows x and weights w (x.k = w.k).  ``dtype`` is that of bias, residual, y, z and of
+ * all gradients: DPA4C_F16 or DPA4C_BF16 (UNSUPPORTED else: the matrix cores align neighbouring 8-bit
+ * products to 2^-14 of the largest before they add, which keeps a sum to 1.5e-5 of itself for
+ * ordinary entries, and to 2^-11 of the sum of the products' sizes at the worst).
+ * group_ptr, order and limits as in dpa4c_grouped.
+ */
+typedef struct dpa4c_grouped8 {
+  int dtype;
+  const int64_t* group_ptr;
+  const int32_t* order;
+  dpa4c_rows8 x;
+  dpa4c_weights8 w;   /* forward: turned and scales; gradients of rows: values and scales */
+} dpa4c_grouped8;
+
+/*
+ * z_r = x_r W_g + b_g, y_r = act(z_r) (+ residual_r); bias [n_groups][n_out] or NULL; residual
+ * [n][n_out], rows ldr entries apart (0: one row for all), or NULL; y, z [n][n_out] contiguous, z may be NULL.
+ * Rows of no group give zeros.
+ */
+int dpa4c_grouped_linear8_work(const dpa4c_grouped8* layer, int64_t* bytes);
+int dpa4c_grouped_linear8(const dpa4c_grouped8* layer, const void* bias, int activation, const void* residual,
+                          int64_t ldr, void* y, void* z, void* work, int64_t work_bytes, void* stream);
+
+/*
+ * The gradients of that layer, x and W being the values that their 8 bits stand for:
+ *     dz_r = dy_r act'(z_r),   dx_r = Q(dz_r) W_g^T,   dW_g = sum_r x_r^T dz_r,   db_g = sum_r dz_r,
+ * Q to 8 bits of ``format`` in blocks of 128.  For dW and db dz is held to 2^-12 of itself or 2^-39 of
+ * the largest finite entry of its block of 128, and x exactly or to 2^-40 of the largest product of up
+ * to 8,192 rows.  dx [n][k], dw [n_groups][k][n_out], db [n_groups][n_out], contiguous, each or NULL.
+ * The residual's gradient is dy itself.  Groups without rows get zeros.
+ */
+int dpa4c_grouped_linear8_backward_work(const dpa4c_grouped8* layer, int dx, int dw, int db, int64_t* bytes);
+int dpa4c_grouped_linear8_backward(const dpa4c_grouped8* layer, int format, const void* dy, int64_t ldy,
+                                   const void* z, int64_t ldz, void* dx, void* dw, void* db, void* work,
+                                   int64_t work_bytes, void* stream);
+
+/*
+ * y = residual + keep x / (1 - p), the residual or zero where an entry is dropped (whatever x is there).
+ * Entry c of row r is kept if word c mod 4 of Philox4x32-10 (J. Salmon et al., 2011) with counter
+ * (floor(c / 4), r, o mod 2^32, floor(o / 2^32)), o = offset + *offset_at, and key (seed mod 2^32, floor(seed / 2^32))
+ * is at least floor(p 2^32 + 1/2).  The gradient of x is this call on dy, with the same p, seed and offset
+ * and no residual.  x, residual (or NULL): rows ldx, ldr entries apart (0: one row for all); y [n][k] contiguous;
+ * 0 <= p <= 1; offset_at: device int64, or NULL (a captured graph reads it at each replay).
+ */
+int dpa4c_dropout(int dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t n, int k,
+                  double p, uint64_t seed, int64_t offset, const int64_t* offset_at, void* y, void* stream);
+
 /* Thread-local description of the last error (library-owned string). */
 const char* dpa4c_last_error(void);
 

@@ -78,6 +78,19 @@ def library():
             "dpa4c_orthogonalize": (i32, [i32, i32, vp, vp, vp, i64, vp]),
             "dpa4c_muon_step_work": (i32, [i32, vp, vp]),
             "dpa4c_muon_step": (i32, [i32, i32, vp, vp, flt, flt, i32, flt, vp, i64, vp]),
+            "dpa4c_quantize_rows": (i32, [i32, vp, i64, vp, vp]),
+            "dpa4c_dequantize_rows": (i32, [vp, i32, vp, vp]),
+            "dpa4c_quantize_weights": (i32, [i32, vp, vp, vp]),
+            "dpa4c_dequantize_weights": (i32, [vp, i32, vp, vp]),
+            "dpa4c_rms_norm": (i32, [vp, vp, i64, vp, i64, flt, vp, vp, vp, vp, vp]),
+            "dpa4c_rms_norm_backward_work": (i32, [vp, i32, vp]),
+            "dpa4c_rms_norm_backward": (i32, [vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, i64, vp]),
+            "dpa4c_grouped_linear8_work": (i32, [vp, vp]),
+            "dpa4c_grouped_linear8": (i32, [vp, vp, i32, vp, i64, vp, vp, vp, i64, vp]),
+            "dpa4c_grouped_linear8_backward_work": (i32, [vp, i32, i32, i32, vp]),
+            "dpa4c_grouped_linear8_backward": (i32, [vp, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp]),
+            "dpa4c_dropout": (i32, [i32, vp, i64, vp, i64, i64, i32, dbl, ctypes.c_uint64, i64, vp, vp,
+                                    vp]),
             "dpa4c_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -97,7 +110,11 @@ def exported_symbols() -> list[str]:
             "dpa4c_group_rows_work", "dpa4c_group_rows", "dpa4c_grouped_linear_work",
             "dpa4c_grouped_linear", "dpa4c_grouped_linear_backward_work",
             "dpa4c_grouped_linear_backward_work_of", "dpa4c_grouped_linear_backward", "dpa4c_orthogonalize_work", "dpa4c_orthogonalize",
-            "dpa4c_muon_step_work", "dpa4c_muon_step", "dpa4c_last_error"]
+            "dpa4c_muon_step_work", "dpa4c_muon_step", "dpa4c_quantize_rows", "dpa4c_dequantize_rows",
+            "dpa4c_quantize_weights", "dpa4c_dequantize_weights", "dpa4c_rms_norm",
+            "dpa4c_rms_norm_backward_work", "dpa4c_rms_norm_backward", "dpa4c_grouped_linear8_work",
+            "dpa4c_grouped_linear8", "dpa4c_grouped_linear8_backward_work",
+            "dpa4c_grouped_linear8_backward", "dpa4c_dropout", "dpa4c_last_error"]
 
 
 def stage_names() -> list[str]:
@@ -403,3 +420,6 @@ class Model:
 
 from .fitting import (group_rows, grouped_linear, grouped_linear_backward,  # noqa: E402
                       muon_step, orthogonalize)
+from .block import (Rows8, Weights8, dequantize, dropout, dropout_backward,  # noqa: E402
+                    grouped_linear8, grouped_linear8_backward, quantize_rows, quantize_weights,
+                    rms_norm, rms_norm_backward)

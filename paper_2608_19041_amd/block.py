@@ -1,0 +1,408 @@
+"""Operators of a residual block of an energy head, its product in 8 bits.
+
+    h' = h + dropout(act(Q(norm(h)) Q(W_g) + b_g))
+
+Root-mean-square norm with gains of each element type, rows and weights in 8 bits
+with a scale for each block of 128, layers of those, and dropout, each with its
+gradients.  As in ``fitting``: argument marshalling only, on the caller's stream, nothing
+recorded by autograd, and tensors that autograd would have to follow are refused.
+
+    n8, rstd = rms_norm(h, gain, ptr, order, quantize="e4m3")
+    w8 = quantize_weights(w)
+    y, z = grouped_linear8(n8, w8, ptr, order, bias=b, activation="silu", preact=True)
+    h1 = dropout(y, 0.1, seed, step, residual=h)
+
+    dy = dropout_backward(dh1, 0.1, seed, step)
+    dn, dw, db = grouped_linear8_backward(dy, n8, w8, ptr, order, preact=z)
+    dh, dgain = rms_norm_backward(dn, h, gain, rstd, ptr, order, dh=dh1)
+"""
+from __future__ import annotations
+
+import ctypes
+import functools
+from typing import NamedTuple
+
+from . import _check, _ptr, library
+from .fitting import (ACTIVATIONS, _dtype_code, _int, _launch, _rows, _same, _scratch, _unrecorded)
+
+#: entries that share a scale; of weights 128 x 128
+SCALE_BLOCK = 128
+FORMATS = {"e4m3": 0, "e5m2": 1}
+
+
+class Rows8(NamedTuple):
+    """Rows in 8 bits: ``values`` float8_e4m3fn or float8_e5m2 [n, k], rows at multiples of 16
+    bytes; ``scales`` float8_e8m0fnu [n, ceil(k / 128)]."""
+    values: object
+    scales: object
+
+
+class Weights8(NamedTuple):
+    """Weights in 8 bits as ``quantize_weights`` lays them out: ``values`` [groups, k, m] (or None,
+    where no gradient of rows is wanted), ``turned`` [groups, m, k], both float8_e4m3fn with rows
+    padded to multiples of 16, and ``scales`` float8_e8m0fnu [groups, ceil(k / 128), ceil(m / 128)]."""
+    values: object
+    turned: object
+    scales: object
+
+
+class _Rows8(ctypes.Structure):
+    _fields_ = [("format", ctypes.c_int), ("k", ctypes.c_int), ("n", ctypes.c_int64),
+                ("values", ctypes.c_void_p), ("ld", ctypes.c_int64), ("scales", ctypes.c_void_p),
+                ("ld_scales", ctypes.c_int64)]
+
+
+class _Weights8(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_int), ("k", ctypes.c_int), ("n_out", ctypes.c_int),
+                ("values", ctypes.c_void_p), ("turned", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p)]
+
+
+class _Norm(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_groups", ctypes.c_int), ("k", ctypes.c_int),
+                ("n", ctypes.c_int64), ("group_ptr", ctypes.c_void_p), ("order", ctypes.c_void_p),
+                ("gain", ctypes.c_void_p)]
+
+
+class _Grouped8(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("group_ptr", ctypes.c_void_p),
+                ("order", ctypes.c_void_p), ("x", _Rows8), ("w", _Weights8)]
+
+
+@functools.lru_cache(maxsize=None)
+def _formats():
+    import torch
+    return {torch.float8_e4m3fn: 0, torch.float8_e5m2: 1}
+
+
+def _format(name):
+    if name not in FORMATS:
+        raise ValueError(f"format must be one of {list(FORMATS)}")
+    return FORMATS[name]
+
+
+def _up16(width):
+    return (width + 15) // 16 * 16
+
+
+def _blocks(width):
+    return (width + SCALE_BLOCK - 1) // SCALE_BLOCK
+
+
+def _matrix(t, name):
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix of rows")
+    return t
+
+
+def _padded8(shape, dtype, device):
+    """Uninitialised 8-bit numbers whose rows are padded to multiples of 16."""
+    import torch
+    *rest, k = shape
+    return torch.empty(*rest, _up16(k), dtype=torch.uint8, device=device).view(dtype)[..., :k]
+
+
+def _empty_rows8(n, k, format, device):
+    import torch
+    dtype = torch.float8_e4m3fn if format == 0 else torch.float8_e5m2
+    return Rows8(_padded8((n, k), dtype, device),
+                 torch.empty(n, _blocks(k), dtype=torch.float8_e8m0fnu, device=device))
+
+
+def _rows8(x, device, name):
+    """The library's view of 8-bit rows."""
+    import torch
+    if not isinstance(x, Rows8):
+        raise ValueError(f"{name} must be Rows8, as quantize_rows and rms_norm give them")
+    q, s = x
+    if not (isinstance(q, torch.Tensor) and q.dtype in _formats() and q.dim() == 2 and q.is_cuda):
+        raise ValueError(f"{name}.values must be a CUDA matrix of float8_e4m3fn or float8_e5m2")
+    if device is not None and q.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    n, k = q.shape
+    ld = q.stride(0) if n > 1 else _up16(k)
+    if n and ((k > 1 and q.stride(1) != 1) or ld % 16 or ld < k or q.data_ptr() % 16):
+        raise ValueError(f"the rows of {name}.values must start at multiples of 16 bytes")
+    if n and q.storage_offset() + (n - 1) * ld + _up16(k) > q.untyped_storage().nbytes():
+        raise ValueError(f"the last row of {name}.values must have room up to a multiple of 16 bytes")
+    lds = _rows(s, torch.float8_e8m0fnu, (n, _blocks(k)), q.device, f"{name}.scales")
+    if lds == 0 and n > 1:
+        raise ValueError(f"the rows of {name}.scales overlap")
+    return _Rows8(_formats()[q.dtype], _int(k), n, q.data_ptr(), ld, s.data_ptr(), lds)
+
+
+def _weights8(w, device, name="weight"):
+    import torch
+    if not isinstance(w, Weights8):
+        raise ValueError(f"{name} must be Weights8, as quantize_weights gives them")
+    given = w.turned if w.turned is not None else w.values
+    if not isinstance(given, torch.Tensor) or given.dim() != 3:
+        raise ValueError(f"{name} must hold matrices of each group")
+    groups, k, m = given.shape if w.turned is None else (given.shape[0], given.shape[2], given.shape[1])
+    device = given.device if device is None else device
+    for part, shape in ((w.values, (groups, k, m)), (w.turned, (groups, m, k))):
+        if part is None:
+            continue
+        pitch = _up16(shape[2])
+        if not (isinstance(part, torch.Tensor) and part.dtype == torch.float8_e4m3fn and part.is_cuda
+                and part.device == device and part.shape == shape):
+            raise ValueError(f"{name} must be float8_e4m3fn on {device}, values {(groups, k, m)} and turned "
+                             f"{(groups, m, k)}")
+        if part.numel() and (part.stride() != (shape[1] * pitch, pitch, 1)
+                             or part.storage_offset() + groups * shape[1] * pitch > part.untyped_storage().nbytes()):
+            raise ValueError(f"the rows of {name} must be padded to multiples of 16 as quantize_weights leaves them")
+    _same(w.scales, torch.float8_e8m0fnu, (groups, _blocks(k), _blocks(m)), device, f"{name}.scales")
+    at = [0 if t is None else t.data_ptr() for t in (w.values, w.turned)]
+    return _Weights8(_int(groups), _int(k), _int(m), at[0] or None, at[1] or None, w.scales.data_ptr())
+
+
+def quantize_rows(x, format: str = "e4m3", stream=None) -> Rows8:
+    """Rows x [n, k] (float32, float16 or bfloat16, any distance apart) in 8 bits.
+
+    Each block of 128 entries of a row has the least power of two as its scale with which its
+    largest entry fits; entries are rounded to nearest even.  ``format``: "e4m3" (largest 448) or "e5m2"
+    (57,344).  A block with an infinity or NaN is NaN as a whole.
+    """
+    code, form = _dtype_code(_matrix(x, "x"), "x"), _format(format)
+    n, k = x.shape
+    ldx = _rows(x, x.dtype, (n, k), x.device, "x")
+    _unrecorded(x=x)
+    lib = library()
+    with _launch(x.device, stream) as st:
+        out = _empty_rows8(n, k, form, x.device)
+        to = _rows8(out, x.device, "out")
+        _check(lib.dpa4c_quantize_rows(code, _ptr(x), ldx, ctypes.byref(to), st))
+    return out
+
+
+def quantize_weights(weight, backward: bool = True, stream=None) -> Weights8:
+    """Weights [groups, k, m] (float32, float16 or bfloat16) in e4m3, a scale for each 128 x 128.
+
+    Laid out for both directions, or for the forward pass alone (``backward=False``).
+    """
+    import torch
+    code = _dtype_code(weight, "weight")
+    if weight.dim() != 3 or not weight.is_contiguous():
+        raise ValueError("weight must be contiguous with shape [groups, k, m]")
+    _unrecorded(weight=weight)
+    groups, k, m = weight.shape
+    dev, lib = weight.device, library()
+    with _launch(dev, stream) as st:
+        out = Weights8(_padded8((groups, k, m), torch.float8_e4m3fn, dev) if backward else None,
+                       _padded8((groups, m, k), torch.float8_e4m3fn, dev),
+                       torch.empty(groups, _blocks(k), _blocks(m), dtype=torch.float8_e8m0fnu, device=dev))
+        to = _weights8(out, dev)
+        _check(lib.dpa4c_quantize_weights(code, _ptr(weight), ctypes.byref(to), st))
+    return out
+
+
+def dequantize(x, dtype=None, stream=None):
+    """The values that ``Rows8`` or ``Weights8`` stand for, of ``dtype`` (default float32), rounded once."""
+    import torch
+    dtype = torch.float32 if dtype is None else dtype
+    weights = isinstance(x, Weights8)
+    if weights and x.values is None:
+        raise ValueError("the weights were laid out for the forward pass alone")
+    at = _weights8(x, None, "x") if weights else _rows8(x, None, "x")
+    dev, lib = x.values.device, library()
+    with _launch(dev, stream) as st:
+        out = torch.empty(x.values.shape, dtype=dtype, device=dev)
+        code = _dtype_code(out, "dtype")
+        call = lib.dpa4c_dequantize_weights if weights else lib.dpa4c_dequantize_rows
+        _check(call(ctypes.byref(at), code, _ptr(out), st))
+    return out
+
+
+def _norm(rows, gain, group_ptr, order):
+    """The norm's groups and gains, for ``rows`` [n, k]."""
+    import torch
+    code = _dtype_code(gain, "gain")
+    n, k = _matrix(rows, "x").shape
+    if gain.dim() == 1:
+        if group_ptr is not None or order is not None:
+            raise ValueError("gain must have shape [groups, k] with group_ptr")
+        _same(gain, rows.dtype, (k,), rows.device, "gain")
+        return _Norm(code, 1, _int(k), n, None, None, gain.data_ptr())
+    if gain.dim() != 2 or group_ptr is None:
+        raise ValueError("gain must have shape [k], or [groups, k] with group_ptr")
+    groups = gain.shape[0]
+    _same(gain, rows.dtype, (groups, k), rows.device, "gain")
+    _same(group_ptr, torch.int64, (groups + 1,), rows.device, "group_ptr")
+    if order is not None:
+        _same(order, torch.int32, (n,), rows.device, "order")
+    return _Norm(code, _int(groups), _int(k), n, group_ptr.data_ptr(),
+                 None if order is None else order.data_ptr(), gain.data_ptr())
+
+
+def rms_norm(x, gain, group_ptr=None, order=None, residual=None, eps: float = 1e-6, quantize=None,
+             stream=None):
+    """y = h s gain_g with h = x (+ residual), s = 1 / sqrt(mean h^2 + eps): (y, s), or (y, s, h).
+
+    x, residual [n, k] (rows may be any distance apart) and the gains are of one type (float32,
+    float16, bfloat16).  gain [k], or [groups, k] with group_ptr and order as ``group_rows`` gives them
+    (order None: the rows are in group order already).  s is float32 [n]; with ``residual`` h is returned too.
+    ``quantize``: "e4m3" or "e5m2" gives y as ``Rows8``.  Rows of no group give y = 0 and s = 0.
+    """
+    import torch
+    _dtype_code(_matrix(x, "x"), "x")
+    norm = _norm(x, gain, group_ptr, order)
+    n, k = x.shape
+    ldx = _rows(x, x.dtype, (n, k), x.device, "x")
+    ldr = 0 if residual is None else _rows(residual, x.dtype, (n, k), x.device, "residual")
+    form = None if quantize is None else _format(quantize)
+    _unrecorded(x=x, gain=gain, residual=residual)
+    lib = library()
+    with _launch(x.device, stream) as st:
+        if form is None:
+            y, y8 = torch.empty(n, k, dtype=x.dtype, device=x.device), None
+        else:
+            y = _empty_rows8(n, k, form, x.device)
+            y8 = _rows8(y, x.device, "y")
+        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+        h = None if residual is None else torch.empty(n, k, dtype=x.dtype, device=x.device)
+        _check(lib.dpa4c_rms_norm(ctypes.byref(norm), _ptr(x), ldx, _ptr(residual), ldr, float(eps),
+                                  None if y8 else _ptr(y), ctypes.byref(y8) if y8 else None,
+                                  _ptr(rstd), _ptr(h), st))
+    return (y, rstd) if residual is None else (y, rstd, h)
+
+
+def rms_norm_backward(dy, h, gain, rstd, group_ptr=None, order=None, dh=None, need=(True, True),
+                      stream=None):
+    """(dx, dgain) of ``rms_norm`` from dy = dL/dy; h = x where the norm had no residual.
+
+    ``dh``: the gradient that reaches h past the norm, added to dx.  dx is the gradient of x and of the
+    residual.  ``need`` says which gradients to form; the others are None.
+    """
+    import torch
+    norm = _norm(h, gain, group_ptr, order)
+    n, k = h.shape
+    ldh = _rows(h, h.dtype, (n, k), h.device, "h")
+    ldy = _rows(dy, h.dtype, (n, k), h.device, "dy")
+    ldd = 0 if dh is None else _rows(dh, h.dtype, (n, k), h.device, "dh")
+    _same(rstd, torch.float32, (n,), h.device, "rstd")
+    _unrecorded(dy=dy, h=h, gain=gain, rstd=rstd, dh=dh)
+    lib = library()
+    with _launch(h.device, stream) as st:
+        work, size = _scratch(h.device, lambda size: lib.dpa4c_rms_norm_backward_work(
+            ctypes.byref(norm), bool(need[1]), size))
+        dx = torch.empty(n, k, dtype=h.dtype, device=h.device) if need[0] else None
+        dgain = torch.empty_like(gain) if need[1] else None
+        _check(lib.dpa4c_rms_norm_backward(ctypes.byref(norm), _ptr(dy), ldy, _ptr(h), ldh, _ptr(rstd),
+                                           _ptr(dh), ldd, _ptr(dx), _ptr(dgain), _ptr(work), size, st))
+    return dx, dgain
+
+
+def _layer8(x, weight, group_ptr, order, dtype):
+    import torch
+    codes = {torch.float16: 1, torch.bfloat16: 2}
+    if dtype not in codes:
+        raise ValueError("results of 8-bit layers are float16 or bfloat16")
+    rows = _rows8(x, None, "x")
+    dev = x.values.device
+    w = _weights8(weight, dev)
+    if w.k != rows.k:
+        raise ValueError(f"x has {rows.k} entries a row, the weights {w.k}")
+    _same(group_ptr, torch.int64, (w.n_groups + 1,), dev, "group_ptr")
+    if order is not None:
+        _same(order, torch.int32, (rows.n,), dev, "order")
+    return _Grouped8(codes[dtype], group_ptr.data_ptr(), None if order is None else order.data_ptr(), rows, w), dev
+
+
+def grouped_linear8(x, weight, group_ptr, order=None, bias=None, activation=None, residual=None,
+                    preact=False, dtype=None, stream=None):
+    """y = act(x W_g + b_g) (+ residual) of 8-bit rows and weights, with the weights of each row's group.
+
+    x ``Rows8`` [n, k], weight ``Weights8`` [groups, k, m]; group_ptr and order as ``group_rows`` gives them.
+    bias [groups, m], residual [n, m] (rows any distance apart) and the results are of ``dtype``,
+    bfloat16 (the default) or float16.  ``activation``: None or "silu".  With ``preact`` returns
+    (y, z), z the value before the activation.  Rows of no group give zeros.
+    """
+    import torch
+    dtype = torch.bfloat16 if dtype is None else dtype
+    layer, dev = _layer8(x, weight, group_ptr, order, dtype)
+    if weight.turned is None:
+        raise ValueError("the forward pass needs weight.turned")
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {list(ACTIVATIONS)}")
+    n, m = layer.x.n, layer.w.n_out
+    if bias is not None:
+        _same(bias, dtype, (layer.w.n_groups, m), dev, "bias")
+    ldr = 0 if residual is None else _rows(residual, dtype, (n, m), dev, "residual")
+    _unrecorded(bias=bias, residual=residual)
+    lib = library()
+    with _launch(dev, stream) as st:
+        work, size = _scratch(dev, lambda need: lib.dpa4c_grouped_linear8_work(ctypes.byref(layer), need))
+        y = torch.empty(n, m, dtype=dtype, device=dev)
+        z = torch.empty_like(y) if preact else None
+        _check(lib.dpa4c_grouped_linear8(ctypes.byref(layer), _ptr(bias), ACTIVATIONS[activation],
+                                         _ptr(residual), ldr, _ptr(y), _ptr(z), _ptr(work), size, st))
+    return (y, z) if preact else y
+
+
+def grouped_linear8_backward(dy, x, weight, group_ptr, order=None, preact=None, format: str = "e4m3",
+                             need=(True, True, True), stream=None):
+    """(dx, dw, db) of ``grouped_linear8`` from dy = dL/dy [n, m] (float16 or bfloat16), all of its type.
+
+    dz = dy act'(z); dx = Q(dz) W_g^T with dz in 8 bits of ``format``, dw = sum x^T dz, db = sum dz.
+    ``preact``: z of the forward pass of a layer with SiLU; None: the layer had no activation.
+    ``need`` says which gradients to form; the others are None.  The residual's gradient is dy.
+    """
+    import torch
+    layer, dev = _layer8(x, weight, group_ptr, order, dy.dtype if isinstance(dy, torch.Tensor) else None)
+    form = _format(format)
+    if need[0] and weight.values is None:
+        raise ValueError("the weights were laid out for the forward pass alone")
+    n, k, m, groups = layer.x.n, layer.w.k, layer.w.n_out, layer.w.n_groups
+    ldy = _rows(dy, dy.dtype, (n, m), dev, "dy")
+    ldz = 0 if preact is None else _rows(preact, dy.dtype, (n, m), dev, "preact")
+    _unrecorded(dy=dy, preact=preact)
+    lib = library()
+    with _launch(dev, stream) as st:
+        work, size = _scratch(dev, lambda size: lib.dpa4c_grouped_linear8_backward_work(
+            ctypes.byref(layer), *(bool(w) for w in need), size))
+        dx = torch.empty(n, k, dtype=dy.dtype, device=dev) if need[0] else None
+        dw = torch.empty(groups, k, m, dtype=dy.dtype, device=dev) if need[1] else None
+        db = torch.empty(groups, m, dtype=dy.dtype, device=dev) if need[2] else None
+        _check(lib.dpa4c_grouped_linear8_backward(
+            ctypes.byref(layer), form, _ptr(dy), ldy, _ptr(preact), ldz, _ptr(dx), _ptr(dw), _ptr(db),
+            _ptr(work), size, st))
+    return dx, dw, db
+
+
+def dropout(x, p: float, seed: int, offset=0, residual=None, stream=None):
+    """y = residual + keep x / (1 - p); the residual, or zero, where an entry is dropped.
+
+    x, residual [n, k] of one type (float32, float16, bfloat16), rows any distance apart.  The mask comes
+    from Philox4x32-10, by row and column, with key ``seed`` (0 .. 2^64 - 1) and ``offset``, a number
+    to change from call to call: an int, or an int64 CUDA tensor of one element, which a captured graph
+    reads at each replay.  It is never stored: ``dropout_backward`` forms it again.
+    """
+    import torch
+    code = _dtype_code(_matrix(x, "x"), "x")
+    n, k = x.shape
+    ldx = _rows(x, x.dtype, (n, k), x.device, "x")
+    ldr = 0 if residual is None else _rows(residual, x.dtype, (n, k), x.device, "residual")
+    if not 0.0 <= p <= 1.0:
+        raise ValueError("p must be 0 .. 1")
+    if not 0 <= seed < 2 ** 64:
+        raise ValueError("seed must be 0 .. 2^64 - 1")
+    at, number = None, offset
+    if isinstance(offset, torch.Tensor):
+        if offset.dtype != torch.int64 or offset.numel() != 1 or offset.device != x.device:
+            raise ValueError(f"offset must be an int, or one int64 on {x.device}")
+        at, number = offset, 0
+    elif not -2 ** 63 <= offset < 2 ** 63:
+        raise ValueError("offset must be of 64 bits")
+    _unrecorded(x=x, residual=residual)
+    lib = library()
+    with _launch(x.device, stream) as st:
+        y = torch.empty(n, k, dtype=x.dtype, device=x.device)
+        _check(lib.dpa4c_dropout(code, _ptr(x), ldx, _ptr(residual), ldr, n, _int(k), float(p), int(seed),
+                                 int(number), _ptr(at), _ptr(y), st))
+    return y
+
+
+def dropout_backward(dy, p: float, seed: int, offset=0, stream=None):
+    """dx of ``dropout`` with the same p, seed and offset, from dy = dL/dy; the residual's gradient is dy."""
+    return dropout(dy, p, seed, offset, stream=stream)

@@ -1,0 +1,209 @@
+// Internal definitions of the operators of a residual block: root-mean-square
+// norm, 8-bit rows and weights, layers of them, dropout (norm.hip, quantize.hip,
+// layer8.hip, dropout.hip).
+#pragma once
+
+#include "train.h"
+
+namespace dpa4c {
+
+constexpr int kScaleBlock = 128;   // entries that share a scale; of weights 128 x 128
+
+constexpr int64_t blocks_of(int64_t width) { return (width + kScaleBlock - 1) / kScaleBlock; }
+constexpr int64_t pitch8(int64_t width) { return align_up(width, 16); }   // bytes of a row of 8-bit numbers
+
+bool rows8_fit(int64_t n, int k);   // every launch over so many rows
+int launch_quantize_rows(int dtype, const void* x, int64_t ldx, const dpa4c_rows8& out, hipStream_t st);
+int launch_dequantize_rows(const dpa4c_rows8& in, int dtype, void* out, hipStream_t st);
+bool weights8_fit(int n_groups, int k, int n_out);
+int launch_quantize_weights(int dtype, const void* w, const dpa4c_weights8& out, hipStream_t st);
+int launch_dequantize_weights(const dpa4c_weights8& in, int dtype, void* out, hipStream_t st);
+
+struct NormIn {
+  const void* x;
+  int64_t ldx;
+  const void* residual;
+  int64_t ldr;
+  float eps;
+};
+int launch_rms_norm(const dpa4c_norm& l, const NormIn& in, void* y, const dpa4c_rows8* y8, float* rstd,
+                    void* h, hipStream_t st);
+struct NormBack {
+  const void* dy;
+  int64_t lddy;
+  const void* h;
+  int64_t ldh;
+  const float* rstd;
+  const void* dh;
+  int64_t lddh;
+};
+int64_t rms_norm_backward_work(const dpa4c_norm& l, bool dgain);
+int launch_rms_norm_backward(const dpa4c_norm& l, const NormBack& in, void* dx, void* dgain, void* work,
+                             hipStream_t st);
+
+bool grouped8_fits(const dpa4c_grouped8& l);
+int64_t grouped8_forward_work(const dpa4c_grouped8& l);
+int launch_grouped8_forward(const dpa4c_grouped8& l, const void* bias, bool silu, const void* residual,
+                            int64_t ldr, void* y, void* z, void* work, hipStream_t st);
+int64_t grouped8_backward_work(const dpa4c_grouped8& l, bool dx, bool dw, bool db);
+int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy, int64_t ldy, const void* z,
+                             int64_t ldz, void* dx, void* dw, void* db, void* work, hipStream_t st);
+
+struct Dropout {
+  const void* x;
+  int64_t ldx;
+  const void* residual;
+  int64_t ldr;
+  int64_t n;
+  int k;
+  double p;
+  uint64_t seed;
+  int64_t offset;
+  const int64_t* offset_at;
+};
+bool dropout_fits(int64_t n, int k);
+int launch_dropout(int dtype, const Dropout& d, void* y, hipStream_t st);
+
+#ifdef __HIPCC__
+// 8-bit numbers by format code: e4m3 (largest 448 = 1.75 2^8) or e5m2 (57,344 = 1.75 2^15)
+template <int F>
+constexpr int kTopExp = F == DPA4C_E4M3 ? 8 : 15;
+constexpr unsigned kNaN8 = 0x7f7f7f7f;   // four NaN of either format
+
+__device__ inline float power_of_two(int e) {   // -126 <= e <= 127
+  return __builtin_bit_cast(float, static_cast<unsigned>(e + 127) << 23);
+}
+// The least e >= -127 with most <= largest 2^e; -127 for a block of zeros.  ``most`` is finite.
+template <int F>
+__device__ inline int scale_exp(float most) {
+  const unsigned bits = __builtin_bit_cast(unsigned, most);
+  const int e = static_cast<int>(bits >> 23) - 127 - kTopExp<F> + ((bits & 0x7fffff) > 0x600000 ? 1 : 0);
+  return e < -127 ? -127 : e;
+}
+// four numbers of magnitude up to the largest, rounded to nearest even
+template <int F>
+__device__ inline unsigned pack8(float a, float b, float c, float d) {
+  if constexpr (F == DPA4C_E4M3) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return static_cast<unsigned>(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true));
+  } else {
+    const int lo = __builtin_amdgcn_cvt_pk_bf8_f32(a, b, 0, false);
+    return static_cast<unsigned>(__builtin_amdgcn_cvt_pk_bf8_f32(c, d, lo, true));
+  }
+}
+template <int F>
+__device__ inline void unpack8(unsigned v, float* f) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  f2 lo, hi;
+  if constexpr (F == DPA4C_E4M3) {
+    lo = __builtin_amdgcn_cvt_pk_f32_fp8(v, false);
+    hi = __builtin_amdgcn_cvt_pk_f32_fp8(v, true);
+  } else {
+    lo = __builtin_amdgcn_cvt_pk_f32_bf8(v, false);
+    hi = __builtin_amdgcn_cvt_pk_f32_bf8(v, true);
+  }
+  f[0] = lo.x, f[1] = lo.y, f[2] = hi.x, f[3] = hi.y;
+}
+// what a scale byte stands for: 2^(b - 127), NaN for 255
+__device__ inline float scale_of(unsigned b) {
+  return __builtin_bit_cast(float, b == 0 ? 0x00400000u : b == 255 ? 0x7fc00000u : b << 23);
+}
+
+// Largest finite magnitude of V entries, and whether one is an infinity or NaN.
+template <int V>
+__device__ inline float finite_most(const float* v, bool* bad) {
+  float m = 0.0f;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float a = fabsf(v[j]);
+    const bool fin = a < INFINITY;
+    *bad |= !fin;
+    m = fin ? fmaxf(m, a) : m;
+  }
+  return m;
+}
+
+// One block of 128 entries spread over ``lanes`` neighbouring lanes (a power of two), V
+// each: V / 4 words of 8-bit numbers to ``out``; returns the scale's byte.  A block
+// with an infinity or NaN is NaN as a whole, with the scale of its finite entries.
+template <int F, int V>
+__device__ inline unsigned quantize_block(const float* v, int lanes, unsigned* out) {
+  bool bad = false;
+  float m = finite_most<V>(v, &bad);
+  int any = bad;
+  for (int d = lanes / 2; d > 0; d /= 2) {
+    m = fmaxf(m, __shfl_xor(m, d));
+    any |= __shfl_xor(any, d);
+  }
+  const int e = scale_exp<F>(m);
+  const float up = power_of_two(-e);
+#pragma unroll
+  for (int j = 0; j < V / 4; ++j)
+    out[j] = any ? kNaN8 : pack8<F>(v[4 * j] * up, v[4 * j + 1] * up, v[4 * j + 2] * up, v[4 * j + 3] * up);
+  return static_cast<unsigned>(e + 127);
+}
+
+// How a launch deals rows to lanes: ``lanes`` of a wave (a power of two) take a row,
+// V entries each at a time, so that ``width`` entries take ceil(width / (lanes V)) turns.
+template <int V>
+__host__ __device__ inline int lanes_for(int width) {
+  int lanes = 1;
+  while (lanes < kWave && lanes * V < width) lanes *= 2;
+  return lanes;
+}
+
+template <class T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Entries {
+  T v[N];
+};
+// entries c .. c + V - 1 of a row of ``width``, zeros past it
+template <class T, int V>
+__device__ inline void load_entries(const T* row, int c, int width, float* f) {
+  if (c + V <= width) {
+    const Entries<T, V> e = *reinterpret_cast<const Entries<T, V>*>(row + c);
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = to_f32(e.v[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = c + j < width ? to_f32(row[c + j]) : 0.0f;
+  }
+}
+template <class T, int V>
+__device__ inline void store_entries(T* row, int c, int width, const float* f) {
+  if (c + V <= width) {
+    Entries<T, V> e;
+#pragma unroll
+    for (int j = 0; j < V; ++j) e.v[j] = from_f32<T>(f[j]);
+    *reinterpret_cast<Entries<T, V>*>(row + c) = e;
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (c + j < width) row[c + j] = from_f32<T>(f[j]);
+  }
+}
+
+// Items (row, part) of rows of ``each`` parts, 0 < each <= 2^14, without a division of 64
+// bits a lane: item ``first`` is uniform, ``past`` below 2^14 + 2^13.
+struct Item {
+  int64_t row;
+  int part;
+};
+__device__ inline Item item_at(int64_t first, int past, int each) {
+  const int64_t row = first / each;
+  const unsigned c = static_cast<unsigned>(first - row * each) + static_cast<unsigned>(past);
+  const unsigned more = each == 1 ? c : __umulhi(c, static_cast<unsigned>(((uint64_t(1) << 32) + each - 1) / each));
+  return {row + more, static_cast<int>(c - more * each)};
+}
+
+// the first group whose places end beyond ``place``; n_groups: none
+__device__ inline int group_of(const int64_t* ptr, int n_groups, int64_t place) {
+  int lo = 0, hi = n_groups;
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (ptr[mid + 1] <= place) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+#endif
+
+}  // namespace dpa4c

@@ -1,0 +1,245 @@
+// C-ABI entry points of the operators of a residual block.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <string>
+
+#include "block.h"
+#include "checks.h"
+
+namespace dpa4c {
+
+namespace {
+
+int unsupported(const std::string& msg) {
+  set_error(msg);
+  return DPA4C_ERR_UNSUPPORTED;
+}
+
+int check_dtype(const std::string& who, int dtype) {
+  if (dtype < DPA4C_F32 || dtype > DPA4C_BF16) return invalid(who + ": unknown dtype");
+  return 0;
+}
+
+int check_width(const std::string& who, int64_t k) {
+  if (k < 1 || k > kMaxWidth) return invalid(who + ": widths must be 1 .. 65536");
+  return 0;
+}
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// rows of ``width`` entries ``ld`` apart; 0: one row for all
+int check_ld(const std::string& who, int64_t ld, int64_t width) {
+  if (ld != 0 && ld < width) return invalid(who + ": rows overlap");
+  return 0;
+}
+
+// 8-bit rows; their pointers too with ``all``
+int check_rows8(const std::string& who, const dpa4c_rows8* r, bool all) {
+  if (!r) return invalid(who + ": null rows");
+  if (r->format != DPA4C_E4M3 && r->format != DPA4C_E5M2) return invalid(who + ": unknown format");
+  if (r->n < 0 || r->n > INT32_MAX) return invalid(who + ": n must be 0 .. 2^31 - 1");
+  DPA4C_TRY(check_width(who, r->k));
+  if (!rows8_fit(r->n, r->k)) return unsupported(who + ": more rows than one launch takes");
+  if (!all || r->n == 0) return 0;
+  if (!r->values || !r->scales) return invalid(who + ": null pointer");
+  if (!aligned16(r->values) || r->ld % 16 != 0 || r->ld < pitch8(r->k))
+    return invalid(who + ": 8-bit rows must start at multiples of 16 bytes");
+  if (r->ld_scales < blocks_of(r->k)) return invalid(who + ": rows of scales overlap");
+  return 0;
+}
+
+int check_weights8(const std::string& who, const dpa4c_weights8* w) {
+  if (!w) return invalid(who + ": null weights");
+  DPA4C_TRY(check_rows(who.c_str(), 0, w->n_groups, kMaxGroups));
+  DPA4C_TRY(check_width(who, w->k));
+  DPA4C_TRY(check_width(who, w->n_out));
+  if (!weights8_fit(w->n_groups, w->k, w->n_out)) return unsupported(who + ": more weights than one launch takes");
+  if (!aligned16(w->values) || !aligned16(w->turned)) return invalid(who + ": 8-bit weights must be 16-byte aligned");
+  return 0;
+}
+
+int check_norm(const std::string& who, const dpa4c_norm* l, bool all) {
+  if (!l) return invalid(who + ": null norm");
+  DPA4C_TRY(check_dtype(who, l->dtype));
+  DPA4C_TRY(check_rows(who.c_str(), l->n, l->n_groups, kMaxGroups));
+  DPA4C_TRY(check_width(who, l->k));
+  if (!all) return 0;
+  if (!l->group_ptr && (l->n_groups != 1 || l->order)) return invalid(who + ": several groups need group_ptr");
+  if (!l->gain) return invalid(who + ": null pointer");
+  return 0;
+}
+
+int check_layer8(const std::string& who, const dpa4c_grouped8* l, bool all) {
+  if (!l) return invalid(who + ": null layer");
+  DPA4C_TRY(check_dtype(who, l->dtype));
+  if (l->dtype == DPA4C_F32) return unsupported(who + ": results of 8-bit layers are float16 or bfloat16");
+  DPA4C_TRY(check_rows8(who, &l->x, all));
+  DPA4C_TRY(check_weights8(who, &l->w));
+  if (l->x.k != l->w.k) return invalid(who + ": x and w differ in k");
+  if (!grouped8_fits(*l)) return unsupported(who + ": more tiles than one launch takes");
+  if (!all) return 0;
+  if (!l->group_ptr || !l->w.scales) return invalid(who + ": null pointer");
+  return 0;
+}
+
+}  // namespace
+
+}  // namespace dpa4c
+
+using namespace dpa4c;
+
+extern "C" {
+
+int dpa4c_quantize_rows(int dtype, const void* x, int64_t ldx, const dpa4c_rows8* out, void* stream) {
+  return guarded([&] {
+    const char* who = "dpa4c_quantize_rows";
+    DPA4C_TRY(check_dtype(who, dtype));
+    DPA4C_TRY(check_rows8(who, out, true));
+    if (out->n > 0 && !x) return invalid("dpa4c_quantize_rows: null pointer");
+    DPA4C_TRY(check_ld(who, ldx, out->k));
+    return launch_quantize_rows(dtype, x, ldx, *out, static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_dequantize_rows(const dpa4c_rows8* in, int dtype, void* out, void* stream) {
+  return guarded([&] {
+    const char* who = "dpa4c_dequantize_rows";
+    DPA4C_TRY(check_dtype(who, dtype));
+    DPA4C_TRY(check_rows8(who, in, true));
+    if (in->n > 0 && !out) return invalid("dpa4c_dequantize_rows: null pointer");
+    return launch_dequantize_rows(*in, dtype, out, static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_quantize_weights(int dtype, const void* w, const dpa4c_weights8* out, void* stream) {
+  return guarded([&] {
+    const char* who = "dpa4c_quantize_weights";
+    DPA4C_TRY(check_dtype(who, dtype));
+    DPA4C_TRY(check_weights8(who, out));
+    if (!w || !out->scales) return invalid("dpa4c_quantize_weights: null pointer");
+    return launch_quantize_weights(dtype, w, *out, static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_dequantize_weights(const dpa4c_weights8* in, int dtype, void* out, void* stream) {
+  return guarded([&] {
+    const char* who = "dpa4c_dequantize_weights";
+    DPA4C_TRY(check_dtype(who, dtype));
+    DPA4C_TRY(check_weights8(who, in));
+    if (!in->values || !in->scales || !out) return invalid("dpa4c_dequantize_weights: null pointer");
+    return launch_dequantize_weights(*in, dtype, out, static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_rms_norm(const dpa4c_norm* norm, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                   float eps, void* y, const dpa4c_rows8* y8, float* rstd, void* h, void* stream) {
+  return guarded([&] {
+    const std::string who = "dpa4c_rms_norm";
+    DPA4C_TRY(check_norm(who, norm, true));
+    if (!(eps > 0) || !std::isfinite(eps)) return invalid(who + ": eps must be positive");
+    DPA4C_TRY(check_ld(who, ldx, norm->k));
+    if (residual) DPA4C_TRY(check_ld(who, ldr, norm->k));
+    if (y8) {
+      DPA4C_TRY(check_rows8(who, y8, true));
+      if (y || y8->n != norm->n || y8->k != norm->k) return invalid(who + ": y8 takes the place of y, of the same shape");
+    }
+    if (norm->n > 0 && (!x || (!y && !y8) || (residual != nullptr) != (h != nullptr)))
+      return invalid(who + ": null pointer, or h without a residual");
+    return launch_rms_norm(*norm, {x, ldx, residual, ldr, eps}, y, y8, rstd, h, static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_rms_norm_backward_work(const dpa4c_norm* norm, int dgain, int64_t* bytes) {
+  return guarded([&] {
+    const std::string who = "dpa4c_rms_norm_backward_work";
+    DPA4C_TRY(check_norm(who, norm, false));
+    if (!bytes) return invalid(who + ": null pointer");
+    *bytes = rms_norm_backward_work(*norm, dgain != 0);
+    return 0;
+  });
+}
+
+int dpa4c_rms_norm_backward(const dpa4c_norm* norm, const void* dy, int64_t lddy, const void* h, int64_t ldh,
+                            const float* rstd, const void* dh, int64_t lddh, void* dx, void* dgain, void* work,
+                            int64_t work_bytes, void* stream) {
+  return guarded([&] {
+    const std::string who = "dpa4c_rms_norm_backward";
+    DPA4C_TRY(check_norm(who, norm, true));
+    DPA4C_TRY(check_ld(who, lddy, norm->k));
+    DPA4C_TRY(check_ld(who, ldh, norm->k));
+    if (dh) DPA4C_TRY(check_ld(who, lddh, norm->k));
+    if (norm->n > 0 && (!dy || !h || !rstd)) return invalid(who + ": null pointer");
+    DPA4C_TRY(check_work(who.c_str(), work, work_bytes, rms_norm_backward_work(*norm, dgain != nullptr)));
+    return launch_rms_norm_backward(*norm, {dy, lddy, h, ldh, rstd, dh, lddh}, dx, dgain, work,
+                                    static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_grouped_linear8_work(const dpa4c_grouped8* layer, int64_t* bytes) {
+  return guarded([&] {
+    DPA4C_TRY(check_layer8("dpa4c_grouped_linear8_work", layer, false));
+    if (!bytes) return invalid("dpa4c_grouped_linear8_work: null pointer");
+    *bytes = grouped8_forward_work(*layer);
+    return 0;
+  });
+}
+
+int dpa4c_grouped_linear8(const dpa4c_grouped8* layer, const void* bias, int activation, const void* residual,
+                          int64_t ldr, void* y, void* z, void* work, int64_t work_bytes, void* stream) {
+  return guarded([&] {
+    const std::string who = "dpa4c_grouped_linear8";
+    DPA4C_TRY(check_layer8(who, layer, true));
+    if (activation != DPA4C_ACT_NONE && activation != DPA4C_ACT_SILU) return invalid(who + ": unknown activation");
+    if (!layer->w.turned || (layer->x.n > 0 && !y)) return invalid(who + ": null pointer");
+    if (residual) DPA4C_TRY(check_ld(who, ldr, layer->w.n_out));
+    DPA4C_TRY(check_work(who.c_str(), work, work_bytes, grouped8_forward_work(*layer)));
+    return launch_grouped8_forward(*layer, bias, activation == DPA4C_ACT_SILU, residual, ldr, y, z, work,
+                                   static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_grouped_linear8_backward_work(const dpa4c_grouped8* layer, int dx, int dw, int db, int64_t* bytes) {
+  return guarded([&] {
+    DPA4C_TRY(check_layer8("dpa4c_grouped_linear8_backward_work", layer, false));
+    if (!bytes) return invalid("dpa4c_grouped_linear8_backward_work: null pointer");
+    *bytes = grouped8_backward_work(*layer, dx != 0, dw != 0, db != 0);
+    return 0;
+  });
+}
+
+int dpa4c_grouped_linear8_backward(const dpa4c_grouped8* layer, int format, const void* dy, int64_t ldy,
+                                   const void* z, int64_t ldz, void* dx, void* dw, void* db, void* work,
+                                   int64_t work_bytes, void* stream) {
+  return guarded([&] {
+    const std::string who = "dpa4c_grouped_linear8_backward";
+    DPA4C_TRY(check_layer8(who, layer, true));
+    if (format != DPA4C_E4M3 && format != DPA4C_E5M2) return invalid(who + ": unknown format");
+    if ((layer->x.n > 0 && !dy) || (dx && !layer->w.values)) return invalid(who + ": null pointer");
+    DPA4C_TRY(check_ld(who, ldy, layer->w.n_out));
+    if (z) DPA4C_TRY(check_ld(who, ldz, layer->w.n_out));
+    DPA4C_TRY(check_work(who.c_str(), work, work_bytes,
+                         grouped8_backward_work(*layer, dx != nullptr, dw != nullptr, db != nullptr)));
+    return launch_grouped8_backward(*layer, format, dy, ldy, z, ldz, dx, dw, db, work,
+                                    static_cast<hipStream_t>(stream));
+  });
+}
+
+int dpa4c_dropout(int dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t n, int k,
+                  double p, uint64_t seed, int64_t offset, const int64_t* offset_at, void* y, void* stream) {
+  return guarded([&] {
+    const std::string who = "dpa4c_dropout";
+    DPA4C_TRY(check_dtype(who, dtype));
+    if (n < 0 || n > INT32_MAX) return invalid(who + ": n must be 0 .. 2^31 - 1");
+    DPA4C_TRY(check_width(who, k));
+    if (!(p >= 0 && p <= 1)) return invalid(who + ": p must be 0 .. 1");
+    if (!dropout_fits(n, k)) return unsupported(who + ": more rows than one launch takes");
+    if (n > 0 && (!x || !y)) return invalid(who + ": null pointer");
+    DPA4C_TRY(check_ld(who, ldx, k));
+    if (residual) DPA4C_TRY(check_ld(who, ldr, k));
+    return launch_dropout(dtype, {x, ldx, residual, ldr, n, k, p, seed, offset, offset_at}, y,
+                          static_cast<hipStream_t>(stream));
+  });
+}
+
+}  // extern "C"

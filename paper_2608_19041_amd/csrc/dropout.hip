@@ -1,0 +1,112 @@
+// Dropout from a counter-based generator: y = residual + keep x / (1 - p).
+//
+// The mask is not stored.  Entry c of row r is kept if word c % 4 of Philox4x32-10 (J. Salmon
+// et al., "Parallel random numbers: as easy as 1, 2, 3", 2011) with the counter
+// (c / 4, r, offset low, offset high) and the key ``seed`` is at least p 2^32, so a
+// row's mask depends neither on how rows lie in memory nor on the launch, and the
+// gradient of the rows is this operator again.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "block.h"
+
+namespace dpa4c {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTurns = 4;
+
+struct Words {
+  unsigned v[4];
+};
+__device__ inline Words philox(unsigned c0, unsigned c1, unsigned c2, unsigned c3, unsigned k0, unsigned k1) {
+#pragma unroll
+  for (int i = 0; i < 10; ++i) {
+    const uint64_t a = uint64_t(c0) * 0xD2511F53u, b = uint64_t(c2) * 0xCD9E8D57u;
+    c0 = static_cast<unsigned>(b >> 32) ^ c1 ^ k0;
+    c1 = static_cast<unsigned>(b);
+    c2 = static_cast<unsigned>(a >> 32) ^ c3 ^ k1;
+    c3 = static_cast<unsigned>(a);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return {{c0, c1, c2, c3}};
+}
+
+struct Args {
+  const void* x;
+  int64_t ldx;
+  const void* res;   // or null
+  int64_t ldr;
+  int64_t n;
+  int k;
+  unsigned drop;     // words below it drop an entry
+  int all;           // every entry is dropped
+  float scale;
+  uint64_t seed;
+  int64_t offset;
+  const int64_t* offset_at;   // added to it, or null
+  void* y;
+};
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) dropout_kernel(Args a) {
+  constexpr int V = 16 / int(sizeof(T));
+  const int parts = (a.k + V - 1) / V;
+  const int64_t first = int64_t(blockIdx.x) * kThreads * kTurns;
+  const uint64_t offset = static_cast<uint64_t>(a.offset) + (a.offset_at ? static_cast<uint64_t>(*a.offset_at) : 0);
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const Item at = item_at(first, i * kThreads + int(threadIdx.x), parts);
+    if (at.row >= a.n) continue;
+    const int c = at.part * V;
+    float x[V], r[V], y[V];
+    load_entries<T, V>(static_cast<const T*>(a.x) + at.row * a.ldx, c, a.k, x);
+    if (a.res)
+      load_entries<T, V>(static_cast<const T*>(a.res) + at.row * a.ldr, c, a.k, r);
+    else
+#pragma unroll
+      for (int j = 0; j < V; ++j) r[j] = 0.0f;
+#pragma unroll
+    for (int q = 0; q < V / 4; ++q) {
+      const Words w = philox(static_cast<unsigned>(c / 4 + q), static_cast<unsigned>(at.row),
+                             static_cast<unsigned>(offset), static_cast<unsigned>(offset >> 32),
+                             static_cast<unsigned>(a.seed), static_cast<unsigned>(a.seed >> 32));
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // a dropped entry does not enter, whatever it is
+        const bool keep = w.v[j] >= a.drop && !a.all;
+        y[4 * q + j] = keep ? fmaf(x[4 * q + j], a.scale, r[4 * q + j]) : r[4 * q + j];
+      }
+    }
+    store_entries<T, V>(static_cast<T*>(a.y) + at.row * int64_t(a.k), c, a.k, y);
+  }
+}
+
+int64_t workgroups(int64_t n, int k, int each) {
+  const int64_t items = n * ((int64_t(k) + each - 1) / each);
+  return (items + kThreads * kTurns - 1) / (kThreads * kTurns);
+}
+
+}  // namespace
+
+bool dropout_fits(int64_t n, int k) { return grid_fits(workgroups(n, k, 4), kThreads); }
+
+int launch_dropout(int dtype, const Dropout& d, void* y, hipStream_t st) {
+  if (d.n == 0) return 0;
+  Args a{d.x, d.ldx, d.residual, d.ldr, d.n, d.k, 0, 0, 0.0f, d.seed, d.offset, d.offset_at, y};
+  const double drop = std::floor(d.p * 4294967296.0 + 0.5);
+  a.all = drop >= 4294967296.0;
+  a.drop = a.all ? 0 : static_cast<unsigned>(drop);
+  a.scale = a.all ? 0.0f : static_cast<float>(1.0 / (1.0 - d.p));
+  return with_dtype(dtype, [&](auto t) {
+    using T = typename Elem<decltype(t)::value>::T;
+    dropout_kernel<T><<<workgroups(d.n, d.k, 16 / int(sizeof(T))), kThreads, 0, st>>>(a);
+    DPA4C_HIP_TRY(hipGetLastError());
+    return 0;
+  });
+}
+
+}  // namespace dpa4c

@@ -1,0 +1,790 @@
+// Grouped layers of 8-bit rows and weights, and their gradients.
+//
+//   forward   y = act(x W_g + b_g) (+ residual)    8-bit product of depth k
+//   dx        Q(dz) W_g^T, dz = dy act'(z)         8-bit product of depth n_out
+//   dW, db    x^T dz, sum of dz over a group       float16 products of depth rows
+//
+// A matrix instruction of 8-bit operands takes their power-of-two scales, one for each 32
+// entries of a row, here one for each block of 128, and adds in float32; within an instruction it
+// aligns the products of some eight neighbouring entries to 2^-14 of the largest, which is
+// 1.5e-5 of a result (2-norm, normal entries) and 2^-11 of the sum of the products' sizes at the
+// worst, far below what 8 bits hold and below the rounding of a half type: results are half types only.
+//
+// The gradient of the weights sums over rows, whose scales differ, so there a step's x becomes
+// float16 under a scale of its row, which holds it exactly, and dz is a single float16 under the
+// scale of its block of 128 (2^-12 of itself; x is off by 2^-4).
+#include <hip/hip_runtime.h>
+
+#include "block.h"
+#include "rows.h"
+
+namespace dpa4c {
+
+namespace {
+
+constexpr int kThreads = kTileThreads;
+constexpr int kStep = kScaleBlock;      // reduction entries of a step, a row of 128 bytes
+constexpr int kSlots8 = kStep / 16;
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+// byte offset of 16-byte slot ``slot`` of row ``row`` in an operand's step: exchanged by
+// bits of the row, so that eight rows at one slot meet all banks
+__device__ inline int slot8_at(int row, int slot) { return row * kStep + ((slot ^ (row & 7)) << 4); }
+
+// the first ``keep`` of sixteen bytes, zeros past them
+__device__ inline u4 keep_bytes(u4 v, int keep) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int left = keep - 4 * j;
+    const unsigned mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+    v[j] &= mask;
+  }
+  return v;
+}
+
+struct RowsArgs {
+  const int32_t* order;
+  int n_groups;
+  int64_t n;
+  const RowTile* tiles;
+  const int32_t* n_tiles;
+  int kin, kout;
+  const char* in;            // 8-bit rows, ldin bytes apart
+  int64_t ldin;
+  const uint8_t* in_scales;
+  int64_t ld_scales;
+  int by_place;              // ``in`` is in group order
+  const char* w;             // [group][kout][pitch8(kin)]
+  const uint8_t* w_scales;   // of a group: block i of kin and j of kout at i at_in + j at_out
+  int64_t w_blocks, at_in, at_out;
+  const void* bias;
+  int silu;
+  const void* residual;      // rows of kout entries, ldres apart, or null
+  int64_t ldres;
+  void* out;
+  void* zout;
+};
+
+// A tile of 64 NB rows x 64 NB columns by four waves; a step is one block of 128 entries.
+template <class T, int F, int NB>
+__global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(RowsArgs a) {
+  constexpr int kTile = kSide<NB>, kOne = kTile * kStep, kHalfLds = 2 * kOne;
+  constexpr int kLoads = kTile * kSlots8 / kThreads;   // of a thread, operand and step
+  static_assert(2 * kHalfLds >= kTile * kTile * 4, "the outputs pass through the operands' place");
+  __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
+  __shared__ int32_t row_of[kTile];   // -1: nothing is stored
+
+  const int col_tiles = (a.kout + kTile - 1) / kTile;
+  const int64_t total = int64_t(*a.n_tiles) * col_tiles;
+  if (blockIdx.x >= total) return;
+  // the column tiles of a row tile follow each other on one XCD
+  const int64_t work = xcd_block(blockIdx.x, total);
+  const RowTile t = a.tiles[work / col_tiles];
+  const int c0 = static_cast<int>(work % col_tiles) * kTile;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave >> 1, wn = wave & 1;
+  T* out = static_cast<T*>(a.out);
+  T* zout = static_cast<T*>(a.zout);
+
+  if (t.group == a.n_groups) {   // rows of no group
+    const int width = a.kout - c0 < kTile ? a.kout - c0 : kTile;
+    for (int i = tid; i < t.count * width; i += kThreads) {
+      const int64_t row = row_at(a.order, t.first + i / width, a.n);
+      if (row < 0) continue;
+      out[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
+      if (zout) zout[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
+    }
+    return;
+  }
+
+  // slot tid % 8 of rows (and columns) tid / 8, + 32, ..; those past the last repeat it,
+  // and nothing of them is stored
+  const int slot = tid % kSlots8, own = tid / kSlots8;
+  const int64_t pitch = pitch8(a.kin);
+  const char* rows[kLoads];
+  const char* cols[kLoads];
+  auto row_in = [&](int r) {
+    r = r < t.count ? r : t.count - 1;
+    const int64_t to = row_at(a.order, t.first + r, a.n);
+    return a.by_place ? t.first + r : to < 0 ? 0 : to;
+  };
+  const char* w = a.w + int64_t(t.group) * a.kout * pitch;
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    rows[i] = a.in + row_in(32 * i + own) * a.ldin;
+    const int c = c0 + 32 * i + own;
+    cols[i] = w + int64_t(c < a.kout ? c : a.kout - 1) * pitch;
+  }
+  if (tid < kTile)
+    row_of[tid] = tid < t.count ? static_cast<int32_t>(row_at(a.order, t.first + tid, a.n)) : -1;
+  // the scales of this lane's rows in a product
+  const uint8_t* scales[NB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+    scales[i] = a.in_scales + row_in(kTile / 2 * wm + 32 * i + (lane & 31)) * a.ld_scales;
+  const uint8_t* wscale = a.w_scales + t.group * a.w_blocks + c0 / kScaleBlock * a.at_out;
+
+  const int steps = static_cast<int>(blocks_of(a.kin)), chunks = static_cast<int>(pitch / 16);
+  constexpr int kFar = NB == 2 ? 2 : 4, kNear = 2;
+  u4 ra[kFar][kLoads], rb[kNear][kLoads];
+  unsigned sa[kFar][NB], sb[kNear];
+  auto chunk_of = [&](int step) {   // any that is there for those past the end
+    const int c = step * kSlots8 + slot;
+    return (c < chunks ? c : chunks - 1) * 16;
+  };
+  auto far = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const int c = chunk_of(step), s = step < steps ? step : steps - 1;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) ra[q][i] = *reinterpret_cast<const u4*>(rows[i] + c);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) sa[q][i] = scales[i][s];
+  };
+  auto near = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const int c = chunk_of(step), s = step < steps ? step : steps - 1;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) rb[q][i] = *reinterpret_cast<const u4*>(cols[i] + c);
+    sb[q] = wscale[s * a.at_in];
+  };
+
+  Sums<NB> acc;
+  acc.clear();
+  unsigned put_a[2][NB], put_b[2];   // of the halves of LDS
+  auto put = [&](auto turn, auto far_turn, int step) {
+    constexpr int n = decltype(turn)::value, f = decltype(far_turn)::value, q = f & 1;
+    char* la = lds + q * kHalfLds;
+    if ((step + 1) * kStep > a.kin) {   // the last step
+      const int keep = a.kin - step * kStep - slot * 16;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        ra[f][i] = keep_bytes(ra[f][i], keep);
+        rb[n][i] = keep_bytes(rb[n][i], keep);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int at = slot8_at(32 * i + own, slot);
+      *reinterpret_cast<u4*>(la + at) = ra[f][i];
+      *reinterpret_cast<u4*>(la + kOne + at) = rb[n][i];
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) put_a[q][i] = sa[f][i];
+    put_b[q] = sb[n];
+  };
+  const bool live = c0 + kTile / 2 * wn < a.kout && kTile / 2 * wm < t.count;
+  v8i fa[2][NB], fb[2][NB];
+  unsigned of_a[2][NB], of_b[2];
+  auto fragment = [&](const char* from, int row, int ks) {
+    u4 h[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      h[j] = *reinterpret_cast<const u4*>(from + slot8_at(row, 4 * ks + 2 * (lane >> 5) + j));
+    v8i r;
+    __builtin_memcpy(&r, h, 32);
+    return r;
+  };
+  auto read = [&](auto half, int step) {
+    constexpr int ks = decltype(half)::value;
+    if (!live) return;
+    const char* la = lds + (step & 1) * kHalfLds;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      fa[ks][i] = fragment(la, kTile / 2 * wm + 32 * i + (lane & 31), ks);
+      fb[ks][i] = fragment(la + kOne, kTile / 2 * wn + 32 * i + (lane & 31), ks);
+      of_a[ks][i] = step & 1 ? put_a[1][i] : put_a[0][i];
+    }
+    of_b[ks] = step & 1 ? put_b[1] : put_b[0];
+  };
+  auto multiply = [&](auto half) {
+    constexpr int ks = decltype(half)::value;
+    if (!live) return;
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+        acc.v[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            fa[ks][i], fb[ks][j], acc.v[i][j], F == DPA4C_E4M3 ? 0 : 1, 0, 0, of_a[ks][i], 0, of_b[ks]);
+  };
+  run_steps<kNear, kFar>(steps, near, far, put, read, [](int) {}, multiply);
+
+  // outputs through LDS, so that rows are written in one piece
+  float* stage = reinterpret_cast<float*>(lds);
+  constexpr int kLanes = kTile / 4, kRowsOnce = kThreads / kLanes;   // lanes a row, rows at a time
+  const int quad = tid % kLanes, c = c0 + quad * 4;
+  const T* bias = a.bias ? static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
+  float bq[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) bq[j] = bias && c + j < a.kout ? to_f32(bias[c + j]) : 0.0f;
+  __syncthreads();
+  stage_sums(stage, acc, kTile / 2 * wm, kTile / 2 * wn, lane, 1.0f);
+  __syncthreads();
+  if (c >= a.kout) return;
+  constexpr int kBatch = 4;   // rows in flight
+#pragma unroll 1
+  for (int r0 = tid / kLanes; r0 < t.count; r0 += kRowsOnce * kBatch) {
+    int64_t row[kBatch];
+    float res[kBatch][4];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const int r = r0 + kRowsOnce * k;
+      row[k] = r < t.count ? row_of[r] : -1;
+      if (a.residual && row[k] >= 0)
+        load_entries<T, 4>(static_cast<const T*>(a.residual) + row[k] * a.ldres, c, a.kout, res[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      if (row[k] < 0) continue;
+      const v4f s = *reinterpret_cast<const v4f*>(stage + stage_at<NB>(r0 + kRowsOnce * k, quad * 4));
+      float y[4], z[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        z[j] = s[j] + bq[j];
+        y[j] = a.silu ? z[j] * logistic(z[j]) : z[j];
+        if (a.residual) y[j] += res[k][j];
+      }
+      store_entries<T, 4>(out + row[k] * a.kout, c, a.kout, y);
+      if (zout) store_entries<T, 4>(zout + row[k] * a.kout, c, a.kout, z);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// What the gradients need first
+// ---------------------------------------------------------------------------
+
+// dz as float16: dz 2^(kHalfUp - e), e the exponent of its block's scale, so that the largest
+// entry of a block lies in (2^13.8, 2^14.8]; as 8-bit numbers: dz 2^-e
+template <int F>
+constexpr int kHalfUp = 14 - kTopExp<F>;
+
+struct PrepArgs {
+  const int64_t* ptr;
+  int n_groups;
+  int64_t n;
+  const int32_t* order;
+  TileList tiles, blocks;   // list = null: not needed
+  // zeros for the groups without rows (null: not formed)
+  void *dw, *db;
+  int k, m;
+  const void *dy, *z;
+  int64_t ldy, ldz;
+  _Float16* dz;             // [n][pitch8(m)] by place
+  uint8_t* dz8;             // the same in 8 bits
+  uint8_t* dz_scales;       // [n][blocks of m] by place
+  int64_t list_blocks, clear_blocks;
+};
+
+constexpr int kPrepThreads = 512, kPrepTurns = 2;
+constexpr int kUnit = kScaleBlock / 8;   // lanes of a block of dz
+constexpr int64_t kClear = 1 << 16;      // entries of a workgroup
+
+template <class T>
+__device__ inline void clear_group(const PrepArgs& a, int g, int64_t part) {
+  const Span s = span_of(a.ptr, g, a.n_groups, a.n);
+  if (s.begin != s.end) return;
+  const Entries<T, 8> none = {};
+  const int64_t each = int64_t(a.k) * a.m;
+  if (a.dw) {
+    T* out = static_cast<T*>(a.dw) + g * each;
+    const int64_t end = (part + 1) * kClear < each ? (part + 1) * kClear : each;
+    for (int64_t i = part * kClear + threadIdx.x * 8; i < end; i += kPrepThreads * 8) {
+      if (i + 8 <= end)
+        *reinterpret_cast<Entries<T, 8>*>(out + i) = none;
+      else
+        for (int64_t j = i; j < end; ++j) out[j] = none.v[0];
+    }
+  }
+  if (a.db && part == 0)
+    for (int i = threadIdx.x; i < a.m; i += kPrepThreads) static_cast<T*>(a.db)[int64_t(g) * a.m + i] = none.v[0];
+}
+
+template <class T, int F>
+__global__ void __launch_bounds__(kPrepThreads) layer8_prepare_kernel(PrepArgs a) {
+  extern __shared__ int32_t starts[];
+  int64_t b = blockIdx.x;
+  if (b < a.list_blocks) {
+    const int block = static_cast<int>(b), blocks = static_cast<int>(a.list_blocks);
+    if (a.tiles.list) list_tiles(a.tiles, a.ptr, a.n_groups, a.n, block, blocks, starts);
+    __syncthreads();
+    if (a.blocks.list) list_tiles(a.blocks, a.ptr, a.n_groups, a.n, block, blocks, starts);
+    return;
+  }
+  b -= a.list_blocks;
+  if (b < a.clear_blocks) {
+    const int64_t each = a.clear_blocks / a.n_groups;
+    clear_group<T>(a, static_cast<int>(b / each), b % each);
+    return;
+  }
+  b -= a.clear_blocks;
+  constexpr int kUnits = kPrepThreads / kUnit;
+  const int blocks = static_cast<int>(blocks_of(a.m)), lane = threadIdx.x % kUnit;
+  const int64_t pitch = pitch8(a.m), live = clamp_place(a.ptr[a.n_groups], a.n);
+  Item at[kPrepTurns];
+  float v[kPrepTurns][8], z[kPrepTurns][8];
+#pragma unroll
+  for (int i = 0; i < kPrepTurns; ++i) {
+    at[i] = item_at(b * kUnits * kPrepTurns, i * kUnits + int(threadIdx.x) / kUnit, blocks);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = z[i][j] = 0.0f;
+    if (at[i].row >= live) continue;
+    const int64_t row = row_at(a.order, at[i].row, a.n);
+    if (row < 0) continue;
+    const int c = at[i].part * kScaleBlock + lane * 8;
+    load_entries<T, 8>(static_cast<const T*>(a.dy) + row * a.ldy, c, a.m, v[i]);
+    if (a.z) load_entries<T, 8>(static_cast<const T*>(a.z) + row * a.ldz, c, a.m, z[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPrepTurns; ++i) {
+    if (at[i].row >= live) continue;   // a unit as a whole
+    if (a.z)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] *= silu_slope(z[i][j]);
+    unsigned q[2];
+    const unsigned scale = quantize_block<F, 8>(v[i], kUnit, q);
+    const int c = at[i].part * kScaleBlock + lane * 8;
+    if (c >= pitch) continue;
+    if (a.dz8) __builtin_memcpy(a.dz8 + at[i].row * pitch + c, q, 8);
+    if (lane == 0) a.dz_scales[at[i].row * blocks + at[i].part] = static_cast<uint8_t>(scale);
+    if (a.dz) {
+      const int e = static_cast<int>(scale) - 127;   // two powers: one may be beyond float32's
+      const float up = power_of_two(-e), more = power_of_two(kHalfUp<F>);
+      v8h h;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = static_cast<_Float16>(v[i][j] * up * more);
+      *reinterpret_cast<v8h*>(a.dz + at[i].row * pitch + c) = h;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Gradients of the weights
+// ---------------------------------------------------------------------------
+
+struct OuterArgs {
+  const int32_t* order;
+  int64_t n;
+  const RowTile* blocks;
+  const int32_t* n_blocks;
+  int k, m;
+  const char* x;             // 8-bit rows, ldx bytes apart
+  int64_t ldx;
+  const uint8_t* x_scales;
+  int64_t ld_scales;
+  const _Float16* dz;        // [n][pitch8(m)] by place
+  const uint8_t* dz_scales;  // [n][blocks of m]
+  int dz_up;                 // kHalfUp of dz's format
+  void *dw, *db;             // null: not formed
+  float *parts, *db_parts;   // [slot][k][m], [slot][m] where a group has several blocks
+  Slots slots;
+};
+
+// two 8-bit numbers of word ``v`` times a power of two, as float16
+template <int F, bool High>
+__device__ inline v2h half_pair(unsigned v, float scale) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  if constexpr (F == DPA4C_E4M3)
+    return __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, scale, High));
+  else
+    return __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_bf8(v, scale, High));
+}
+
+// Tiles of 128 x 128 of x^T dz over a block of rows, 32 rows a step; transposing reads turn
+// both operands.  A row's factor, of x's scale and dz's, is applied to x: relative to
+// the largest of the block, 2^kXUp of which brings x's largest entry to 2^15.8, so that an entry is
+// held exactly, or to 2^-40 of the largest product of the block.
+template <class T, int F>
+__global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) {
+  constexpr int kOne = kPlane<2>, kHalfLds = 2 * kOne;
+  constexpr int kXUp = 15 - kTopExp<F>;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
+  __shared__ float bias_part[16][kOuterTile];
+  __shared__ int32_t tops[kThreads / kWave];
+  const int row_tiles = a.dw ? (a.k + kOuterTile - 1) / kOuterTile : 1;
+  const int col_tiles = (a.m + kOuterTile - 1) / kOuterTile;
+  const int64_t total = int64_t(*a.n_blocks) * row_tiles * col_tiles;
+  if (blockIdx.x >= total) return;
+  // the tiles of a block of rows follow each other on one XCD
+  const int64_t work = xcd_block(blockIdx.x, total);
+  const int64_t block = work / (row_tiles * col_tiles);
+  const RowTile t = a.blocks[block];
+  const int64_t group_slot =
+      a.slots.by_start ? a.slots.of(t.first - int64_t(t.part) * a.slots.rows, t.part) : block;
+  const int r0 = static_cast<int>(work / col_tiles % row_tiles) * kOuterTile;
+  const int c0 = static_cast<int>(work % col_tiles) * kOuterTile;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave >> 1, wn = wave & 1;
+  const int64_t end = t.first + t.count, pitch = pitch8(a.m);
+  const int z_blocks = static_cast<int>(blocks_of(a.m));
+  const uint8_t* xs = a.x_scales + r0 / kScaleBlock;
+  const uint8_t* zs = a.dz_scales + c0 / kScaleBlock;
+  const int steps = (t.count + kDepth - 1) / kDepth;
+  const bool sums_bias = a.db && r0 == 0;
+
+  // the largest exponent of a row of the block
+  int top = 0;
+  if (a.dw) {
+    for (int i = tid; i < t.count; i += kThreads) {
+      const int64_t row = row_at(a.order, t.first + i, a.n);
+      const int ex = row < 0 ? 255 : xs[row * a.ld_scales];
+      const int s = ex + zs[(t.first + i) * z_blocks];
+      top = ex < 255 && s > top ? s : top;
+    }
+    for (int d = kWave / 2; d > 0; d /= 2) top = max(top, __shfl_xor(top, d));
+    if (lane == 0) tops[wave] = top;
+    __syncthreads();
+    for (int i = 0; i < kThreads / kWave; ++i) top = max(top, tops[i]);
+  }
+
+  // x: place tid / 8 of a step, sixteen columns; dz: places tid / 16 and + 16, eight columns
+  const int x_own = tid / 8, x_slot = tid % 8, z_own = tid / 16, z_slot = tid % 16;
+  const int x_last = static_cast<int>(pitch8(a.k)) - 16, z_last = static_cast<int>(pitch) - 8;
+  const int xc = r0 + 16 * x_slot < x_last ? r0 + 16 * x_slot : x_last;   // columns past the end: any
+  const int zc = c0 + 8 * z_slot < z_last ? c0 + 8 * z_slot : z_last;
+  // the rows of a step are looked up one fetch before its loads, and before that fetch's own:
+  // loads arrive in order, so they are there in time without the operands having to be
+  int64_t next;
+  auto look = [&](int step) {
+    const int64_t place = t.first + int64_t(step) * kDepth + x_own;
+    const int64_t at = place < end ? place : end - 1;
+    const int64_t row = a.order ? a.order[at] : at;   // without a condition
+    next = place < end && row >= 0 && row < a.n ? row : -1;
+  };
+  u4 rx[2], rz[2][2];
+  bool there[2];
+  unsigned ex[2], ez[2], zscale[2][2];
+  look(0);
+  auto fetch = [&](auto turn, int step) {
+    constexpr int q = decltype(turn)::value;
+    const int64_t row = next < 0 ? 0 : next;
+    there[q] = next >= 0;
+    look(step + 1);
+    rx[q] = *reinterpret_cast<const u4*>(a.x + row * a.ldx + xc);
+    ex[q] = xs[row * a.ld_scales];
+    const int64_t first = t.first + int64_t(step) * kDepth;
+    ez[q] = zs[(first + x_own < end ? first + x_own : end - 1) * z_blocks];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t place = first + z_own + 16 * i, at = place < end ? place : end - 1;
+      rz[q][i] = *reinterpret_cast<const u4*>(a.dz + at * pitch + zc);
+      zscale[q][i] = place < end ? zs[at * z_blocks] : 256;
+    }
+  };
+  float bias[8] = {};
+  auto put = [&](auto turn, auto, int) {
+    constexpr int q = decltype(turn)::value;
+    char* to = lds + q * kHalfLds;
+    if (a.dw) {
+      const int d = static_cast<int>(ex[q] + ez[q]) - top + kXUp;   // at most kXUp
+      const float scale = ex[q] == 255 ? NAN : power_of_two(d < -126 ? -126 : d);
+      v8h h[2] = {};
+      if (there[q])
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const v2h lo = half_pair<F, false>(rx[q][j], scale), hi = half_pair<F, true>(rx[q][j], scale);
+          h[j / 2][4 * (j % 2)] = lo.x, h[j / 2][4 * (j % 2) + 1] = lo.y;
+          h[j / 2][4 * (j % 2) + 2] = hi.x, h[j / 2][4 * (j % 2) + 3] = hi.y;
+        }
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        *reinterpret_cast<v8h*>(to + x_slot / 2 * 32 * kRowBytes + slot_at(x_own, x_slot % 2 * 2 + j)) = h[j];
+    }
+    const u4 none = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const u4 v = zscale[q][i] < 256 ? rz[q][i] : none;
+      if (sums_bias) {
+        const v8h f = __builtin_bit_cast(v8h, v);
+        const float own = scale_of(zscale[q][i] & 255) * power_of_two(-a.dz_up);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bias[j] += static_cast<float>(f[j]) * own;
+      }
+      *reinterpret_cast<u4*>(to + kOne + z_slot / 4 * 32 * kRowBytes + slot_at(z_own + 16 * i, z_slot % 4)) = v;
+    }
+  };
+  Sums<2> acc;
+  acc.clear();
+  const bool live = a.dw && r0 + 64 * wm < a.k && c0 + 64 * wn < a.m;
+  Part<2, 1> fa[2], fb[2];
+  auto read = [&](auto half, int step) {
+    constexpr int ks = decltype(half)::value;
+    if (!live) return;
+    load_part_turned(fa[ks], lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes, kOne, lane, ks);
+    load_part_turned(fb[ks], lds + (step & 1) * kHalfLds + kOne + wn * 64 * kRowBytes, kOne, lane, ks);
+  };
+  auto multiply = [&](auto half) {
+    constexpr int ks = decltype(half)::value;
+    if (live) multiply_parts<false>(acc, fa[ks], fb[ks]);
+  };
+  run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
+
+  const bool whole = t.parts == 1;
+  if (a.dw) {
+    T* dw = static_cast<T*>(a.dw) + int64_t(t.group) * a.k * a.m;
+    float* part = a.parts + group_slot * a.k * a.m;
+    const int e = top - 254 - kXUp - a.dz_up;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int c = c0 + 64 * wn + 32 * j + (lane & 31);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = r0 + 64 * wm + 32 * i + sum_row(lane, r);
+          if (row >= a.k || c >= a.m) continue;
+          const float v = ldexpf(acc.v[i][j][r], e);
+          if (whole)
+            dw[int64_t(row) * a.m + c] = from_f32<T>(v);
+          else
+            part[int64_t(row) * a.m + c] = v;
+        }
+      }
+  }
+  if (sums_bias) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bias_part[z_own][8 * z_slot + j] = bias[j];
+    __syncthreads();
+    if (tid < kOuterTile && c0 + tid < a.m) {
+      float v = 0.0f;
+      for (int i = 0; i < 16; ++i) v += bias_part[i][tid];
+      if (whole)
+        static_cast<T*>(a.db)[int64_t(t.group) * a.m + c0 + tid] = from_f32<T>(v);
+      else
+        a.db_parts[group_slot * a.m + c0 + tid] = v;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+
+// 128 x 128 tiles where they fill the compute units, else 64 x 64
+bool large_tiles(int64_t n, int cols) { return cols > 64 && (n / 128) * ((cols + 127) / 128) >= 256; }
+int tile_rows(int64_t n, int cols) { return large_tiles(n, cols) ? kSide<2> : kSide<1>; }
+
+struct Plan {
+  TileList tiles, blocks;
+  _Float16* dz;
+  uint8_t *dz8, *dz_scales;
+  float *parts, *db_parts;
+  Slots slots;
+};
+Plan plan_forward(const dpa4c_grouped8& l, void* work, int64_t* bytes) {
+  Arena ar{static_cast<char*>(work)};
+  Plan p{};
+  p.tiles = list_of(ar, l.x.n, l.w.n_groups, tile_rows(l.x.n, l.w.n_out), true);
+  *bytes = ar.used;
+  return p;
+}
+Plan plan_backward(const dpa4c_grouped8& l, bool dx, bool dw, bool db, void* work, int64_t* bytes) {
+  Arena ar{static_cast<char*>(work)};
+  Plan p{};
+  const int64_t n = l.x.n;
+  const int k = l.w.k, m = l.w.n_out, groups = l.w.n_groups, rows = outer_rows(n, k, m);
+  if (dx) p.tiles = list_of(ar, n, groups, tile_rows(n, k), true);
+  if (dw || db) p.blocks = list_of(ar, n, groups, rows, false);
+  p.dz = ar.take<_Float16>(dw || db ? n * pitch8(m) : 0);
+  p.dz8 = ar.take<uint8_t>(dx ? n * pitch8(m) : 0);
+  p.dz_scales = ar.take<uint8_t>(n * blocks_of(m));
+  // only groups of more than ``rows`` rows have several blocks
+  const int64_t blocks = tiles_at_most(n, groups, rows), ends = n > rows ? (2 * n + rows - 1) / rows : 0;
+  p.slots = {rows, ends < blocks};
+  p.parts = ar.take<float>(dw ? std::min(blocks, ends) * k * m : 0);
+  p.db_parts = ar.take<float>(db ? std::min(blocks, ends) * m : 0);
+  *bytes = ar.used;
+  return p;
+}
+
+int64_t list_workgroups(int64_t tiles) {
+  return std::max<int64_t>(1, std::min<int64_t>(64, tiles / kPrepThreads));
+}
+
+// the lists alone
+template <class T, int F>
+int prepare(const PrepArgs& a, int64_t grid, hipStream_t st) {
+  layer8_prepare_kernel<T, F><<<grid, kPrepThreads, (a.n_groups + 2) * sizeof(int32_t), st>>>(a);
+  DPA4C_HIP_TRY(hipGetLastError());
+  return 0;
+}
+
+template <class T, int F>
+int run_rows(const RowsArgs& a, const TileList& tiles, hipStream_t st) {
+  const int64_t most = tiles_at_most(a.n, a.n_groups, tiles.rows);
+  if (tiles.rows == kSide<2>)
+    layer8_rows_kernel<T, F, 2><<<most * ((a.kout + 127) / 128), kThreads, 0, st>>>(a);
+  else
+    layer8_rows_kernel<T, F, 1><<<most * ((a.kout + 63) / 64), kThreads, 0, st>>>(a);
+  DPA4C_HIP_TRY(hipGetLastError());
+  return 0;
+}
+
+template <class Fn>
+int with_types(int dtype, int format, Fn&& fn) {
+  using E4 = std::integral_constant<int, DPA4C_E4M3>;
+  using E5 = std::integral_constant<int, DPA4C_E5M2>;
+  if (dtype == DPA4C_F16) return format == DPA4C_E4M3 ? fn(_Float16{}, E4{}) : fn(_Float16{}, E5{});
+  return format == DPA4C_E4M3 ? fn(__bf16{}, E4{}) : fn(__bf16{}, E5{});
+}
+
+}  // namespace
+
+bool grouped8_fits(const dpa4c_grouped8& l) {
+  auto up = [](int64_t x, int64_t by) { return (x + by - 1) / by; };
+  const int64_t n = l.x.n, k = l.w.k, m = l.w.n_out;
+  const int64_t prep = 64 + l.w.n_groups * up(k * m, kClear) + up(n * blocks_of(m), kPrepThreads / kUnit * kPrepTurns);
+  const int64_t rows = tiles_at_most(n, l.w.n_groups, kSide<1>) * up(std::max(k, m), kSide<1>);
+  const int64_t outer = tiles_at_most(n, l.w.n_groups, outer_rows(n, l.w.k, l.w.n_out)) * up(k, kOuterTile) * up(m, kOuterTile);
+  return grid_fits(prep, kPrepThreads) && grid_fits(rows, kThreads) && grid_fits(outer, kThreads);
+}
+
+int64_t grouped8_forward_work(const dpa4c_grouped8& l) {
+  int64_t bytes;
+  plan_forward(l, nullptr, &bytes);
+  return bytes;
+}
+int64_t grouped8_backward_work(const dpa4c_grouped8& l, bool dx, bool dw, bool db) {
+  int64_t bytes;
+  plan_backward(l, dx, dw, db, nullptr, &bytes);
+  return bytes;
+}
+
+int launch_grouped8_forward(const dpa4c_grouped8& l, const void* bias, bool silu, const void* residual,
+                            int64_t ldr, void* y, void* z, void* work, hipStream_t st) {
+  if (l.x.n == 0) return 0;
+  return with_types(l.dtype, l.x.format, [&](auto t, auto f) {
+    using T = decltype(t);
+    constexpr int F = decltype(f)::value;
+    int64_t bytes;
+    const Plan p = plan_forward(l, work, &bytes);
+    PrepArgs pre{};
+    pre.ptr = l.group_ptr;
+    pre.n_groups = l.w.n_groups;
+    pre.n = l.x.n;
+    pre.tiles = p.tiles;
+    pre.list_blocks = list_workgroups(p.tiles.room);
+    DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks, st)));
+    RowsArgs a{};
+    a.order = l.order;
+    a.n_groups = l.w.n_groups;
+    a.n = l.x.n;
+    a.tiles = p.tiles.list;
+    a.n_tiles = p.tiles.count;
+    a.kin = l.w.k;
+    a.kout = l.w.n_out;
+    a.in = static_cast<const char*>(l.x.values);
+    a.ldin = l.x.ld;
+    a.in_scales = static_cast<const uint8_t*>(l.x.scales);
+    a.ld_scales = l.x.ld_scales;
+    a.w = static_cast<const char*>(l.w.turned);
+    a.w_scales = static_cast<const uint8_t*>(l.w.scales);
+    a.w_blocks = blocks_of(l.w.k) * blocks_of(l.w.n_out);
+    a.at_in = blocks_of(l.w.n_out);
+    a.at_out = 1;
+    a.bias = bias;
+    a.silu = silu;
+    a.residual = residual;
+    a.ldres = ldr;
+    a.out = y;
+    a.zout = z;
+    return run_rows<T, F>(a, p.tiles, st);
+  });
+}
+
+int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy, int64_t ldy, const void* z,
+                             int64_t ldz, void* dx, void* dw, void* db, void* work, hipStream_t st) {
+  const int64_t n = l.x.n;
+  const int k = l.w.k, m = l.w.n_out, groups = l.w.n_groups;
+  const bool rows = dx && n > 0, outer = dw || db;
+  if (!rows && !outer) return 0;
+  int64_t bytes;
+  const Plan p = plan_backward(l, dx, dw, db, work, &bytes);
+  DPA4C_TRY(with_types(l.dtype, format, [&](auto t, auto f) {
+    using T = decltype(t);
+    constexpr int F = decltype(f)::value;
+    PrepArgs pre{};
+    pre.ptr = l.group_ptr;
+    pre.n_groups = groups;
+    pre.n = n;
+    pre.order = l.order;
+    if (rows) pre.tiles = p.tiles;
+    if (outer) pre.blocks = p.blocks;
+    pre.dw = dw;
+    pre.db = db;
+    pre.k = k;
+    pre.m = m;
+    pre.dy = dy;
+    pre.z = z;
+    pre.ldy = ldy;
+    pre.ldz = ldz;
+    pre.dz = outer ? p.dz : nullptr;
+    pre.dz8 = rows ? p.dz8 : nullptr;
+    pre.dz_scales = p.dz_scales;
+    pre.list_blocks = list_workgroups(std::max(p.tiles.room, p.blocks.room));
+    const int64_t each = dw ? int64_t(k) * m : 1;
+    pre.clear_blocks = outer ? int64_t(groups) * ((each + kClear - 1) / kClear) : 0;
+    const int64_t units = kPrepThreads / kUnit * kPrepTurns, dz_blocks = (n * blocks_of(m) + units - 1) / units;
+    DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks + pre.clear_blocks + dz_blocks, st)));
+    if (!rows) return 0;
+    RowsArgs a{};
+    a.order = l.order;
+    a.n_groups = groups;
+    a.n = n;
+    a.tiles = p.tiles.list;
+    a.n_tiles = p.tiles.count;
+    a.kin = m;
+    a.kout = k;
+    a.in = reinterpret_cast<const char*>(p.dz8);
+    a.ldin = pitch8(m);
+    a.in_scales = p.dz_scales;
+    a.ld_scales = blocks_of(m);
+    a.by_place = 1;
+    a.w = static_cast<const char*>(l.w.values);
+    a.w_scales = static_cast<const uint8_t*>(l.w.scales);
+    a.w_blocks = blocks_of(k) * blocks_of(m);
+    a.at_in = 1;
+    a.at_out = blocks_of(m);
+    a.out = dx;
+    return run_rows<T, F>(a, p.tiles, st);
+  }));
+  if (!outer) return 0;
+  return with_types(l.dtype, l.x.format, [&](auto t, auto f) {
+    using T = decltype(t);
+    constexpr int F = decltype(f)::value;
+    if (n > 0) {
+      OuterArgs a{};
+      a.order = l.order;
+      a.n = n;
+      a.blocks = p.blocks.list;
+      a.n_blocks = p.blocks.count;
+      a.k = k;
+      a.m = m;
+      a.x = static_cast<const char*>(l.x.values);
+      a.ldx = l.x.ld;
+      a.x_scales = static_cast<const uint8_t*>(l.x.scales);
+      a.ld_scales = l.x.ld_scales;
+      a.dz = p.dz;
+      a.dz_scales = p.dz_scales;
+      a.dz_up = format == DPA4C_E4M3 ? kHalfUp<DPA4C_E4M3> : kHalfUp<DPA4C_E5M2>;
+      a.dw = dw;
+      a.db = db;
+      a.parts = p.parts;
+      a.db_parts = p.db_parts;
+      a.slots = p.slots;
+      const int64_t tiles = (dw ? (k + kOuterTile - 1) / kOuterTile : 1) * int64_t((m + kOuterTile - 1) / kOuterTile);
+      layer8_outer_kernel<T, F><<<tiles_at_most(n, groups, p.blocks.rows) * tiles, kThreads, 0, st>>>(a);
+      DPA4C_HIP_TRY(hipGetLastError());
+    }
+    const int64_t each_w = int64_t(k) * m;
+    const int64_t all = (dw ? align_up(each_w, kJoin) : 0) + (db ? m : 0);
+    const dim3 grid((all + kTileThreads * kJoin - 1) / (kTileThreads * kJoin), groups);
+    grouped_join_kernel<T><<<grid, kTileThreads, 0, st>>>(p.blocks.first_of, l.group_ptr, n, p.slots, each_w, m,
+                                                          p.parts, p.db_parts, static_cast<T*>(dw),
+                                                          static_cast<T*>(db));
+    DPA4C_HIP_TRY(hipGetLastError());
+    return 0;
+  });
+}
+
+}  // namespace dpa4c

@@ -1,0 +1,243 @@
+// Rows and weights to 8 bits with a power-of-two scale for each block of 128
+// (of weights 128 x 128), and the values they stand for.
+//
+//   e = the least with max |x| <= 448 2^e,   q = x 2^-e to nearest even
+//
+// A scale that is a power of two costs a block no accuracy: a number of 8 bits holds
+// an entry to 2^-4 of itself wherever in (224, 448] the largest entry lies, and the
+// product with the scale is exact, in a matrix instruction too.  All of these are bound by HBM.
+#include <hip/hip_runtime.h>
+
+#include "block.h"
+
+namespace dpa4c {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTurns = 4;   // of a workgroup, so that a few loads of a lane are in flight
+
+template <class T>
+constexpr int kEach = 16 / int(sizeof(T));   // entries of a lane
+template <class T>
+constexpr int kUnit = kScaleBlock / kEach<T>;   // lanes of a block
+
+template <class T, int F>
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __restrict__ x, int64_t ldx, int64_t n, int k,
+                                                                 uint8_t* __restrict__ values, int64_t ld,
+                                                                 uint8_t* __restrict__ scales, int64_t lds) {
+  constexpr int V = kEach<T>, L = kUnit<T>, kUnits = kThreads / L;
+  const int blocks = static_cast<int>(blocks_of(k)), lane = threadIdx.x % L;
+  const int64_t first = int64_t(blockIdx.x) * kUnits * kTurns;
+  Item at[kTurns];
+  float v[kTurns][V];
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    at[i] = item_at(first, i * kUnits + int(threadIdx.x) / L, blocks);
+    if (at[i].row >= n) continue;
+    load_entries<T, V>(x + at[i].row * ldx, at[i].part * kScaleBlock + lane * V, k, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    if (at[i].row >= n) continue;   // a unit as a whole
+    unsigned q[V / 4];
+    const unsigned scale = quantize_block<F, V>(v[i], L, q);
+    const int c = at[i].part * kScaleBlock + lane * V;
+    if (c < pitch8(k)) __builtin_memcpy(values + at[i].row * ld + c, q, V);
+    if (lane == 0) scales[at[i].row * lds + at[i].part] = static_cast<uint8_t>(scale);
+  }
+}
+
+typedef unsigned u4v __attribute__((ext_vector_type(4)));
+
+// sixteen 8-bit numbers under one scale
+template <int F, class T>
+__device__ inline void write_values(u4v q, float scale, T* out, int c, int width) {
+  float f[16];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) unpack8<F>(q[j], f + 4 * j);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) f[j] *= scale;
+  if (c + 16 <= width) {
+    Entries<T, 16> e;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) e.v[j] = from_f32<T>(f[j]);
+    *reinterpret_cast<Entries<T, 16>*>(out + c) = e;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (c + j < width) out[c + j] = from_f32<T>(f[j]);
+  }
+}
+
+// Row r takes scales from row r / of (weights: the 128 rows of a block share them).
+template <class T, int F>
+__global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint8_t* __restrict__ values, int64_t ld,
+                                                              const uint8_t* __restrict__ scales, int64_t lds,
+                                                              int64_t n, int k, int group_rows,
+                                                              T* __restrict__ out) {
+  const int parts = (k + 15) / 16;
+  const int64_t first = int64_t(blockIdx.x) * kThreads * kTurns;
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const Item at = item_at(first, i * kThreads + int(threadIdx.x), parts);
+    if (at.row >= n) continue;
+    const u4v q = *reinterpret_cast<const u4v*>(values + at.row * ld + at.part * 16);
+    int64_t of = at.row;
+    if (group_rows) {   // weights: rows of a group, and of its blocks
+      const int64_t g = at.row / group_rows;
+      of = g * blocks_of(group_rows) + (at.row - g * group_rows) / kScaleBlock;
+    }
+    write_values<F, T>(q, scale_of(scales[of * lds + at.part / (kScaleBlock / 16)]), out + at.row * int64_t(k),
+                       at.part * 16, k);
+  }
+}
+
+// A block of 128 x 128 of one group's weights by a workgroup, as it is and turned.
+template <class T>
+__global__ void __launch_bounds__(kThreads) quantize_weights_kernel(const T* __restrict__ w, int k, int m,
+                                                                    uint8_t* __restrict__ values,
+                                                                    uint8_t* __restrict__ turned,
+                                                                    uint8_t* __restrict__ scales) {
+  constexpr int V = 4, L = kScaleBlock / V, kRows = kThreads / L, kPasses = kScaleBlock / kRows;
+  constexpr int kPitch = kScaleBlock + 4;   // of a row in LDS
+  __shared__ __attribute__((aligned(16))) uint8_t tile[kScaleBlock * kPitch];
+  __shared__ float most[kThreads / kWave];
+  __shared__ int odd[kThreads / kWave];
+  const int kb = static_cast<int>(blocks_of(k)), mb = static_cast<int>(blocks_of(m));
+  const int g = blockIdx.x / (kb * mb), of = blockIdx.x % (kb * mb), r0 = of / mb * kScaleBlock,
+            c0 = of % mb * kScaleBlock;
+  const int tid = threadIdx.x, lane = tid & 63, own = tid / L, c = c0 + tid % L * V;
+  w += int64_t(g) * k * m;
+  float v[kPasses][V];
+  float top = 0.0f;
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int r = r0 + i * kRows + own;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[i][j] = 0.0f;
+    if (r < k) load_entries<T, V>(w + int64_t(r) * m, c, m, v[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) top = fmaxf(top, finite_most<V>(v[i], &bad));
+  for (int d = kWave / 2; d > 0; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) most[tid >> 6] = top, odd[tid >> 6] = 0;
+  __syncthreads();
+  if (bad) odd[tid >> 6] = 1;
+  __syncthreads();
+  int any = 0;
+  for (int i = 0; i < kThreads / kWave; ++i) {
+    top = fmaxf(top, most[i]);
+    any |= odd[i];
+  }
+  const int e = scale_exp<DPA4C_E4M3>(top);
+  const float up = power_of_two(-e);
+  if (tid == 0) scales[blockIdx.x] = static_cast<uint8_t>(e + 127);
+  const int64_t pm = pitch8(m), pk = pitch8(k);
+#pragma unroll
+  for (int i = 0; i < kPasses; ++i) {
+    const int rl = i * kRows + own, r = r0 + rl;
+    unsigned q = pack8<DPA4C_E4M3>(v[i][0] * up, v[i][1] * up, v[i][2] * up, v[i][3] * up);
+    if (any) q = kNaN8;
+    if (values && r < k && c < pm) *reinterpret_cast<unsigned*>(values + (int64_t(g) * k + r) * pm + c) = q;
+    *reinterpret_cast<unsigned*>(tile + rl * kPitch + (c - c0)) = q;
+  }
+  if (!turned) return;
+  __syncthreads();
+  // a lane turns 64 entries of a column
+  const int col = tid % kScaleBlock, half = tid / kScaleBlock * 64;
+  if (c0 + col >= m) return;
+  uint8_t* to = turned + (int64_t(g) * m + c0 + col) * pk;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = half + 16 * i;
+    if (r0 + r >= pk) continue;
+    u4v q;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      unsigned x = 0;
+#pragma unroll
+      for (int b = 0; b < 4; ++b) x |= unsigned(tile[(r + 4 * j + b) * kPitch + col]) << (8 * b);
+      q[j] = x;
+    }
+    *reinterpret_cast<u4v*>(to + r0 + r) = q;
+  }
+}
+
+int64_t units(int64_t items, int each) { return (items + each - 1) / each; }
+
+template <class T, int F>
+int quantize_rows(const void* x, int64_t ldx, const dpa4c_rows8& out, hipStream_t st) {
+  const int64_t grid = units(out.n * blocks_of(out.k), kThreads / kUnit<T> * kTurns);
+  quantize_rows_kernel<T, F><<<grid, kThreads, 0, st>>>(
+      static_cast<const T*>(x), ldx, out.n, out.k, static_cast<uint8_t*>(out.values), out.ld,
+      static_cast<uint8_t*>(out.scales), out.ld_scales);
+  DPA4C_HIP_TRY(hipGetLastError());
+  return 0;
+}
+
+template <class T, int F>
+int dequantize(const void* values, int64_t ld, const void* scales, int64_t lds, int64_t n, int k, int group_rows,
+               void* out, hipStream_t st) {
+  const int64_t grid = units(n * ((k + 15) / 16), kThreads * kTurns);
+  dequantize_kernel<T, F><<<grid, kThreads, 0, st>>>(static_cast<const uint8_t*>(values), ld,
+                                                     static_cast<const uint8_t*>(scales), lds, n, k, group_rows,
+                                                     static_cast<T*>(out));
+  DPA4C_HIP_TRY(hipGetLastError());
+  return 0;
+}
+
+}  // namespace
+
+bool rows8_fit(int64_t n, int k) {
+  // the most workgroups: float32 to 8 bits, or back
+  return grid_fits(std::max(units(n * blocks_of(k), kThreads / kUnit<float> * kTurns),
+                            units(n * ((int64_t(k) + 15) / 16), kThreads * kTurns)), kThreads);
+}
+
+int launch_quantize_rows(int dtype, const void* x, int64_t ldx, const dpa4c_rows8& out, hipStream_t st) {
+  if (out.n == 0) return 0;
+  return with_dtype(dtype, [&](auto d) {
+    using T = typename Elem<decltype(d)::value>::T;
+    if (out.format == DPA4C_E4M3) return quantize_rows<T, DPA4C_E4M3>(x, ldx, out, st);
+    return quantize_rows<T, DPA4C_E5M2>(x, ldx, out, st);
+  });
+}
+
+int launch_dequantize_rows(const dpa4c_rows8& in, int dtype, void* out, hipStream_t st) {
+  if (in.n == 0) return 0;
+  return with_dtype(dtype, [&](auto d) {
+    using T = typename Elem<decltype(d)::value>::T;
+    if (in.format == DPA4C_E4M3)
+      return dequantize<T, DPA4C_E4M3>(in.values, in.ld, in.scales, in.ld_scales, in.n, in.k, 0, out, st);
+    return dequantize<T, DPA4C_E5M2>(in.values, in.ld, in.scales, in.ld_scales, in.n, in.k, 0, out, st);
+  });
+}
+
+bool weights8_fit(int n_groups, int k, int n_out) {
+  const int64_t blocks = n_groups * blocks_of(k) * blocks_of(n_out);
+  return grid_fits(blocks, kThreads) && rows8_fit(int64_t(n_groups) * k, n_out);
+}
+
+int launch_quantize_weights(int dtype, const void* w, const dpa4c_weights8& out, hipStream_t st) {
+  return with_dtype(dtype, [&](auto d) {
+    using T = typename Elem<decltype(d)::value>::T;
+    const int64_t grid = out.n_groups * blocks_of(out.k) * blocks_of(out.n_out);
+    quantize_weights_kernel<T><<<grid, kThreads, 0, st>>>(
+        static_cast<const T*>(w), out.k, out.n_out, static_cast<uint8_t*>(out.values),
+        static_cast<uint8_t*>(out.turned), static_cast<uint8_t*>(out.scales));
+    DPA4C_HIP_TRY(hipGetLastError());
+    return 0;
+  });
+}
+
+int launch_dequantize_weights(const dpa4c_weights8& in, int dtype, void* out, hipStream_t st) {
+  return with_dtype(dtype, [&](auto d) {
+    using T = typename Elem<decltype(d)::value>::T;
+    return dequantize<T, DPA4C_E4M3>(in.values, pitch8(in.n_out), in.scales, blocks_of(in.n_out),
+                                     int64_t(in.n_groups) * in.k, in.n_out, in.k, out, st);
+  });
+}
+
+}  // namespace dpa4c
