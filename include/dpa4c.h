@@ -515,7 +515,7 @@ int dpa4c_muon_step(int dtype, int count, const dpa4c_update* updates, const dpa
  * Rows of 8-bit numbers with a scale for each block of 128 entries of a row.
  *   values  [n] rows of k bytes, ld bytes apart: ld and the address multiples of 16; the
  *           bytes from k up to the next multiple of 16 are there, and hold any values
- *           (rows written here have zeros in them)
+ *           (rows written here have zeros in them, or NaN behind a block of NaN)
  *   scales  [n][ceil(k / 128)] bytes, rows ld_scales apart: 2^(byte - 127), 255 is NaN
  * e4m3 has 3 fraction bits and ends at 448, e5m2 has 2 and ends at 57,344; both have NaN, and
  * no infinity is written.  A block gets the least scale with which its largest finite entry
@@ -626,7 +626,7 @@ int dpa4c_grouped_linear8(const dpa4c_grouped8* layer, const void* bias, int act
 /*
  * The gradients of that layer, x and W being the values that their 8 bits stand for:
  *     dz_r = dy_r act'(z_r),   dx_r = Q(dz_r) W_g^T,   dW_g = sum_r x_r^T dz_r,   db_g = sum_r dz_r,
- * Q to 8 bits of ``format`` in blocks of 128.  For dW and db dz is held to 2^-12 of itself or 2^-39 of
+ * Q to 8 bits of ``format`` in blocks of 128.  For dW and db dz is held to 2^-11 of itself or 2^-39 of
  * the largest finite entry of its block of 128, and x exactly or to 2^-40 of the largest product of up
  * to 8,192 rows.  dx [n][k], dw [n_groups][k][n_out], db [n_groups][n_out], contiguous, each or NULL.
  * The residual's gradient is dy itself.  Groups without rows get zeros.

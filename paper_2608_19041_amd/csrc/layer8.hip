@@ -12,7 +12,7 @@
 //
 // The gradient of the weights sums over rows, whose scales differ, so there a step's x becomes
 // float16 under a scale of its row, which holds it exactly, and dz is a single float16 under the
-// scale of its block of 128 (2^-12 of itself; x is off by 2^-4).
+// scale of its block of 128 (2^-11 of itself; x is off by 2^-4).
 #include <hip/hip_runtime.h>
 
 #include "block.h"

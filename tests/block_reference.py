@@ -37,11 +37,13 @@ def row_scales(x, form):
 
 
 def quantize(x, form):
-    """Values (64 bits) and scales of finite rows."""
+    """Values (64 bits) and scales; a block with an infinity or NaN is NaN, with the scale of the rest."""
     x = x.to(F64)
-    s = row_scales(x, form)
-    step = step_of(x, spread(s, x.shape[-1]), form)
-    return torch.round(x / step) * step, s
+    k, bad = x.shape[-1], ~torch.isfinite(x)
+    s = row_scales(torch.where(bad, 0, x), form)
+    step = step_of(x, spread(s, k), form)
+    blocks = torch.stack([bad[..., at:at + 128].any(-1) for at in range(0, k, 128)], -1)
+    return torch.where(spread(blocks, k), float("nan"), torch.round(x / step) * step), s
 
 
 def quantize_weights(w):

@@ -6,7 +6,7 @@ The norm and its gradients are formed in float64 and rounded through float32: RO
 result.  Sums of 8-bit products: a matrix instruction aligns the products of a few
 neighbouring entries to 2^-14 of the largest; eight products lose at most 8 2^-14 of it each time, so a sum is off
 by 2^-11 sum |x||w| at the most, and k u sum |x||w| in float32; products of small whole numbers lose
-nothing, so those results are exact but for their own rounding.  dW: dz to 2^-12 of itself, x exactly, sums in
+nothing, so those results are exact but for their own rounding.  dW: dz to 2^-11 (a float16) of itself, x exactly, sums in
 float32.  act' has slope below 1.1 and is known to 16 u absolute (its terms cancel at z = -1.28).
 """
 import numpy as np
@@ -47,7 +47,12 @@ def types(n, groups, kind, seed=0):
 
 
 def grouped(ids, groups):
-    return dp.group_rows(ids.cuda(), groups)
+    if groups <= 512:
+        return dp.group_rows(ids.cuda(), groups)
+    key = torch.where((ids < 0) | (ids >= groups), groups, ids).long()
+    ptr = torch.zeros(groups + 1, dtype=torch.int64)
+    ptr[1:] = torch.bincount(key, minlength=groups + 1)[:groups].cumsum(0)
+    return ptr.cuda(), torch.argsort(key, stable=True).to(torch.int32).cuda()
 
 
 def normal(n, k, dtype, seed, spread=1.0):
@@ -78,12 +83,14 @@ def test_quantize_rows(n, k, form, dtype):
     assert q.values.dtype == ref.F8[form] and q.values.shape == (n, k) and q.scales.shape == scales.shape
     assert torch.equal(q.scales.cpu().to(torch.float32).to(F64), scales)
     assert torch.equal(as_bits(q.values), as_bits((want / ref.spread(scales, k)).float().to(ref.F8[form])))
-    assert torch.equal(dp.dequantize(q).cpu().to(F64), want)
-    half = dp.dequantize(q, torch.bfloat16)
-    assert torch.equal(half.cpu(), want.float().to(torch.bfloat16))
-    # the bytes that pad a row are zeros
+    for dt in (torch.float32, torch.bfloat16):
+        back = dp.dequantize(q, dt).cpu()
+        assert torch.equal(torch.isnan(back), torch.isnan(want))   # float16 ends at 65,504
+        assert torch.equal(back.nan_to_num(), want.nan_to_num().float().to(dt))
+    # the bytes that pad a row are zeros, or NaN behind a block of NaN
     pad = q.values.untyped_storage().nbytes() // n
-    assert not torch.as_strided(q.values.view(torch.uint8), (n, pad - k), (pad, 1), k).any()
+    behind = torch.as_strided(q.values.view(torch.uint8), (n, pad - k), (pad, 1), k).cpu()
+    assert torch.equal(behind, torch.where(torch.isnan(want[:, -1:]), 0x7f, 0).to(torch.uint8).expand(n, pad - k))
 
 
 @pytest.mark.parametrize("form", ["e4m3", "e5m2"])
@@ -118,7 +125,7 @@ def test_quantize_rows_at_the_ends():
     want, scales = ref.quantize(x, "e4m3")
     q = dp.quantize_rows(x.cuda())
     assert torch.equal(q.scales.cpu().float().to(F64), scales)
-    assert torch.equal(dp.dequantize(q).cpu().to(F64), want)
+    assert torch.equal(dp.dequantize(q).cpu(), want.float())   # 2^128 is beyond float32
     assert scales[2, 0] == 1 and scales[3, 0] == 2 and scales[1, 0] == 2.0 ** -127
 
 
@@ -427,11 +434,11 @@ def test_gradients(n, k, m, groups, kind, silu, dtype, form):
     wt = w.transpose(1, 2)
     want, mag = ref.product(dz8, wt, ids), ref.product(dz8.abs(), wt.abs(), ids)
     check(dx, want, (2.0 ** -11 + m * U) * mag + ref.product(flip, wt.abs(), ids) * 1.01, dtype)
-    want, mag = ref.outer(x, dz, ids, groups), ref.outer(x.abs(), dz.abs() * (2.0 ** -12 + n * U) + unsure, ids, groups)
+    want, mag = ref.outer(x, dz, ids, groups), ref.outer(x.abs(), dz.abs() * (2.0 ** -11 + n * U) + unsure, ids, groups)
     floor = ref.outer(x.abs(), 2.0 ** -38 * top / 448, ids, groups)
     check(dw, want, mag * 1.01 + floor, dtype)
     want = ref.group_sum(dz, ids, groups)
-    check(db, want, ref.group_sum(dz.abs() * (2.0 ** -12 + n * U) + unsure + 2.0 ** -38 * top, ids, groups) * 1.01, dtype)
+    check(db, want, ref.group_sum(dz.abs() * (2.0 ** -11 + n * U) + unsure + 2.0 ** -38 * top, ids, groups) * 1.01, dtype)
 
 
 @pytest.mark.parametrize("form", ["e4m3", "e5m2"])
@@ -450,7 +457,7 @@ def test_weight_gradients_of_rows_far_apart_in_size(form):
         x, dz = dp.dequantize(x8).cpu().to(F64), dy.to(F64)
         want, mag = ref.outer(x, dz, ids, groups), ref.outer(x.abs(), dz.abs(), ids, groups)
         largest = torch.stack([(x.abs().amax(1) * dz.abs().amax(1))[ids == t].max() for t in range(groups)])
-        check(dw, want, (2.0 ** -12 + n * U) * mag * 1.01 + n * 2.0 ** -38 * largest[:, None, None], "bf16")
+        check(dw, want, (2.0 ** -11 + n * U) * mag * 1.01 + n * 2.0 ** -38 * largest[:, None, None], "bf16")
 
 
 @pytest.mark.parametrize("bad", [float("inf"), float("nan")])
