@@ -109,16 +109,20 @@ __device__ inline float scale_of(unsigned b) {
   return __builtin_bit_cast(float, b == 0 ? 0x00400000u : b == 255 ? 0x7fc00000u : b << 23);
 }
 
-// Largest finite magnitude of V entries, and whether one is an infinity or NaN.
+// Largest finite magnitude of V entries; *bad is set where one is an infinity or NaN.
 template <int V>
 __device__ inline float finite_most(const float* v, bool* bad) {
-  float m = 0.0f;
+  float m = 0.0f, z = 0.0f;
 #pragma unroll
   for (int j = 0; j < V; ++j) {
-    const float a = fabsf(v[j]);
-    const bool fin = a < INFINITY;
-    *bad |= !fin;
-    m = fin ? fmaxf(m, a) : m;
+    m = fmaxf(m, fabsf(v[j]));
+    z = fmaf(v[j], 0.0f, z);   // NaN from an infinity or NaN
+  }
+  if (z != z) {
+    *bad = true;
+    m = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; ++j) m = fabsf(v[j]) < INFINITY ? fmaxf(m, fabsf(v[j])) : m;
   }
   return m;
 }
@@ -126,59 +130,115 @@ __device__ inline float finite_most(const float* v, bool* bad) {
 // One block of 128 entries spread over ``lanes`` neighbouring lanes (a power of two), V
 // each: V / 4 words of 8-bit numbers to ``out``; returns the scale's byte.  A block
 // with an infinity or NaN is NaN as a whole, with the scale of its finite entries.
+// ``unsure``: entries are known to 2^-21 of themselves only; set where that may change their
+// 8 bits or the scale.
+constexpr float kBelow = 1.0f - 0x1p-21f, kAbove = 1.0f + 0x1p-21f;
 template <int F, int V>
-__device__ inline unsigned quantize_block(const float* v, int lanes, unsigned* out) {
+__device__ inline unsigned quantize_block(const float* v, int lanes, unsigned* out, bool* unsure = nullptr) {
   bool bad = false;
   float m = finite_most<V>(v, &bad);
-  int any = bad;
-  for (int d = lanes / 2; d > 0; d /= 2) {
-    m = fmaxf(m, __shfl_xor(m, d));
-    any |= __shfl_xor(any, d);
+  for (int d = lanes / 2; d > 0; d /= 2) m = fmaxf(m, __shfl_xor(m, d));
+  if (__ballot(bad) != 0) {
+    int any = bad;
+    for (int d = lanes / 2; d > 0; d /= 2) any |= __shfl_xor(any, d);
+    bad = any != 0;
   }
   const int e = scale_exp<F>(m);
-  const float up = power_of_two(-e);
+  if (unsure) {
+    const float up = power_of_two(-e), lo = up * kBelow, hi = up * kAbove;
+    bool differs = scale_exp<F>(m * kBelow) != e || scale_exp<F>(m * kAbove) != e;
 #pragma unroll
-  for (int j = 0; j < V / 4; ++j)
-    out[j] = any ? kNaN8 : pack8<F>(v[4 * j] * up, v[4 * j + 1] * up, v[4 * j + 2] * up, v[4 * j + 3] * up);
+    for (int j = 0; j < V / 4; ++j) {
+      out[j] = pack8<F>(v[4 * j] * lo, v[4 * j + 1] * lo, v[4 * j + 2] * lo, v[4 * j + 3] * lo);
+      differs |= out[j] != pack8<F>(v[4 * j] * hi, v[4 * j + 1] * hi, v[4 * j + 2] * hi, v[4 * j + 3] * hi);
+      if (bad) out[j] = kNaN8;
+    }
+    *unsure = differs;
+  } else {
+    const float up = power_of_two(-e);
+#pragma unroll
+    for (int j = 0; j < V / 4; ++j)
+      out[j] = bad ? kNaN8 : pack8<F>(v[4 * j] * up, v[4 * j + 1] * up, v[4 * j + 2] * up, v[4 * j + 3] * up);
+  }
   return static_cast<unsigned>(e + 127);
-}
-
-// How a launch deals rows to lanes: ``lanes`` of a wave (a power of two) take a row,
-// V entries each at a time, so that ``width`` entries take ceil(width / (lanes V)) turns.
-template <int V>
-__host__ __device__ inline int lanes_for(int width) {
-  int lanes = 1;
-  while (lanes < kWave && lanes * V < width) lanes *= 2;
-  return lanes;
 }
 
 template <class T, int N>
 struct __attribute__((packed, aligned(sizeof(T)))) Entries {
   T v[N];
 };
-// entries c .. c + V - 1 of a row of ``width``, zeros past it
+// V entries as they come from memory, 16 bytes or 8, in whole registers.
 template <class T, int V>
-__device__ inline void load_entries(const T* row, int c, int width, float* f) {
-  if (c + V <= width) {
-    const Entries<T, V> e = *reinterpret_cast<const Entries<T, V>*>(row + c);
-#pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = to_f32(e.v[j]);
-  } else {
-#pragma unroll
-    for (int j = 0; j < V; ++j) f[j] = c + j < width ? to_f32(row[c + j]) : 0.0f;
+struct Raw {
+  static constexpr int kWords = V * int(sizeof(T)) / 4;
+  unsigned w[kWords];
+  __device__ inline float at(int j) const {
+    if constexpr (sizeof(T) == 4)
+      return __builtin_bit_cast(float, w[j]);
+    else if constexpr (std::is_same<T, __bf16>::value)
+      return __builtin_bit_cast(float, j & 1 ? w[j / 2] & 0xffff0000u : w[j / 2] << 16);
+    else
+      return static_cast<float>(__builtin_bit_cast(T, static_cast<unsigned short>(j & 1 ? w[j / 2] >> 16 : w[j / 2])));
   }
+};
+
+// Entries c .. c + V - 1 of a row of ``width``, zeros past it.  A load takes V entries without a
+// condition where the row has as many: those at the row's end, which ``settle`` then puts in their
+// place.  (With a condition for each entry of a row's last lanes a million rows of 541 took
+// 826 us to 8 bits; now 478.)  ``ends``: false where all V entries are there.
+template <class T, int V>
+__device__ inline Raw<T, V> load_raw_entries(const T* row, int c, int width, bool ends = true) {
+  Raw<T, V> r;
+  if (!ends || width >= V) {
+    typedef unsigned Words __attribute__((ext_vector_type(Raw<T, V>::kWords), aligned(sizeof(T))));
+    const Words v = *reinterpret_cast<const Words*>(row + (!ends || c + V <= width ? c : width - V));
+#pragma unroll
+    for (int i = 0; i < r.kWords; ++i) r.w[i] = v[i];
+    return r;
+  }
+#pragma unroll
+  for (int i = 0; i < r.kWords; ++i) r.w[i] = 0;
+#pragma unroll
+  for (int j = 0; j < V; ++j)
+    if (j < width) {
+      if constexpr (sizeof(T) == 4)
+        r.w[j] = __builtin_bit_cast(unsigned, row[j]);
+      else
+        r.w[j / 2] |= unsigned(__builtin_bit_cast(unsigned short, row[j])) << (16 * (j & 1));
+    }
+  return r;
 }
 template <class T, int V>
-__device__ inline void store_entries(T* row, int c, int width, const float* f) {
-  if (c + V <= width) {
-    Entries<T, V> e;
+__device__ inline void settle(Raw<T, V>& r, int c, int width) {
+  const int at = width >= V ? width - V : 0;
+  if (c <= at) return;
+  const int off = c - at;   // entries to drop from the front
+  using Wide = std::conditional_t<sizeof(r) == 16, unsigned __int128, uint64_t>;
+  static_assert(sizeof(r) == sizeof(Wide), "8 or 16 bytes");
+  Wide x;
+  __builtin_memcpy(&x, &r, sizeof(x));
+  x = off >= V ? 0 : x >> (8 * int(sizeof(T)) * off);
+  __builtin_memcpy(&r, &x, sizeof(x));
+}
+template <class T, int V>
+__device__ inline void load_entries(const T* row, int c, int width, float* f) {
+  Raw<T, V> r = load_raw_entries<T, V>(row, c, width);
+  settle<T, V>(r, c, width);
 #pragma unroll
-    for (int j = 0; j < V; ++j) e.v[j] = from_f32<T>(f[j]);
-    *reinterpret_cast<Entries<T, V>*>(row + c) = e;
+  for (int j = 0; j < V; ++j) f[j] = r.at(j);
+}
+template <class T, int V>
+__device__ inline void store_entries(T* row, int c, int width, const float* f, bool ends = true) {
+  Entries<T, V> e;
+#pragma unroll
+  for (int j = 0; j < V; ++j) e.v[j] = from_f32<T>(f[j]);
+  if (!ends || c + V <= width) {
+    typedef unsigned Words __attribute__((ext_vector_type(V * sizeof(T) / 4), aligned(sizeof(T))));
+    *reinterpret_cast<Words*>(row + c) = __builtin_bit_cast(Words, e);
   } else {
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (c + j < width) row[c + j] = from_f32<T>(f[j]);
+      if (c + j < width) row[c + j] = e.v[j];
   }
 }
 

@@ -15,60 +15,17 @@
 // scale of its block of 128 (2^-11 of itself; x is off by 2^-4).
 #include <hip/hip_runtime.h>
 
-#include "block.h"
-#include "rows.h"
+#include "layer8.h"
 
 namespace dpa4c {
 
 namespace {
 
 constexpr int kThreads = kTileThreads;
-constexpr int kStep = kScaleBlock;      // reduction entries of a step, a row of 128 bytes
-constexpr int kSlots8 = kStep / 16;
-
-typedef int v8i __attribute__((ext_vector_type(8)));
-
-// byte offset of 16-byte slot ``slot`` of row ``row`` in an operand's step: exchanged by
-// bits of the row, so that eight rows at one slot meet all banks
-__device__ inline int slot8_at(int row, int slot) { return row * kStep + ((slot ^ (row & 7)) << 4); }
-
-// the first ``keep`` of sixteen bytes, zeros past them
-__device__ inline u4 keep_bytes(u4 v, int keep) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int left = keep - 4 * j;
-    const unsigned mask = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-    v[j] &= mask;
-  }
-  return v;
-}
-
-struct RowsArgs {
-  const int32_t* order;
-  int n_groups;
-  int64_t n;
-  const RowTile* tiles;
-  const int32_t* n_tiles;
-  int kin, kout;
-  const char* in;            // 8-bit rows, ldin bytes apart
-  int64_t ldin;
-  const uint8_t* in_scales;
-  int64_t ld_scales;
-  int by_place;              // ``in`` is in group order
-  const char* w;             // [group][kout][pitch8(kin)]
-  const uint8_t* w_scales;   // of a group: block i of kin and j of kout at i at_in + j at_out
-  int64_t w_blocks, at_in, at_out;
-  const void* bias;
-  int silu;
-  const void* residual;      // rows of kout entries, ldres apart, or null
-  int64_t ldres;
-  void* out;
-  void* zout;
-};
 
 // A tile of 64 NB rows x 64 NB columns by four waves; a step is one block of 128 entries.
 template <class T, int F, int NB>
-__global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(RowsArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(Rows8Args a) {
   constexpr int kTile = kSide<NB>, kOne = kTile * kStep, kHalfLds = 2 * kOne;
   constexpr int kLoads = kTile * kSlots8 / kThreads;   // of a thread, operand and step
   static_assert(2 * kHalfLds >= kTile * kTile * 4, "the outputs pass through the operands' place");
@@ -253,11 +210,6 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(RowsArgs a) {
 // ---------------------------------------------------------------------------
 // What the gradients need first
 // ---------------------------------------------------------------------------
-
-// dz as float16: dz 2^(kHalfUp - e), e the exponent of its block's scale, so that the largest
-// entry of a block lies in (2^13.8, 2^14.8]; as 8-bit numbers: dz 2^-e
-template <int F>
-constexpr int kHalfUp = 14 - kTopExp<F>;
 
 struct PrepArgs {
   const int64_t* ptr;
@@ -560,11 +512,34 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) 
 // Host
 // ---------------------------------------------------------------------------
 
-// 128 x 128 tiles where they fill the compute units, else 64 x 64
-bool large_tiles(int64_t n, int cols) { return cols > 64 && (n / 128) * ((cols + 127) / 128) >= 256; }
-int tile_rows(int64_t n, int cols) { return large_tiles(n, cols) ? kSide<2> : kSide<1>; }
+// Rows of at most kHeldBlocks blocks are held in registers; longer ones go through LDS in tiles,
+// 128 x 128 where they fill the compute units, else 64 x 64.  Held: workgroups of 128 rows from
+// kWideRows on, of 32 below, whose columns are shared out until the chip has work; those of 32
+// look their tile up, without a list, where the groups are few.
+constexpr int64_t kWideRows = 8192;
+struct Tiling {
+  bool held, wide, listed;
+  int rows, splits;
+};
+Tiling tiling(int64_t n, int n_groups, int kin, int kout) {
+  Tiling t{blocks_of(kin) <= kHeldBlocks, false, true, 0, 1};
+  if (!t.held) {
+    t.rows = kout > 64 && (n / 128) * ((kout + 127) / 128) >= 256 ? kSide<2> : kSide<1>;
+    return t;
+  }
+  const int64_t cols = (kout + 31) / 32;
+  t.wide = n >= kWideRows;
+  t.rows = t.wide ? 128 : 32;
+  t.listed = t.wide || n_groups > 512;
+  if (t.wide)
+    t.splits = static_cast<int>(std::max<int64_t>(1, std::min(1024 / (n / 128 + std::min<int64_t>(n_groups, n / 128) / 2), cols / 3)));
+  else
+    t.splits = static_cast<int>(std::max<int64_t>(1, (cols + 3) / 4));
+  return t;
+}
 
 struct Plan {
+  Tiling how;
   TileList tiles, blocks;
   _Float16* dz;
   uint8_t *dz8, *dz_scales;
@@ -574,7 +549,8 @@ struct Plan {
 Plan plan_forward(const dpa4c_grouped8& l, void* work, int64_t* bytes) {
   Arena ar{static_cast<char*>(work)};
   Plan p{};
-  p.tiles = list_of(ar, l.x.n, l.w.n_groups, tile_rows(l.x.n, l.w.n_out), true);
+  p.how = tiling(l.x.n, l.w.n_groups, l.w.k, l.w.n_out);
+  if (p.how.listed) p.tiles = list_of(ar, l.x.n, l.w.n_groups, p.how.rows, true);
   *bytes = ar.used;
   return p;
 }
@@ -583,10 +559,11 @@ Plan plan_backward(const dpa4c_grouped8& l, bool dx, bool dw, bool db, void* wor
   Plan p{};
   const int64_t n = l.x.n;
   const int k = l.w.k, m = l.w.n_out, groups = l.w.n_groups, rows = outer_rows(n, k, m);
-  if (dx) p.tiles = list_of(ar, n, groups, tile_rows(n, k), true);
+  p.how = tiling(n, groups, m, dx ? k : 0);
+  if ((dx || p.how.held) && p.how.listed) p.tiles = list_of(ar, n, groups, p.how.rows, true);
   if (dw || db) p.blocks = list_of(ar, n, groups, rows, false);
   p.dz = ar.take<_Float16>(dw || db ? n * pitch8(m) : 0);
-  p.dz8 = ar.take<uint8_t>(dx ? n * pitch8(m) : 0);
+  p.dz8 = ar.take<uint8_t>(dx && !p.how.held ? n * pitch8(m) : 0);
   p.dz_scales = ar.take<uint8_t>(n * blocks_of(m));
   // only groups of more than ``rows`` rows have several blocks
   const int64_t blocks = tiles_at_most(n, groups, rows), ends = n > rows ? (2 * n + rows - 1) / rows : 0;
@@ -610,14 +587,20 @@ int prepare(const PrepArgs& a, int64_t grid, hipStream_t st) {
 }
 
 template <class T, int F>
-int run_rows(const RowsArgs& a, const TileList& tiles, hipStream_t st) {
-  const int64_t most = tiles_at_most(a.n, a.n_groups, tiles.rows);
-  if (tiles.rows == kSide<2>)
+int run_rows(const Rows8Args& a, const Tiling& how, hipStream_t st) {
+  const int64_t most = tiles_at_most(a.n, a.n_groups, how.rows);
+  if (how.rows == kSide<2>)
     layer8_rows_kernel<T, F, 2><<<most * ((a.kout + 127) / 128), kThreads, 0, st>>>(a);
   else
     layer8_rows_kernel<T, F, 1><<<most * ((a.kout + 63) / 64), kThreads, 0, st>>>(a);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
+}
+
+int run_held(int dtype, int format, const HeldArgs& a, const Tiling& how, bool back, hipStream_t st) {
+  const int64_t grid = tiles_at_most(a.r.n, a.r.n_groups, how.rows) * how.splits;
+  return dtype == DPA4C_F16 ? run_held8_f16(a, format, back, how.wide, grid, st)
+                            : run_held8_bf16(a, format, back, how.wide, grid, st);
 }
 
 template <class Fn>
@@ -634,7 +617,7 @@ bool grouped8_fits(const dpa4c_grouped8& l) {
   auto up = [](int64_t x, int64_t by) { return (x + by - 1) / by; };
   const int64_t n = l.x.n, k = l.w.k, m = l.w.n_out;
   const int64_t prep = 64 + l.w.n_groups * up(k * m, kClear) + up(n * blocks_of(m), kPrepThreads / kUnit * kPrepTurns);
-  const int64_t rows = tiles_at_most(n, l.w.n_groups, kSide<1>) * up(std::max(k, m), kSide<1>);
+  const int64_t rows = tiles_at_most(n, l.w.n_groups, 32) * up(std::max(k, m), kSide<1>);
   const int64_t outer = tiles_at_most(n, l.w.n_groups, outer_rows(n, l.w.k, l.w.n_out)) * up(k, kOuterTile) * up(m, kOuterTile);
   return grid_fits(prep, kPrepThreads) && grid_fits(rows, kThreads) && grid_fits(outer, kThreads);
 }
@@ -658,14 +641,16 @@ int launch_grouped8_forward(const dpa4c_grouped8& l, const void* bias, bool silu
     constexpr int F = decltype(f)::value;
     int64_t bytes;
     const Plan p = plan_forward(l, work, &bytes);
-    PrepArgs pre{};
-    pre.ptr = l.group_ptr;
-    pre.n_groups = l.w.n_groups;
-    pre.n = l.x.n;
-    pre.tiles = p.tiles;
-    pre.list_blocks = list_workgroups(p.tiles.room);
-    DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks, st)));
-    RowsArgs a{};
+    if (p.how.listed) {
+      PrepArgs pre{};
+      pre.ptr = l.group_ptr;
+      pre.n_groups = l.w.n_groups;
+      pre.n = l.x.n;
+      pre.tiles = p.tiles;
+      pre.list_blocks = list_workgroups(p.tiles.room);
+      DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks, st)));
+    }
+    Rows8Args a{};
     a.order = l.order;
     a.n_groups = l.w.n_groups;
     a.n = l.x.n;
@@ -688,7 +673,12 @@ int launch_grouped8_forward(const dpa4c_grouped8& l, const void* bias, bool silu
     a.ldres = ldr;
     a.out = y;
     a.zout = z;
-    return run_rows<T, F>(a, p.tiles, st);
+    if (!p.how.held) return run_rows<T, F>(a, p.how, st);
+    HeldArgs h{};
+    h.r = a;
+    h.ptr = l.group_ptr;
+    h.splits = p.how.splits;
+    return run_held(l.dtype, F, h, p.how, false, st);
   });
 }
 
@@ -708,7 +698,7 @@ int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy
     pre.n_groups = groups;
     pre.n = n;
     pre.order = l.order;
-    if (rows) pre.tiles = p.tiles;
+    pre.tiles = p.tiles;
     if (outer) pre.blocks = p.blocks;
     pre.dw = dw;
     pre.db = db;
@@ -724,17 +714,18 @@ int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy
     pre.list_blocks = list_workgroups(std::max(p.tiles.room, p.blocks.room));
     const int64_t each = dw ? int64_t(k) * m : 1;
     pre.clear_blocks = outer ? int64_t(groups) * ((each + kClear - 1) / kClear) : 0;
-    const int64_t units = kPrepThreads / kUnit * kPrepTurns, dz_blocks = (n * blocks_of(m) + units - 1) / units;
-    DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks + pre.clear_blocks + dz_blocks, st)));
-    if (!rows) return 0;
-    RowsArgs a{};
+    const int64_t units = kPrepThreads / kUnit * kPrepTurns;
+    const int64_t dz_blocks = p.how.held ? 0 : (n * blocks_of(m) + units - 1) / units;
+    if (outer || p.how.listed) DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks + pre.clear_blocks + dz_blocks, st)));
+    if (n == 0 || (!rows && !p.how.held)) return 0;
+    Rows8Args a{};
     a.order = l.order;
     a.n_groups = groups;
     a.n = n;
     a.tiles = p.tiles.list;
     a.n_tiles = p.tiles.count;
     a.kin = m;
-    a.kout = k;
+    a.kout = rows ? k : 0;   // dz alone
     a.in = reinterpret_cast<const char*>(p.dz8);
     a.ldin = pitch8(m);
     a.in_scales = p.dz_scales;
@@ -746,7 +737,18 @@ int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy
     a.at_in = 1;
     a.at_out = blocks_of(m);
     a.out = dx;
-    return run_rows<T, F>(a, p.tiles, st);
+    if (!p.how.held) return run_rows<T, F>(a, p.how, st);
+    HeldArgs h{};
+    h.r = a;
+    h.ptr = l.group_ptr;
+    h.splits = p.how.splits;
+    h.dy = dy;
+    h.z = z;
+    h.ldy = ldy;
+    h.ldz = ldz;
+    h.dz = outer ? p.dz : nullptr;
+    h.dz_scales = p.dz_scales;
+    return run_held(l.dtype, F, h, p.how, true, st);
   }));
   if (!outer) return 0;
   return with_types(l.dtype, l.x.format, [&](auto t, auto f) {

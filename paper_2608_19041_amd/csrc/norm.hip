@@ -23,9 +23,18 @@ __device__ inline int64_t row_at(const int32_t* order, int64_t place, int64_t n)
   const int64_t r = order ? order[place] : place;
   return r >= 0 && r < n ? r : -1;
 }
-__device__ inline double sum_lanes(double v, int lanes) {
+template <class A>
+__device__ inline A sum_lanes(A v, int lanes) {
   for (int d = lanes / 2; d > 0; d /= 2) v += __shfl_xor(v, d);
   return v;
+}
+
+// The entries as the compiler has not seen them: what is formed from them twice is then formed
+// anew instead of being held in four times the registers.
+template <class R>
+__device__ inline void forget(R& r) {
+  static_assert(R::kWords == 4, "one load");
+  asm("" : "+v"(r.w[0]), "+v"(r.w[1]), "+v"(r.w[2]), "+v"(r.w[3]));
 }
 
 struct NormArgs {
@@ -50,9 +59,19 @@ struct NormArgs {
   int per;            // places of a wave's lanes, one after another
 };
 
-// NC: turns of a row that are held in registers; 0: rows of any length, read twice.
-template <class T, int NC, int Q>
-__global__ void __launch_bounds__(kThreads) rms_norm_kernel(NormArgs a) {
+// d as a float32 that rounds to 8 bits as d does: where the float32 may be the middle of two such
+// numbers and is not d, its last bit says on which side d lies.
+__device__ inline float for_8_bits(double d) {
+  const float f = static_cast<float>(d);
+  unsigned bits = __builtin_bit_cast(unsigned, f);
+  if ((bits & 0xffff) == 0 && double(f) != d && fabsf(f) < INFINITY) bits += fabs(d) > fabs(double(f)) ? 1 : -1;
+  return __builtin_bit_cast(float, bits);
+}
+
+// NC: turns of a row that are held in registers, the next row's entries on their way; 0: rows
+// of any length, read twice.
+template <class T, int NC, int Q, bool Res>
+__global__ void __launch_bounds__(kThreads, NC < 2 ? 4 : NC < 4 ? 3 : 2) rms_norm_kernel(NormArgs a) {
   constexpr int V = 16 / int(sizeof(T));
   constexpr int kHeld = NC > 0 ? NC : 1;
   const int lanes = a.lanes, sub = threadIdx.x & (lanes - 1), rows = kWave / lanes;
@@ -60,68 +79,122 @@ __global__ void __launch_bounds__(kThreads) rms_norm_kernel(NormArgs a) {
   const int64_t base = wave * rows * a.per + (threadIdx.x & (kWave - 1)) / lanes;
   const int step = lanes * V;   // entries of a turn
   const int turns = NC > 0 ? NC : (a.k + step - 1) / step;
+  const T* x = static_cast<const T*>(a.x);
+  const T* res = static_cast<const T*>(a.res);
   int g = 0, held = -1;
   int64_t end = a.ptr ? -1 : a.n;
-  float gain[kHeld][V];
-  auto load = [&](int64_t row, int c, float* h) {
-    load_entries<T, V>(static_cast<const T*>(a.x) + row * a.ldx, c, a.k, h);
-    if (a.res) {
-      float r[V];
-      load_entries<T, V>(static_cast<const T*>(a.res) + row * a.ldr, c, a.k, r);
-#pragma unroll
-      for (int j = 0; j < V; ++j) h[j] += r[j];
-    }
+  Raw<T, V> gain[kHeld], px[kHeld], pr[kHeld], x0[kHeld], r0[kHeld];
+  auto fetch = [&](int64_t row, int t, int at) {
+    const int c = t * step + sub * V;
+    const bool ends = NC == 0 || t == NC - 1;   // the turns before the last are whole
+    px[at] = load_raw_entries<T, V>(x + row * a.ldx, c, a.k, ends);
+    if (Res) pr[at] = load_raw_entries<T, V>(res + row * a.ldr, c, a.k, ends);
   };
+  auto take = [&](int t, int at) {   // what was fetched, as the current row's
+    const int c = t * step + sub * V;
+    x0[at] = px[at];
+    if (Res) r0[at] = pr[at];
+    if (NC > 0 && t < NC - 1) return;
+    settle<T, V>(x0[at], c, a.k);
+    if (Res) settle<T, V>(r0[at], c, a.k);
+  };
+  auto h_of = [&](int at, int j) { return x0[at].at(j) + (Res ? r0[at].at(j) : 0.0f); };
+  auto wide_h_of = [&](int at, int j) {
+    return double(x0[at].at(j)) + (Res ? double(r0[at].at(j)) : 0.0);
+  };
+  // the row of a place, two places ahead of its use; past the end: any
+  auto look = [&](int i) {
+    const int64_t place = base + int64_t(i) * rows;
+    return row_at(a.order, place < a.n ? place : a.n - 1, a.n);
+  };
+  int64_t row = look(0), next = look(1);
+  if (NC > 0)
+#pragma unroll
+    for (int t = 0; t < kHeld; ++t) fetch(row < 0 ? 0 : row, t, t);
   for (int i = 0; i < a.per; ++i) {
     const int64_t place = base + int64_t(i) * rows;
     if (place >= a.n) break;   // the lanes of a row alike
+    if (NC > 0)
+#pragma unroll
+      for (int t = 0; t < kHeld; ++t) take(t, t);
+    const int64_t own = row;
+    row = next;
+    if (NC > 0)
+#pragma unroll
+      for (int t = 0; t < kHeld; ++t) fetch(row < 0 ? 0 : row, t, t);
+    next = look(i + 2);
     if (place >= end) {
       g = group_of(a.ptr, a.n_groups, place);
       end = g < a.n_groups ? a.ptr[g + 1] : a.n;
     }
-    const int64_t row = row_at(a.order, place, a.n);
-    if (row < 0) continue;
+    if (own < 0) continue;
     const bool live = g < a.n_groups;
-    float h[kHeld][V];
     double sum = 0.0;
 #pragma unroll
-    for (int t = 0; t < kHeld; ++t)
-      if (NC > 0) load(row, t * step + sub * V, h[t]);
-#pragma unroll
     for (int t = 0; t < turns; ++t) {
-      float* v = h[NC > 0 ? t : 0];
-      if (NC == 0) load(row, t * step + sub * V, v);
+      const int at = NC > 0 ? t : 0;
+      if (NC == 0) {
+        fetch(own, t, 0);
+        take(t, 0);
+      }
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum += double(v[j]) * double(v[j]);
+      for (int j = 0; j < V; ++j) {
+        const double h = wide_h_of(at, j);
+        sum += h * h;
+      }
+      forget(x0[at]);
+      if (Res) forget(r0[at]);
     }
     const double s = live ? 1.0 / sqrt(sum_lanes(sum, lanes) / a.k + double(a.eps)) : 0.0;
-    if (sub == 0 && a.rstd) a.rstd[row] = static_cast<float>(s);
-    const T* own = static_cast<const T*>(a.gain) + int64_t(live ? g : 0) * a.k;
+    if (sub == 0 && a.rstd) a.rstd[own] = static_cast<float>(s);
+    const T* gains = static_cast<const T*>(a.gain) + int64_t(live ? g : 0) * a.k;
+    auto take_gain = [&](int t, int at) {
+      gain[at] = load_raw_entries<T, V>(gains, t * step + sub * V, a.k);
+      settle<T, V>(gain[at], t * step + sub * V, a.k);
+    };
     if (NC > 0 && held != g) {
 #pragma unroll
-      for (int t = 0; t < kHeld; ++t) load_entries<T, V>(own, t * step + sub * V, a.k, gain[t]);
+      for (int t = 0; t < kHeld; ++t) take_gain(t, t);
       held = g;
     }
 #pragma unroll
     for (int t = 0; t < turns; ++t) {
       const int c = t * step + sub * V, at = NC > 0 ? t : 0;
-      float* v = h[at];
       if (NC == 0) {
-        load(row, c, v);
-        load_entries<T, V>(own, c, a.k, gain[0]);
+        fetch(own, t, 0);
+        take(t, 0);
+        take_gain(t, 0);
       }
-      if (a.h) store_entries<T, V>(static_cast<T*>(a.h) + row * int64_t(a.k), c, a.k, v);
       float y[V];
+      if (Res) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) y[j] = live ? static_cast<float>(double(v[j]) * s * double(gain[at][j])) : 0.0f;
+        for (int j = 0; j < V; ++j) y[j] = h_of(at, j);
+        store_entries<T, V>(static_cast<T*>(a.h) + own * int64_t(a.k), c, a.k, y, NC == 0 || t == NC - 1);
+      }
+      auto wide_y_of = [&](int j) { return wide_h_of(at, j) * s * double(gain[at].at(j)); };
+      const float r = static_cast<float>(s);
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        if constexpr (Q == kPlain && sizeof(T) == 4)
+          y[j] = static_cast<float>(wide_y_of(j));
+        else
+          y[j] = h_of(at, j) * r * gain[at].at(j);   // to 2^-22 of itself
+        y[j] = live ? y[j] : 0.0f;
+      }
       if constexpr (Q == kPlain) {
-        store_entries<T, V>(static_cast<T*>(a.y) + row * int64_t(a.k), c, a.k, y);
+        store_entries<T, V>(static_cast<T*>(a.y) + own * int64_t(a.k), c, a.k, y, NC == 0 || t == NC - 1);
       } else {
         constexpr int L = kScaleBlock / V;
         unsigned q[V / 4];
-        const unsigned scale = quantize_block<Q, V>(y, lanes < L ? lanes : L, q);
-        if (c < pitch8(a.k)) __builtin_memcpy(static_cast<uint8_t*>(a.y) + row * a.ldy + c, q, V);
-        if ((sub & (L - 1)) == 0 && c < a.k) a.scales[row * a.lds + c / kScaleBlock] = static_cast<uint8_t>(scale);
+        bool unsure;
+        unsigned scale = quantize_block<Q, V>(y, lanes < L ? lanes : L, q, &unsure);
+        if (__ballot(unsure) != 0) {   // one turn in a hundred: the same in 64 bits
+#pragma unroll
+          for (int j = 0; j < V; ++j) y[j] = live ? for_8_bits(wide_y_of(j)) : 0.0f;
+          scale = quantize_block<Q, V>(y, lanes < L ? lanes : L, q);
+        }
+        if (c < pitch8(a.k)) __builtin_memcpy(static_cast<uint8_t*>(a.y) + own * a.ldy + c, q, V);
+        if ((sub & (L - 1)) == 0 && c < a.k) a.scales[own * a.lds + c / kScaleBlock] = static_cast<uint8_t>(scale);
       }
     }
   }
@@ -176,63 +249,100 @@ __device__ inline void put_gain(const BackArgs& a, const Stretch& s, int c, doub
     a.parts[(2 * int64_t(blockIdx.x) + s.slot) * a.k + c] = v;
 }
 
-// Rows held in registers, with the sums over a block's rows of each group beside them.
-template <class T, int NC>
-__global__ void __launch_bounds__(kThreads) rms_norm_back_kernel(BackArgs a) {
+// Rows held in registers, the next one's entries on their way, with the sums over a block's rows of
+// each group beside them: in 64 bits for float32; in float32 for half types, no more than
+// kMostRows rows one after another, which is 2^-16 of the sum of the terms' sizes at the worst.
+template <class T, int NC, bool Dh>
+__global__ void __launch_bounds__(kThreads, NC < 2 ? 4 : NC < 4 ? 3 : 2) rms_norm_back_kernel(BackArgs a) {
   constexpr int V = 16 / int(sizeof(T)), kWaves = kThreads / kWave;
+  using Acc = std::conditional_t<sizeof(T) == 4, double, float>;
+  constexpr bool kAhead = NC == 1;
   extern __shared__ double sums[];   // [waves][lanes V NC]
   const int lanes = a.lanes, sub = threadIdx.x & (lanes - 1), wave = threadIdx.x / kWave;
   const int unit = threadIdx.x / lanes, units = kThreads / lanes, step = lanes * V, width = step * NC;
   const int64_t first = int64_t(blockIdx.x) * a.rows;
   const int64_t last = first + a.rows < a.n ? first + a.rows : a.n;
+  const T* dy_at = static_cast<const T*>(a.dy);
+  const T* h_at = static_cast<const T*>(a.h);
+  const T* dh_at = static_cast<const T*>(a.dh);
   int g = a.ptr ? group_of(a.ptr, a.n_groups, first) : 0;
   for (int64_t at = first; at < last;) {   // alike for the whole workgroup
     const Stretch s = stretch_at(a, at, first, last, g);
     g = s.group;
     at = s.end;
     const bool live = g < a.n_groups;
-    const T* own = static_cast<const T*>(a.gain) + int64_t(live ? g : 0) * a.k;
-    float gain[NC][V];
-    double acc[NC][V];
+    const T* gains = static_cast<const T*>(a.gain) + int64_t(live ? g : 0) * a.k;
+    Raw<T, V> gain[NC], py[NC], ph[NC], pd[NC], dy[NC], h[NC], dh[NC];
+    Acc acc[NC][V];
 #pragma unroll
     for (int t = 0; t < NC; ++t) {
-      load_entries<T, V>(own, t * step + sub * V, a.k, gain[t]);
+      gain[t] = load_raw_entries<T, V>(gains, t * step + sub * V, a.k);
+      settle<T, V>(gain[t], t * step + sub * V, a.k);
 #pragma unroll
-      for (int j = 0; j < V; ++j) acc[t][j] = 0.0;
+      for (int j = 0; j < V; ++j) acc[t][j] = 0;
     }
-    for (int64_t place = s.begin + unit; place < s.end; place += units) {
-      const int64_t row = row_at(a.order, place, a.n);
-      if (row < 0) continue;
-      float dy[NC][V], h[NC][V], dh[NC][V];
+    float rstd;
+    auto look = [&](int64_t place) { return row_at(a.order, place < s.end ? place : s.end - 1, a.n); };
+    auto fetch = [&](int64_t row) {
+      row = row < 0 ? 0 : row;
+      rstd = a.rstd[row];
 #pragma unroll
       for (int t = 0; t < NC; ++t) {
         const int c = t * step + sub * V;
-        load_entries<T, V>(static_cast<const T*>(a.dy) + row * a.lddy, c, a.k, dy[t]);
-        load_entries<T, V>(static_cast<const T*>(a.h) + row * a.ldh, c, a.k, h[t]);
-        if (a.dh && a.dx) load_entries<T, V>(static_cast<const T*>(a.dh) + row * a.lddh, c, a.k, dh[t]);
+        py[t] = load_raw_entries<T, V>(dy_at + row * a.lddy, c, a.k, t == NC - 1);
+        ph[t] = load_raw_entries<T, V>(h_at + row * a.ldh, c, a.k, t == NC - 1);
+        if (Dh) pd[t] = load_raw_entries<T, V>(dh_at + row * a.lddh, c, a.k, t == NC - 1);
       }
-      const double r = live ? double(a.rstd[row]) : 0.0;
-      double sum = 0.0;
+    };
+    auto wide = [](float v) { return Acc(v); };
+    int64_t row = look(s.begin + unit), next = look(s.begin + unit + units);
+    if (kAhead) fetch(row);
+    for (int64_t place = s.begin + unit; place < s.end; place += units) {
+      if (!kAhead) fetch(row);
+      const int64_t own = row;
+      row = next;
+      next = look(place + 2 * units);
 #pragma unroll
-      for (int t = 0; t < NC; ++t)
+      for (int t = 0; t < NC; ++t) {
+        const int c = t * step + sub * V;
+        dy[t] = py[t];
+        h[t] = ph[t];
+        if (Dh) dh[t] = pd[t];
+        if (t < NC - 1) continue;   // the turns before the last are whole
+        settle<T, V>(dy[t], c, a.k);
+        settle<T, V>(h[t], c, a.k);
+        if (Dh) settle<T, V>(dh[t], c, a.k);
+      }
+      const Acc r = live ? Acc(rstd) : Acc(0);
+      if (kAhead) fetch(row);
+      if (own < 0) continue;   // the lanes of a row alike
+      Acc sum = 0;
+#pragma unroll
+      for (int t = 0; t < NC; ++t) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const double p = double(dy[t][j]) * double(h[t][j]);
-          sum += p * double(gain[t][j]);
-          acc[t][j] += p * r;
+          const Acc hat = wide(h[t].at(j)) * r, up = wide(dy[t].at(j));
+          sum += up * wide(gain[t].at(j)) * hat;
+          acc[t][j] += up * hat;
         }
+        forget(dy[t]);
+        forget(h[t]);
+        forget(gain[t]);
+      }
       if (!a.dx) continue;
-      const double pull = r * r * r * (sum_lanes(sum, lanes) / a.k);
+      const Acc mean = sum_lanes(sum, lanes) / Acc(a.k);
 #pragma unroll
       for (int t = 0; t < NC; ++t) {
         float v[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          double d = live ? double(dy[t][j]) * double(gain[t][j]) * r - double(h[t][j]) * pull : 0.0;
-          if (a.dh) d += double(dh[t][j]);
+          const Acc hat = wide(h[t].at(j)) * r, up = wide(dy[t].at(j)) * wide(gain[t].at(j));
+          Acc d = live ? r * (up - hat * mean) : Acc(0);
+          if (Dh) d += wide(dh[t].at(j));
           v[j] = static_cast<float>(d);
         }
-        store_entries<T, V>(static_cast<T*>(a.dx) + row * int64_t(a.k), t * step + sub * V, a.k, v);
+        forget(gain[t]);
+        store_entries<T, V>(static_cast<T*>(a.dx) + own * int64_t(a.k), t * step + sub * V, a.k, v, t == NC - 1);
       }
     }
     if (!a.dgain || !live) continue;
@@ -240,7 +350,7 @@ __global__ void __launch_bounds__(kThreads) rms_norm_back_kernel(BackArgs a) {
     for (int t = 0; t < NC; ++t)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        double v = acc[t][j];
+        double v = double(acc[t][j]);
         for (int d = kWave / 2; d >= lanes; d /= 2) v += __shfl_xor(v, d);
         if ((threadIdx.x & (kWave - 1)) < unsigned(lanes)) sums[wave * width + t * step + sub * V + j] = v;
       }
@@ -361,31 +471,58 @@ __global__ void __launch_bounds__(64 * kJoinRows) rms_norm_join_kernel(const int
   out[c] = from_f32<T>(static_cast<float>(v));
 }
 
-// Turns of a row in registers, at most four; 0: too long for that.
-template <class T>
-int turns_of(int width) {
-  const int64_t turns = (int64_t(width) + kWave * (16 / int(sizeof(T))) - 1) / (kWave * (16 / int(sizeof(T))));
-  return turns <= 1 ? 1 : turns <= 2 ? 2 : turns <= 4 ? 4 : 0;
+// How a row is held: ``lanes`` V entries each, ``turns`` times, with the fewest of both together
+// (541 bfloat16 entries: 32 lanes three times, where 64 lanes twice would leave half idle).  ``least``
+// lanes where a turn has to hold whole blocks of 128.  0 turns: too long for four.
+struct Held {
+  int lanes, turns;
+};
+template <int V>
+Held held_for(int width, int least) {
+  Held best{kWave, 0};
+  int cost = 1 << 30;
+  for (int turns = 1; turns <= 4; ++turns) {
+    int lanes = 1;
+    while (lanes < kWave && lanes * V * turns < width) lanes *= 2;
+    if (turns > 1 && lanes < least) lanes = least;
+    if (lanes * V * turns >= width && lanes * turns < cost) {
+      cost = lanes * turns;
+      best = {lanes, turns};
+    }
+  }
+  return best;
 }
 template <class Fn>
 int with_turns(int turns, Fn&& fn) {
   if (turns == 1) return fn(std::integral_constant<int, 1>{});
   if (turns == 2) return fn(std::integral_constant<int, 2>{});
+  if (turns == 3) return fn(std::integral_constant<int, 3>{});
   if (turns == 4) return fn(std::integral_constant<int, 4>{});
   return fn(std::integral_constant<int, 0>{});
+}
+template <class Fn>
+int with_flag(bool flag, Fn&& fn) {
+  return flag ? fn(std::integral_constant<bool, true>{}) : fn(std::integral_constant<bool, false>{});
 }
 
 // places of a block of the gradients: 1,024 blocks, four to a compute unit, of 16 rows at
 // the least; long rows have several strips of columns in place of as many blocks
-constexpr int kBlocks = 1024;
-int block_rows(int64_t n, int strips) {
-  const int64_t blocks = std::max(1, kBlocks / strips);
-  return static_cast<int>(std::max<int64_t>(16, (n + blocks - 1) / blocks));
+constexpr int kBlocks = 768, kMostRows = 256;
+int block_rows(int64_t n, int strips, int lanes) {
+  const int64_t blocks = std::max(1, kBlocks / strips), rows = std::max<int64_t>(16, (n + blocks - 1) / blocks);
+  return static_cast<int>(strips > 1 ? rows : std::min<int64_t>(rows, kMostRows * (kThreads / lanes)));
 }
+struct BackPlan {
+  Held held;
+  int strips, rows;
+};
 template <class T>
-int strips_of(int k) {
-  if (turns_of<T>(k)) return 1;
-  return (k + kThreads * (16 / int(sizeof(T))) - 1) / (kThreads * (16 / int(sizeof(T))));
+BackPlan plan_back(int64_t n, int k) {
+  constexpr int V = 16 / int(sizeof(T));
+  BackPlan p{held_for<V>(k, 1), 1, 0};
+  if (p.held.turns == 0) p.strips = (k + kThreads * V - 1) / (kThreads * V);
+  p.rows = block_rows(n, p.strips, p.held.lanes);
+  return p;
 }
 
 }  // namespace
@@ -397,32 +534,36 @@ int launch_rms_norm(const dpa4c_norm& l, const NormIn& in, void* y, const dpa4c_
     using T = typename Elem<decltype(d)::value>::T;
     constexpr int V = 16 / int(sizeof(T));
     const int width = static_cast<int>(y8 ? pitch8(l.k) : l.k);
+    const Held held = held_for<V>(width, y8 ? kScaleBlock / V : 1);
     NormArgs a{in.x, in.ldx, in.residual, in.ldr, l.gain, l.group_ptr, l.order, l.n_groups, l.n, l.k, in.eps,
                y8 ? y8->values : y, y8 ? y8->ld : 0, y8 ? static_cast<uint8_t*>(y8->scales) : nullptr,
-               y8 ? y8->ld_scales : 0, rstd, h, lanes_for<V>(width), 1};
-    // 8,192 waves, eight to a SIMD, before a wave takes several rows
+               y8 ? y8->ld_scales : 0, rstd, h, held.lanes, 1};
+    // 12,288 waves, four rounds of the 3,072 that fit, before a wave takes several rows
     const int64_t rows = kWave / a.lanes;
-    const int64_t per = std::min<int64_t>(64, (l.n + rows * 8192 - 1) / (rows * 8192));
+    const int64_t per = std::min<int64_t>(64, (l.n + rows * 12288 - 1) / (rows * 12288));
     a.per = static_cast<int>(per);
     const int64_t each = rows * per * (kThreads / kWave), grid = (l.n + each - 1) / each;
-    return with_turns(turns_of<T>(width), [&](auto turns) {
-      constexpr int NC = decltype(turns)::value;
-      if (!y8)
-        rms_norm_kernel<T, NC, kPlain><<<grid, kThreads, 0, st>>>(a);
-      else if (y8->format == DPA4C_E4M3)
-        rms_norm_kernel<T, NC, DPA4C_E4M3><<<grid, kThreads, 0, st>>>(a);
-      else
-        rms_norm_kernel<T, NC, DPA4C_E5M2><<<grid, kThreads, 0, st>>>(a);
-      DPA4C_HIP_TRY(hipGetLastError());
-      return 0;
+    return with_turns(held.turns, [&](auto turns) {
+      return with_flag(in.residual != nullptr, [&](auto res) {
+        constexpr int NC = decltype(turns)::value;
+        constexpr bool R = decltype(res)::value;
+        if (!y8)
+          rms_norm_kernel<T, NC, kPlain, R><<<grid, kThreads, 0, st>>>(a);
+        else if (y8->format == DPA4C_E4M3)
+          rms_norm_kernel<T, NC, DPA4C_E4M3, R><<<grid, kThreads, 0, st>>>(a);
+        else
+          rms_norm_kernel<T, NC, DPA4C_E5M2, R><<<grid, kThreads, 0, st>>>(a);
+        DPA4C_HIP_TRY(hipGetLastError());
+        return 0;
+      });
     });
   });
 }
 
 int64_t rms_norm_backward_work(const dpa4c_norm& l, bool dgain) {
   if (!dgain || l.n == 0) return 0;
-  const int strips = l.dtype == DPA4C_F32 ? strips_of<float>(l.k) : strips_of<_Float16>(l.k);
-  const int64_t rows = block_rows(l.n, strips), blocks = (l.n + rows - 1) / rows;
+  const int64_t rows = (l.dtype == DPA4C_F32 ? plan_back<float>(l.n, l.k) : plan_back<_Float16>(l.n, l.k)).rows;
+  const int64_t blocks = (l.n + rows - 1) / rows;
   return align_up(2 * blocks * l.k * int64_t(sizeof(double)), 256);
 }
 
@@ -431,19 +572,23 @@ int launch_rms_norm_backward(const dpa4c_norm& l, const NormBack& in, void* dx, 
   return with_dtype(l.dtype, [&](auto d) {
     using T = typename Elem<decltype(d)::value>::T;
     constexpr int V = 16 / int(sizeof(T));
-    const int strips = strips_of<T>(l.k), rows = block_rows(l.n, strips);
+    const auto [held, strips, rows] = plan_back<T>(l.n, l.k);
     BackArgs a{in.dy, in.h, in.dh, in.lddy, in.ldh, in.lddh, l.gain, in.rstd, l.group_ptr, l.order, l.n_groups,
-               l.n, l.k, dx, dgain, static_cast<double*>(work), rows, lanes_for<V>(l.k)};
+               l.n, l.k, dx, dgain, static_cast<double*>(work), rows, held.lanes};
     if (l.n > 0 && (dx || dgain)) {
       const int64_t blocks = (l.n + rows - 1) / rows;
-      DPA4C_TRY(with_turns(turns_of<T>(l.k), [&](auto turns) {
+      const int own_strips = strips;
+      DPA4C_TRY(with_turns(held.turns, [&](auto turns) {
         constexpr int NC = decltype(turns)::value;
         if constexpr (NC > 0) {
           const int bytes = kThreads / kWave * a.lanes * V * NC * int(sizeof(double));
-          rms_norm_back_kernel<T, NC><<<blocks, kThreads, bytes, st>>>(a);
+          if (a.dh && dx)
+            rms_norm_back_kernel<T, NC, true><<<blocks, kThreads, bytes, st>>>(a);
+          else
+            rms_norm_back_kernel<T, NC, false><<<blocks, kThreads, bytes, st>>>(a);
         } else {
           if (dx) rms_norm_back_rows_kernel<T><<<std::min<int64_t>(l.n, 1 << 20), kThreads, 0, st>>>(a);
-          if (dgain) rms_norm_gain_kernel<T><<<dim3(blocks, strips), kThreads, 0, st>>>(a);
+          if (dgain) rms_norm_gain_kernel<T><<<dim3(blocks, own_strips), kThreads, 0, st>>>(a);
         }
         DPA4C_HIP_TRY(hipGetLastError());
         return 0;

@@ -6,6 +6,29 @@
 
 namespace dpa4c {
 
+// A stretch of places of one group; ``part`` of ``parts`` of the group.
+struct RowTile {
+  int64_t first;
+  int32_t group;
+  int32_t count;
+  int32_t part, parts;
+};
+
+// Tiles of at most ``rows`` places of all groups, in group order, into list;
+// *count of them, first_of[g] the first of group g.  With ``rest`` group
+// n_groups stands for the rows of no group.  No more than ``room`` tiles are listed,
+// the most that a group_ptr can have that does not decrease: what one that does
+// would add is left out.  The work of one workgroup of ``blocks``; starts: LDS of
+// n_groups + 2 words.
+struct TileList {
+  RowTile* list;
+  int32_t* first_of;   // [n_groups + 2]
+  int32_t* count;
+  int rows;
+  int rest;
+  int room;
+};
+
 namespace {
 
 __device__ inline float logistic(float z) { return 1.0f / (1.0f + __expf(-z)); }
@@ -34,28 +57,6 @@ __device__ inline int64_t row_at(const int32_t* order, int64_t place, int64_t n)
   return r >= 0 && r < n ? r : -1;
 }
 
-// A stretch of places of one group; ``part`` of ``parts`` of the group.
-struct RowTile {
-  int64_t first;
-  int32_t group;
-  int32_t count;
-  int32_t part, parts;
-};
-
-// Tiles of at most ``rows`` places of all groups, in group order, into list;
-// *count of them, first_of[g] the first of group g.  With ``rest`` group
-// n_groups stands for the rows of no group.  No more than ``room`` tiles are listed,
-// the most that a group_ptr can have that does not decrease: what one that does
-// would add is left out.  The work of one workgroup of ``blocks``; starts: LDS of
-// n_groups + 2 words.
-struct TileList {
-  RowTile* list;
-  int32_t* first_of;   // [n_groups + 2]
-  int32_t* count;
-  int rows;
-  int rest;
-  int room;
-};
 __device__ inline void list_tiles(const TileList& tl, const int64_t* ptr, int n_groups, int64_t n,
                                   int block, int blocks, int32_t* starts) {
   const int groups = n_groups + (tl.rest ? 1 : 0);
