@@ -208,6 +208,11 @@ __device__ inline Raw<T, V> load_raw_entries(const T* row, int c, int width, boo
     }
   return r;
 }
+// the same of a row that has V entries at least, without a branch
+template <class T, int V>
+__device__ inline Raw<T, V> load_raw_of_many(const T* row, int c, int width) {
+  return load_raw_entries<T, V>(row, c + V <= width ? c : width - V, width, false);
+}
 template <class T, int V>
 __device__ inline void settle(Raw<T, V>& r, int c, int width) {
   const int at = width >= V ? width - V : 0;

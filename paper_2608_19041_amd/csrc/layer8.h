@@ -35,23 +35,17 @@ struct Rows8Args {
   void* zout;
 };
 
-constexpr int kHeldBlocks = 8;   // of 128 entries
+constexpr int kHeldBlocks = 8, kWideBlocks = 5;   // of 128 entries: of few rows, and of many
 
 struct HeldArgs {
-  Rows8Args r;              // tiles = null: a workgroup looks its tile up
+  Rows8Args r;             // tiles = null: a workgroup looks its tile up
   const int64_t* ptr;
   int splits;              // workgroups that share the columns of a tile
-  // gradients: rows are formed from dy act'(z) (z = null: dy) of kin entries, not read
-  const void *dy, *z;
-  int64_t ldy, ldz;
-  _Float16* dz;            // [n][pitch8(kin)] by place, or null
-  uint8_t* dz_scales;      // [n][blocks of kin] by place
 };
 
-// The product over rows of up to kHeldBlocks blocks, by workgroups of 128 rows (wide) or 32; ``back``: dx,
-// and dz on the way.  ``format``: of the rows in 8 bits.
-int run_held8_f16(const HeldArgs& a, int format, bool back, bool wide, int64_t grid, hipStream_t st);
-int run_held8_bf16(const HeldArgs& a, int format, bool back, bool wide, int64_t grid, hipStream_t st);
+// The product over rows of up to kHeldBlocks blocks, by workgroups of 128 rows (wide) or 32.
+int run_held8_f16(const HeldArgs& a, int format, bool wide, int64_t grid, hipStream_t st);
+int run_held8_bf16(const HeldArgs& a, int format, bool wide, int64_t grid, hipStream_t st);
 
 namespace {
 
@@ -69,11 +63,6 @@ __device__ inline u4 keep_bytes(u4 v, int keep) {
   }
   return v;
 }
-
-// dz as float16: dz 2^(kHalfUp - e), e the exponent of its block's scale, so that the largest
-// entry of a block lies in (2^13.8, 2^14.8]; as 8-bit numbers: dz 2^-e
-template <int F>
-constexpr int kHalfUp = 14 - kTopExp<F>;
 
 // tile ``index`` of at most ``rows`` places; false past the last.  By every wave.
 __device__ inline bool find_tile(const int64_t* ptr, int n_groups, int64_t n, int rows, int64_t index, RowTile* t) {
@@ -106,248 +95,391 @@ __device__ inline bool find_tile(const int64_t* ptr, int n_groups, int64_t n, in
   return false;
 }
 
-// At most KB blocks of 128 entries a row.  A wave has 32 rows, a lane (its row lane % 32, and of each 64
-// entries the half lane / 32) 64 KB bytes of them in registers, and forms 32 columns at a time:
-// the weights are the first operand of the product, in an order in which a lane's sixteen sums are
-// neighbouring columns of its row, so that outputs leave from the registers.  Wide: the four waves have
-// 128 rows, and the columns' weights pass through LDS, the next ones on their way; else
-// they have the same 32 rows and 32 columns each, whose weights they read on their own.
-template <class T, int F, int KB, bool Back, bool Wide>
-__global__ void __launch_bounds__(kTileThreads, Wide ? (KB < 4 ? 3 : 2) : KB < 3 ? 3 : KB < 4 ? 2 : 1) layer8_held_kernel(HeldArgs h) {
-  const Rows8Args& a = h.r;
-  constexpr int kRows = Wide ? 128 : 32, kCols = 32;
-  constexpr int kBuffer = Wide ? kCols * KB * kStep : 16;
-  __shared__ __attribute__((aligned(16))) char lds[2][kBuffer];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = lane >> 5, col_tiles = (a.kout + kCols - 1) / kCols;
-  int64_t work = blockIdx.x;
-  RowTile t;
-  if (a.tiles) {
-    const int64_t total = int64_t(*a.n_tiles) * h.splits;
-    if (work >= total) return;
-    // the parts of a row tile follow each other on one XCD
-    work = xcd_block(work, total);
-    t = a.tiles[work / h.splits];
-  } else if (!find_tile(h.ptr, a.n_groups, a.n, kRows, work / h.splits, &t)) {
-    return;
+// 1 / (1 + exp(-z)) to 2^-22 of itself, and SiLU's slope from it: a division's own steps would be a
+// third of an output's instructions.
+__device__ inline float quick_logistic(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+__device__ inline float quick_slope(float z) {
+  const float p = quick_logistic(z);
+  return p * (1.0f + z * (1.0f - p));
+}
+
+// acc + a b over 64 entries, with byte ``op`` (a constant) of the lanes' scales
+template <int FB>
+__device__ __forceinline__ v16f multiply8(v8i a, v8i b, v16f acc, unsigned sa, unsigned sb, int op) {
+  constexpr int kB = FB == DPA4C_E4M3 ? 0 : 1;
+  switch (op) {
+    case 0: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, kB, 0, sa, 0, sb);
+    case 1: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, kB, 1, sa, 1, sb);
+    case 2: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, kB, 2, sa, 2, sb);
+    default: return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, kB, 3, sa, 3, sb);
   }
-  const int split = static_cast<int>(work % h.splits);
-  // this workgroup's column tiles, and of them this wave's
-  const int first = static_cast<int>(int64_t(col_tiles) * split / h.splits);
-  const int last = static_cast<int>(int64_t(col_tiles) * (split + 1) / h.splits);
+}
+// the words that hold KB scales, four each
+template <int KB>
+constexpr int kScaleWords = (KB + 3) / 4;
+
+// The row of a lane, place t.first + mine; past the tile its last one.
+struct HeldRow {
+  int64_t in;   // of the 8-bit rows
+  int to;       // of the results, -1: it is not there
+};
+__device__ inline HeldRow held_row(const Rows8Args& a, const RowTile& t, int mine) {
+  const int64_t place = t.first + (mine < t.count ? mine : t.count - 1);
+  const int64_t to = row_at(a.order, place, a.n);
+  return {a.by_place ? place : to < 0 ? 0 : to, static_cast<int>(to)};
+}
+// Of each 64 entries half lane / 32.
+template <int KB>
+__device__ __forceinline__ void read_held(const Rows8Args& a, const HeldRow& r, int half, v8i (*x)[2], unsigned* xs) {
+  const int chunks = static_cast<int>(pitch8(a.kin) / 16);
+  const char* from = a.in + r.in * a.ldin;
+  const uint8_t* scales = a.in_scales + r.in * a.ld_scales;
+#pragma unroll
+  for (int i = 0; i < kScaleWords<KB>; ++i) xs[i] = 0;
+#pragma unroll
+  for (int b = 0; b < KB; ++b) {
+    xs[b / 4] |= unsigned(scales[b]) << (8 * (b & 3));
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u4 v[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int chunk = b * kSlots8 + 4 * s + 2 * half + j;
+        v[j] = *reinterpret_cast<const u4*>(from + (b < KB - 1 || chunk < chunks ? chunk : chunks - 1) * 16);
+        if (b == KB - 1) v[j] = keep_bytes(v[j], a.kin - chunk * 16);
+      }
+      __builtin_memcpy(&x[b][s], v, 32);
+    }
+  }
+}
+// the same tile in every lane, as the compiler then knows
+__device__ inline RowTile uniform(RowTile t) {
+  auto one = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  t.first = int64_t(static_cast<uint64_t>(static_cast<unsigned>(one(static_cast<int>(t.first >> 32)))) << 32 |
+                    static_cast<unsigned>(one(static_cast<int>(t.first))));
+  t.group = one(t.group);
+  t.count = one(t.count);
+  t.part = one(t.part);
+  t.parts = one(t.parts);
+  return t;
+}
+
+// Zeros for a tile of rows of no group, columns c0 .. c1.
+template <class T>
+__device__ inline void clear_rows(const Rows8Args& a, const RowTile& t, int c0, int c1) {
   T* out = static_cast<T*>(a.out);
   T* zout = static_cast<T*>(a.zout);
+  for (int i = threadIdx.x; i < t.count * (c1 - c0); i += kTileThreads) {
+    const int64_t row = row_at(a.order, t.first + i / (c1 - c0), a.n);
+    if (row < 0) continue;
+    out[row * a.kout + c0 + i % (c1 - c0)] = from_f32<T>(0.0f);
+    if (zout) zout[row * a.kout + c0 + i % (c1 - c0)] = from_f32<T>(0.0f);
+  }
+}
 
-  if (t.group == a.n_groups) {   // rows of no group
-    const int c0 = first * kCols, width = (last * kCols < a.kout ? last * kCols : a.kout) - c0;
-    for (int i = tid; i < t.count * width; i += kTileThreads) {
-      const int64_t row = row_at(a.order, t.first + i / width, a.n);
-      if (row < 0) continue;
-      out[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
-      if (zout) zout[row * a.kout + c0 + i % width] = from_f32<T>(0.0f);
-    }
+// V outputs of a row from column c on, from their sums with the bias in them.
+template <class T, int V>
+__device__ __forceinline__ void finish_row(const Rows8Args& a, const Raw<T, V>& res, int64_t row, int c,
+                                           const float* sums) {
+  const bool ends = c + V > a.kout;
+  if (a.zout) store_entries<T, V>(static_cast<T*>(a.zout) + row * a.kout, c, a.kout, sums, ends);
+  float y[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    y[j] = a.silu ? sums[j] * quick_logistic(sums[j]) : sums[j];
+    if (a.residual) y[j] += res.at(j);
+  }
+  store_entries<T, V>(static_cast<T*>(a.out) + row * a.kout, c, a.kout, y, ends);
+}
+
+// KB blocks of 128 entries a row, eight columns at least.  A wave has 32 rows, a lane its row lane % 32 and of each 64
+// entries half lane / 32, 64 KB bytes of registers, which are read once for all columns; the four waves
+// have 128 rows.  32 columns' weights at a time pass through LDS, the next ones on their way, and are
+// the first operand of a product, in an order in which a lane's sums are sixteen neighbouring columns of
+// its row; the sums of two parts pass through LDS to lanes that have eight columns of four rows, so that
+// eight lanes write 128 bytes of a row.
+//
+// Loads are waited for by counting what was issued after them, so what stands between a load and its use
+// must not depend on conditions: weights are fetched before the stores of a part, and those are made by
+// every lane (rows past the tile repeat its last one, and write the same once more), but for the
+// last columns and rows that are not to be stored, after which the wave waits for all (kDrain).
+constexpr int kDrain = 0x0f70;   // s_waitcnt vmcnt(0)
+template <class T, int F, int KB, bool Z>
+__global__ void __launch_bounds__(kTileThreads, KB < 4 ? 3 : 2) layer8_held_kernel(HeldArgs h) {
+  const Rows8Args& a = h.r;
+  constexpr int kCols = 32, kPair = 2 * kCols;
+  __shared__ __attribute__((aligned(16))) char lds[2][kCols * KB * kStep];
+  __shared__ __attribute__((aligned(16))) float stage[kTileThreads / kWave][kCols * kPair];
+  __shared__ __attribute__((aligned(16))) float biases[4][kCols];
+  __shared__ unsigned wscales[kMaxWidth / kScaleBlock * kScaleWords<KB>];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col_tiles = (a.kout + kPair - 1) / kPair;
+  const int64_t total = int64_t(*a.n_tiles) * h.splits;
+  if (blockIdx.x >= total) return;
+  // the parts of a row tile follow each other on one XCD
+  const int64_t work = xcd_block(blockIdx.x, total);
+  const RowTile t = uniform(a.tiles[work / h.splits]);
+  const int split = static_cast<int>(work % h.splits);
+  // parts of 32 columns, two to a tile
+  const int first = 2 * static_cast<int>(int64_t(col_tiles) * split / h.splits);
+  const int last = 2 * static_cast<int>(int64_t(col_tiles) * (split + 1) / h.splits);
+  if (t.group == a.n_groups) {
+    clear_rows<T>(a, t, first * kCols, last * kCols < a.kout ? last * kCols : a.kout);
     return;
   }
+  const HeldRow r = held_row(a, t, 32 * wave + (lane & 31));
+  const bool live = 32 * wave < t.count;
+  const int pitch = static_cast<int>(pitch8(a.kin)), chunks = pitch / 16;
+  const T* bias = a.bias ? static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
+  const T* res = static_cast<const T*>(a.residual);
 
-  const int mine = (Wide ? 32 * wave : 0) + (lane & 31);
-  const int64_t place = t.first + (mine < t.count ? mine : t.count - 1);
-  const int64_t to = row_at(a.order, place, a.n), row = to < 0 ? 0 : to;
-  const bool stored = mine < t.count && to >= 0;
-  const bool live = !Wide || 32 * wave < t.count;
-  const int64_t pitch = pitch8(a.kin);
-  const int chunks = static_cast<int>(pitch / 16), blocks = static_cast<int>(blocks_of(a.kin));   // blocks <= KB
-
-  // weights: slot tid % 8 of row tid / 8 of the operand, which is column ``column(tid / 8)``
-  auto column = [](int m) { return 16 * (m >> 2 & 1) + 4 * (m >> 3) + (m & 3); };
+  // weights: slot tid % 8 of row tid / 8 of the operand, the column that a lane's sums have there; a
+  // group's are below 2^26 bytes
   const char* weights = a.w + int64_t(t.group) * a.kout * pitch;
-  const uint8_t* wscales = a.w_scales + t.group * a.w_blocks;
+  const int block0 = first * kCols / kScaleBlock;   // of columns
+  for (int i = tid; i < ((last * kCols - 1) / kScaleBlock - block0 + 1) * KB; i += kTileThreads)
+    reinterpret_cast<uint8_t*>(wscales)[i / KB * 4 * kScaleWords<KB> + i % KB] =
+        a.w_scales[t.group * a.w_blocks + (block0 + i / KB) * a.at_out + i % KB * a.at_in];
   const int slot = tid % kSlots8, own = tid / kSlots8;
+  const int column = 16 * (own >> 2 & 1) + 4 * (own >> 3) + (own & 3);
+  const int last_chunk = (KB - 1) * kSlots8 + slot < chunks ? (KB - 1) * kSlots8 + slot : chunks - 1;
   u4 wreg[KB];
-  auto fetch = [&](int tile) {   // past the end: the last column
-    const int c = tile * kCols + column(own);
-    const char* from = weights + int64_t(c < a.kout ? c : a.kout - 1) * pitch;
+  T breg = from_f32<T>(0.0f);
+  auto fetch = [&](int p) __attribute__((always_inline)) {   // past the end: the last one
+    p = p < last ? p : last - 1;
+    if (bias) breg = bias[p * kCols + (lane & 31) < a.kout ? p * kCols + (lane & 31) : a.kout - 1];
+    const int c = p * kCols + column;
+    const unsigned from = static_cast<unsigned>((c < a.kout ? c : a.kout - 1) * pitch);
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      const int chunk = b * kSlots8 + slot;
-      wreg[b] = *reinterpret_cast<const u4*>(from + (chunk < chunks ? chunk : chunks - 1) * 16);
-    }
+    for (int b = 0; b < KB; ++b)
+      wreg[b] = *reinterpret_cast<const u4*>(weights + (b < KB - 1 ? from + slot * 16 + b * kStep : from + last_chunk * 16));
   };
-  auto put = [&](int buffer) {
+  auto put = [&](int p) __attribute__((always_inline)) {
+    wreg[KB - 1] = keep_bytes(wreg[KB - 1], a.kin - (KB - 1) * kStep - slot * 16);
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      if (b >= blocks - 1) wreg[b] = keep_bytes(wreg[b], a.kin - b * kStep - slot * 16);
-      *reinterpret_cast<u4*>(lds[buffer] + b * kCols * kStep + slot8_at(own, slot)) = wreg[b];
-    }
+    for (int b = 0; b < KB; ++b)
+      *reinterpret_cast<u4*>(lds[p & 1] + b * kCols * kStep + slot8_at(own, slot)) = wreg[b];
+    if (tid < kCols) biases[p & 3][tid] = to_f32(breg);
+    // what is fetched next takes these registers, not others that would be copied, and waited for
+    __builtin_amdgcn_sched_barrier(0);
   };
-  if (Wide && first < last) fetch(first);
-
-  // the rows
+  fetch(first);
   v8i x[KB][2];
-  unsigned xs[KB];
-  if constexpr (!Back) {
-    const char* from = a.in + row * a.ldin;
-    const uint8_t* scales = a.in_scales + row * a.ld_scales;
+  unsigned xs[kScaleWords<KB>];
+  read_held<KB>(a, r, half, x, xs);
+  // where this lane's outputs go: rows 8 i + lane / 8, columns 8 (lane % 8) .. of a tile
+  int to[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) to[i] = __shfl(r.to, 8 * i + (lane >> 3));
+  const bool gaps = __ballot(r.to < 0) != 0;
+  put(first);
+  fetch(first + 1);
+  __syncthreads();
+  auto at = [](int row, int quad) { return row * kPair + ((quad ^ (quad >> 3) ^ (row & 7)) << 2); };
+  float* mine = stage[wave];
+  // the products of part p, whose buffer is ``odd``, and on to the next
+  auto multiply = [&](auto odd, int p) __attribute__((always_inline)) {
+    constexpr int o = decltype(odd)::value;
+    if (live) {
+      v16f acc = {};
+      // the weights of a block while the one before is multiplied
+      v8i f[2][2];
+      auto read = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          u4 v[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            v[j] = *reinterpret_cast<const u4*>(lds[o] + b * kCols * kStep +
+                                                slot8_at(lane & 31, 4 * s + 2 * half + j));
+          __builtin_memcpy(&f[b & 1][s], v, 32);
+        }
+      };
+      unsigned ws[kScaleWords<KB>];
+#pragma unroll
+      for (int i = 0; i < kScaleWords<KB>; ++i)
+        ws[i] = wscales[(p * kCols / kScaleBlock - block0) * kScaleWords<KB> + i];
+      read(0);
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        if (b + 1 < KB) read(b + 1);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) acc = multiply8<F>(f[b & 1][s], x[b][s], acc, ws[b / 4], xs[b / 4], b & 3);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<v4f*>(mine + at(lane & 31, 8 * o + 4 * half + q)) =
+            v4f{acc[4 * q], acc[4 * q + 1], acc[4 * q + 2], acc[4 * q + 3]};
+    }
+    put(p + 1);   // last read before the barrier of the part before
+    fetch(p + 2);
+  };
+  for (int p = first; p < last; p += 2) {
+    multiply(Const<0>{}, p);
+    __syncthreads();
+    const int c = p * kCols + 8 * (lane & 7);
+    const bool ends = p * kCols + kPair > a.kout;
+    Raw<T, 8> rv[4];
+    if (res)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        rv[i] = load_raw_of_many<T, 8>(res + (to[i] < 0 ? 0 : to[i]) * a.ldres, c, a.kout);
+    multiply(Const<1>{}, p + 1);
+    if (live) {
+      // of this wave alone: in order, no barrier
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      v4f bv[2];
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+        bv[q] = *reinterpret_cast<const v4f*>(biases[(p + (lane >> 2 & 1)) & 3] + 8 * (lane & 3) + 4 * q);
+      auto finish = [&](int i, bool tail) __attribute__((always_inline)) {
+        float z[8], y[8];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const v4f sum = *reinterpret_cast<const v4f*>(mine + at(8 * i + (lane >> 3), 2 * (lane & 7) + q));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) z[4 * q + j] = sum[j] + bv[q][j];
+        }
+        if (a.silu) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = z[j] * quick_logistic(z[j]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] = z[j];
+        }
+        if (res)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) y[j] += rv[i].at(j);
+        const int64_t row = int64_t(to[i]) * a.kout;
+        if (Z) store_entries<T, 8>(static_cast<T*>(a.zout) + row, c, a.kout, z, tail);
+        store_entries<T, 8>(static_cast<T*>(a.out) + row, c, a.kout, y, tail);
+      };
+      if (!ends && !gaps) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) finish(i, false);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (res) settle<T, 8>(rv[i], c, a.kout);
+          if (to[i] >= 0 && c < a.kout) finish(i, true);
+        }
+        __builtin_amdgcn_s_waitcnt(kDrain);
+      }
+    } else {
+      __builtin_amdgcn_s_waitcnt(kDrain);
+    }
+    __syncthreads();
+  }
+}
+
+// The same for few rows: the four waves have the same 32 rows and 32 columns each, whose weights they
+// read on their own, all at once; a tile is looked up in group_ptr where there is no list.
+template <class T, int F, int KB>
+__global__ void __launch_bounds__(kTileThreads, KB < 3 ? 3 : KB < 4 ? 2 : 1) layer8_few_kernel(HeldArgs h) {
+  const Rows8Args& a = h.r;
+  constexpr int kCols = 32, kWaves = kTileThreads / kWave;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col_tiles = (a.kout + kCols - 1) / kCols;
+  const int64_t index = blockIdx.x / h.splits;
+  const int split = static_cast<int>(blockIdx.x % h.splits);
+  RowTile t;
+  if (a.tiles) {
+    if (index >= *a.n_tiles) return;
+    t = a.tiles[index];
+  } else if (!find_tile(h.ptr, a.n_groups, a.n, 32, index, &t)) {
+    return;
+  }
+  const int first = kWaves * split, last = first + kWaves < col_tiles ? first + kWaves : col_tiles;
+  if (t.group == a.n_groups) {
+    clear_rows<T>(a, t, first * kCols, last * kCols < a.kout ? last * kCols : a.kout);
+    return;
+  }
+  const HeldRow r = held_row(a, t, lane & 31);
+  const int64_t pitch = pitch8(a.kin);
+  const int chunks = static_cast<int>(pitch / 16);
+  const int tile = first + wave;
+  const bool works = tile < last;   // of the whole wave
+  const int m = lane & 31, c = tile * kCols + 16 * (m >> 2 & 1) + 4 * (m >> 3) + (m & 3);
+  const char* from = a.w + (int64_t(t.group) * a.kout + (c < a.kout ? c : a.kout - 1)) * pitch;
+  const uint8_t* ws = a.w_scales + t.group * a.w_blocks + tile * kCols / kScaleBlock * a.at_out;
+  v8i w[KB][2];
+  unsigned scale[kScaleWords<KB>] = {};
+  if (works)
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      xs[b] = scales[b < blocks ? b : blocks - 1];
+      scale[b / 4] |= unsigned(ws[b * a.at_in]) << (8 * (b & 3));
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         u4 v[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const int chunk = b * kSlots8 + 4 * s + 2 * half + j;
-          v[j] = *reinterpret_cast<const u4*>(from + (chunk < chunks ? chunk : chunks - 1) * 16);
-          if (b >= blocks - 1) v[j] = keep_bytes(v[j], a.kin - chunk * 16);
+          v[j] = *reinterpret_cast<const u4*>(from + (b < KB - 1 || chunk < chunks ? chunk : chunks - 1) * 16);
+          if (b == KB - 1) v[j] = keep_bytes(v[j], a.kin - chunk * 16);
         }
-        __builtin_memcpy(&x[b][s], v, 32);
+        __builtin_memcpy(&w[b][s], v, 32);
       }
     }
-  } else {
-    const T* dy = static_cast<const T*>(h.dy) + row * h.ldy;
-    const T* z = h.z ? static_cast<const T*>(h.z) + row * h.ldz : nullptr;
-    const bool keeps = split == 0 && h.dz && mine < t.count && (Wide || wave == 0);
+  v8i x[KB][2];
+  unsigned xs[kScaleWords<KB>];
+  read_held<KB>(a, r, half, x, xs);
+  if (!works) return;
+  v16f acc = {};
+  const int c0 = tile * kCols + 16 * half;
+  if (a.bias) {
+    const T* bias = static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout;
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      const bool ends = b >= blocks - 1;
-      float v[2][32];
+    for (int q = 0; q < 2; ++q) {
+      float v[8];
+      load_entries<T, 8>(bias, c0 + 8 * q, a.kout, v);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int c = b * kStep + 64 * s + 32 * half + 8 * j;
-          Raw<T, 8> d = load_raw_entries<T, 8>(dy, c, a.kin, ends), e;
-          if (z) e = load_raw_entries<T, 8>(z, c, a.kin, ends);
-          if (ends) {
-            settle<T, 8>(d, c, a.kin);
-            if (z) settle<T, 8>(e, c, a.kin);
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            float f = to < 0 ? 0.0f : d.at(i);
-            if (z) f = to < 0 ? 0.0f : f * silu_slope(e.at(i));
-            v[s][8 * j + i] = f;
-          }
-        }
-      bool bad = false;
-      float most = fmaxf(finite_most<32>(v[0], &bad), finite_most<32>(v[1], &bad));
-      most = fmaxf(most, __shfl_xor(most, 32));
-      bad |= __shfl_xor(int(bad), 32) != 0;
-      const int e = scale_exp<F>(most);
-      const float up = power_of_two(-e);
-      xs[b] = static_cast<unsigned>(e + 127);
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[s][j] *= up;
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          x[b][s][j] = bad ? kNaN8 : pack8<F>(v[s][4 * j], v[s][4 * j + 1], v[s][4 * j + 2], v[s][4 * j + 3]);
-        if (keeps)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int c = b * kStep + 64 * s + 32 * half + 8 * j;
-            if (ends && c >= pitch) continue;
-            v8h f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = static_cast<_Float16>(v[s][8 * j + i] * power_of_two(kHalfUp<F>));
-            *reinterpret_cast<v8h*>(h.dz + place * pitch + c) = f;
-          }
-      }
-      if (keeps && half == 0 && b < blocks) h.dz_scales[place * blocks + b] = static_cast<uint8_t>(xs[b]);
+      for (int j = 0; j < 8; ++j) acc[8 * q + j] = v[j];
     }
   }
-
-  if (Wide && first < last) {
-    put(0);
-    fetch(first + 1);
-    __syncthreads();
-  }
-  const T* bias = a.bias ? static_cast<const T*>(a.bias) + int64_t(t.group) * a.kout : nullptr;
-  const T* res = a.residual ? static_cast<const T*>(a.residual) + row * a.ldres : nullptr;
-  for (int tile = first + (Wide ? 0 : wave); tile < last; tile += Wide ? 1 : 4) {
-    const uint8_t* ws = wscales + tile * kCols / kScaleBlock * a.at_out;
-    v16f acc = {};
-    const int buffer = (tile - first) & 1;
-    if (live) {
-      const char* direct = nullptr;
-      if (!Wide) {
-        const int c = tile * kCols + column(lane & 31);
-        direct = weights + int64_t(c < a.kout ? c : a.kout - 1) * pitch;
-      }
 #pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        const unsigned scale = ws[(b < blocks ? b : blocks - 1) * a.at_in];
+  for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          u4 v[2];
+    for (int s = 0; s < 2; ++s)
+      acc = multiply8<F>(w[b][s], x[b][s], acc, scale[b / 4], xs[b / 4], b & 3);
+  // here, with all lanes: a product reads the registers of every lane, but loads before it, were they
+  // moved to where its sums are used, only those of the lanes whose rows are stored
+  asm volatile("" : "+v"(acc));
+  if (r.to < 0 || m >= t.count) return;
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const int in = 4 * s + 2 * half + j, chunk = b * kSlots8 + in;
-            if constexpr (Wide) {
-              v[j] = *reinterpret_cast<const u4*>(lds[buffer] + b * kCols * kStep + slot8_at(lane & 31, in));
-            } else {
-              v[j] = *reinterpret_cast<const u4*>(direct + (chunk < chunks ? chunk : chunks - 1) * 16);
-              if (b >= blocks - 1) v[j] = keep_bytes(v[j], a.kin - chunk * 16);
-            }
-          }
-          v8i f;
-          __builtin_memcpy(&f, v, 32);
-          acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(f, x[b][s], acc, 0, F == DPA4C_E4M3 ? 0 : 1, 0, scale,
-                                                                0, xs[b]);
-        }
-      }
-      // here, with all lanes: a product reads the registers of every lane, but the loads before it, were
-      // they moved to where its sums are used, only those of the lanes whose rows are stored
-      asm volatile("" : "+v"(acc));
+  for (int q = 0; q < 2; ++q) {
+    const int at = c0 + 8 * q;
+    if (at >= a.kout) continue;
+    float sums[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[j] = acc[8 * q + j];
+    Raw<T, 8> res;
+    if (a.residual) {
+      res = load_raw_entries<T, 8>(static_cast<const T*>(a.residual) + r.to * a.ldres, at, a.kout);
+      settle<T, 8>(res, at, a.kout);
     }
-    if constexpr (Wide) {
-      put(buffer ^ 1);   // last read before the barrier of the tile before
-      fetch(tile + 2);
-    }
-    // sixteen neighbouring columns of a row a lane
-    if (live && stored) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int c = tile * kCols + 16 * half + 8 * q;
-        if (c >= a.kout) continue;
-        float y[8], zv[8], v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) zv[j] = acc[8 * q + j];
-        if (bias) {
-          load_entries<T, 8>(bias, c, a.kout, v);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) zv[j] += v[j];
-        }
-        if (res) load_entries<T, 8>(res, c, a.kout, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          y[j] = a.silu ? zv[j] * logistic(zv[j]) : zv[j];
-          if (res) y[j] += v[j];
-        }
-        store_entries<T, 8>(out + row * a.kout, c, a.kout, y);
-        if (zout) store_entries<T, 8>(zout + row * a.kout, c, a.kout, zv);
-      }
-    }
-    if (Wide) __syncthreads();
+    finish_row<T, 8>(a, res, r.to, at, sums);
   }
 }
 
 template <class T, int KB>
-int run_held(const HeldArgs& a, int format, bool back, bool wide, int64_t grid, hipStream_t st) {
-  auto launch = [&](auto f, auto b, auto w) {
-    layer8_held_kernel<T, decltype(f)::value, KB, decltype(b)::value, decltype(w)::value>
-        <<<grid, kTileThreads, 0, st>>>(a);
+int run_held(const HeldArgs& a, int format, bool wide, int64_t grid, hipStream_t st) {
+  auto launch = [&](auto f) {
+    constexpr int F = decltype(f)::value;
+    if (!wide) {
+      layer8_few_kernel<T, F, KB><<<grid, kTileThreads, 0, st>>>(a);
+    } else if constexpr (KB <= kWideBlocks) {
+      if (a.r.zout)
+        layer8_held_kernel<T, F, KB, true><<<grid, kTileThreads, 0, st>>>(a);
+      else
+        layer8_held_kernel<T, F, KB, false><<<grid, kTileThreads, 0, st>>>(a);
+    }
     DPA4C_HIP_TRY(hipGetLastError());
     return 0;
   };
-  auto of_format = [&](auto b, auto w) {
-    if (format == DPA4C_E4M3) return launch(std::integral_constant<int, DPA4C_E4M3>{}, b, w);
-    return launch(std::integral_constant<int, DPA4C_E5M2>{}, b, w);
-  };
-  using Yes = std::true_type;
-  using No = std::false_type;
-  if (back) return wide ? of_format(Yes{}, Yes{}) : of_format(Yes{}, No{});
-  return wide ? of_format(No{}, Yes{}) : of_format(No{}, No{});
+  if (format == DPA4C_E4M3) return launch(std::integral_constant<int, DPA4C_E4M3>{});
+  return launch(std::integral_constant<int, DPA4C_E5M2>{});
 }
 
 }  // namespace

@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(Rows8Args a) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         z[j] = s[j] + bq[j];
-        y[j] = a.silu ? z[j] * logistic(z[j]) : z[j];
+        y[j] = a.silu ? z[j] * quick_logistic(z[j]) : z[j];
         if (a.residual) y[j] += res[k][j];
       }
       store_entries<T, 4>(out + row[k] * a.kout, c, a.kout, y);
@@ -210,6 +210,11 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(Rows8Args a) {
 // ---------------------------------------------------------------------------
 // What the gradients need first
 // ---------------------------------------------------------------------------
+
+// dz as float16: dz 2^(kHalfUp - e), e the exponent of its block's scale, so that the largest
+// entry of a block lies in (2^13.8, 2^14.8]; as 8-bit numbers: dz 2^-e
+template <int F>
+constexpr int kHalfUp = 14 - kTopExp<F>;
 
 struct PrepArgs {
   const int64_t* ptr;
@@ -292,7 +297,7 @@ __global__ void __launch_bounds__(kPrepThreads) layer8_prepare_kernel(PrepArgs a
     if (at[i].row >= live) continue;   // a unit as a whole
     if (a.z)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[i][j] *= silu_slope(z[i][j]);
+      for (int j = 0; j < 8; ++j) v[i][j] *= quick_slope(z[i][j]);
     unsigned q[2];
     const unsigned scale = quantize_block<F, 8>(v[i], kUnit, q);
     const int c = at[i].part * kScaleBlock + lane * 8;
@@ -522,17 +527,18 @@ struct Tiling {
   int rows, splits;
 };
 Tiling tiling(int64_t n, int n_groups, int kin, int kout) {
-  Tiling t{blocks_of(kin) <= kHeldBlocks, false, true, 0, 1};
+  const bool many = n >= kWideRows && kout >= 8;
+  Tiling t{blocks_of(kin) <= (many ? kWideBlocks : kHeldBlocks), false, true, 0, 1};
   if (!t.held) {
     t.rows = kout > 64 && (n / 128) * ((kout + 127) / 128) >= 256 ? kSide<2> : kSide<1>;
     return t;
   }
   const int64_t cols = (kout + 31) / 32;
-  t.wide = n >= kWideRows;
+  t.wide = many;
   t.rows = t.wide ? 128 : 32;
   t.listed = t.wide || n_groups > 512;
   if (t.wide)
-    t.splits = static_cast<int>(std::max<int64_t>(1, std::min(1024 / (n / 128 + std::min<int64_t>(n_groups, n / 128) / 2), cols / 3)));
+    t.splits = static_cast<int>(std::max<int64_t>(1, std::min(1024 / (n / 128 + std::min<int64_t>(n_groups, n / 128) / 2), (cols + 1) / 4)));
   else
     t.splits = static_cast<int>(std::max<int64_t>(1, (cols + 3) / 4));
   return t;
@@ -559,11 +565,11 @@ Plan plan_backward(const dpa4c_grouped8& l, bool dx, bool dw, bool db, void* wor
   Plan p{};
   const int64_t n = l.x.n;
   const int k = l.w.k, m = l.w.n_out, groups = l.w.n_groups, rows = outer_rows(n, k, m);
-  p.how = tiling(n, groups, m, dx ? k : 0);
-  if ((dx || p.how.held) && p.how.listed) p.tiles = list_of(ar, n, groups, p.how.rows, true);
+  p.how = tiling(n, groups, m, k);
+  if (dx && p.how.listed) p.tiles = list_of(ar, n, groups, p.how.rows, true);
   if (dw || db) p.blocks = list_of(ar, n, groups, rows, false);
   p.dz = ar.take<_Float16>(dw || db ? n * pitch8(m) : 0);
-  p.dz8 = ar.take<uint8_t>(dx && !p.how.held ? n * pitch8(m) : 0);
+  p.dz8 = ar.take<uint8_t>(dx ? n * pitch8(m) : 0);
   p.dz_scales = ar.take<uint8_t>(n * blocks_of(m));
   // only groups of more than ``rows`` rows have several blocks
   const int64_t blocks = tiles_at_most(n, groups, rows), ends = n > rows ? (2 * n + rows - 1) / rows : 0;
@@ -597,10 +603,10 @@ int run_rows(const Rows8Args& a, const Tiling& how, hipStream_t st) {
   return 0;
 }
 
-int run_held(int dtype, int format, const HeldArgs& a, const Tiling& how, bool back, hipStream_t st) {
+int run_held(int dtype, int format, const HeldArgs& a, const Tiling& how, hipStream_t st) {
   const int64_t grid = tiles_at_most(a.r.n, a.r.n_groups, how.rows) * how.splits;
-  return dtype == DPA4C_F16 ? run_held8_f16(a, format, back, how.wide, grid, st)
-                            : run_held8_bf16(a, format, back, how.wide, grid, st);
+  return dtype == DPA4C_F16 ? run_held8_f16(a, format, how.wide, grid, st)
+                            : run_held8_bf16(a, format, how.wide, grid, st);
 }
 
 template <class Fn>
@@ -678,7 +684,7 @@ int launch_grouped8_forward(const dpa4c_grouped8& l, const void* bias, bool silu
     h.r = a;
     h.ptr = l.group_ptr;
     h.splits = p.how.splits;
-    return run_held(l.dtype, F, h, p.how, false, st);
+    return run_held(l.dtype, F, h, p.how, st);
   });
 }
 
@@ -715,9 +721,9 @@ int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy
     const int64_t each = dw ? int64_t(k) * m : 1;
     pre.clear_blocks = outer ? int64_t(groups) * ((each + kClear - 1) / kClear) : 0;
     const int64_t units = kPrepThreads / kUnit * kPrepTurns;
-    const int64_t dz_blocks = p.how.held ? 0 : (n * blocks_of(m) + units - 1) / units;
-    if (outer || p.how.listed) DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks + pre.clear_blocks + dz_blocks, st)));
-    if (n == 0 || (!rows && !p.how.held)) return 0;
+    const int64_t dz_blocks = (n * blocks_of(m) + units - 1) / units;
+    DPA4C_TRY((prepare<T, F>(pre, pre.list_blocks + pre.clear_blocks + dz_blocks, st)));
+    if (!rows) return 0;
     Rows8Args a{};
     a.order = l.order;
     a.n_groups = groups;
@@ -725,7 +731,7 @@ int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy
     a.tiles = p.tiles.list;
     a.n_tiles = p.tiles.count;
     a.kin = m;
-    a.kout = rows ? k : 0;   // dz alone
+    a.kout = k;
     a.in = reinterpret_cast<const char*>(p.dz8);
     a.ldin = pitch8(m);
     a.in_scales = p.dz_scales;
@@ -742,13 +748,7 @@ int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy
     h.r = a;
     h.ptr = l.group_ptr;
     h.splits = p.how.splits;
-    h.dy = dy;
-    h.z = z;
-    h.ldy = ldy;
-    h.ldz = ldz;
-    h.dz = outer ? p.dz : nullptr;
-    h.dz_scales = p.dz_scales;
-    return run_held(l.dtype, F, h, p.how, true, st);
+    return run_held(l.dtype, F, h, p.how, st);
   }));
   if (!outer) return 0;
   return with_types(l.dtype, l.x.format, [&](auto t, auto f) {

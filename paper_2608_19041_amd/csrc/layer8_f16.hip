@@ -5,14 +5,17 @@
 
 namespace dpa4c {
 
-int run_held8_f16(const HeldArgs& a, int format, bool back, bool wide, int64_t grid, hipStream_t st) {
-  // three blocks take rows of three, five those of four and five, eight the longer ones
-  const int64_t blocks = blocks_of(a.r.kin);
-  if (blocks <= 1) return run_held<_Float16, 1>(a, format, back, wide, grid, st);
-  if (blocks <= 2) return run_held<_Float16, 2>(a, format, back, wide, grid, st);
-  if (blocks <= 3) return run_held<_Float16, 3>(a, format, back, wide, grid, st);
-  if (blocks <= 5) return run_held<_Float16, 5>(a, format, back, wide, grid, st);
-  return run_held<_Float16, kHeldBlocks>(a, format, back, wide, grid, st);
+int run_held8_f16(const HeldArgs& a, int format, bool wide, int64_t grid, hipStream_t st) {
+  switch (blocks_of(a.r.kin)) {
+    case 1: return run_held<_Float16, 1>(a, format, wide, grid, st);
+    case 2: return run_held<_Float16, 2>(a, format, wide, grid, st);
+    case 3: return run_held<_Float16, 3>(a, format, wide, grid, st);
+    case 4: return run_held<_Float16, 4>(a, format, wide, grid, st);
+    case 5: return run_held<_Float16, 5>(a, format, wide, grid, st);
+    case 6: return run_held<_Float16, 6>(a, format, wide, grid, st);
+    case 7: return run_held<_Float16, 7>(a, format, wide, grid, st);
+    default: return run_held<_Float16, kHeldBlocks>(a, format, wide, grid, st);
+  }
 }
 
 }  // namespace dpa4c
