@@ -353,7 +353,11 @@ __device__ inline v2h half_pair(unsigned v, float scale) {
 // held exactly, or to 2^-40 of the largest product of the block.
 template <class T, int F>
 __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) {
-  constexpr int kOne = kPlane<2>, kHalfLds = 2 * kOne;
+  // blocks of 32 columns, [block][32 rows][32 columns], set off so that the lanes of one LDS cycle, eight
+  // neighbouring slots of a row of x's sixteen or dz's, meet all banks
+  constexpr int kBlock = 32 * kRowBytes, kOne = 4 * kBlock + 128, kHalfLds = 2 * kOne;
+  auto x_block = [](int b) { return b * kBlock + 16 * (b & 1) + 64 * (b >> 1); };
+  auto z_block = [](int b) { return kOne + b * kBlock + 64 * (b & 1); };
   constexpr int kXUp = 15 - kTopExp<F>;
   __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
   __shared__ float bias_part[16][kOuterTile];
@@ -365,14 +369,14 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) 
   // the tiles of a block of rows follow each other on one XCD
   const int64_t work = xcd_block(blockIdx.x, total);
   const int64_t block = work / (row_tiles * col_tiles);
-  const RowTile t = a.blocks[block];
+  const RowTile t = uniform(a.blocks[block]);
   const int64_t group_slot =
       a.slots.by_start ? a.slots.of(t.first - int64_t(t.part) * a.slots.rows, t.part) : block;
   const int r0 = static_cast<int>(work / col_tiles % row_tiles) * kOuterTile;
   const int c0 = static_cast<int>(work % col_tiles) * kOuterTile;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1;
-  const int64_t end = t.first + t.count, pitch = pitch8(a.m);
+  const int64_t pitch = pitch8(a.m);
   const int z_blocks = static_cast<int>(blocks_of(a.m));
   const uint8_t* xs = a.x_scales + r0 / kScaleBlock;
   const uint8_t* zs = a.dz_scales + c0 / kScaleBlock;
@@ -400,64 +404,80 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) 
   const int xc = r0 + 16 * x_slot < x_last ? r0 + 16 * x_slot : x_last;   // columns past the end: any
   const int zc = c0 + 8 * z_slot < z_last ? c0 + 8 * z_slot : z_last;
   // the rows of a step are looked up one fetch before its loads, and before that fetch's own:
-  // loads arrive in order, so they are there in time without the operands having to be
-  int64_t next;
-  auto look = [&](int step) {
-    const int64_t place = t.first + int64_t(step) * kDepth + x_own;
-    const int64_t at = place < end ? place : end - 1;
-    const int64_t row = a.order ? a.order[at] : at;   // without a condition
-    next = place < end && row >= 0 && row < a.n ? row : -1;
+  // loads arrive in order, so they are there in time without the operands having to be.  Nothing is
+  // done with what is loaded, and no load made under a condition, before it is needed.
+  // Offsets into the block (below 2^31 bytes) go on by a step's and stop at its last row: a
+  // product of 64 bits for each address would be a third of the kernel's vector cycles.
+  const unsigned rows_end = static_cast<unsigned>(t.count - 1);
+  const unsigned z_row = static_cast<unsigned>(pitch) * 2, s_row = static_cast<unsigned>(z_blocks);
+  const char* dz0 = reinterpret_cast<const char*>(a.dz) + t.first * pitch * 2;
+  const uint8_t* zs0 = zs + t.first * z_blocks;
+  unsigned at_row = x_own, at_xs = x_own * s_row;
+  unsigned at_z[2], at_zs[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    at_z[i] = (z_own + 16 * i) * z_row + zc * 2;
+    at_zs[i] = (z_own + 16 * i) * s_row;
+  }
+  int next;
+  auto look = [&]() {
+    const unsigned at = at_row < rows_end ? at_row : rows_end;
+    next = a.order ? a.order[t.first + at] : static_cast<int>(t.first) + static_cast<int>(at);
   };
-  u4 rx[2], rz[2][2];
-  bool there[2];
-  unsigned ex[2], ez[2], zscale[2][2];
-  look(0);
-  auto fetch = [&](auto turn, int step) {
+  constexpr int kFar = 2;   // steps whose loads are in flight
+  u4 rx[kFar], rz[kFar][2];
+  bool there[kFar];
+  unsigned ex[kFar], ez[kFar], zscale[kFar][2];
+  look();
+  auto fetch = [&](auto turn, int) {
     constexpr int q = decltype(turn)::value;
-    const int64_t row = next < 0 ? 0 : next;
-    there[q] = next >= 0;
-    look(step + 1);
+    there[q] = next >= 0 && next < a.n && at_row <= rows_end;
+    const int64_t row = there[q] ? next : 0;
+    at_row += kDepth;
+    look();
     rx[q] = *reinterpret_cast<const u4*>(a.x + row * a.ldx + xc);
     ex[q] = xs[row * a.ld_scales];
-    const int64_t first = t.first + int64_t(step) * kDepth;
-    ez[q] = zs[(first + x_own < end ? first + x_own : end - 1) * z_blocks];
+    ez[q] = zs0[at_xs < rows_end * s_row ? at_xs : rows_end * s_row];
+    at_xs += kDepth * s_row;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int64_t place = first + z_own + 16 * i, at = place < end ? place : end - 1;
-      rz[q][i] = *reinterpret_cast<const u4*>(a.dz + at * pitch + zc);
-      zscale[q][i] = place < end ? zs[at * z_blocks] : 256;
+      const unsigned z_end = rows_end * z_row + zc * 2, s_end = rows_end * s_row;
+      rz[q][i] = *reinterpret_cast<const u4*>(dz0 + (at_z[i] < z_end ? at_z[i] : z_end));
+      zscale[q][i] = zs0[at_zs[i] < s_end ? at_zs[i] : s_end];
+      at_z[i] += kDepth * z_row;
+      at_zs[i] += kDepth * s_row;
     }
   };
   float bias[8] = {};
-  auto put = [&](auto turn, auto, int) {
+  auto put = [&](auto turn, auto, int step) {
     constexpr int q = decltype(turn)::value;
-    char* to = lds + q * kHalfLds;
+    char* to = lds + (q & 1) * kHalfLds;
     if (a.dw) {
       const int d = static_cast<int>(ex[q] + ez[q]) - top + kXUp;   // at most kXUp
-      const float scale = ex[q] == 255 ? NAN : power_of_two(d < -126 ? -126 : d);
-      v8h h[2] = {};
-      if (there[q])
+      const float scale = !there[q] ? 1.0f : ex[q] == 255 ? NAN : power_of_two(d < -126 ? -126 : d);
+      v8h h[2];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const v2h lo = half_pair<F, false>(rx[q][j], scale), hi = half_pair<F, true>(rx[q][j], scale);
+          const unsigned x = there[q] ? rx[q][j] : 0;
+          const v2h lo = half_pair<F, false>(x, scale), hi = half_pair<F, true>(x, scale);
           h[j / 2][4 * (j % 2)] = lo.x, h[j / 2][4 * (j % 2) + 1] = lo.y;
           h[j / 2][4 * (j % 2) + 2] = hi.x, h[j / 2][4 * (j % 2) + 3] = hi.y;
         }
 #pragma unroll
       for (int j = 0; j < 2; ++j)
-        *reinterpret_cast<v8h*>(to + x_slot / 2 * 32 * kRowBytes + slot_at(x_own, x_slot % 2 * 2 + j)) = h[j];
+        *reinterpret_cast<v8h*>(to + x_block(x_slot / 2) + slot_at(x_own, x_slot % 2 * 2 + j)) = h[j];
     }
     const u4 none = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const u4 v = zscale[q][i] < 256 ? rz[q][i] : none;
+      const u4 v = step * kDepth + z_own + 16 * i < t.count ? rz[q][i] : none;
       if (sums_bias) {
         const v8h f = __builtin_bit_cast(v8h, v);
-        const float own = scale_of(zscale[q][i] & 255) * power_of_two(-a.dz_up);
+        const float own = scale_of(zscale[q][i]) * power_of_two(-a.dz_up);
 #pragma unroll
         for (int j = 0; j < 8; ++j) bias[j] += static_cast<float>(f[j]) * own;
       }
-      *reinterpret_cast<u4*>(to + kOne + z_slot / 4 * 32 * kRowBytes + slot_at(z_own + 16 * i, z_slot % 4)) = v;
+      *reinterpret_cast<u4*>(to + z_block(z_slot / 4) + slot_at(z_own + 16 * i, z_slot % 4)) = v;
     }
   };
   Sums<2> acc;
@@ -467,14 +487,21 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) 
   auto read = [&](auto half, int step) {
     constexpr int ks = decltype(half)::value;
     if (!live) return;
-    load_part_turned(fa[ks], lds + (step & 1) * kHalfLds + wm * 64 * kRowBytes, kOne, lane, ks);
-    load_part_turned(fb[ks], lds + (step & 1) * kHalfLds + kOne + wn * 64 * kRowBytes, kOne, lane, ks);
+    const char* half_of = lds + (step & 1) * kHalfLds;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      Part<1, 1> p;
+      load_part_turned(p, half_of + x_block(2 * wm + i), 0, lane, ks);
+      fa[ks].v[i][0] = p.v[0][0];
+      load_part_turned(p, half_of + z_block(2 * wn + i), 0, lane, ks);
+      fb[ks].v[i][0] = p.v[0][0];
+    }
   };
   auto multiply = [&](auto half) {
     constexpr int ks = decltype(half)::value;
     if (live) multiply_parts<false>(acc, fa[ks], fb[ks]);
   };
-  run_steps<2, 2>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
+  run_steps<kFar, kFar>(steps, fetch, [](auto, int) {}, put, read, [](int) {}, multiply);
 
   const bool whole = t.parts == 1;
   if (a.dw) {
@@ -516,6 +543,16 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) 
 // ---------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------
+
+// Rows of a block of dW: four rounds of the 512 workgroups that are resident, between 512 and 8,192 rows, or
+// as few as outer_rows gives where there are few.  (65,536 x 1,024 x 1,024: blocks of 2,048 rows
+// in place of 1,024 save half of the sums that are written and joined, 717 us to 680.)
+int block_rows(int64_t n, int k, int m) {
+  const int64_t tiles = ((k + kOuterTile - 1) / kOuterTile) * int64_t((m + kOuterTile - 1) / kOuterTile);
+  const int few = outer_rows(n, k, m);
+  const int64_t rows = align_up((n * tiles + 2047) / 2048, kDepth);
+  return static_cast<int>(few < 512 || rows < few ? few : rows > 8192 ? 8192 : rows);
+}
 
 // Rows of at most kHeldBlocks blocks are held in registers; longer ones go through LDS in tiles,
 // 128 x 128 where they fill the compute units, else 64 x 64.  Held: workgroups of 128 rows from
@@ -564,7 +601,7 @@ Plan plan_backward(const dpa4c_grouped8& l, bool dx, bool dw, bool db, void* wor
   Arena ar{static_cast<char*>(work)};
   Plan p{};
   const int64_t n = l.x.n;
-  const int k = l.w.k, m = l.w.n_out, groups = l.w.n_groups, rows = outer_rows(n, k, m);
+  const int k = l.w.k, m = l.w.n_out, groups = l.w.n_groups, rows = block_rows(n, k, m);
   p.how = tiling(n, groups, m, k);
   if (dx && p.how.listed) p.tiles = list_of(ar, n, groups, p.how.rows, true);
   if (dw || db) p.blocks = list_of(ar, n, groups, rows, false);
@@ -624,7 +661,7 @@ bool grouped8_fits(const dpa4c_grouped8& l) {
   const int64_t n = l.x.n, k = l.w.k, m = l.w.n_out;
   const int64_t prep = 64 + l.w.n_groups * up(k * m, kClear) + up(n * blocks_of(m), kPrepThreads / kUnit * kPrepTurns);
   const int64_t rows = tiles_at_most(n, l.w.n_groups, 32) * up(std::max(k, m), kSide<1>);
-  const int64_t outer = tiles_at_most(n, l.w.n_groups, outer_rows(n, l.w.k, l.w.n_out)) * up(k, kOuterTile) * up(m, kOuterTile);
+  const int64_t outer = tiles_at_most(n, l.w.n_groups, block_rows(n, l.w.k, l.w.n_out)) * up(k, kOuterTile) * up(m, kOuterTile);
   return grid_fits(prep, kPrepThreads) && grid_fits(rows, kThreads) && grid_fits(outer, kThreads);
 }
 

@@ -53,21 +53,15 @@ typedef unsigned u4v __attribute__((ext_vector_type(4)));
 // sixteen 8-bit numbers under one scale
 template <int F, class T>
 __device__ inline void write_values(u4v q, float scale, T* out, int c, int width) {
+  constexpr int V = 16 / int(sizeof(T));
   float f[16];
 #pragma unroll
   for (int j = 0; j < 4; ++j) unpack8<F>(q[j], f + 4 * j);
 #pragma unroll
   for (int j = 0; j < 16; ++j) f[j] *= scale;
-  if (c + 16 <= width) {
-    Entries<T, 16> e;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) e.v[j] = from_f32<T>(f[j]);
-    *reinterpret_cast<Entries<T, 16>*>(out + c) = e;
-  } else {
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-      if (c + j < width) out[c + j] = from_f32<T>(f[j]);
-  }
+  for (int j = 0; j < 16; j += V)
+    if (c + j < width) store_entries<T, V>(out, c + j, width, f + j);
 }
 
 // Row r takes scales from row r / of (weights: the 128 rows of a block share them).
@@ -78,19 +72,25 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint8_t* __r
                                                               T* __restrict__ out) {
   const int parts = (k + 15) / 16;
   const int64_t first = int64_t(blockIdx.x) * kThreads * kTurns;
+  Item at[kTurns];
+  u4v q[kTurns];
+  unsigned scale[kTurns];
 #pragma unroll
-  for (int i = 0; i < kTurns; ++i) {
-    const Item at = item_at(first, i * kThreads + int(threadIdx.x), parts);
-    if (at.row >= n) continue;
-    const u4v q = *reinterpret_cast<const u4v*>(values + at.row * ld + at.part * 16);
-    int64_t of = at.row;
+  for (int i = 0; i < kTurns; ++i) {   // past the end: the last one
+    at[i] = item_at(first, i * kThreads + int(threadIdx.x), parts);
+    const int64_t row = at[i].row < n ? at[i].row : n - 1;
+    q[i] = *reinterpret_cast<const u4v*>(values + row * ld + at[i].part * 16);
+    int64_t of = row;
     if (group_rows) {   // weights: rows of a group, and of its blocks
-      const int64_t g = at.row / group_rows;
-      of = g * blocks_of(group_rows) + (at.row - g * group_rows) / kScaleBlock;
+      const int64_t g = row / group_rows;
+      of = g * blocks_of(group_rows) + (row - g * group_rows) / kScaleBlock;
     }
-    write_values<F, T>(q, scale_of(scales[of * lds + at.part / (kScaleBlock / 16)]), out + at.row * int64_t(k),
-                       at.part * 16, k);
+    scale[i] = scales[of * lds + at[i].part / (kScaleBlock / 16)];
   }
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i)
+    if (at[i].row < n)
+      write_values<F, T>(q[i], scale_of(scale[i]), out + at[i].row * int64_t(k), at[i].part * 16, k);
 }
 
 // A block of 128 x 128 of one group's weights by a workgroup, as it is and turned.
