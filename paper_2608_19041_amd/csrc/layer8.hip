@@ -355,9 +355,9 @@ template <class T, int F>
 __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) {
   // blocks of 32 columns, [block][32 rows][32 columns], set off so that the lanes of one LDS cycle, eight
   // neighbouring slots of a row of x's sixteen or dz's, meet all banks
-  constexpr int kBlock = 32 * kRowBytes, kOne = 4 * kBlock + 128, kHalfLds = 2 * kOne;
+  constexpr int kBlock = 32 * kRowBytes, kOne = 4 * kBlock + 256, kHalfLds = 2 * kOne;
   auto x_block = [](int b) { return b * kBlock + 16 * (b & 1) + 64 * (b >> 1); };
-  auto z_block = [](int b) { return kOne + b * kBlock + 64 * (b & 1); };
+  auto z_block = [](int b) { return kOne + b * (kBlock + 64); };
   constexpr int kXUp = 15 - kTopExp<F>;
   __shared__ __attribute__((aligned(16))) char lds[2 * kHalfLds];
   __shared__ float bias_part[16][kOuterTile];
