@@ -49,6 +49,15 @@ int64_t grouped8_backward_work(const dpa4c_grouped8& l, bool dx, bool dw, bool d
 int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy, int64_t ldy, const void* z,
                              int64_t ldz, void* dx, void* dw, void* db, void* work, hipStream_t st);
 
+// how many parts a row has, and the reciprocals with which 64 and 32 bits are divided by that: rounded
+// up they give the quotient where dividend x parts stays below 2^64 and 2^32
+struct Parts {
+  int each;
+  uint64_t wide;
+  uint32_t narrow;
+  explicit Parts(int64_t n) : each(static_cast<int>(n)), wide(UINT64_MAX / n + 1), narrow(static_cast<uint32_t>(UINT32_MAX / n + 1)) {}
+};
+
 struct Dropout {
   const void* x;
   int64_t ldx;
@@ -247,17 +256,18 @@ __device__ inline void store_entries(T* row, int c, int width, const float* f, b
   }
 }
 
-// Items (row, part) of rows of ``each`` parts, 0 < each <= 2^14, without a division of 64
-// bits a lane: item ``first`` is uniform, ``past`` below 2^14 + 2^13.
+// Items (row, part) of rows of ``each`` parts, 0 < each <= 2^14, without a division: ``first`` is the same
+// in all lanes (below 2^48), ``past`` below 2^14.
 struct Item {
   int64_t row;
   int part;
 };
-__device__ inline Item item_at(int64_t first, int past, int each) {
-  const int64_t row = first / each;
-  const unsigned c = static_cast<unsigned>(first - row * each) + static_cast<unsigned>(past);
-  const unsigned more = each == 1 ? c : __umulhi(c, static_cast<unsigned>(((uint64_t(1) << 32) + each - 1) / each));
-  return {row + more, static_cast<int>(c - more * each)};
+__device__ inline Item item_at(int64_t first, int past, const Parts& p) {
+  if (p.each == 1) return {first + past, 0};
+  const int64_t row = static_cast<int64_t>(__umul64hi(static_cast<uint64_t>(first), p.wide));
+  const unsigned c = static_cast<unsigned>(first - row * p.each) + static_cast<unsigned>(past);
+  const unsigned more = __umulhi(c, p.narrow);
+  return {row + more, static_cast<int>(c - more * p.each)};
 }
 
 // the first group whose places end beyond ``place``; n_groups: none

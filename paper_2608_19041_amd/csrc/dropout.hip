@@ -49,17 +49,17 @@ struct Args {
   int64_t offset;
   const int64_t* offset_at;   // added to it, or null
   void* y;
+  Parts parts;
 };
 
 template <class T>
 __global__ void __launch_bounds__(kThreads) dropout_kernel(Args a) {
   constexpr int V = 16 / int(sizeof(T));
-  const int parts = (a.k + V - 1) / V;
   const int64_t first = int64_t(blockIdx.x) * kThreads * kTurns;
   const uint64_t offset = static_cast<uint64_t>(a.offset) + (a.offset_at ? static_cast<uint64_t>(*a.offset_at) : 0);
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
-    const Item at = item_at(first, i * kThreads + int(threadIdx.x), parts);
+    const Item at = item_at(first, i * kThreads + int(threadIdx.x), a.parts);
     if (at.row >= a.n) continue;
     const int c = at.part * V;
     float x[V], r[V], y[V];
@@ -96,13 +96,14 @@ bool dropout_fits(int64_t n, int k) { return grid_fits(workgroups(n, k, 4), kThr
 
 int launch_dropout(int dtype, const Dropout& d, void* y, hipStream_t st) {
   if (d.n == 0) return 0;
-  Args a{d.x, d.ldx, d.residual, d.ldr, d.n, d.k, 0, 0, 0.0f, d.seed, d.offset, d.offset_at, y};
+  Args a{d.x, d.ldx, d.residual, d.ldr, d.n, d.k, 0, 0, 0.0f, d.seed, d.offset, d.offset_at, y, Parts(1)};
   const double drop = std::floor(d.p * 4294967296.0 + 0.5);
   a.all = drop >= 4294967296.0;
   a.drop = a.all ? 0 : static_cast<unsigned>(drop);
   a.scale = a.all ? 0.0f : static_cast<float>(1.0 / (1.0 - d.p));
   return with_dtype(dtype, [&](auto t) {
     using T = typename Elem<decltype(t)::value>::T;
+    a.parts = Parts((d.k + 16 / int(sizeof(T)) - 1) / (16 / int(sizeof(T))));
     dropout_kernel<T><<<workgroups(d.n, d.k, 16 / int(sizeof(T))), kThreads, 0, st>>>(a);
     DPA4C_HIP_TRY(hipGetLastError());
     return 0;

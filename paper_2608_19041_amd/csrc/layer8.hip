@@ -231,6 +231,7 @@ struct PrepArgs {
   uint8_t* dz8;             // the same in 8 bits
   uint8_t* dz_scales;       // [n][blocks of m] by place
   int64_t list_blocks, clear_blocks;
+  Parts parts{1};            // blocks of a row of dz
 };
 
 constexpr int kPrepThreads = 512, kPrepTurns = 2;
@@ -282,7 +283,7 @@ __global__ void __launch_bounds__(kPrepThreads) layer8_prepare_kernel(PrepArgs a
   float v[kPrepTurns][8], z[kPrepTurns][8];
 #pragma unroll
   for (int i = 0; i < kPrepTurns; ++i) {
-    at[i] = item_at(b * kUnits * kPrepTurns, i * kUnits + int(threadIdx.x) / kUnit, blocks);
+    at[i] = item_at(b * kUnits * kPrepTurns, i * kUnits + int(threadIdx.x) / kUnit, a.parts);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[i][j] = z[i][j] = 0.0f;
     if (at[i].row >= live) continue;
@@ -754,6 +755,7 @@ int launch_grouped8_backward(const dpa4c_grouped8& l, int format, const void* dy
     pre.dz = outer ? p.dz : nullptr;
     pre.dz8 = rows ? p.dz8 : nullptr;
     pre.dz_scales = p.dz_scales;
+    pre.parts = Parts(blocks_of(m));
     pre.list_blocks = list_workgroups(std::max(p.tiles.room, p.blocks.room));
     const int64_t each = dw ? int64_t(k) * m : 1;
     pre.clear_blocks = outer ? int64_t(groups) * ((each + kClear - 1) / kClear) : 0;

@@ -23,11 +23,11 @@ template <class T>
 constexpr int kUnit = kScaleBlock / kEach<T>;   // lanes of a block
 
 template <class T, int F>
-__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __restrict__ x, int64_t ldx, int64_t n, int k,
+__global__ void __launch_bounds__(kThreads) quantize_rows_kernel(const T* __restrict__ x, int64_t ldx, int64_t n, int k, Parts blocks,
                                                                  uint8_t* __restrict__ values, int64_t ld,
                                                                  uint8_t* __restrict__ scales, int64_t lds) {
   constexpr int V = kEach<T>, L = kUnit<T>, kUnits = kThreads / L;
-  const int blocks = static_cast<int>(blocks_of(k)), lane = threadIdx.x % L;
+  const int lane = threadIdx.x % L;
   const int64_t first = int64_t(blockIdx.x) * kUnits * kTurns;
   Item at[kTurns];
   float v[kTurns][V];
@@ -68,9 +68,8 @@ __device__ inline void write_values(u4v q, float scale, T* out, int c, int width
 template <class T, int F>
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const uint8_t* __restrict__ values, int64_t ld,
                                                               const uint8_t* __restrict__ scales, int64_t lds,
-                                                              int64_t n, int k, int group_rows,
+                                                              int64_t n, int k, Parts parts, int group_rows,
                                                               T* __restrict__ out) {
-  const int parts = (k + 15) / 16;
   const int64_t first = int64_t(blockIdx.x) * kThreads * kTurns;
   Item at[kTurns];
   u4v q[kTurns];
@@ -171,7 +170,7 @@ template <class T, int F>
 int quantize_rows(const void* x, int64_t ldx, const dpa4c_rows8& out, hipStream_t st) {
   const int64_t grid = units(out.n * blocks_of(out.k), kThreads / kUnit<T> * kTurns);
   quantize_rows_kernel<T, F><<<grid, kThreads, 0, st>>>(
-      static_cast<const T*>(x), ldx, out.n, out.k, static_cast<uint8_t*>(out.values), out.ld,
+      static_cast<const T*>(x), ldx, out.n, out.k, Parts(blocks_of(out.k)), static_cast<uint8_t*>(out.values), out.ld,
       static_cast<uint8_t*>(out.scales), out.ld_scales);
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
@@ -182,7 +181,7 @@ int dequantize(const void* values, int64_t ld, const void* scales, int64_t lds, 
                void* out, hipStream_t st) {
   const int64_t grid = units(n * ((k + 15) / 16), kThreads * kTurns);
   dequantize_kernel<T, F><<<grid, kThreads, 0, st>>>(static_cast<const uint8_t*>(values), ld,
-                                                     static_cast<const uint8_t*>(scales), lds, n, k, group_rows,
+                                                     static_cast<const uint8_t*>(scales), lds, n, k, Parts((k + 15) / 16), group_rows,
                                                      static_cast<T*>(out));
   DPA4C_HIP_TRY(hipGetLastError());
   return 0;
