@@ -194,7 +194,7 @@ struct Raw {
 // Entries c .. c + V - 1 of a row of ``width``, zeros past it.  A load takes V entries without a
 // condition where the row has as many: those at the row's end, which ``settle`` then puts in their
 // place.  (With a condition for each entry of a row's last lanes a million rows of 541 took
-// 826 us to 8 bits; now 478.)  ``ends``: false where all V entries are there.
+// 826 us to 8 bits, without 478.)  ``ends``: false where all V entries are there.
 template <class T, int V>
 __device__ inline Raw<T, V> load_raw_entries(const T* row, int c, int width, bool ends = true) {
   Raw<T, V> r;

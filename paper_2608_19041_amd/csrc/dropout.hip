@@ -4,7 +4,9 @@
 // et al., "Parallel random numbers: as easy as 1, 2, 3", 2011) with the counter
 // (c / 4, r, offset low, offset high) and the key ``seed`` is at least p 2^32, so a
 // row's mask depends neither on how rows lie in memory nor on the launch, and the
-// gradient of the rows is this operator again.
+// gradient of the rows is this operator again.  Ten rounds are twenty products of 32 bits for
+// four entries, two thirds of what the vector units can do in the time that HBM takes: a million
+// bfloat16 rows of 384 with a residual 410 us (2.3 GB at 5.6 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <cmath>

@@ -23,7 +23,9 @@ namespace {
 
 constexpr int kThreads = kTileThreads;
 
-// A tile of 64 NB rows x 64 NB columns by four waves; a step is one block of 128 entries.
+// A tile of 64 NB rows x 64 NB columns by four waves; a step is one block of 128 entries.  For rows of more
+// blocks than registers hold: 65,536 x 1,024 -> 1,024 in 174 us (0.8 PFLOP/s, matrix cores busy 17 %, LDS 29 %,
+// of which conflicts 8).
 template <class T, int F, int NB>
 __global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(Rows8Args a) {
   constexpr int kTile = kSide<NB>, kOne = kTile * kStep, kHalfLds = 2 * kOne;
@@ -258,6 +260,8 @@ __device__ inline void clear_group(const PrepArgs& a, int g, int64_t part) {
     for (int i = threadIdx.x; i < a.m; i += kPrepThreads) static_cast<T*>(a.db)[int64_t(g) * a.m + i] = none.v[0];
 }
 
+// All of it by workgroups of their own, as it is bound by HBM: 65,536 rows of 1,024 with the zeros of 113 groups
+// 0.7 GB in 155 us.
 template <class T, int F>
 __global__ void __launch_bounds__(kPrepThreads) layer8_prepare_kernel(PrepArgs a) {
   extern __shared__ int32_t starts[];
@@ -351,7 +355,9 @@ __device__ inline v2h half_pair(unsigned v, float scale) {
 // Tiles of 128 x 128 of x^T dz over a block of rows, 32 rows a step; transposing reads turn
 // both operands.  A row's factor, of x's scale and dz's, is applied to x: relative to
 // the largest of the block, 2^kXUp of which brings x's largest entry to 2^15.8, so that an entry is
-// held exactly, or to 2^-40 of the largest product of the block.
+// held exactly, or to 2^-40 of the largest product of the block.  65,536 rows of 1,024 x 1,024 take 313 us (0.44
+// PFLOP/s, matrix cores busy 20 %, vector units 30 %, LDS 20 %), 31,250 of 541 x 384 in 118 groups 59 us: a step has 256
+// matrix cycles of a wave beside some 100 vector instructions and a barrier.
 template <class T, int F>
 __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) {
   // blocks of 32 columns, [block][32 rows][32 columns], set off so that the lanes of one LDS cycle, eight
@@ -555,23 +561,26 @@ int block_rows(int64_t n, int k, int m) {
   return static_cast<int>(few < 512 || rows < few ? few : rows > 8192 ? 8192 : rows);
 }
 
-// Rows of at most kHeldBlocks blocks are held in registers; longer ones go through LDS in tiles,
-// 128 x 128 where they fill the compute units, else 64 x 64.  Held: workgroups of 128 rows from
-// kWideRows on, of 32 below, whose columns are shared out until the chip has work; those of 32
-// look their tile up, without a list, where the groups are few.
-constexpr int64_t kWideRows = 8192;
+// Rows are held in registers, by workgroups of 32 rows that look their tile up (without a list, where the
+// groups are few) below kManyBlocks blocks of 32 columns x 128 entries of all rows, 2^30 products, and by
+// workgroups of 128 rows from there on, whose columns are shared out until the chip has work.  (us, with
+// SiLU and z, in a graph, 32 and 128 rows; 541 -> 384 in 5 groups: 1,000 rows 7, 12; 4,000 11, 13; 8,000 16, 14;
+// 32,000 50, 27; in 118 groups 9, 13; 18, 16; 25, 18; 66, 32.  144 -> 192 in 5 groups: 4,000 6, 12; 16,000 11, 13;
+// 32,000 18, 15.)  Longer rows than kWideBlocks and kHeldBlocks leave too few registers, or LDS for one workgroup a
+// compute unit: they go through LDS in tiles, 128 x 128 where they fill the compute units, else 64 x 64.
+constexpr int64_t kManyBlocks = 1 << 18;
 struct Tiling {
   bool held, wide, listed;
   int rows, splits;
 };
 Tiling tiling(int64_t n, int n_groups, int kin, int kout) {
-  const bool many = n >= kWideRows && kout >= 8;
+  const int64_t cols = (kout + 31) / 32;
+  const bool many = n >= 4096 && n * blocks_of(kin) * cols >= kManyBlocks && kout >= 8;
   Tiling t{blocks_of(kin) <= (many ? kWideBlocks : kHeldBlocks), false, true, 0, 1};
   if (!t.held) {
     t.rows = kout > 64 && (n / 128) * ((kout + 127) / 128) >= 256 ? kSide<2> : kSide<1>;
     return t;
   }
-  const int64_t cols = (kout + 31) / 32;
   t.wide = many;
   t.rows = t.wide ? 128 : 32;
   t.listed = t.wide || n_groups > 512;

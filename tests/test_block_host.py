@@ -160,6 +160,20 @@ def test_layer_calls_refused():
     assert sizes[0] >= max(sizes[1:]) and sizes[3] <= sizes[2]
 
 
+def test_scratch_of_every_size():
+    """Sizes of all kinds of tiles, and the ends of the ranges, have a plan."""
+    lib, need = dp.library(), ctypes.c_int64(0)
+    for n in (0, 1, 30, 127, 4095, 4096, 100000, 2 ** 24):
+        for groups in (1, 5, 600, 4096):
+            for k in (1, 128, 640, 641, 1024, 1025, 65536):
+                for m in (1, 7, 8, 384, 1025, 65536):
+                    l = layer(x=dict(n=n, k=k, ld=65536, ld_scales=512), w=dict(n_groups=groups, k=k, n_out=m))
+                    rc = lib.dpa4c_grouped_linear8_work(REF(l), REF(need))
+                    assert rc in (0, UNSUPPORTED) and (rc or need.value >= 0)
+                    assert lib.dpa4c_grouped_linear8_backward_work(REF(l), 1, 1, 1, REF(need)) == rc
+                    assert rc == 0 or n * max(k, m) > 2 ** 29 or groups * k * m > 2 ** 28
+
+
 def test_scratch_of_gradients_is_what_the_rows_can_use():
     """dz in 16 and in 8 bits with its scales, and the blocks' sums."""
     lib, need = dp.library(), ctypes.c_int64(0)

@@ -333,7 +333,8 @@ SHAPES = [  # n, k, m, groups, kind
     (64, 128, 64, 1, "one"), (65, 129, 65, 2, "all"), (108, 144, 192, 118, "few"), (200, 15, 17, 3, "all"),
     (130, 256, 130, 2, "all"), (777, 541, 384, 118, "all"), (1000, 384, 541, 5, "few"), (300, 1024, 40, 4, "few"),
     (5000, 33, 300, 600, "all"), (40, 2000, 8, 3, "all")]
-LARGE = [(33000, 130, 129, 5, "few"), (66000, 64, 70, 118, "all"), (20000, 300, 257, 3, "all")]
+LARGE = [(33000, 130, 129, 5, "few"), (66000, 64, 70, 118, "all"), (20000, 300, 257, 3, "all"),
+         (33000, 700, 129, 5, "few"), (33000, 129, 700, 5, "all"), (9000, 541, 384, 5, "few"), (140000, 100, 50, 118, "few"), (12000, 500, 200, 7, "all"), (140000, 70, 7, 2, "one")]
 
 
 def whole(n, k, seed, top=4):

@@ -118,7 +118,7 @@ def test_rows_in_any_order_and_entries_outside_it():
     bad[gone] = torch.tensor([-1, n, 2 ** 31 - 1, -2 ** 31, n + 7], dtype=torch.int32, device="cuda")
     left = torch.ones(n, dtype=torch.bool, device="cuda")
     left[order[gone].long()] = False
-    for many in (1, 40):   # the kernels of few rows and of many
+    for many in (1, 40, 450):   # the kernels of few rows and of many
         xs, dys = x.repeat(many, 1), dy.repeat(many, 1)
         p = ptr * many
         at = torch.arange(many, device="cuda", dtype=torch.int32)[None] * n
