@@ -1,0 +1,99 @@
+"""The residual block's operators on more than 2^31 entries, and on scales that stand for NaN (GPU)."""
+import pytest
+import torch
+
+import block_reference as ref
+import paper_2608_19041_amd as dp
+
+pytestmark = pytest.mark.gpu
+
+
+def same8(a, b):
+    return torch.equal(a.values.contiguous().view(torch.uint8), b.values.contiguous().view(torch.uint8)) and \
+        torch.equal(a.scales.contiguous().view(torch.uint8), b.scales.contiguous().view(torch.uint8))
+
+
+def test_rows_beyond_32_bits():
+    """The last rows of many are those of a call of their own."""
+    n, k, m, tail = 4_200_000, 541, 520, 500   # n k = 2.27e9, n m = 2.18e9
+    x = torch.empty(n, k, dtype=torch.bfloat16, device="cuda")
+    x.view(-1, 1000 * k).copy_(torch.randn(1000 * k, device="cuda").bfloat16()[None].expand(n // 1000, -1))
+    x[-tail:] = torch.randn(tail, k, device="cuda")
+    last = x[-tail:].clone()
+    gain = torch.rand(k, device="cuda").bfloat16()
+    x8 = dp.quantize_rows(x)
+    last8 = dp.quantize_rows(last)
+    assert same8(dp.Rows8(x8.values[-tail:], x8.scales[-tail:]), last8)
+    back = dp.dequantize(x8, torch.bfloat16)
+    assert torch.equal(back[-tail:], dp.dequantize(last8, torch.bfloat16))
+    del back
+    y, s = dp.rms_norm(x, gain)
+    yt, st = dp.rms_norm(last, gain)
+    assert torch.equal(y[-tail:], yt) and torch.equal(s[-tail:], st)
+    dx, dgain = dp.rms_norm_backward(x, y, gain, s)
+    assert torch.equal(dx[-tail:], dp.rms_norm_backward(last, yt, gain, st)[0]) and torch.isfinite(dgain).all()
+    del y, dx
+    d = dp.dropout(x, 0.3, 7, 1)
+    keep = ref.keep_mask(n, 4, 0.3, 7, 1)[-tail:].cuda()
+    assert torch.equal(d[-tail:, :4] != 0, keep & (last[:, :4] != 0))
+    del d
+    w8 = dp.quantize_weights(torch.randn(2, k, m, device="cuda") * k ** -0.5)
+    ptr = torch.tensor([0, n - 1000, n], device="cuda")
+    few = torch.tensor([0, 0, tail], device="cuda")
+    y, z = dp.grouped_linear8(x8, w8, ptr, activation="silu", preact=True)
+    yt, zt = dp.grouped_linear8(last8, w8, few, activation="silu", preact=True)
+    assert torch.equal(y[-tail:], yt) and torch.equal(z[-tail:], zt)
+    dx, dw, db = dp.grouped_linear8_backward(y, x8, w8, ptr, preact=z)
+    dxt, _, _ = dp.grouped_linear8_backward(yt, last8, w8, few, preact=zt)
+    assert torch.equal(dx[-tail:], dxt)
+    # the second group's sums, of the last thousand rows
+    _, dwt, dbt = dp.grouped_linear8_backward(y[-1000:], dp.Rows8(x8.values[-1000:], x8.scales[-1000:]), w8,
+                                              torch.tensor([0, 0, 1000], device="cuda"), preact=z[-1000:])
+    for a, b in ((dw, dwt), (db, dbt)):
+        # blocks of other lengths: float32 sums of a thousand terms, then half a step of bfloat16 each
+        off = (a[1].float() - b[1].float()).norm() / b[1].float().norm()
+        assert off <= 2 * 2.0 ** -8
+
+
+def test_scales_that_stand_for_nan():
+    """A scale byte of 255 makes its block NaN, in rows and in weights, and nothing else."""
+    n, k, m = 200, 300, 140
+    x8 = dp.quantize_rows(torch.randn(n, k, device="cuda"))
+    w8 = dp.quantize_weights(torch.randn(1, k, m, device="cuda"))
+    dy = torch.randn(n, m, device="cuda").bfloat16()
+    ptr = torch.tensor([0, n], device="cuda")
+    clean, (cx, cw, cb) = dp.grouped_linear8(x8, w8, ptr), dp.grouped_linear8_backward(dy, x8, w8, ptr)
+    x8.scales.view(torch.uint8)[17, 1] = 255
+    assert torch.isnan(dp.dequantize(x8)[17, 128:256]).all() and torch.isfinite(dp.dequantize(x8)[17, :128]).all()
+    y, (dx, dw, db) = dp.grouped_linear8(x8, w8, ptr), dp.grouped_linear8_backward(dy, x8, w8, ptr)
+    other = torch.arange(n, device="cuda") != 17
+    assert torch.isnan(y[17]).all() and torch.equal(y[other], clean[other]) and torch.equal(dx, cx)
+    assert torch.isnan(dw[0, 128:256]).all() and torch.equal(db, cb)
+    assert torch.equal(dw[0, :128], cw[0, :128]) and torch.equal(dw[0, 256:], cw[0, 256:])
+    x8 = dp.quantize_rows(dp.dequantize(x8).nan_to_num())
+    clean, cx = dp.grouped_linear8(x8, w8, ptr), dp.grouped_linear8_backward(dy, x8, w8, ptr)[0]
+    w8.scales.view(torch.uint8)[0, 2, 1] = 255
+    y, dx = dp.grouped_linear8(x8, w8, ptr), dp.grouped_linear8_backward(dy, x8, w8, ptr)[0]
+    assert torch.isnan(y[:, 128:]).all() and torch.equal(y[:, :128], clean[:, :128])
+    assert torch.isnan(dx[:, 256:]).all() and torch.equal(dx[:, :256], cx[:, :256])
+
+
+@pytest.mark.parametrize("n", [12000, 300])
+def test_repeated_calls_give_the_same_bits(n):
+    k, m, groups = 541, 384, 5
+    ids = torch.randint(0, groups, (n,), device="cuda").to(torch.int32)
+    ptr, order = dp.group_rows(ids, groups)
+    x8 = dp.quantize_rows(torch.randn(n, k, device="cuda"))
+    w8 = dp.quantize_weights(torch.randn(groups, k, m, device="cuda"))
+    h, dy = torch.randn(n, k, device="cuda").bfloat16(), torch.randn(n, m, device="cuda").bfloat16()
+    gain = torch.rand(groups, k, device="cuda").bfloat16()
+
+    def everything():
+        y, s = dp.rms_norm(h, gain, ptr, order)
+        return [y, s, *dp.rms_norm_backward(y, h, gain, s, ptr, order), dp.grouped_linear8(x8, w8, ptr, order),
+                *dp.grouped_linear8_backward(dy, x8, w8, ptr, order, preact=dy), dp.dropout(h, 0.5, 3)]
+
+    first = everything()
+    for _ in range(3):
+        for a, b in zip(first, everything()):
+            assert torch.equal(a, b)
