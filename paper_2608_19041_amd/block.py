@@ -20,6 +20,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 from typing import NamedTuple
 
 from . import _check, _ptr, library
@@ -205,6 +206,7 @@ def dequantize(x, dtype=None, stream=None):
     if weights and x.values is None:
         raise ValueError("the weights were laid out for the forward pass alone")
     at = _weights8(x, None, "x") if weights else _rows8(x, None, "x")
+    _unrecorded(x=x.values)
     dev, lib = x.values.device, library()
     with _launch(dev, stream) as st:
         out = torch.empty(x.values.shape, dtype=dtype, device=dev)
@@ -301,6 +303,7 @@ def _layer8(x, weight, group_ptr, order, dtype):
     rows = _rows8(x, None, "x")
     dev = x.values.device
     w = _weights8(weight, dev)
+    _unrecorded(x=x.values, values=weight.values, turned=weight.turned)
     if w.k != rows.k:
         raise ValueError(f"x has {rows.k} entries a row, the weights {w.k}")
     _same(group_ptr, torch.int64, (w.n_groups + 1,), dev, "group_ptr")
@@ -385,21 +388,24 @@ def dropout(x, p: float, seed: int, offset=0, residual=None, stream=None):
     ldr = 0 if residual is None else _rows(residual, x.dtype, (n, k), x.device, "residual")
     if not 0.0 <= p <= 1.0:
         raise ValueError("p must be 0 .. 1")
+    seed = operator.index(seed)   # a fraction is no other mask than the number below it
     if not 0 <= seed < 2 ** 64:
         raise ValueError("seed must be 0 .. 2^64 - 1")
-    at, number = None, offset
+    at = None
     if isinstance(offset, torch.Tensor):
         if offset.dtype != torch.int64 or offset.numel() != 1 or offset.device != x.device:
             raise ValueError(f"offset must be an int, or one int64 on {x.device}")
         at, number = offset, 0
-    elif not -2 ** 63 <= offset < 2 ** 63:
-        raise ValueError("offset must be of 64 bits")
+    else:
+        number = operator.index(offset)
+        if not -2 ** 63 <= number < 2 ** 63:
+            raise ValueError("offset must be of 64 bits")
     _unrecorded(x=x, residual=residual)
     lib = library()
     with _launch(x.device, stream) as st:
         y = torch.empty(n, k, dtype=x.dtype, device=x.device)
-        _check(lib.dpa4c_dropout(code, _ptr(x), ldx, _ptr(residual), ldr, n, _int(k), float(p), int(seed),
-                                 int(number), _ptr(at), _ptr(y), st))
+        _check(lib.dpa4c_dropout(code, _ptr(x), ldx, _ptr(residual), ldr, n, _int(k), float(p), seed, number,
+                                 _ptr(at), _ptr(y), st))
     return y
 
 

@@ -142,3 +142,22 @@ def test_rows_in_any_order_and_entries_outside_it():
         dn, dg = dp.rms_norm_backward(xs, xs, gain, sn, p, some)
         en, eg = dp.rms_norm_backward(torch.where(keep[:, None], xs, 0), xs, gain, sn, p, full)
         assert torch.equal(dn[keep], en[keep]) and torch.equal(dg, eg)
+
+
+def test_numbers_that_are_no_integers():
+    x = rows(10, 40)
+    for call in (lambda: dp.dropout(x, 0.5, 1.5), lambda: dp.dropout(x, 0.5, 1, 0.5)):
+        with pytest.raises(TypeError):
+            call()
+
+
+def test_8_bit_tensors_that_require_gradients():
+    ptr, x8, w8 = parts()
+    dy = rows(10, 24, torch.bfloat16)
+    q = x8.values.detach().requires_grad_()
+    w = w8.turned.detach().requires_grad_()
+    x_wants, w_wants = dp.Rows8(q, x8.scales), dp.Weights8(w8.values, w, w8.scales)
+    refused(lambda: dp.dequantize(x_wants), lambda: dp.grouped_linear8(x_wants, w8, ptr),
+            lambda: dp.grouped_linear8(x8, w_wants, ptr), lambda: dp.grouped_linear8_backward(dy, x8, w_wants, ptr))
+    with torch.no_grad():
+        assert torch.equal(dp.grouped_linear8(x_wants, w_wants, ptr), dp.grouped_linear8(x8, w8, ptr))
