@@ -7,8 +7,8 @@
 // read once; a wave walks neighbouring places, so that it keeps its group's gains. Squares, and
 // the sums over a row and over the rows of a group, are in 64 bits; the gradients of half types are
 // formed in 32, as 64 would make their vector instructions the bound.  A million bfloat16 rows of 384 with a
-// residual and an output in 8 bits take 640 us (2.8 GB at 4.3 TB/s, vector units busy 63 %), the gradients of
-// a million rows of 541 840 us (3.5 GB at 4.1 TB/s, 62 %).  Rows that leave registers to scratch
+// residual and an output in 8 bits take 640 us (2.8 GB at 4.3 TB/s, vector units busy 62 %), the gradients of
+// a million rows of 541 840 us (3.5 GB at 4.1 TB/s, 59 %).  Rows that leave registers to scratch
 // lose more than a wave more to a SIMD gives: 1,200 us with four waves, 840 with three.
 #include <hip/hip_runtime.h>
 
@@ -508,8 +508,9 @@ int with_flag(bool flag, Fn&& fn) {
   return flag ? fn(std::integral_constant<bool, true>{}) : fn(std::integral_constant<bool, false>{});
 }
 
-// places of a block of the gradients: 1,024 blocks, four to a compute unit, of 16 rows at
-// the least; long rows have several strips of columns in place of as many blocks
+// places of a block of the gradients: 768 blocks, three to a compute unit, of 16 rows at
+// the least (4,000 rows of 384: 28 us, 8 or 32 rows 30); long rows have several strips of columns in
+// place of as many blocks
 constexpr int kBlocks = 768, kMostRows = 256;
 int block_rows(int64_t n, int strips, int lanes) {
   const int64_t blocks = std::max(1, kBlocks / strips), rows = std::max<int64_t>(16, (n + blocks - 1) / blocks);

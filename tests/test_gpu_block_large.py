@@ -97,3 +97,37 @@ def test_repeated_calls_give_the_same_bits(n):
     for _ in range(3):
         for a, b in zip(first, everything()):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [7, 5000])
+def test_4096_groups(n):
+    """As many groups as are allowed, most of them without rows: whole numbers, so that sums are exact."""
+    k, m, groups = 40, 24, 4096
+    make = torch.Generator().manual_seed(5)
+    ids = torch.randint(0, groups, (n,), generator=make)
+    ids[:3] = torch.tensor([0, groups - 1, groups - 1])
+    order = torch.argsort(ids, stable=True).to(torch.int32)
+    ptr = torch.zeros(groups + 1, dtype=torch.int64)
+    ptr[1:] = torch.bincount(ids, minlength=groups).cumsum(0)
+
+    def whole(*shape):
+        return torch.randint(-1, 2, shape, generator=make).float()
+
+    x, w, dy = whole(n, k), whole(groups, k, m), whole(n, m)
+    on = (ptr.cuda(), order.cuda())
+    x8, w8 = dp.quantize_rows(x.cuda()), dp.quantize_weights(w.cuda())
+    y = torch.stack([x[i] @ w[ids[i]] for i in range(n)])
+    assert torch.equal(dp.grouped_linear8(x8, w8, *on).float().cpu(), y)
+    dx, dw, db = dp.grouped_linear8_backward(dy.bfloat16().cuda(), x8, w8, *on)
+    assert torch.equal(dx.float().cpu(), torch.stack([w[ids[i]] @ dy[i] for i in range(n)]))
+    want_w, want_b = torch.zeros(groups, k, m), torch.zeros(groups, m)
+    want_w.index_add_(0, ids, x[:, :, None] * dy[:, None])
+    assert torch.equal(dw.float().cpu(), want_w) and torch.equal(db.float().cpu(), want_b.index_add_(0, ids, dy))
+    # rows of entries of one size, and a tiny eps: s is 1 / that size, a power of two
+    h = torch.where(whole(n, k) > 0, 4.0, -4.0)
+    gain = whole(groups, k)
+    z, s = dp.rms_norm(h.cuda(), gain.cuda(), *on, eps=1e-30)
+    assert torch.equal(s.cpu(), torch.full((n,), 0.25)) and torch.equal(z.cpu(), h / 4 * gain[ids])
+    g = whole(n, k)
+    _, dgain = dp.rms_norm_backward(g.cuda(), h.cuda(), gain.cuda(), s, *on)
+    assert torch.equal(dgain.cpu(), torch.zeros(groups, k).index_add_(0, ids, g * h / 4))
