@@ -24,7 +24,7 @@ namespace {
 constexpr int kThreads = kTileThreads;
 
 // A tile of 64 NB rows x 64 NB columns by four waves; a step is one block of 128 entries.  For rows of more
-// blocks than registers hold: 65,536 x 1,024 -> 1,024 in 174 us (0.8 PFLOP/s, matrix cores busy 17 %, LDS 29 %,
+// blocks than registers hold: 65,536 x 1,024 -> 1,024 in 177 us (0.8 PFLOP/s, matrix cores busy 17 %, LDS 29 %,
 // of which conflicts 8).
 template <class T, int F, int NB>
 __global__ void __launch_bounds__(kThreads, 2) layer8_rows_kernel(Rows8Args a) {
@@ -261,7 +261,7 @@ __device__ inline void clear_group(const PrepArgs& a, int g, int64_t part) {
 }
 
 // All of it by workgroups of their own, as it is bound by HBM: 65,536 rows of 1,024 with the zeros of 113 groups
-// 0.7 GB in 155 us.
+// 0.7 GB in 157 us.
 template <class T, int F>
 __global__ void __launch_bounds__(kPrepThreads) layer8_prepare_kernel(PrepArgs a) {
   extern __shared__ int32_t starts[];
@@ -345,7 +345,6 @@ struct OuterArgs {
 // two 8-bit numbers of word ``v`` times a power of two, as float16
 template <int F, bool High>
 __device__ inline v2h half_pair(unsigned v, float scale) {
-  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
   if constexpr (F == DPA4C_E4M3)
     return __builtin_bit_cast(v2h, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, scale, High));
   else
@@ -355,7 +354,7 @@ __device__ inline v2h half_pair(unsigned v, float scale) {
 // Tiles of 128 x 128 of x^T dz over a block of rows, 32 rows a step; transposing reads turn
 // both operands.  A row's factor, of x's scale and dz's, is applied to x: relative to
 // the largest of the block, 2^kXUp of which brings x's largest entry to 2^15.8, so that an entry is
-// held exactly, or to 2^-40 of the largest product of the block.  65,536 rows of 1,024 x 1,024 take 313 us (0.44
+// held exactly, or to 2^-40 of the largest product of the block.  65,536 rows of 1,024 x 1,024 take 315 us (0.44
 // PFLOP/s, matrix cores busy 20 %, vector units 30 %, LDS 20 %), 31,250 of 541 x 384 in 118 groups 59 us: a step has 256
 // matrix cycles of a wave beside some 100 vector instructions and a barrier.
 template <class T, int F>
@@ -464,12 +463,12 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) 
       const float scale = !there[q] ? 1.0f : ex[q] == 255 ? NAN : power_of_two(d < -126 ? -126 : d);
       v8h h[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const unsigned x = there[q] ? rx[q][j] : 0;
-          const v2h lo = half_pair<F, false>(x, scale), hi = half_pair<F, true>(x, scale);
-          h[j / 2][4 * (j % 2)] = lo.x, h[j / 2][4 * (j % 2) + 1] = lo.y;
-          h[j / 2][4 * (j % 2) + 2] = hi.x, h[j / 2][4 * (j % 2) + 3] = hi.y;
-        }
+      for (int j = 0; j < 4; ++j) {
+        const unsigned x = there[q] ? rx[q][j] : 0;
+        const v2h lo = half_pair<F, false>(x, scale), hi = half_pair<F, true>(x, scale);
+        h[j / 2][4 * (j % 2)] = lo.x, h[j / 2][4 * (j % 2) + 1] = lo.y;
+        h[j / 2][4 * (j % 2) + 2] = hi.x, h[j / 2][4 * (j % 2) + 3] = hi.y;
+      }
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         *reinterpret_cast<v8h*>(to + x_block(x_slot / 2) + slot_at(x_own, x_slot % 2 * 2 + j)) = h[j];
@@ -553,7 +552,8 @@ __global__ void __launch_bounds__(kThreads, 2) layer8_outer_kernel(OuterArgs a) 
 
 // Rows of a block of dW: four rounds of the 512 workgroups that are resident, between 512 and 8,192 rows, or
 // as few as outer_rows gives where there are few.  (65,536 x 1,024 x 1,024: blocks of 2,048 rows
-// in place of 1,024 save half of the sums that are written and joined, 717 us to 680.)
+// in place of 1,024 save half of the sums that are written and joined, 717 us to 680; of two rounds, 4,096
+// rows, or of one the last workgroups wait longer, 645 us to 653 and 720.)
 int block_rows(int64_t n, int k, int m) {
   const int64_t tiles = ((k + kOuterTile - 1) / kOuterTile) * int64_t((m + kOuterTile - 1) / kOuterTile);
   const int few = outer_rows(n, k, m);
